@@ -9,7 +9,9 @@
  * through Gradient Threshold Compression with residual error feedback (§VI-A).
  * Two pieces of the multi-worker trainers run per GPU as well: the aggregate
  * of several workers' compressed updates (§VI-A) and the BMUF-NBM global
- * model step (§VI-B).
+ * model step (§VI-B).  Beside the LSTM there are the operators of a student
+ * made of gated linear recurrences: the recurrence, what stands between two of
+ * its blocks, and an AdamW step.
  *
  * Conventions for every entry point:
  *  - Pointers are device pointers unless the comment says [host].
@@ -360,6 +362,116 @@ am_status sgd_apply(int64_t n, float* master, void* weights_bf16, const float* u
 /* fp32 -> bf16 (round to nearest even, NaN -> 0x7FC0), e.g. input frames. */
 am_status am_cast_f32_to_bf16(int64_t n, const float* src, void* dst_bf16, void* stream);
 
+/* ---- gated linear recurrences ------------------------------------------- */
+
+/* A recurrent layer without a product inside its time loop, over packed frames
+ * (layout and lengths as in lstm_am_forward).  Per channel:
+ *   L_t = c softplus(lam) sigm(r_t),  a_t = exp(-L_t),
+ *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigm(i_t) x_t.
+ * Evaluated in fp32, each output rounded once.  A gate that is shut (L_t = 0)
+ * keeps the state.  Rows may be columns of a wider matrix: x, r, i (and dh, dx,
+ * dr, di) have row strides in elements.
+ *   dtype   AM_F32 or AM_BF16: type of x, r, i, h, dh, dx, dr, di
+ *   x, r, i [N] rows of H;  lam [H] fp32, finite;  c > 0
+ *   lengths [host] [B] or NULL; variable-length batches allow B <= 1024
+ *   h0      [B][H] fp32 or NULL (zero);  hT [B][H] fp32 or NULL: state after
+ *           each sequence's last frame (h0 where it has none; may be h0 itself)
+ *   h       [N][H] (written)
+ *   ws      workspace of am_gated_recurrence_workspace_bytes (256-byte aligned;
+ *           may be NULL where that is 0).  train = 1 keeps in it what
+ *           gated_recurrence_backward reads; it must not be modified between.
+ * A batch of one frame per sequence with train = 0 is one launch. */
+int64_t am_gated_recurrence_workspace_bytes(int32_t T, int32_t B, int32_t H, int32_t varlen,
+                                            int32_t train);
+am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtype,
+                                   const int32_t* lengths, const void* x, int64_t ldx, const void* r,
+                                   int64_t ldr, const void* i, int64_t ldi, const float* lam, float c,
+                                   const float* h0, void* h, float* hT, int32_t train, void* ws,
+                                   int64_t ws_bytes, void* stream);
+/* The gradient of the forward call (train = 1) that filled `ws`, whose T, B, H,
+ * dtype, lengths, x, r, i, lam and c are given again:
+ *   dh  [N] rows: dL/dh;  dhT [B][H] fp32 or NULL: dL/dhT
+ *   dx, dr, di [N] rows (written);  dlam [H] fp32 (written)
+ *   dh0 [B][H] fp32 or NULL (written)
+ * No atomics: the same inputs give the same bits.                           */
+am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dtype,
+                                    const int32_t* lengths, const void* x, int64_t ldx, const void* r,
+                                    int64_t ldr, const void* i, int64_t ldi, const float* lam, float c,
+                                    const void* dh, int64_t lddh, const float* dhT, void* dx,
+                                    int64_t lddx, void* dr, int64_t lddr, void* di, int64_t lddi,
+                                    float* dlam, float* dh0, void* ws, int64_t ws_bytes, void* stream);
+
+/* Between two blocks of a residual stack, per row of H:
+ *   u = o * gate * sigm(gate)                         (gate NULL: u = o)
+ *   p = u / sqrt(mean(u^2) + eps)                     (w_post NULL: p = u)
+ *   res_out = res + scale * w_post * p                (NULL: factor 1)
+ *   y = w_next * res_out / sqrt(mean(res_out^2) + eps)
+ * o NULL: the norm alone, y = w_next * res / rms (a stack's first block; gate,
+ * w_post, scale and res_out NULL).  w_next NULL: no second norm (y NULL).
+ * Evaluated in fp32, each output rounded once; y is made from res_out before it
+ * is rounded.
+ *   dtype: type of o, gate, y;  res_dtype: type of res and res_out
+ *   o, gate [N] rows, ldo and ldg elements apart;  res, res_out, y [N][H]
+ *   w_post, scale, w_next [H] fp32
+ *   rstd [N][2] fp32 or NULL: kept for gated_norm_backward (written)
+ * 1 <= H <= 8192, eps > 0.  res_out may be res.                             */
+am_status gated_norm_forward(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, const void* o,
+                             int64_t ldo, const void* gate, int64_t ldg, const float* w_post,
+                             const float* scale, const void* res, const float* w_next, float eps,
+                             void* res_out, void* y, float* rstd, void* stream);
+/* The gradient of that forward call, from its inputs (res as it was before the
+ * call) and the rstd it wrote:
+ *   dy [N][H] of dtype (NULL if there was no y); dres_out [N][H] of res_dtype or
+ *   NULL (zero): the gradient of res_out but for what passes through y
+ *   d_o, dgate [N] rows of dtype, lddo and lddg elements apart; dres [N][H] of
+ *   res_dtype (written; may be dres_out)
+ *   dw_post, dscale, dw_next [H] fp32, each NULL where its factor is (written)
+ * No atomics: the same inputs give the same bits.                           */
+int64_t am_gated_norm_workspace_bytes(int64_t N, int32_t H);
+am_status gated_norm_backward(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, const void* o,
+                              int64_t ldo, const void* gate, int64_t ldg, const float* w_post,
+                              const float* scale, const void* res, const float* w_next, float eps,
+                              const float* rstd, const void* dy, const void* dres_out, void* d_o,
+                              int64_t lddo, void* dgate, int64_t lddg, void* dres, float* dw_post,
+                              float* dscale, float* dw_next, void* ws, int64_t ws_bytes, void* stream);
+
+/* One tensor of an AdamW step.  Any element alignment. */
+typedef struct {
+  int64_t n;              /* elements */
+  float* master;          /* [n] fp32 (updated) */
+  void* weights_bf16;     /* [n] bf16 copy of master, rounded to nearest even, or NULL (written) */
+  const void* grad;       /* [n] of grad_dtype */
+  void* m;                /* [n] first moment (updated): fp32, or 8-bit codes */
+  void* v;                /* [n] second moment (updated): fp32, or 8-bit codes of its root */
+  float* m_scale;         /* 8-bit: [ceil(n / 256)] scales (updated); else NULL */
+  float* v_scale;
+  double weight_decay;
+} am_adamw_tensor;
+
+/* AdamW step `step` (1, 2, ...) of `count` tensors ([host]; nothing of it is
+ * kept), per element, each operation rounded to fp32, in this order:
+ *   g = grad * *grad_scale           (grad_scale [device] or NULL: g = grad)
+ *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) (g g)
+ *   master = master (1 - lr weight_decay)
+ *            - (m / (sqrt(v) / sqrt(1 - beta2^step) + eps)) (lr / (1 - beta1^step))
+ * with every coefficient evaluated in fp64 and rounded once.  A grad_scale that
+ * is not finite leaves everything as it was (a step whose gradient norm
+ * overflowed).
+ * state_bits 32: m and v are fp32.  state_bits 8: m and sqrt(v) are 8-bit floats
+ * (4 exponent bits of bias 7, 3 fraction bits, as torch.float8_e4m3fn) in units
+ * of a scale for each 256 elements of the tensor: the power of two (2^-126 at
+ * least) that puts the block's largest finite magnitude into [128, 256).  Codes
+ * are rounded down, or up with the probability of what is cut off, by 16 bits of
+ *   x = i * 0x85EBCA6B + (seed + t * 0x9E3779B9);  x = (x ^ x >> 15) * 0xD168AAAD;
+ *   x = (x ^ x >> 15) * 0xAF723597;  x = x ^ x >> 15        (modulo 2^32)
+ * for element i of tensor t: the low half for m, the high half for sqrt(v).  A
+ * nonzero sqrt(v) has code 1 at least; what is not finite has code 0x7F (NaN).
+ * All codes and scales 0 is the state before the first step.  A caller gives
+ * each step another seed.  0 <= beta < 1; eps, lr >= 0 and finite.          */
+am_status adamw_apply(int32_t count, const am_adamw_tensor* tensors, int32_t grad_dtype,
+                      int32_t state_bits, double lr, double beta1, double beta2, double eps,
+                      int64_t step, const float* grad_scale, uint32_t seed, void* stream);
+
 /* ---- kernel timing ------------------------------------------------------ */
 
 /* Kernel classes for timing with HIP events. */
@@ -375,7 +487,10 @@ typedef enum {
   AM_K_SGD = 8,
   AM_K_MISC = 9,          /* casts, transposes, bias reductions, gathers */
   AM_K_BMUF = 10,         /* BMUF-NBM global step */
-  AM_K_NCLASSES = 11
+  AM_K_GATED = 11,        /* gated linear recurrence, forward and backward */
+  AM_K_NORM = 12,         /* gate, norm, residual and next norm, and their gradient */
+  AM_K_ADAMW = 13,        /* AdamW step */
+  AM_K_NCLASSES = 14
 } am_kernel_class;
 
 /* Starts recording: every later launch of a class whose bit is set in

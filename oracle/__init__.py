@@ -28,6 +28,9 @@ What it computes, in the order the training step runs it
 * ``teacher``  -- target generation: the bidirectional LSTM teacher's logits,
   the k best logits per frame and the posterior rebuilt from them (§V-A,
   §V-C, §VII).
+* ``gated``, ``adamw`` -- the operators of a student of gated linear
+  recurrences (recurrence, the norms between blocks, AdamW step); imported as
+  modules.
 
 Floating point: the model, loss and their gradients are computed in fp64;
 the quantiser and SGD use the exact fp32 operation order that the method

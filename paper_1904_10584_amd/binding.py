@@ -20,8 +20,9 @@ F32, BF16 = 0, 1
 MEAN_VALID, SUM = 0, 1
 K_GEMM_FWD, K_GEMM_BWD_DATA, K_GEMM_BWD_WGT, K_LSTM_FWD, K_LSTM_BWD = 0, 1, 2, 3, 4
 K_CE, K_ENCODE, K_DECODE, K_SGD, K_MISC, K_BMUF = 5, 6, 7, 8, 9, 10
+K_GATED, K_NORM, K_ADAMW = 11, 12, 13
 KERNEL_CLASSES = ["gemm_fwd", "gemm_bwd_data", "gemm_bwd_wgt", "lstm_fwd", "lstm_bwd",
-                  "soft_ce", "encode", "decode", "sgd", "misc", "bmuf"]
+                  "soft_ce", "encode", "decode", "sgd", "misc", "bmuf", "gated", "norm", "adamw"]
 
 
 OK, EINVAL, ECAPACITY, EUNSUPPORTED, EHIP, EWORKSPACE, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6
@@ -60,6 +61,7 @@ class Model:
 
 _lib = None
 _P, _I32, _I64, _F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+_U32, _F64 = ctypes.c_uint32, ctypes.c_double
 _PROTOS = {
     "am_param_count": (_I64, [_P]),
     "am_param_offsets": (_I32, [_P, _P]),
@@ -89,6 +91,18 @@ _PROTOS = {
     "kbest_posteriors": (_I32, [_I64, _I32, _P, _P, _P]),
     "lfr_features": (_I32, [_I32, _P, _P, _I32, _I32, _I32, _I32, _P, _P, _P, _I32, _P]),
     "delay_targets": (_I32, [_I32, _I32, _P, _I32, _I32, _P, _P, _P, _P, _P, _P]),
+    "am_gated_recurrence_workspace_bytes": (_I64, [_I32, _I32, _I32, _I32, _I32]),
+    "gated_recurrence_forward": (_I32, [_I32, _I32, _I32, _I32, _P, _P, _I64, _P, _I64, _P, _I64, _P,
+                                        _F32, _P, _P, _P, _I32, _P, _I64, _P]),
+    "gated_recurrence_backward": (_I32, [_I32, _I32, _I32, _I32, _P, _P, _I64, _P, _I64, _P, _I64, _P,
+                                         _F32, _P, _I64, _P, _P, _I64, _P, _I64, _P, _I64, _P, _P, _P,
+                                         _I64, _P]),
+    "am_gated_norm_workspace_bytes": (_I64, [_I64, _I32]),
+    "gated_norm_forward": (_I32, [_I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _F32, _P,
+                                  _P, _P, _P]),
+    "gated_norm_backward": (_I32, [_I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _F32, _P,
+                                   _P, _P, _P, _I64, _P, _I64, _P, _P, _P, _P, _P, _I64, _P]),
+    "adamw_apply": (_I32, [_I32, _P, _I32, _I32, _F64, _F64, _F64, _F64, _I64, _P, _U32, _P]),
     "am_cast_f32_to_bf16": (_I32, [_I64, _P, _P, _P]),
     "am_workspace_check": (_I32, [_P, _I64, _P]),
     "am_profile_begin": (_I32, [ctypes.c_uint32]),
@@ -374,6 +388,203 @@ def cast_f32_to_bf16(src, dst, stream=None):
     _check(lib().am_cast_f32_to_bf16(
         src.numel(), _dev(src, "src", torch.float32), _dev(dst, "dst", torch.bfloat16),
         _stream(stream)))
+
+
+# ------------------------------------------- gated linear recurrences --
+
+def _dtype(t, name):
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, torch.bfloat16):
+        raise AmError(f"{name} must be a float32 or bfloat16 tensor")
+    return BF16 if t.dtype == torch.bfloat16 else F32
+
+
+def _shaped(t, name, shape, dtype=torch.float32):
+    """Device pointer of a contiguous GPU tensor of this shape, or None."""
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise AmError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _dev(t, name, dtype)
+
+
+def _rows(t, name, N, H, dtype):
+    """Device pointer and row stride of [N][H] rows, which may be columns of a
+    wider matrix; (None, H) for None."""
+    if t is None:
+        return None, H
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise AmError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise AmError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != (N, H):
+        raise AmError(f"{name} must have shape {(N, H)}, got {tuple(t.shape)}")
+    if N > 0 and H > 1 and t.stride(1) != 1:
+        raise AmError(f"{name} must have unit stride along its rows")
+    ld = t.stride(0) if N > 1 else H
+    if N > 1 and ld < H:
+        raise AmError(f"{name} has overlapping rows")
+    return ctypes.c_void_p(t.data_ptr()), ld
+
+
+def _packed_rows(T, B, lengths):
+    if lengths is None:
+        return None, None, T * B
+    arr, lp = _host_i32(lengths)
+    if arr.shape != (B,):
+        raise AmError(f"lengths must hold B = {B} values")
+    return arr, lp, int(arr.sum())
+
+
+def _workspace(ws):
+    if ws is None:
+        return None, 0
+    return _dev(ws, "ws"), ws.numel() * ws.element_size()
+
+
+def gated_recurrence_workspace_bytes(T, B, H, lengths=None, train=False) -> int:
+    n = lib().am_gated_recurrence_workspace_bytes(T, B, H, int(lengths is not None), int(bool(train)))
+    if n < 0:
+        raise AmError("invalid sizes for workspace query", EINVAL)
+    return int(n)
+
+
+def gated_recurrence_forward(x, r, i, lam, T, B, h, ws=None, lengths=None, h0=None, hT=None, c=8.0,
+                             train=False, stream=None):
+    """x, r, i: [N][H] rows (columns of one projection, say); h: [N][H]; lam:
+    [H]; h0, hT: [B][H] fp32 (hT may be h0)."""
+    dt, (N, H) = _dtype(x, "x"), h.shape
+    arr, lp, rows = _packed_rows(T, B, lengths)
+    if rows != N:
+        raise AmError(f"h must have {rows} rows, got {N}")
+    (xp, ldx), (rp, ldr), (ip, ldi) = (_rows(t, n, N, H, x.dtype)
+                                       for t, n in ((x, "x"), (r, "r"), (i, "i")))
+    wp, wn = _workspace(ws)
+    _check(lib().gated_recurrence_forward(
+        T, B, H, dt, lp, xp, ldx, rp, ldr, ip, ldi, _shaped(lam, "lam", (H,)), float(c),
+        _shaped(h0, "h0", (B, H)), _shaped(h, "h", (N, H), x.dtype), _shaped(hT, "hT", (B, H)),
+        int(bool(train)), wp, wn, _stream(stream)))
+
+
+def gated_recurrence_backward(x, r, i, lam, T, B, dh, ws, dx, dr, di, dlam, lengths=None, dhT=None,
+                              dh0=None, c=8.0, stream=None):
+    """The gradient of the forward call (train=True) that filled `ws`."""
+    dt, (N, H) = _dtype(x, "x"), x.shape
+    arr, lp, rows = _packed_rows(T, B, lengths)
+    if rows != N:
+        raise AmError(f"x must have {rows} rows, got {N}")
+    ((xp, ldx), (rp, ldr), (ip, ldi), (dhp, lddh), (dxp, lddx), (drp, lddr), (dip, lddi)) = (
+        _rows(t, n, N, H, x.dtype) for t, n in ((x, "x"), (r, "r"), (i, "i"), (dh, "dh"), (dx, "dx"),
+                                                (dr, "dr"), (di, "di")))
+    wp, wn = _workspace(ws)
+    _check(lib().gated_recurrence_backward(
+        T, B, H, dt, lp, xp, ldx, rp, ldr, ip, ldi, _shaped(lam, "lam", (H,)), float(c), dhp, lddh,
+        _shaped(dhT, "dhT", (B, H)), dxp, lddx, drp, lddr, dip, lddi, _shaped(dlam, "dlam", (H,)),
+        _shaped(dh0, "dh0", (B, H)), wp, wn, _stream(stream)))
+
+
+def gated_norm_workspace_bytes(N, H) -> int:
+    n = lib().am_gated_norm_workspace_bytes(N, H)
+    if n < 0:
+        raise AmError("invalid sizes for workspace query", EINVAL)
+    return int(n)
+
+
+def gated_norm_forward(res, o=None, gate=None, w_post=None, scale=None, w_next=None, res_out=None,
+                       y=None, rstd=None, eps=1e-6, stream=None):
+    """res, res_out: the residual stream, [N][H] fp32 or bf16; o, gate: [N][H]
+    rows; y: [N][H] of their type.  Every part may be left out (see the C ABI)."""
+    (N, H), act = res.shape, next((t for t in (o, y, res) if t is not None))
+    (op, ldo), (gp, ldg) = _rows(o, "o", N, H, act.dtype), _rows(gate, "gate", N, H, act.dtype)
+    _check(lib().gated_norm_forward(
+        N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
+        _shaped(scale, "scale", (H,)), _shaped(res, "res", (N, H), res.dtype),
+        _shaped(w_next, "w_next", (H,)), float(eps), _shaped(res_out, "res_out", (N, H), res.dtype),
+        _shaped(y, "y", (N, H), act.dtype), _shaped(rstd, "rstd", (N, 2)), _stream(stream)))
+
+
+def gated_norm_backward(res, rstd, dres, ws, o=None, gate=None, w_post=None, scale=None, w_next=None,
+                        dy=None, dres_out=None, do=None, dgate=None, dw_post=None, dscale=None,
+                        dw_next=None, eps=1e-6, stream=None):
+    """The gradient of gated_norm_forward with the same res (as it was before),
+    o, gate and factors, and the rstd it wrote."""
+    (N, H), act = res.shape, next((t for t in (o, dy, res) if t is not None))
+    ((op, ldo), (gp, ldg), (dop, lddo), (dgp, lddg)) = (
+        _rows(t, n, N, H, act.dtype) for t, n in ((o, "o"), (gate, "gate"), (do, "do"), (dgate, "dgate")))
+    wp, wn = _workspace(ws)
+    _check(lib().gated_norm_backward(
+        N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
+        _shaped(scale, "scale", (H,)), _shaped(res, "res", (N, H), res.dtype),
+        _shaped(w_next, "w_next", (H,)), float(eps), _shaped(rstd, "rstd", (N, 2)),
+        _shaped(dy, "dy", (N, H), act.dtype), _shaped(dres_out, "dres_out", (N, H), res.dtype),
+        dop, lddo, dgp, lddg, _shaped(dres, "dres", (N, H), res.dtype),
+        _shaped(dw_post, "dw_post", (H,)), _shaped(dscale, "dscale", (H,)),
+        _shaped(dw_next, "dw_next", (H,)), wp, wn, _stream(stream)))
+
+
+class _AdamWTensor(ctypes.Structure):
+    _fields_ = [("n", _I64)] + [(k, _P) for k in ("master", "weights_bf16", "grad", "m", "v", "m_scale",
+                                                  "v_scale")] + [("weight_decay", _F64)]
+
+
+ADAMW_BLOCK = 256  # elements that share a scale of 8-bit moments
+
+
+def adamw_scales(n) -> int:
+    """Scales of each 8-bit moment of a tensor of n elements."""
+    return -(-n // ADAMW_BLOCK)
+
+
+class AdamWTensors:
+    """The tensors of an optimizer step, as adamw_apply takes them: a list of
+    dicts of contiguous GPU tensors `master` (fp32), `grad` (fp32 or bf16, alike
+    in all of them), `m` and `v` (fp32, or 8-bit: torch.float8_e4m3fn or uint8,
+    then with fp32 `m_scale` and `v_scale` of adamw_scales(n) elements),
+    optionally `weights_bf16`, and a number `weight_decay`.  The list keeps the
+    tensors alive and passes their addresses; it holds nothing of a step."""
+
+    def __init__(self, tensors):
+        self.tensors = [dict(t) for t in tensors]
+        self.array = (_AdamWTensor * max(1, len(self.tensors)))()
+        for k, t in enumerate(self.tensors):
+            for name in ("master", "grad", "m", "v"):
+                if not isinstance(t.get(name), torch.Tensor):
+                    raise AmError(f"tensor {k} has no {name}")
+        first = self.tensors[0] if self.tensors else None
+        self.grad_dtype = _dtype(first["grad"], "grad") if first else F32
+        self.state_bits = 32 if first is None or first["m"].dtype == torch.float32 else 8
+        codes = (torch.float8_e4m3fn, torch.uint8)
+        for k, t in enumerate(self.tensors):
+            n, out = t["master"].numel(), self.array[k]
+            out.n, out.weight_decay = n, float(t.get("weight_decay", 0.0))
+            kinds = {"master": torch.float32, "weights_bf16": torch.bfloat16, "grad": first["grad"].dtype,
+                     "m": torch.float32, "v": torch.float32, "m_scale": torch.float32,
+                     "v_scale": torch.float32}
+            for name, kind in kinds.items():
+                v = t.get(name)
+                if v is None:
+                    if self.state_bits == 8 and "scale" in name:
+                        raise AmError(f"tensor {k} has no {name}")
+                    continue
+                if name in ("m", "v") and self.state_bits == 8:
+                    if v.dtype not in codes:
+                        raise AmError(f"tensor {k}: {name} must be torch.float8_e4m3fn or uint8")
+                    kind = v.dtype
+                if "scale" in name and self.state_bits == 32:
+                    raise AmError(f"tensor {k}: {name} with 32-bit moments")
+                if v.numel() != (adamw_scales(n) if "scale" in name else n):
+                    raise AmError(f"tensor {k}: {name} has {v.numel()} elements")
+                setattr(out, name, _dev(v, f"tensor {k}: {name}", kind))
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def adamw_apply(tensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, seed=0,
+                stream=None):
+    """One AdamW step of an AdamWTensors; grad_scale: [1] fp32 GPU tensor that the
+    gradients are multiplied by; seed: of the rounding of 8-bit moments."""
+    _check(lib().adamw_apply(
+        len(tensors), tensors.array, tensors.grad_dtype, tensors.state_bits, float(lr), float(beta1),
+        float(beta2), float(eps), int(step), _shaped(grad_scale, "grad_scale", (1,)),
+        int(seed) & 0xFFFFFFFF, _stream(stream)))
 
 
 # ------------------------------------------------------------------ timing --

@@ -293,6 +293,83 @@ hipError_t bmuf_update(int64_t n, int count, int workers, const float* models, i
                        float* wg, float* delta, float eta, float eta_next, float zeta,
                        float* local, uint16_t* local_bf16, hipStream_t s);
 
+// Gated linear recurrence (see gated_recurrence_forward in the C ABI).  A tile
+// of GR_TILE frames is GR_WAVES stretches of GR_STRETCH; a training forward pass
+// saves the state each tile starts from.
+constexpr int GR_STRETCH = 8, GR_WAVES = 8, GR_TILE = GR_STRETCH * GR_WAVES;
+struct GatedRecurrence {
+  const void *x, *r, *i;       // [N] rows of H, ldx, ldr, ldi apart
+  const void* dh;              // backward: [N] rows
+  void *dx, *dr, *di;          // backward: [N] rows (written)
+  int64_t ldx, ldr, ldi, lddh, lddx, lddr, lddi;
+  const float* lam;            // [H]
+  const float* h0;             // [B][H] or null (zero)
+  void* h;                     // forward: [N][H] (written)
+  float* hT;                   // forward: [B][H] or null
+  const float* dhT;            // backward: [B][H] or null (zero)
+  float* dh0;                  // backward: [B][H] or null
+  float* dlam;                 // backward: [H]
+  float* saved;                // [tiles][B][H] (written forward if not null)
+  float* parts;                // backward: [B][H] scratch
+  const int32_t *offs, *lens;  // [T + 1], [B], or null (every sequence has T frames)
+  int64_t N;
+  int T, B, H;                 // (T: the longest length)
+  float c;
+};
+hipError_t gated_forward(const GatedRecurrence& a, bool bf16, hipStream_t s);
+hipError_t gated_backward(const GatedRecurrence& a, bool bf16, hipStream_t s);
+// The tables of a batch of sorted lengths, MAX sequences a launch.
+struct GatedSchedule {
+  static constexpr int MAX = 400;
+  int32_t *offs, *lens, *tails;  // [T + 1], [B], [B] (written)
+  int T, B, first, count, last;
+  int32_t len[MAX], tail[MAX];   // tail: frames of this sequence and those after it
+};
+hipError_t gated_schedule(GatedSchedule a, const int32_t* lengths, hipStream_t s);
+
+// Gate, norm, residual and next norm (see gated_norm_forward in the C ABI); at
+// most GATED_NORM_BLOCKS workgroups, a row of parts each.
+constexpr int GATED_NORM_BLOCKS = 1024, GATED_NORM_MAX_H = 8192;
+struct GatedNorm {
+  int64_t N;
+  int H;
+  float eps;
+  const void *o, *gate;  // [N] rows ldo, ldg apart, or null
+  int64_t ldo, ldg;
+  const void* res;       // [N][H] of the stream's type
+  const float *w_post, *scale, *w_next;  // [H] or null
+  void *res_out, *y;     // forward: [N][H] (written)
+  float* rstd;           // [N][2]: written forward if not null, read backward
+  const void *dy, *dres_out;  // backward: [N][H], dres_out may be null
+  void *d_o, *dgate;     // backward: [N] rows lddo, lddg apart (written)
+  int64_t lddo, lddg;
+  void* dres;            // backward: [N][H] (written)
+  float *dw_post, *dscale, *dw_next;  // backward: [H] or null (written)
+  float* parts;          // backward: [GATED_NORM_BLOCKS][2][H] scratch
+};
+hipError_t gated_norm_forward(const GatedNorm& a, bool bf16, bool stream_bf16, hipStream_t s);
+hipError_t gated_norm_backward(const GatedNorm& a, bool bf16, bool stream_bf16, hipStream_t s);
+
+// AdamW step of up to MAX tensors, a workgroup for ADAMW_CHUNK elements of one.
+constexpr int ADAMW_CHUNK = 2048;
+struct AdamwOne {
+  float* w; uint16_t* w16; const void* g;
+  void *m, *v;                // fp32, or 8-bit codes with a scale per 256 elements
+  float *m_scale, *v_scale;
+  int64_t n;
+  float keep;                 // 1 - lr weight_decay
+  uint32_t key;               // of the rounding draws
+};
+struct AdamwBatch {
+  static constexpr int MAX = 48;
+  AdamwOne t[MAX];
+  uint32_t first[MAX + 1];    // first workgroup of each tensor; first[count] = all
+  int count;
+  float b1, c1, b2, c2, root, eps, step;
+  const float* grad_scale;    // device, or null
+};
+hipError_t adamw_launch(const AdamwBatch& a, bool grad_bf16, bool codes, hipStream_t s);
+
 // Elementwise and data-movement helpers.
 hipError_t sgd_apply_f32(int64_t n, float* master, uint16_t* w_bf16, const float* u, float lr,
                          hipStream_t s);

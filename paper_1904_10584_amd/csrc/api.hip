@@ -3,6 +3,7 @@
 // backward passes, and per-class kernel timing with HIP events.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -609,6 +610,115 @@ am_status encode_scratch_of(hipStream_t s, void** out) {
   }
   *out = g_scratch_ptr[dev];
   return AM_OK;
+}
+
+// ------------------------------------------- gated linear recurrences --
+
+// Rows of H elements that an operator reads or writes.
+am_status check_rows(int64_t N, int32_t H, int32_t dtype, const void* p, int64_t ld, const char* name) {
+  if (N > 0 && !p) return fail(AM_EINVAL, "NULL %s", name);
+  if (!aligned(p, (uintptr_t)esz_of(dtype))) return fail(AM_EINVAL, "%s is not aligned to its elements", name);
+  if (ld < H) return fail(AM_EINVAL, "row stride %lld of %s is less than %d", (long long)ld, name, H);
+  return AM_OK;
+}
+
+struct GatedLayout {
+  int64_t offs, lens, tails, saved, parts, total;
+};
+GatedLayout gated_layout(int64_t T, int64_t B, int64_t H, bool varlen, bool train) {
+  GatedLayout l{};
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += align256(bytes);
+    return here;
+  };
+  if (varlen) {
+    l.offs = take((T + 1) * 4);
+    l.lens = take(B * 4);
+    l.tails = take(B * 4);
+  }
+  if (train) {
+    l.saved = take((T + am::GR_TILE - 1) / am::GR_TILE * B * H * 4);
+    l.parts = take(B * H * 4);
+  }
+  l.total = at;
+  return l;
+}
+
+// The arguments that forward and backward share; fills in a's schedule.
+am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int32_t* lengths,
+                      const float* lam, float c, bool train, void* ws, int64_t ws_bytes,
+                      am::GatedRecurrence& a, GatedLayout& l) {
+  if (T < 0 || B < 1 || H < 1) return fail(AM_EINVAL, "need T >= 0, B >= 1 and H >= 1 (T=%d, B=%d, H=%d)", T, B, H);
+  if (dtype != AM_F32 && dtype != AM_BF16) return fail(AM_EINVAL, "dtype %d unknown", dtype);
+  if (!lam || !aligned(lam, 4)) return fail(AM_EINVAL, "NULL or unaligned lam");
+  if (!(c > 0.f && c <= 3.4e38f)) return fail(AM_EINVAL, "c must be positive and finite");
+  a.N = (int64_t)T * B;
+  a.T = T;
+  if (lengths) {
+    if (B > 1024) return fail(AM_EUNSUPPORTED, "variable-length batches allow B <= 1024");
+    a.N = 0;
+    for (int b = 0; b < B; ++b) {
+      if (lengths[b] < 0 || lengths[b] > T)
+        return fail(AM_EINVAL, "lengths[%d] = %d outside [0, %d]", b, lengths[b], T);
+      if (b > 0 && lengths[b] > lengths[b - 1])
+        return fail(AM_EINVAL, "lengths must be non-increasing (lengths[%d] > lengths[%d])", b, b - 1);
+      a.N += lengths[b];
+    }
+    a.T = lengths[0];
+  }
+  if (a.N >= (1ll << 31)) return fail(AM_EUNSUPPORTED, "too many frames");
+  if ((int64_t)B * H >= (1ll << 36)) return fail(AM_EUNSUPPORTED, "too many channels");
+  l = gated_layout(T, B, H, lengths != nullptr, train);
+  if (l.total > 0 && (!ws || !aligned(ws, 256) || ws_bytes < l.total))
+    return fail(AM_EWORKSPACE, "needs %lld workspace bytes, 256-byte aligned", (long long)l.total);
+  a.B = B;
+  a.H = H;
+  a.lam = lam;
+  a.c = c;
+  if (lengths) {
+    a.offs = at<int32_t>(ws, l.offs);
+    a.lens = at<int32_t>(ws, l.lens);
+  }
+  return AM_OK;
+}
+
+am_status check_norm(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, const void* o, int64_t ldo,
+                     const void* gate, int64_t ldg, const float* w_post, const float* scale, const void* res,
+                     const float* w_next, float eps, am::GatedNorm& a) {
+  if (N < 0 || H < 1) return fail(AM_EINVAL, "need N >= 0 and H >= 1 (N=%lld, H=%d)", (long long)N, H);
+  if (H > am::GATED_NORM_MAX_H) return fail(AM_EUNSUPPORTED, "rows of at most %d elements", am::GATED_NORM_MAX_H);
+  if ((dtype != AM_F32 && dtype != AM_BF16) || (res_dtype != AM_F32 && res_dtype != AM_BF16))
+    return fail(AM_EINVAL, "dtype %d or res_dtype %d unknown", dtype, res_dtype);
+  if (!(eps > 0.f && eps <= 3.4e38f)) return fail(AM_EINVAL, "eps must be positive and finite");
+  // (an empty matrix may have no address)
+  if (N > 0 && !o && (gate || w_post || scale)) return fail(AM_EINVAL, "gate, w_post or scale without o");
+  if (N > 0 && !o && !w_next) return fail(AM_EINVAL, "neither o nor w_next: nothing to do");
+  AM_TRY(check_rows(N, H, res_dtype, res, H, "res"));
+  if (o) AM_TRY(check_rows(N, H, dtype, o, ldo, "o"));
+  if (gate) AM_TRY(check_rows(N, H, dtype, gate, ldg, "gate"));
+  if (!aligned(w_post, 4) || !aligned(scale, 4) || !aligned(w_next, 4))
+    return fail(AM_EINVAL, "w_post, scale and w_next must be 4-byte aligned");
+  a.N = N;
+  a.H = H;
+  a.eps = eps;
+  a.o = N > 0 ? o : nullptr;
+  a.ldo = ldo;
+  a.gate = gate;
+  a.ldg = ldg;
+  a.res = res;
+  a.w_post = w_post;
+  a.scale = scale;
+  a.w_next = w_next;
+  return AM_OK;
+}
+
+double norm_bytes(const am::GatedNorm& a, int dtype, int res_dtype, bool backward) {
+  const double e = esz_of(dtype), f = esz_of(res_dtype);
+  const double act = (a.o ? 1 : 0) + (a.gate ? 1 : 0);
+  if (!backward) return (double)a.N * a.H * (e * (act + (a.w_next ? 1 : 0)) + f * (a.o ? 2 : 1));
+  return (double)a.N * a.H * (e * (2 * act + (a.w_next ? 1 : 0)) + f * (a.dres_out ? 3 : 2));
 }
 
 }  // namespace
@@ -1306,6 +1416,216 @@ am_status lstm_am_backward(const am_model* m, const void* params, const void* x,
   // its residual or weights
   Timed tm(AM_K_MISC, s, 0.0, 4.0);
   return hip_check(am::zero_if_set(sync_err(at<void>(ws, w.sync)), grads, po.n, s), "time-out guard");
+}
+
+// ------------------------------------------- gated linear recurrences --
+
+int64_t am_gated_recurrence_workspace_bytes(int32_t T, int32_t B, int32_t H, int32_t varlen, int32_t train) {
+  if (T < 0 || B < 1 || H < 1) return -1;
+  return gated_layout(T, B, H, varlen != 0, train != 0).total;
+}
+
+am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtype, const int32_t* lengths,
+                                   const void* x, int64_t ldx, const void* r, int64_t ldr, const void* i,
+                                   int64_t ldi, const float* lam, float c, const float* h0, void* h,
+                                   float* hT, int32_t train, void* ws, int64_t ws_bytes, void* stream) {
+  am::GatedRecurrence a{};
+  GatedLayout l;
+  AM_TRY(check_gated(T, B, H, dtype, lengths, lam, c, train != 0, ws, ws_bytes, a, l));
+  AM_TRY(check_rows(a.N, H, dtype, x, ldx, "x"));
+  AM_TRY(check_rows(a.N, H, dtype, r, ldr, "r"));
+  AM_TRY(check_rows(a.N, H, dtype, i, ldi, "i"));
+  AM_TRY(check_rows(a.N, H, dtype, h, H, "h"));
+  if (!aligned(h0, 4) || !aligned(hT, 4)) return fail(AM_EINVAL, "h0 and hT must be 4-byte aligned");
+  a.x = x; a.r = r; a.i = i;
+  a.ldx = ldx; a.ldr = ldr; a.ldi = ldi;
+  a.h0 = h0;
+  a.h = h;
+  a.hT = hT;
+  if (train) a.saved = at<float>(ws, l.saved);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (lengths) {
+    am::GatedSchedule g;
+    g.offs = at<int32_t>(ws, l.offs);
+    g.lens = at<int32_t>(ws, l.lens);
+    g.tails = at<int32_t>(ws, l.tails);
+    g.T = a.T;
+    g.B = B;
+    Timed tm(AM_K_MISC, s, 0.0, 4.0 * a.T + 8.0 * B);
+    AM_TRY(hip_check(am::gated_schedule(g, lengths, s), "schedule"));
+  }
+  Timed tm(AM_K_GATED, s, 20.0 * a.N * H, 4.0 * esz_of(dtype) * a.N * H + 8.0 * B * H);
+  return hip_check(am::gated_forward(a, dtype == AM_BF16, s), "gated recurrence");
+}
+
+am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dtype, const int32_t* lengths,
+                                    const void* x, int64_t ldx, const void* r, int64_t ldr, const void* i,
+                                    int64_t ldi, const float* lam, float c, const void* dh, int64_t lddh,
+                                    const float* dhT, void* dx, int64_t lddx, void* dr, int64_t lddr,
+                                    void* di, int64_t lddi, float* dlam, float* dh0, void* ws,
+                                    int64_t ws_bytes, void* stream) {
+  am::GatedRecurrence a{};
+  GatedLayout l;
+  AM_TRY(check_gated(T, B, H, dtype, lengths, lam, c, true, ws, ws_bytes, a, l));
+  AM_TRY(check_rows(a.N, H, dtype, x, ldx, "x"));
+  AM_TRY(check_rows(a.N, H, dtype, r, ldr, "r"));
+  AM_TRY(check_rows(a.N, H, dtype, i, ldi, "i"));
+  AM_TRY(check_rows(a.N, H, dtype, dh, lddh, "dh"));
+  AM_TRY(check_rows(a.N, H, dtype, dx, lddx, "dx"));
+  AM_TRY(check_rows(a.N, H, dtype, dr, lddr, "dr"));
+  AM_TRY(check_rows(a.N, H, dtype, di, lddi, "di"));
+  if (!dlam) return fail(AM_EINVAL, "NULL dlam");
+  if (!aligned(dhT, 4) || !aligned(dh0, 4) || !aligned(dlam, 4))
+    return fail(AM_EINVAL, "dhT, dh0 and dlam must be 4-byte aligned");
+  a.x = x; a.r = r; a.i = i; a.dh = dh;
+  a.dx = dx; a.dr = dr; a.di = di;
+  a.ldx = ldx; a.ldr = ldr; a.ldi = ldi; a.lddh = lddh;
+  a.lddx = lddx; a.lddr = lddr; a.lddi = lddi;
+  a.dhT = dhT;
+  a.dh0 = dh0;
+  a.dlam = dlam;
+  a.saved = at<float>(ws, l.saved);
+  a.parts = at<float>(ws, l.parts);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Timed tm(AM_K_GATED, s, 40.0 * a.N * H, 7.0 * esz_of(dtype) * a.N * H + 8.0 * B * H);
+  return hip_check(am::gated_backward(a, dtype == AM_BF16, s), "gated recurrence backward");
+}
+
+am_status gated_norm_forward(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, const void* o,
+                             int64_t ldo, const void* gate, int64_t ldg, const float* w_post,
+                             const float* scale, const void* res, const float* w_next, float eps,
+                             void* res_out, void* y, float* rstd, void* stream) {
+  am::GatedNorm a{};
+  AM_TRY(check_norm(N, H, dtype, res_dtype, o, ldo, gate, ldg, w_post, scale, res, w_next, eps, a));
+  if (o) AM_TRY(check_rows(N, H, res_dtype, res_out, H, "res_out"));
+  else if (N > 0 && res_out) return fail(AM_EINVAL, "res_out without o");
+  if (w_next) AM_TRY(check_rows(N, H, dtype, y, H, "y"));
+  else if (y) return fail(AM_EINVAL, "y without w_next");
+  if (!aligned(rstd, 4)) return fail(AM_EINVAL, "rstd must be 4-byte aligned");
+  a.res_out = res_out;
+  a.y = y;
+  a.rstd = rstd;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Timed tm(AM_K_NORM, s, 16.0 * N * H, norm_bytes(a, dtype, res_dtype, false));
+  return hip_check(am::gated_norm_forward(a, dtype == AM_BF16, res_dtype == AM_BF16, s), "gated norm");
+}
+
+int64_t am_gated_norm_workspace_bytes(int64_t N, int32_t H) {
+  if (N < 0 || H < 1 || H > am::GATED_NORM_MAX_H) return -1;
+  return align256((int64_t)am::GATED_NORM_BLOCKS * 2 * H * 4);
+}
+
+am_status gated_norm_backward(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, const void* o,
+                              int64_t ldo, const void* gate, int64_t ldg, const float* w_post,
+                              const float* scale, const void* res, const float* w_next, float eps,
+                              const float* rstd, const void* dy, const void* dres_out, void* d_o,
+                              int64_t lddo, void* dgate, int64_t lddg, void* dres, float* dw_post,
+                              float* dscale, float* dw_next, void* ws, int64_t ws_bytes, void* stream) {
+  am::GatedNorm a{};
+  AM_TRY(check_norm(N, H, dtype, res_dtype, o, ldo, gate, ldg, w_post, scale, res, w_next, eps, a));
+  if (N > 0 && (!rstd || !aligned(rstd, 4))) return fail(AM_EINVAL, "NULL or unaligned rstd");
+  if (w_next) AM_TRY(check_rows(N, H, dtype, dy, H, "dy"));
+  else if (dy) return fail(AM_EINVAL, "dy without w_next");
+  if (dres_out) AM_TRY(check_rows(N, H, res_dtype, dres_out, H, "dres_out"));
+  AM_TRY(check_rows(N, H, res_dtype, dres, H, "dres"));
+  if (o) AM_TRY(check_rows(N, H, dtype, d_o, lddo, "d_o"));
+  else if (N > 0 && d_o) return fail(AM_EINVAL, "d_o without o");
+  if (gate) AM_TRY(check_rows(N, H, dtype, dgate, lddg, "dgate"));
+  else if (N > 0 && dgate) return fail(AM_EINVAL, "dgate without gate");
+  if ((dw_post && !w_post) || (dscale && !scale) || (dw_next && !w_next))
+    return fail(AM_EINVAL, "gradient of a factor that is NULL");
+  if ((w_post && !dw_post) || (scale && !dscale) || (w_next && !dw_next))
+    return fail(AM_EINVAL, "NULL gradient of w_post, scale or w_next");
+  if (!aligned(dw_post, 4) || !aligned(dscale, 4) || !aligned(dw_next, 4))
+    return fail(AM_EINVAL, "gradients of the factors must be 4-byte aligned");
+  if (!ws || !aligned(ws, 256)) return fail(AM_EWORKSPACE, "NULL or unaligned workspace");
+  if (ws_bytes < am_gated_norm_workspace_bytes(N, H))
+    return fail(AM_EWORKSPACE, "backward needs %lld workspace bytes",
+                (long long)am_gated_norm_workspace_bytes(N, H));
+  a.rstd = const_cast<float*>(rstd);
+  a.dy = dy;
+  a.dres_out = dres_out;
+  a.d_o = d_o;
+  a.lddo = lddo;
+  a.dgate = dgate;
+  a.lddg = lddg;
+  a.dres = dres;
+  a.dw_post = dw_post;
+  a.dscale = dscale;
+  a.dw_next = dw_next;
+  a.parts = static_cast<float*>(ws);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Timed tm(AM_K_NORM, s, 44.0 * N * H, norm_bytes(a, dtype, res_dtype, true));
+  return hip_check(am::gated_norm_backward(a, dtype == AM_BF16, res_dtype == AM_BF16, s), "gated norm backward");
+}
+
+am_status adamw_apply(int32_t count, const am_adamw_tensor* tensors, int32_t grad_dtype, int32_t state_bits,
+                      double lr, double beta1, double beta2, double eps, int64_t step,
+                      const float* grad_scale, uint32_t seed, void* stream) {
+  if (count < 0 || (count > 0 && !tensors)) return fail(AM_EINVAL, "bad tensor list");
+  if (grad_dtype != AM_F32 && grad_dtype != AM_BF16) return fail(AM_EINVAL, "grad_dtype %d unknown", grad_dtype);
+  if (state_bits != 32 && state_bits != 8) return fail(AM_EINVAL, "state_bits must be 32 or 8");
+  if (!(lr >= 0.0 && lr <= 3.4e38) || !(eps >= 0.0 && eps <= 3.4e38))
+    return fail(AM_EINVAL, "lr and eps must be finite and not negative");
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0))
+    return fail(AM_EINVAL, "beta1 and beta2 must be in [0, 1)");
+  if (step < 1) return fail(AM_EINVAL, "step counts from 1");
+  if (!aligned(grad_scale, 4)) return fail(AM_EINVAL, "grad_scale must be 4-byte aligned");
+  const bool codes = state_bits == 8;
+  int64_t all = 0;
+  for (int k = 0; k < count; ++k) {
+    const am_adamw_tensor& t = tensors[k];
+    if (t.n < 0 || t.n >= (1ll << 40)) return fail(AM_EINVAL, "tensor %d: %lld elements", k, (long long)t.n);
+    if (!(t.weight_decay >= 0.0 && t.weight_decay <= 3.4e38))
+      return fail(AM_EINVAL, "tensor %d: weight_decay must be finite and not negative", k);
+    if (t.n == 0) continue;
+    if (!t.master || !t.grad || !t.m || !t.v || (codes && (!t.m_scale || !t.v_scale)))
+      return fail(AM_EINVAL, "tensor %d: NULL master, grad, moment or scale", k);
+    const uintptr_t ga = grad_dtype == AM_BF16 ? 2 : 4, ma = codes ? 1 : 4;
+    if (!aligned(t.master, 4) || !aligned(t.weights_bf16, 2) || !aligned(t.grad, ga) || !aligned(t.m, ma) ||
+        !aligned(t.v, ma) || !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4))
+      return fail(AM_EINVAL, "tensor %d: pointer not aligned to its elements", k);
+    all += t.n;
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Timed tm(AM_K_ADAMW, s, 14.0 * all, (10.0 + (grad_dtype == AM_BF16 ? 2 : 4) + (codes ? 4 : 16)) * all);
+  am::AdamwBatch a{};
+  a.b1 = (float)beta1;
+  a.c1 = (float)(1.0 - beta1);
+  a.b2 = (float)beta2;
+  a.c2 = (float)(1.0 - beta2);
+  a.eps = (float)eps;
+  a.root = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
+  a.step = (float)(lr / (1.0 - pow(beta1, (double)step)));
+  a.grad_scale = grad_scale;
+  uint64_t groups = 0;
+  for (int k = 0; k < count; ++k) {
+    const am_adamw_tensor& t = tensors[k];
+    if (t.n > 0) {
+      const uint64_t need = (uint64_t)((t.n + am::ADAMW_CHUNK - 1) / am::ADAMW_CHUNK);
+      if (a.count == am::AdamwBatch::MAX || (a.count > 0 && groups + need >= (1ull << 31))) {
+        AM_TRY(hip_check(am::adamw_launch(a, grad_dtype == AM_BF16, codes, s), "adamw"));
+        a.count = 0;
+        groups = 0;
+      }
+      am::AdamwOne& o = a.t[a.count];
+      o.w = t.master;
+      o.w16 = static_cast<uint16_t*>(t.weights_bf16);
+      o.g = t.grad;
+      o.m = t.m;
+      o.v = t.v;
+      o.m_scale = t.m_scale;
+      o.v_scale = t.v_scale;
+      o.n = t.n;
+      o.keep = (float)(1.0 - lr * t.weight_decay);
+      o.key = seed + (uint32_t)k * 0x9E3779B9u;
+      a.first[a.count] = (uint32_t)groups;
+      groups += need;
+      a.first[++a.count] = (uint32_t)groups;
+    }
+  }
+  if (a.count > 0) return hip_check(am::adamw_launch(a, grad_dtype == AM_BF16, codes, s), "adamw");
+  return AM_OK;
 }
 
 // ---------------------------------------------------------------- timing --

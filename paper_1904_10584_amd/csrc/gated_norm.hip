@@ -1,0 +1,330 @@
+// What stands between two blocks of a residual stack, a row (frame) at a time:
+//   u = o silu(gate)            the block's output under its gate
+//   p = u / rms(u)              normed,
+//   R = res + scale w_post p    scaled and added to the residual stream, and
+//   y = R / rms(R) w_next       the norm that the next block reads,
+// rms(z) = sqrt(mean z^2 + eps), and the gradient of it all.  HBM bounds it:
+// every input is read once and every output written once, so a row stays in the
+// registers of its wave (of its four waves if it is long) across both norms.
+#include "am_device.h"
+#include "am_internal.h"
+
+namespace am {
+namespace {
+
+typedef f32x4_t f32x4_u __attribute__((aligned(4)));
+typedef uint16_t u16x4_t __attribute__((ext_vector_type(4)));
+typedef u16x4_t u16x4_u __attribute__((aligned(2)));
+
+// Four elements from a place of a row of H, those past its end as zeros; rows of
+// odd lengths start at any element, which the memory instructions take.
+__device__ __forceinline__ f32x4_t wide(f32x4_t v) { return v; }
+__device__ __forceinline__ f32x4_t wide(u16x4_t v) {
+  f32x4_t o;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = bf16_to_f32(v[k]);
+  return o;
+}
+template <typename T> struct Four;
+template <> struct Four<float> { typedef f32x4_t type; typedef f32x4_u at; };
+template <> struct Four<bf16_t> { typedef u16x4_t type; typedef u16x4_u at; };
+
+template <typename T>
+__device__ __forceinline__ typename Four<T>::type load4(const T* row, int e, int H) {
+  typename Four<T>::type v = {0, 0, 0, 0};
+  if (e + 4 <= H) {
+    v = *reinterpret_cast<const typename Four<T>::at*>(row + e);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (e + k < H) v[k] = row[e + k];
+  }
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* row, int e, int H, f32x4_t v) {
+  typename Four<T>::type o;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = from_f32<T>(v[k]);
+  if (e + 4 <= H) {
+    *reinterpret_cast<typename Four<T>::at*>(row + e) = o;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (e + k < H) row[e + k] = o[k];
+  }
+}
+
+constexpr int WAVES = 4;  // waves of a workgroup
+
+// The sum over the row's WPR waves (1, or all of the workgroup), in each of them.
+template <int WPR>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+  v = wave_sum(v);
+  if constexpr (WPR == 1) return v;
+  const int w = threadIdx.x >> 6;
+  __syncthreads();  // the last sum has been read
+  if ((threadIdx.x & 63) == 0) red[w] = v;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+template <typename T, typename R, int NV, int WPR>
+__global__ __launch_bounds__(256) void norm_forward_kernel(GatedNorm a) {
+  __shared__ float red[WAVES];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int H = a.H, e0 = 4 * (WPR == 1 ? lane : (int)threadIdx.x);
+  const float inv = 1.f / (float)H;
+  f32x4_t add[NV], next[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int e = e0 + k * 256 * WPR;
+    const f32x4_t one = {1.f, 1.f, 1.f, 1.f};
+    add[k] = (a.w_post ? load4(a.w_post, e, H) : one) * (a.scale ? load4(a.scale, e, H) : one);
+    next[k] = a.w_next ? load4(a.w_next, e, H) : one;
+  }
+  constexpr int ROWS = WAVES / WPR;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + (WPR == 1 ? w : 0); row < a.N;
+       row += (int64_t)gridDim.x * ROWS) {
+    f32x4_t u[NV], t[NV];
+    const R* res = static_cast<const R*>(a.res) + row * H;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) t[k] = wide(load4(res, e0 + k * 256 * WPR, H));
+    float rstd_u = 1.f;
+    if (a.o) {
+      const T* o = static_cast<const T*>(a.o) + row * a.ldo;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) u[k] = wide(load4(o, e0 + k * 256 * WPR, H));
+      if (a.gate) {
+        const T* gate = static_cast<const T*>(a.gate) + row * a.ldg;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const f32x4_t g = wide(load4(gate, e0 + k * 256 * WPR, H));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) u[k][j] *= g[j] * sigm(g[j]);
+        }
+      }
+      if (a.w_post) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s = fmaf(u[k][j], u[k][j], s);
+        rstd_u = rsqrtf(row_sum<WPR>(s, red) * inv + a.eps);
+      }
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[k][j] = fmaf(u[k][j] * rstd_u, add[k][j], t[k][j]);
+      R* out = static_cast<R*>(a.res_out) + row * H;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) store4(out, e0 + k * 256 * WPR, H, t[k]);
+    }
+    float rstd_n = 1.f;
+    if (a.w_next) {
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = fmaf(t[k][j], t[k][j], s);
+      rstd_n = rsqrtf(row_sum<WPR>(s, red) * inv + a.eps);
+      T* y = static_cast<T*>(a.y) + row * H;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) store4(y, e0 + k * 256 * WPR, H, t[k] * rstd_n * next[k]);
+    }
+    if (a.rstd && (WPR == 1 ? lane : (int)threadIdx.x) == 0) {
+      a.rstd[2 * row] = rstd_u;
+      a.rstd[2 * row + 1] = rstd_n;
+    }
+  }
+}
+
+// With n = R / rms(R), dn = dy w_next:  dR = dres_out + (dn - n mean(dn n)) / rms(R),
+// the gradient of res; dp = dR scale w_post;  du = (dp - p mean(dp p)) / rms(u), and
+// from it those of o and gate.  R and p are evaluated again from the forward
+// pass's inputs (in 32 bits, whatever the stream holds) with its 1 / rms.  The
+// gradients of w_post and scale are scale and w_post times the same column sum
+// of dR p; the sums run down a wave's rows in its registers and leave as one row
+// per workgroup.
+template <typename T, typename R, int NV, int WPR>
+__global__ __launch_bounds__(256) void norm_backward_kernel(GatedNorm a) {
+  __shared__ float red[WAVES];
+  __shared__ f32x4_t sums[2][WPR == 1 ? NV * 64 : 1];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int H = a.H, e0 = 4 * (WPR == 1 ? lane : (int)threadIdx.x);
+  const float inv = 1.f / (float)H;
+  f32x4_t add[NV], next[NV], along[NV], ndy[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int e = e0 + k * 256 * WPR;
+    const f32x4_t one = {1.f, 1.f, 1.f, 1.f};
+    add[k] = (a.w_post ? load4(a.w_post, e, H) : one) * (a.scale ? load4(a.scale, e, H) : one);
+    next[k] = a.w_next ? load4(a.w_next, e, H) : one;
+    along[k] = ndy[k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  constexpr int ROWS = WAVES / WPR;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + (WPR == 1 ? w : 0); row < a.N;
+       row += (int64_t)gridDim.x * ROWS) {
+    f32x4_t p[NV], t[NV], d[NV];
+    typename Four<T>::type o[NV], g[NV];
+    const float rstd_u = a.rstd[2 * row], rstd_n = a.rstd[2 * row + 1];
+    const R* res = static_cast<const R*>(a.res) + row * H;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) t[k] = wide(load4(res, e0 + k * 256 * WPR, H));
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      d[k] = a.dres_out ? wide(load4(static_cast<const R*>(a.dres_out) + row * H, e0 + k * 256 * WPR, H))
+                        : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if (a.o) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        o[k] = load4(static_cast<const T*>(a.o) + row * a.ldo, e0 + k * 256 * WPR, H);
+        if (a.gate) g[k] = load4(static_cast<const T*>(a.gate) + row * a.ldg, e0 + k * 256 * WPR, H);
+      }
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        p[k] = wide(o[k]) * rstd_u;
+        if (a.gate) {
+          const f32x4_t gv = wide(g[k]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) p[k][j] *= gv[j] * sigm(gv[j]);
+        }
+        t[k] += p[k] * add[k];
+      }
+    }
+    if (a.w_next) {
+      f32x4_t dy[NV];
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        dy[k] = wide(load4(static_cast<const T*>(a.dy) + row * H, e0 + k * 256 * WPR, H));
+        t[k] *= rstd_n;
+        ndy[k] += dy[k] * t[k];
+        dy[k] *= next[k];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = fmaf(dy[k][j], t[k][j], s);
+      }
+      s = row_sum<WPR>(s, red) * inv;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) d[k] += (dy[k] - t[k] * s) * rstd_n;
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      store4(static_cast<R*>(a.dres) + row * H, e0 + k * 256 * WPR, H, d[k]);
+    if (a.o) {
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        along[k] += d[k] * p[k];
+        d[k] *= add[k];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = fmaf(d[k][j], p[k][j], s);
+      }
+      if (a.w_post) s = row_sum<WPR>(s, red) * inv;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const f32x4_t ov = wide(o[k]);
+        f32x4_t du = d[k];
+        if (a.w_post) du = (du - p[k] * s) * rstd_u;
+        f32x4_t dov = du;
+        if (a.gate) {
+          const f32x4_t gv = wide(g[k]);
+          f32x4_t dg;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float sg = sigm(gv[j]);
+            dov[j] = du[j] * gv[j] * sg;
+            dg[j] = du[j] * ov[j] * sg * (1.f + gv[j] * (1.f - sg));
+          }
+          store4(static_cast<T*>(a.dgate) + row * a.lddg, e0 + k * 256 * WPR, H, dg);
+        }
+        store4(static_cast<T*>(a.d_o) + row * a.lddo, e0 + k * 256 * WPR, H, dov);
+      }
+    }
+  }
+  // the column sums of this workgroup's rows, wave after wave
+  if constexpr (WPR == 1) {
+    for (int s = 0; s < WAVES; ++s) {
+      if (w == s)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          if (s > 0) {
+            along[k] += sums[0][k * 64 + lane];
+            ndy[k] += sums[1][k * 64 + lane];
+          }
+          sums[0][k * 64 + lane] = along[k];
+          sums[1][k * 64 + lane] = ndy[k];
+        }
+      __syncthreads();
+    }
+    if (w != WAVES - 1) return;
+  }
+  float* parts = a.parts + (int64_t)blockIdx.x * 2 * H;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    store4(parts, e0 + k * 256 * WPR, H, along[k]);
+    store4(parts + H, e0 + k * 256 * WPR, H, ndy[k]);
+  }
+}
+
+// Column sums of parts [rows][2][H] in order: 16 columns a workgroup, 16 threads
+// each.
+__global__ __launch_bounds__(256) void norm_weights_kernel(const float* __restrict__ parts, int rows,
+                                                           GatedNorm a) {
+  __shared__ float sum[16][17];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4;
+  float s = 0.f;
+  if (c < 2 * a.H)
+    for (int k = q; k < rows; k += 16) s += parts[(int64_t)k * 2 * a.H + c];
+  sum[q][threadIdx.x & 15] = s;
+  __syncthreads();
+  if (q != 0 || c >= 2 * a.H) return;
+  for (int k = 1; k < 16; ++k) s += sum[k][threadIdx.x & 15];
+  if (c >= a.H) {
+    if (a.dw_next) a.dw_next[c - a.H] = s;
+  } else {
+    if (a.dw_post) a.dw_post[c] = s * (a.scale ? a.scale[c] : 1.f);
+    if (a.dscale) a.dscale[c] = s * (a.w_post ? a.w_post[c] : 1.f);
+  }
+}
+
+template <typename T, typename R, int NV, int WPR>
+hipError_t launch(const GatedNorm& a, bool forward, hipStream_t s) {
+  const int64_t blocks = (a.N * WPR + WAVES - 1) / WAVES;
+  const unsigned grid = (unsigned)(blocks < GATED_NORM_BLOCKS ? blocks : GATED_NORM_BLOCKS);
+  if (forward) {
+    hipLaunchKernelGGL((norm_forward_kernel<T, R, NV, WPR>), dim3(grid), dim3(256), 0, s, a);
+  } else {
+    if (grid > 0) hipLaunchKernelGGL((norm_backward_kernel<T, R, NV, WPR>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2 * a.H + 15) / 16)), dim3(256), 0, s, a.parts,
+                       (int)grid, a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, typename R>
+hipError_t sized(const GatedNorm& a, bool forward, hipStream_t s) {
+  if (a.H <= 256) return launch<T, R, 1, 1>(a, forward, s);
+  if (a.H <= 512) return launch<T, R, 2, 1>(a, forward, s);
+  if (a.H <= 768) return launch<T, R, 3, 1>(a, forward, s);
+  if (a.H <= 1024) return launch<T, R, 4, 1>(a, forward, s);
+  if (a.H <= 2048) return launch<T, R, 2, 4>(a, forward, s);
+  if (a.H <= 4096) return launch<T, R, 4, 4>(a, forward, s);
+  return launch<T, R, 8, 4>(a, forward, s);
+}
+
+hipError_t route(const GatedNorm& a, bool bf16, bool stream_bf16, bool forward, hipStream_t s) {
+  if (bf16) return stream_bf16 ? sized<bf16_t, bf16_t>(a, forward, s) : sized<bf16_t, float>(a, forward, s);
+  return stream_bf16 ? sized<float, bf16_t>(a, forward, s) : sized<float, float>(a, forward, s);
+}
+
+}  // namespace
+
+hipError_t gated_norm_forward(const GatedNorm& a, bool bf16, bool stream_bf16, hipStream_t s) {
+  return a.N == 0 ? hipSuccess : route(a, bf16, stream_bf16, true, s);
+}
+hipError_t gated_norm_backward(const GatedNorm& a, bool bf16, bool stream_bf16, hipStream_t s) {
+  return route(a, bf16, stream_bf16, false, s);
+}
+
+}  // namespace am

@@ -1,0 +1,154 @@
+"""Refusals of the gated recurrence, the norms and the AdamW step, on the host:
+the status, a message, and nothing enqueued (no GPU is needed to get there)."""
+
+import ctypes
+
+import pytest
+import torch
+
+from paper_1904_10584_amd import binding as am
+
+P = ctypes.c_void_p(0x100000)  # never dereferenced: validation fails first
+ODD = ctypes.c_void_p(0x100001)
+
+
+@pytest.fixture(scope="module")
+def L():
+    return am.lib()
+
+
+def _lens(*v):
+    return (ctypes.c_int32 * len(v))(*v)
+
+
+def _forward(L, T=5, B=2, H=64, dtype=am.BF16, lengths=None, x=P, ldx=64, r=P, ldr=64, i=P, ldi=64, lam=P,
+             c=8.0, h0=None, h=P, hT=None, train=0, ws=None, ws_bytes=0):
+    st = L.gated_recurrence_forward(T, B, H, dtype, lengths, x, ldx, r, ldr, i, ldi, lam, c, h0, h, hT,
+                                    train, ws, ws_bytes, None)
+    return st, L.am_last_error().decode()
+
+
+@pytest.mark.parametrize("bad,status,word", [
+    (dict(T=-1), am.EINVAL, "T"), (dict(B=0), am.EINVAL, "B"), (dict(H=0), am.EINVAL, "H"),
+    (dict(dtype=2), am.EINVAL, "dtype"), (dict(lam=None), am.EINVAL, "lam"), (dict(c=0.0), am.EINVAL, "c must"),
+    (dict(c=float("nan")), am.EINVAL, "c must"), (dict(c=float("inf")), am.EINVAL, "c must"),
+    (dict(x=None), am.EINVAL, "x"), (dict(r=None), am.EINVAL, "r"), (dict(i=None), am.EINVAL, "i"),
+    (dict(h=None), am.EINVAL, "h"), (dict(ldx=63), am.EINVAL, "row stride"), (dict(r=ODD), am.EINVAL, "aligned"),
+    (dict(h0=ODD), am.EINVAL, "aligned"), (dict(lengths=_lens(2, 5)), am.EINVAL, "non-increasing"),
+    (dict(lengths=_lens(6, 5)), am.EINVAL, "outside"), (dict(lengths=_lens(5, -1)), am.EINVAL, "outside"),
+    (dict(lengths=_lens(5, 4)), am.EWORKSPACE, "workspace"), (dict(train=1), am.EWORKSPACE, "workspace"),
+    (dict(train=1, ws=P, ws_bytes=100), am.EWORKSPACE, "workspace"),
+    (dict(train=1, ws=ODD, ws_bytes=1 << 30), am.EWORKSPACE, "256"),
+    (dict(T=1 << 20, B=1 << 12), am.EUNSUPPORTED, "frames"),
+])
+def test_recurrence_refusals(L, bad, status, word):
+    st, msg = _forward(L, **bad)
+    assert st == status and word in msg
+
+
+def test_recurrence_batches_of_lengths_are_bounded(L):
+    st, msg = _forward(L, B=1025, lengths=_lens(*([1] * 1025)))
+    assert st == am.EUNSUPPORTED and "1024" in msg
+
+
+def test_recurrence_backward_refusals(L):
+    need = L.am_gated_recurrence_workspace_bytes(5, 2, 64, 0, 1)
+    good = dict(T=5, B=2, H=64, dtype=am.BF16, lengths=None, x=P, ldx=64, r=P, ldr=64, i=P, ldi=64, lam=P,
+                c=8.0, dh=P, lddh=64, dhT=None, dx=P, lddx=64, dr=P, lddr=64, di=P, lddi=64, dlam=P, dh0=None,
+                ws=P, ws_bytes=need)
+    for bad, status in ((dict(dh=None), am.EINVAL), (dict(dx=None), am.EINVAL), (dict(lddi=10), am.EINVAL),
+                        (dict(dlam=None), am.EINVAL), (dict(dlam=ODD), am.EINVAL), (dict(ws=None), am.EWORKSPACE),
+                        (dict(ws_bytes=need - 1), am.EWORKSPACE), (dict(lddh=0), am.EINVAL)):
+        st = L.gated_recurrence_backward(*{**good, **bad}.values(), None)
+        assert st == status and L.am_last_error(), bad
+
+
+def test_recurrence_workspace(L):
+    assert L.am_gated_recurrence_workspace_bytes(1, 64, 768, 0, 0) == 0
+    assert L.am_gated_recurrence_workspace_bytes(-1, 1, 1, 0, 0) == -1
+    assert L.am_gated_recurrence_workspace_bytes(1, 0, 1, 0, 0) == -1
+    assert L.am_gated_recurrence_workspace_bytes(1, 1, 0, 0, 0) == -1
+    assert L.am_gated_recurrence_workspace_bytes(100, 2, 64, 1, 1) % 256 == 0
+
+
+def test_norm_refusals(L):
+    good = dict(N=4, H=64, dtype=am.BF16, res_dtype=am.F32, o=P, ldo=64, gate=P, ldg=64, w_post=P, scale=P,
+                res=P, w_next=P, eps=1e-6, res_out=P, y=P, rstd=None)
+    for bad, status, word in (
+            (dict(N=-1), am.EINVAL, "N"), (dict(H=0), am.EINVAL, "H"), (dict(H=8193), am.EUNSUPPORTED, "8192"),
+            (dict(dtype=5), am.EINVAL, "dtype"), (dict(res_dtype=-1), am.EINVAL, "dtype"),
+            (dict(eps=0.0), am.EINVAL, "eps"), (dict(eps=float("nan")), am.EINVAL, "eps"),
+            (dict(o=None), am.EINVAL, "without o"), (dict(ldg=3), am.EINVAL, "row stride"),
+            (dict(res=None), am.EINVAL, "res"), (dict(res_out=None), am.EINVAL, "res_out"),
+            (dict(y=None), am.EINVAL, "y"), (dict(w_next=None), am.EINVAL, "y without"),
+            (dict(o=None, gate=None, w_post=None, scale=None), am.EINVAL, "res_out without"),
+            (dict(o=None, gate=None, w_post=None, scale=None, w_next=None, res_out=None, y=None), am.EINVAL,
+             "nothing to do"), (dict(scale=ODD), am.EINVAL, "aligned"), (dict(o=ODD), am.EINVAL, "aligned")):
+        st = L.gated_norm_forward(*{**good, **bad}.values(), None)
+        assert st == status and word in L.am_last_error().decode(), bad
+
+
+def test_norm_backward_refusals(L):
+    need = L.am_gated_norm_workspace_bytes(4, 64)
+    good = dict(N=4, H=64, dtype=am.BF16, res_dtype=am.F32, o=P, ldo=64, gate=P, ldg=64, w_post=P, scale=P,
+                res=P, w_next=P, eps=1e-6, rstd=P, dy=P, dres_out=P, d_o=P, lddo=64, dgate=P, lddg=64, dres=P,
+                dw_post=P, dscale=P, dw_next=P, ws=P, ws_bytes=need)
+    for bad, status in ((dict(rstd=None), am.EINVAL), (dict(dy=None), am.EINVAL), (dict(dres=None), am.EINVAL),
+                        (dict(d_o=None), am.EINVAL), (dict(dgate=None), am.EINVAL), (dict(lddg=1), am.EINVAL),
+                        (dict(dw_post=None), am.EINVAL), (dict(scale=None), am.EINVAL),
+                        (dict(w_next=None), am.EINVAL), (dict(ws=None), am.EWORKSPACE),
+                        (dict(ws_bytes=need - 1), am.EWORKSPACE), (dict(dw_next=ODD), am.EINVAL)):
+        st = L.gated_norm_backward(*{**good, **bad}.values(), None)
+        assert st == status and L.am_last_error(), bad
+    assert L.am_gated_norm_workspace_bytes(-1, 64) == -1 and L.am_gated_norm_workspace_bytes(1, 8193) == -1
+
+
+def _tensor(**kw):
+    t = am._AdamWTensor()
+    t.n, t.weight_decay = kw.pop("n", 10), kw.pop("weight_decay", 0.0)
+    for k in ("master", "grad", "m", "v"):
+        setattr(t, k, 0x100000)
+    for k, v in kw.items():
+        setattr(t, k, v)
+    return (am._AdamWTensor * 1)(t)
+
+
+def test_adamw_refusals(L):
+    good = dict(count=1, tensors=_tensor(), grad_dtype=am.F32, state_bits=32, lr=1e-3, beta1=0.9, beta2=0.999,
+                eps=1e-8, step=1, grad_scale=None, seed=0)
+    nan = float("nan")
+    for bad in (dict(count=-1), dict(tensors=None), dict(grad_dtype=2), dict(state_bits=16), dict(lr=-1.0),
+                dict(lr=nan), dict(lr=float("inf")), dict(beta1=1.0), dict(beta1=nan), dict(beta2=-0.1),
+                dict(eps=-1e-9), dict(eps=nan), dict(step=0), dict(grad_scale=ODD), dict(tensors=_tensor(n=-1)),
+                dict(tensors=_tensor(master=None)), dict(tensors=_tensor(grad=None)),
+                dict(tensors=_tensor(m=None)), dict(tensors=_tensor(v=0x100002)),
+                dict(tensors=_tensor(master=0x100002)), dict(tensors=_tensor(weights_bf16=0x100001)),
+                dict(tensors=_tensor(weight_decay=-1.0)), dict(tensors=_tensor(weight_decay=nan)),
+                dict(state_bits=8), dict(tensors=_tensor(n=1 << 40))):
+        st = L.adamw_apply(*{**good, **bad}.values(), None)
+        assert st == am.EINVAL and L.am_last_error(), bad
+
+
+def test_adamw_nothing_to_do(L):
+    assert L.adamw_apply(0, None, am.F32, 32, 1e-3, 0.9, 0.999, 1e-8, 1, None, 0, None) == am.OK
+    assert L.adamw_apply(1, _tensor(n=0), am.F32, 8, 1e-3, 0.9, 0.999, 1e-8, 1, None, 0, None) == am.OK
+
+
+def test_binding_refuses_host_tensors_and_wrong_types():
+    x = torch.zeros(4, 8)
+    with pytest.raises(am.AmError, match="GPU"):
+        am.gated_recurrence_forward(x, x, x, torch.zeros(8), 4, 1, x)
+    with pytest.raises(am.AmError, match="rows"):
+        am.gated_recurrence_forward(x, x, x, torch.zeros(8), 5, 1, x)
+    with pytest.raises(am.AmError, match="float32 or bfloat16"):
+        am.gated_recurrence_forward(x.double(), x, x, torch.zeros(8), 4, 1, x)
+    with pytest.raises(am.AmError, match="GPU"):
+        am.gated_norm_forward(x, w_next=torch.ones(8), y=x)
+    with pytest.raises(am.AmError, match="no m"):
+        am.AdamWTensors([dict(master=x, grad=x, m=None, v=x)])
+    with pytest.raises(am.AmError, match="elements|GPU"):
+        am.AdamWTensors([dict(master=x, grad=x, m=x[:2], v=x)])
+    with pytest.raises(am.AmError):
+        am.gated_recurrence_workspace_bytes(-1, 1, 1)
+    with pytest.raises(am.AmError):
+        am.gated_norm_workspace_bytes(1, 9000)

@@ -1,0 +1,256 @@
+"""Gated linear recurrence: forward and backward against the fp64 oracle.
+
+Tolerances: every value is evaluated in fp32 and rounded once.  An error of a
+few units of 2^-24 in a_t is carried on for 1 / (1 - a) frames, at most the few
+hundred of these cases: 300 * 3 * 2^-24 = 5e-5, so 1e-4 for fp32 outputs; a bf16
+output adds its own rounding of 2^-9: 2^-8 covers both."""
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import assert_close
+from oracle import gated
+from paper_1904_10584_amd import binding as am
+
+pytestmark = pytest.mark.gpu
+
+F32_TOL, BF16_TOL = 1e-4, 2.0 ** -8
+
+
+class Case:
+    """Inputs on the GPU (columns of one matrix with `pad` columns before them)
+    and, as the library sees them, in fp64."""
+
+    def __init__(self, T, B, H, dtype=torch.bfloat16, lengths=None, pad=0, seed=0, lam=(-6.0, 0.0)):
+        rng = np.random.default_rng(seed)
+        self.T, self.B, self.H, self.lengths, self.dtype = T, B, H, lengths, dtype
+        self.N = T * B if lengths is None else int(sum(lengths))
+        self.proj = torch.from_numpy(rng.standard_normal((self.N, pad + 3 * H)).astype(np.float32)).cuda().to(dtype)
+        self.pad = pad
+        self.lam = torch.from_numpy(rng.uniform(*lam, H).astype(np.float32)).cuda()
+        dev = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).cuda()  # noqa: E731
+        self.h0, self.dhT = dev(B, H), dev(B, H)
+        self.dh = dev(self.N, H).to(dtype)
+
+    def cols(self, t):
+        p, H = self.pad, self.H
+        return t[:, p:p + H], t[:, p + H:p + 2 * H], t[:, p + 2 * H:p + 3 * H]
+
+    def forward(self, h0=True, hT=None, train=True, ws=None):
+        need = am.gated_recurrence_workspace_bytes(self.T, self.B, self.H, self.lengths, train)
+        # (torch's allocations are 512-byte aligned; what they hold is arbitrary)
+        self.ws = torch.full((max(need, 1),), 0xFF, dtype=torch.uint8, device="cuda")
+        h = torch.full((self.N, self.H), float("nan"), dtype=self.dtype, device="cuda")
+        hT = torch.full((self.B, self.H), float("nan"), device="cuda") if hT is None else hT
+        am.gated_recurrence_forward(*self.cols(self.proj), self.lam, self.T, self.B, h, self.ws,
+                                    lengths=self.lengths, h0=self.h0 if h0 else None, hT=hT, train=train)
+        return h, hT
+
+    def backward(self, dhT=True):
+        dproj = torch.full_like(self.proj, float("nan"))
+        dlam = torch.full((self.H,), float("nan"), device="cuda")
+        dh0 = torch.full((self.B, self.H), float("nan"), device="cuda")
+        am.gated_recurrence_backward(*self.cols(self.proj), self.lam, self.T, self.B, self.dh, self.ws,
+                                     *self.cols(dproj), dlam, lengths=self.lengths,
+                                     dhT=self.dhT if dhT else None, dh0=dh0)
+        return (*self.cols(dproj), dlam, dh0)
+
+    def oracle(self, h0=True, dhT=True):
+        f = lambda t: t.float().cpu().numpy().astype(np.float64)  # noqa: E731
+        x, r, i = (f(t) for t in self.cols(self.proj))
+        lam = f(self.lam)
+        h, hT, cache = gated.gated_recurrence_forward(x, r, i, lam, self.T, self.B, self.lengths,
+                                                      f(self.h0) if h0 else None)
+        back = gated.gated_recurrence_backward(x, r, i, lam, self.T, self.B, f(self.dh), cache,
+                                               self.lengths, f(self.dhT) if dhT else None)
+        return (h, hT) + back
+
+    def check(self, h0=True, dhT=True):
+        got = self.forward(h0) + self.backward(dhT)
+        names = ("h", "hT", "dx", "dr", "di", "dlam", "dh0")
+        for name, g, ref in zip(names, got, self.oracle(h0, dhT)):
+            if g.numel():
+                tol = BF16_TOL if g.dtype == torch.bfloat16 else F32_TOL
+                assert_close(name, g.float().cpu().numpy(), ref, tol)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,B,H", [(1, 1, 1), (1, 64, 768), (2, 3, 2), (7, 5, 64), (8, 1, 130), (9, 2, 66),
+                                   (63, 3, 33), (64, 4, 96), (65, 2, 128), (129, 1, 300), (257, 2, 70),
+                                   (300, 5, 31)])
+def test_against_oracle(T, B, H, dtype):
+    Case(T, B, H, dtype, seed=T + B + H).check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lengths", [[5], [1, 0], [0, 0, 0], [7, 7, 3, 1, 0], [65, 64, 64, 63, 1],
+                                     [200, 130, 129, 128, 127, 64, 8, 2], [300] + [1] * 40,
+                                     list(range(450, 0, -1))])
+def test_ragged(lengths, dtype):
+    Case(max(max(lengths), 1) + 2, len(lengths), 38, dtype, lengths, seed=len(lengths)).check()
+
+
+@pytest.mark.parametrize("H", [64, 77])
+@pytest.mark.parametrize("pad", [1, 2, 3, 8])
+def test_columns_at_any_offset(H, pad):
+    for dtype in (torch.float32, torch.bfloat16):
+        c = Case(20, 3, H, dtype, pad=pad, seed=pad)
+        c.check()
+
+
+def test_the_columns_beside_stay_untouched():
+    c = Case(20, 3, 64, pad=3)
+    c.forward()
+    wide = torch.full((c.N, 3 + 3 * 64 + 5), 7.0, dtype=torch.bfloat16, device="cuda")
+    dlam = torch.empty(64, device="cuda")
+    am.gated_recurrence_backward(*c.cols(c.proj), c.lam, 20, 3, c.dh, c.ws, *c.cols(wide), dlam)
+    assert torch.all(wide[:, :3] == 7) and torch.all(wide[:, 3 + 3 * 64:] == 7)
+
+
+def test_without_states():
+    Case(70, 3, 40, torch.float32, seed=4).check(h0=False, dhT=False)
+    Case(70, 3, 40, torch.float32, [70, 20, 0], seed=5).check(h0=False, dhT=False)
+
+
+def test_no_frames():
+    c = Case(0, 3, 40, torch.float32)
+    _, hT = c.forward()
+    assert torch.equal(hT, c.h0)
+    *_, dlam, dh0 = c.backward()
+    assert torch.equal(dh0, c.dhT) and torch.all(dlam == 0)
+
+
+@pytest.mark.parametrize("B,H", [(1, 768), (64, 768), (7, 65)])
+def test_frame_by_frame_is_the_whole(B, H):
+    """The state carried in place, a frame a call: the bits of one call are not
+    asked for (its products associate otherwise), its values are."""
+    T = 20
+    c = Case(T, B, H, seed=B)
+    want, end = c.forward()
+    state = c.h0.clone()
+    got = torch.empty_like(want)
+    for t in range(T):
+        rows = slice(t * B, (t + 1) * B)
+        am.gated_recurrence_forward(*(v[rows] for v in c.cols(c.proj)), c.lam, 1, B, got[rows], h0=state,
+                                    hT=state)
+    assert_close("state", state.cpu().numpy(), end.cpu().numpy(), F32_TOL)
+    assert_close("h", got.float().cpu().numpy(), want.float().cpu().numpy(), 2 * BF16_TOL)
+
+
+def test_extreme_gates():
+    """Shut and open gates, and rates that vanish or that forget at once: every
+    output finite and the oracle's."""
+    T, B, H = 24, 2, 8
+    c = Case(T, B, H, torch.float32, seed=9)
+    c.lam[:4] = torch.tensor([-100.0, -25.0, 20.0, 80.0], device="cuda")
+    r = c.cols(c.proj)[1]
+    r[3], r[7], r[11], r[12] = -200.0, 200.0, float("-inf"), float("inf")
+    c.cols(c.proj)[2][5] = -200.0
+    c.check()
+
+
+def test_what_is_not_finite_stays_in_its_sequence_and_channel():
+    T, B, H = 70, 3, 64
+    c = Case(T, B, H, seed=10)
+    clean = [t.clone() for t in c.forward() + c.backward()]
+    x = c.cols(c.proj)[0]
+    x[5 * B + 1, 10] = float("nan")
+    x[40 * B + 2, 11] = float("inf")
+    got = c.forward() + c.backward()
+    rows = torch.ones(T * B, H, dtype=torch.bool, device="cuda")
+    rows[1::B, 10] = False
+    rows[2::B, 11] = False
+    for g, w in zip(got, clean):
+        if g.shape == rows.shape:
+            assert torch.equal(g[rows], w[rows])
+        else:
+            keep = torch.tensor([k not in (10, 11) for k in range(H)], device="cuda")
+            assert torch.equal(g[..., keep], w[..., keep])
+    assert torch.all(torch.isnan(got[0][5 * B + 1::B, 10])) and not torch.isnan(got[0][:5 * B, 10]).any()
+
+
+def test_long_sequences():
+    """One sequence of many tiles; gates that remember for a few hundred frames."""
+    Case(20011, 1, 64, torch.float32, seed=11, lam=(-6.0, -2.0)).check()
+    Case(3001, 2, 130, seed=12).check()
+    Case(9000, 5, 20, torch.float32, [9000, 8999, 4096, 65, 0], seed=13, lam=(-6.0, -2.0)).check()
+
+
+def test_rows_past_32_bit_offsets():
+    """More than 2^31 elements in x, r and i: the last sequences equal the same
+    ones run by themselves."""
+    T, B, H = 1190, 1024, 600
+    proj = torch.empty((T * B, 3 * H), dtype=torch.bfloat16, device="cuda").normal_()
+    assert proj.numel() > 1 << 31
+    lam = torch.full((H,), -4.0, device="cuda")
+    cols = lambda t: (t[:, :H], t[:, H:2 * H], t[:, 2 * H:])  # noqa: E731
+    h = torch.empty((T * B, H), dtype=torch.bfloat16, device="cuda")
+    dproj = torch.empty_like(proj)
+    dlam = torch.empty(H, device="cuda")
+    ws = torch.empty(am.gated_recurrence_workspace_bytes(T, B, H, train=True), dtype=torch.uint8, device="cuda")
+    am.gated_recurrence_forward(*cols(proj), lam, T, B, h, ws, train=True)
+    am.gated_recurrence_backward(*cols(proj), lam, T, B, h, ws, *cols(dproj), dlam)
+    pick = lambda t: t.view(T, B, -1)[:, -2:].reshape(T * 2, -1).contiguous()  # noqa: E731
+    few, few_h = pick(proj), pick(h)
+    h2, d2 = torch.empty_like(few_h), torch.empty_like(few)
+    ws2 = torch.empty(am.gated_recurrence_workspace_bytes(T, 2, H, train=True), dtype=torch.uint8, device="cuda")
+    am.gated_recurrence_forward(*cols(few), lam, T, 2, h2, ws2, train=True)
+    am.gated_recurrence_backward(*cols(few), lam, T, 2, few_h, ws2, *cols(d2), dlam)
+    assert_close("h", h2.float().cpu().numpy(), few_h.float().cpu().numpy(), BF16_TOL)
+    assert_close("dproj", d2.float().cpu().numpy(), pick(dproj).float().cpu().numpy(), BF16_TOL)
+
+
+def test_same_bits_every_time():
+    for lengths in (None, [90, 70, 70, 3]):
+        c = Case(90, 4, 768, lengths=lengths)
+        first = [t.clone() for t in c.forward() + c.backward()]
+        for _ in range(3):
+            assert all(torch.equal(a, b) for a, b in zip(first, c.forward() + c.backward()))
+    c = Case(30000, 1, 192, torch.float32)
+    first = [t.clone() for t in c.forward() + c.backward()]
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, c.forward() + c.backward()))
+
+
+def test_on_a_stream_of_its_own():
+    c = Case(130, 3, 128, seed=14)
+    want = [t.clone() for t in c.forward() + c.backward()]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = c.forward() + c.backward()
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("T,B,H,lengths", [(1, 8, 96, None), (70, 3, 96, None), (70, 3, 96, [70, 33, 1]),
+                                           (9000, 1, 96, None)])
+def test_replayed_from_a_graph(T, B, H, lengths):
+    c = Case(T, B, H, lengths=lengths, seed=15)
+    ws = torch.empty(am.gated_recurrence_workspace_bytes(T, B, H, lengths, True), dtype=torch.uint8, device="cuda")
+    h, hT = torch.empty(c.N, H, dtype=c.dtype, device="cuda"), torch.empty(B, H, device="cuda")
+    dproj, dlam, dh0 = torch.empty_like(c.proj), torch.empty(H, device="cuda"), torch.empty(B, H, device="cuda")
+
+    def both():
+        am.gated_recurrence_forward(*c.cols(c.proj), c.lam, T, B, h, ws, lengths=lengths, h0=c.h0, hT=hT, train=True)
+        am.gated_recurrence_backward(*c.cols(c.proj), c.lam, T, B, c.dh, ws, *c.cols(dproj), dlam,
+                                     lengths=lengths, dhT=c.dhT, dh0=dh0)
+
+    both()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+    outs = (h, hT, dproj, dlam, dh0)
+    for k in range(4):
+        c.proj.normal_()
+        for o in outs:
+            o.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        replayed = [o.clone() for o in outs]
+        ws.fill_(0xFF)
+        both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, outs)), k
