@@ -369,8 +369,9 @@ am_status am_cast_f32_to_bf16(int64_t n, const float* src, void* dst_bf16, void*
  *   L_t = c softplus(lam) sigm(r_t),  a_t = exp(-L_t),
  *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigm(i_t) x_t.
  * Evaluated in fp32, each output rounded once.  A gate that is shut (L_t = 0)
- * keeps the state.  Rows may be columns of a wider matrix: x, r, i (and dh, dx,
- * dr, di) have row strides in elements.
+ * keeps the state.  Rows may be columns of a wider matrix, the projection that
+ * makes all three, say: x, r and i are `ld` elements from row to row, dh lddh, dx,
+ * dr and di ldd.
  *   dtype   AM_F32 or AM_BF16: type of x, r, i, h, dh, dx, dr, di
  *   x, r, i [N] rows of H;  lam [H] fp32, finite;  c > 0
  *   lengths [host] [B] or NULL; variable-length batches allow B <= 1024
@@ -380,14 +381,14 @@ am_status am_cast_f32_to_bf16(int64_t n, const float* src, void* dst_bf16, void*
  *   ws      workspace of am_gated_recurrence_workspace_bytes (256-byte aligned;
  *           may be NULL where that is 0).  train = 1 keeps in it what
  *           gated_recurrence_backward reads; it must not be modified between.
- * A batch of one frame per sequence with train = 0 is one launch. */
+ * B times a row stride is at most 2^30.  A batch of one frame per sequence with
+ * train = 0 and without lengths is one launch. */
 int64_t am_gated_recurrence_workspace_bytes(int32_t T, int32_t B, int32_t H, int32_t varlen,
                                             int32_t train);
 am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtype,
-                                   const int32_t* lengths, const void* x, int64_t ldx, const void* r,
-                                   int64_t ldr, const void* i, int64_t ldi, const float* lam, float c,
-                                   const float* h0, void* h, float* hT, int32_t train, void* ws,
-                                   int64_t ws_bytes, void* stream);
+                                   const int32_t* lengths, const void* x, const void* r, const void* i,
+                                   int64_t ld, const float* lam, float c, const float* h0, void* h,
+                                   float* hT, int32_t train, void* ws, int64_t ws_bytes, void* stream);
 /* The gradient of the forward call (train = 1) that filled `ws`, whose T, B, H,
  * dtype, lengths, x, r, i, lam and c are given again:
  *   dh  [N] rows: dL/dh;  dhT [B][H] fp32 or NULL: dL/dhT
@@ -395,10 +396,9 @@ am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtyp
  *   dh0 [B][H] fp32 or NULL (written)
  * No atomics: the same inputs give the same bits.                           */
 am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dtype,
-                                    const int32_t* lengths, const void* x, int64_t ldx, const void* r,
-                                    int64_t ldr, const void* i, int64_t ldi, const float* lam, float c,
-                                    const void* dh, int64_t lddh, const float* dhT, void* dx,
-                                    int64_t lddx, void* dr, int64_t lddr, void* di, int64_t lddi,
+                                    const int32_t* lengths, const void* x, const void* r, const void* i,
+                                    int64_t ld, const float* lam, float c, const void* dh, int64_t lddh,
+                                    const float* dhT, void* dx, void* dr, void* di, int64_t ldd,
                                     float* dlam, float* dh0, void* ws, int64_t ws_bytes, void* stream);
 
 /* Between two blocks of a residual stack, per row of H:

@@ -92,11 +92,10 @@ _PROTOS = {
     "lfr_features": (_I32, [_I32, _P, _P, _I32, _I32, _I32, _I32, _P, _P, _P, _I32, _P]),
     "delay_targets": (_I32, [_I32, _I32, _P, _I32, _I32, _P, _P, _P, _P, _P, _P]),
     "am_gated_recurrence_workspace_bytes": (_I64, [_I32, _I32, _I32, _I32, _I32]),
-    "gated_recurrence_forward": (_I32, [_I32, _I32, _I32, _I32, _P, _P, _I64, _P, _I64, _P, _I64, _P,
-                                        _F32, _P, _P, _P, _I32, _P, _I64, _P]),
-    "gated_recurrence_backward": (_I32, [_I32, _I32, _I32, _I32, _P, _P, _I64, _P, _I64, _P, _I64, _P,
-                                         _F32, _P, _I64, _P, _P, _I64, _P, _I64, _P, _I64, _P, _P, _P,
-                                         _I64, _P]),
+    "gated_recurrence_forward": (_I32, [_I32, _I32, _I32, _I32, _P, _P, _P, _P, _I64, _P, _F32, _P, _P,
+                                        _P, _I32, _P, _I64, _P]),
+    "gated_recurrence_backward": (_I32, [_I32, _I32, _I32, _I32, _P, _P, _P, _P, _I64, _P, _F32, _P, _I64,
+                                         _P, _P, _P, _P, _I64, _P, _P, _P, _I64, _P]),
     "am_gated_norm_workspace_bytes": (_I64, [_I64, _I32]),
     "gated_norm_forward": (_I32, [_I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _F32, _P,
                                   _P, _P, _P]),
@@ -400,28 +399,43 @@ def _dtype(t, name):
 
 def _shaped(t, name, shape, dtype=torch.float32):
     """Device pointer of a contiguous GPU tensor of this shape, or None."""
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise AmError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    return _dev(t, name, dtype)
-
-
-def _rows(t, name, N, H, dtype):
-    """Device pointer and row stride of [N][H] rows, which may be columns of a
-    wider matrix; (None, H) for None."""
     if t is None:
-        return None, H
+        return None
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise AmError(f"{name} must be a GPU tensor")
-    if t.dtype != dtype:
-        raise AmError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != (N, H):
-        raise AmError(f"{name} must have shape {(N, H)}, got {tuple(t.shape)}")
-    if N > 0 and H > 1 and t.stride(1) != 1:
-        raise AmError(f"{name} must have unit stride along its rows")
-    ld = t.stride(0) if N > 1 else H
-    if N > 1 and ld < H:
-        raise AmError(f"{name} has overlapping rows")
-    return ctypes.c_void_p(t.data_ptr()), ld
+    if t.shape != shape:
+        raise AmError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype is not dtype or not t.is_contiguous():
+        raise AmError(f"{name} must be contiguous {dtype}, got {t.dtype}")
+    return t.data_ptr()
+
+
+def _rows(N, H, dtype, **named):
+    """Device pointers and the row stride of [N][H] rows (None for None), which
+    may be columns of a wider matrix; they share one stride."""
+    ld, out = None, []
+    for name, t in named.items():
+        if t is None:
+            out.append(None)
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise AmError(f"{name} must be a GPU tensor")
+        if t.dtype is not dtype:
+            raise AmError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.shape != (N, H):
+            raise AmError(f"{name} must have shape {(N, H)}, got {tuple(t.shape)}")
+        if N > 1:
+            s0, s1 = t.stride()
+            if (s1 != 1 and H > 1) or s0 < H:
+                raise AmError(f"{name} must have rows of unit stride that do not overlap")
+            if ld is None:
+                ld = s0
+            elif ld != s0:
+                raise AmError(f"{name} must have the same row stride as {next(iter(named))}")
+        elif N == 1 and H > 1 and t.stride(1) != 1:
+            raise AmError(f"{name} must have rows of unit stride")
+        out.append(t.data_ptr())
+    return (*out, H if ld is None else ld)
 
 
 def _packed_rows(T, B, lengths):
@@ -448,35 +462,35 @@ def gated_recurrence_workspace_bytes(T, B, H, lengths=None, train=False) -> int:
 
 def gated_recurrence_forward(x, r, i, lam, T, B, h, ws=None, lengths=None, h0=None, hT=None, c=8.0,
                              train=False, stream=None):
-    """x, r, i: [N][H] rows (columns of one projection, say); h: [N][H]; lam:
-    [H]; h0, hT: [B][H] fp32 (hT may be h0)."""
+    """x, r, i: [N][H] rows of one stride (columns of one projection, say); h:
+    [N][H]; lam: [H]; h0, hT: [B][H] fp32 (hT may be h0)."""
     dt, (N, H) = _dtype(x, "x"), h.shape
     arr, lp, rows = _packed_rows(T, B, lengths)
     if rows != N:
         raise AmError(f"h must have {rows} rows, got {N}")
-    (xp, ldx), (rp, ldr), (ip, ldi) = (_rows(t, n, N, H, x.dtype)
-                                       for t, n in ((x, "x"), (r, "r"), (i, "i")))
+    xp, rp, ip, ld = _rows(N, H, x.dtype, x=x, r=r, i=i)
     wp, wn = _workspace(ws)
     _check(lib().gated_recurrence_forward(
-        T, B, H, dt, lp, xp, ldx, rp, ldr, ip, ldi, _shaped(lam, "lam", (H,)), float(c),
-        _shaped(h0, "h0", (B, H)), _shaped(h, "h", (N, H), x.dtype), _shaped(hT, "hT", (B, H)),
-        int(bool(train)), wp, wn, _stream(stream)))
+        T, B, H, dt, lp, xp, rp, ip, ld, _shaped(lam, "lam", (H,)), c, _shaped(h0, "h0", (B, H)),
+        _shaped(h, "h", (N, H), x.dtype), _shaped(hT, "hT", (B, H)), 1 if train else 0, wp, wn,
+        _stream(stream)))
 
 
 def gated_recurrence_backward(x, r, i, lam, T, B, dh, ws, dx, dr, di, dlam, lengths=None, dhT=None,
                               dh0=None, c=8.0, stream=None):
-    """The gradient of the forward call (train=True) that filled `ws`."""
+    """The gradient of the forward call (train=True) that filled `ws`; dx, dr, di:
+    [N][H] rows of one stride."""
     dt, (N, H) = _dtype(x, "x"), x.shape
     arr, lp, rows = _packed_rows(T, B, lengths)
     if rows != N:
         raise AmError(f"x must have {rows} rows, got {N}")
-    ((xp, ldx), (rp, ldr), (ip, ldi), (dhp, lddh), (dxp, lddx), (drp, lddr), (dip, lddi)) = (
-        _rows(t, n, N, H, x.dtype) for t, n in ((x, "x"), (r, "r"), (i, "i"), (dh, "dh"), (dx, "dx"),
-                                                (dr, "dr"), (di, "di")))
+    xp, rp, ip, ld = _rows(N, H, x.dtype, x=x, r=r, i=i)
+    dhp, lddh = _rows(N, H, x.dtype, dh=dh)
+    dxp, drp, dip, ldd = _rows(N, H, x.dtype, dx=dx, dr=dr, di=di)
     wp, wn = _workspace(ws)
     _check(lib().gated_recurrence_backward(
-        T, B, H, dt, lp, xp, ldx, rp, ldr, ip, ldi, _shaped(lam, "lam", (H,)), float(c), dhp, lddh,
-        _shaped(dhT, "dhT", (B, H)), dxp, lddx, drp, lddr, dip, lddi, _shaped(dlam, "dlam", (H,)),
+        T, B, H, dt, lp, xp, rp, ip, ld, _shaped(lam, "lam", (H,)), c, dhp, lddh,
+        _shaped(dhT, "dhT", (B, H)), dxp, drp, dip, ldd, _shaped(dlam, "dlam", (H,)),
         _shaped(dh0, "dh0", (B, H)), wp, wn, _stream(stream)))
 
 
@@ -491,8 +505,8 @@ def gated_norm_forward(res, o=None, gate=None, w_post=None, scale=None, w_next=N
                        y=None, rstd=None, eps=1e-6, stream=None):
     """res, res_out: the residual stream, [N][H] fp32 or bf16; o, gate: [N][H]
     rows; y: [N][H] of their type.  Every part may be left out (see the C ABI)."""
-    (N, H), act = res.shape, next((t for t in (o, y, res) if t is not None))
-    (op, ldo), (gp, ldg) = _rows(o, "o", N, H, act.dtype), _rows(gate, "gate", N, H, act.dtype)
+    (N, H), act = res.shape, o if o is not None else y if y is not None else res
+    (op, ldo), (gp, ldg) = _rows(N, H, act.dtype, o=o), _rows(N, H, act.dtype, gate=gate)
     _check(lib().gated_norm_forward(
         N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
         _shaped(scale, "scale", (H,)), _shaped(res, "res", (N, H), res.dtype),
@@ -505,9 +519,9 @@ def gated_norm_backward(res, rstd, dres, ws, o=None, gate=None, w_post=None, sca
                         dw_next=None, eps=1e-6, stream=None):
     """The gradient of gated_norm_forward with the same res (as it was before),
     o, gate and factors, and the rstd it wrote."""
-    (N, H), act = res.shape, next((t for t in (o, dy, res) if t is not None))
-    ((op, ldo), (gp, ldg), (dop, lddo), (dgp, lddg)) = (
-        _rows(t, n, N, H, act.dtype) for t, n in ((o, "o"), (gate, "gate"), (do, "do"), (dgate, "dgate")))
+    (N, H), act = res.shape, o if o is not None else dy if dy is not None else res
+    (op, ldo), (gp, ldg) = _rows(N, H, act.dtype, o=o), _rows(N, H, act.dtype, gate=gate)
+    (dop, lddo), (dgp, lddg) = _rows(N, H, act.dtype, do=do), _rows(N, H, act.dtype, dgate=dgate)
     wp, wn = _workspace(ws)
     _check(lib().gated_norm_backward(
         N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),

@@ -217,4 +217,31 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// The sum of column 32 blockIdx.x + threadIdx.x % 32 of parts [rows][width], by a
+// workgroup of 1024: 32 threads take every 32nd row each, eight loads ahead of
+// their adds, and the first 32 threads return the sums (in a fixed order).
+__device__ __forceinline__ float column_sum(const float* __restrict__ parts, int64_t rows, int width,
+                                            float (&sum)[32][33]) {
+  const int c = threadIdx.x & 31, q = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+  float s = 0.f;
+  if (col < width) {
+    const float* p = parts + (int64_t)q * width + col;
+    int64_t k = q;
+    for (; k + 7 * 32 < rows; k += 8 * 32, p += (int64_t)8 * 32 * width) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = p[(int64_t)u * 32 * width];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; k < rows; k += 32, p += (int64_t)32 * width) s += *p;
+  }
+  sum[q][c] = s;
+  __syncthreads();
+  if (q == 0)
+#pragma unroll
+    for (int k = 1; k < 32; ++k) s += sum[k][c];
+  return s;
+}
+
 }  // namespace am

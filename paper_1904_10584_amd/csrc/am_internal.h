@@ -298,10 +298,10 @@ hipError_t bmuf_update(int64_t n, int count, int workers, const float* models, i
 // saves the state each tile starts from.
 constexpr int GR_STRETCH = 8, GR_WAVES = 8, GR_TILE = GR_STRETCH * GR_WAVES;
 struct GatedRecurrence {
-  const void *x, *r, *i;       // [N] rows of H, ldx, ldr, ldi apart
-  const void* dh;              // backward: [N] rows
-  void *dx, *dr, *di;          // backward: [N] rows (written)
-  int64_t ldx, ldr, ldi, lddh, lddx, lddr, lddi;
+  const void *x, *r, *i;       // [N] rows of H, ld apart
+  const void* dh;              // backward: [N] rows, lddh apart
+  void *dx, *dr, *di;          // backward: [N] rows, ldd apart (written)
+  int64_t ld, lddh, ldd;
   const float* lam;            // [H]
   const float* h0;             // [B][H] or null (zero)
   void* h;                     // forward: [N][H] (written)
@@ -310,12 +310,16 @@ struct GatedRecurrence {
   float* dh0;                  // backward: [B][H] or null
   float* dlam;                 // backward: [H]
   float* saved;                // [tiles][B][H] (written forward if not null)
-  float* parts;                // backward: [B][H] scratch
+  float* parts;                // backward: [spans][B][H] scratch
+  float *spans_a, *spans_s;    // [spans][B][H] scratch
   const int32_t *offs, *lens;  // [T + 1], [B], or null (every sequence has T frames)
   int64_t N;
   int T, B, H;                 // (T: the longest length)
+  int span_tiles;              // (set by the launcher)
   float c;
 };
+// Spans that time is cut into for `groups` workgroups' worth of channels.
+int gated_spans(int T, int64_t groups);
 hipError_t gated_forward(const GatedRecurrence& a, bool bf16, hipStream_t s);
 hipError_t gated_backward(const GatedRecurrence& a, bool bf16, hipStream_t s);
 // The tables of a batch of sorted lengths, MAX sequences a launch.

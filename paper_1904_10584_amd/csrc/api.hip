@@ -615,15 +615,18 @@ am_status encode_scratch_of(hipStream_t s, void** out) {
 // ------------------------------------------- gated linear recurrences --
 
 // Rows of H elements that an operator reads or writes.
-am_status check_rows(int64_t N, int32_t H, int32_t dtype, const void* p, int64_t ld, const char* name) {
+// (`frame`: rows that a kernel reaches by 32-bit offsets from the first.)
+am_status check_rows(int64_t N, int32_t H, int32_t dtype, const void* p, int64_t ld, const char* name,
+                     int64_t frame = 0) {
   if (N > 0 && !p) return fail(AM_EINVAL, "NULL %s", name);
   if (!aligned(p, (uintptr_t)esz_of(dtype))) return fail(AM_EINVAL, "%s is not aligned to its elements", name);
   if (ld < H) return fail(AM_EINVAL, "row stride %lld of %s is less than %d", (long long)ld, name, H);
+  if (frame > 0 && ld > (1ll << 30) / frame) return fail(AM_EUNSUPPORTED, "frames of %s beyond 2^30 elements", name);
   return AM_OK;
 }
 
 struct GatedLayout {
-  int64_t offs, lens, tails, saved, parts, total;
+  int64_t offs, lens, tails, saved, parts, spans_a, spans_s, total;
 };
 GatedLayout gated_layout(int64_t T, int64_t B, int64_t H, bool varlen, bool train) {
   GatedLayout l{};
@@ -638,9 +641,15 @@ GatedLayout gated_layout(int64_t T, int64_t B, int64_t H, bool varlen, bool trai
     l.lens = take(B * 4);
     l.tails = take(B * 4);
   }
+  // (two channels a lane make the fewest groups, and so the most spans)
+  const int64_t spans = am::gated_spans((int)T, (B * (H / 2) + 63) / 64 > 0 ? (B * (H / 2) + 63) / 64 : 1);
   if (train) {
     l.saved = take((T + am::GR_TILE - 1) / am::GR_TILE * B * H * 4);
-    l.parts = take(B * H * 4);
+    l.parts = take(spans * B * H * 4);
+  }
+  if (spans > 1) {
+    l.spans_a = take(spans * B * H * 4);
+    l.spans_s = take(spans * B * H * 4);
   }
   l.total = at;
   return l;
@@ -669,7 +678,6 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
     a.T = lengths[0];
   }
   if (a.N >= (1ll << 31)) return fail(AM_EUNSUPPORTED, "too many frames");
-  if ((int64_t)B * H >= (1ll << 36)) return fail(AM_EUNSUPPORTED, "too many channels");
   l = gated_layout(T, B, H, lengths != nullptr, train);
   if (l.total > 0 && (!ws || !aligned(ws, 256) || ws_bytes < l.total))
     return fail(AM_EWORKSPACE, "needs %lld workspace bytes, 256-byte aligned", (long long)l.total);
@@ -677,6 +685,8 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
   a.H = H;
   a.lam = lam;
   a.c = c;
+  a.spans_a = at<float>(ws, l.spans_a);
+  a.spans_s = at<float>(ws, l.spans_s);
   if (lengths) {
     a.offs = at<int32_t>(ws, l.offs);
     a.lens = at<int32_t>(ws, l.lens);
@@ -1426,19 +1436,19 @@ int64_t am_gated_recurrence_workspace_bytes(int32_t T, int32_t B, int32_t H, int
 }
 
 am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtype, const int32_t* lengths,
-                                   const void* x, int64_t ldx, const void* r, int64_t ldr, const void* i,
-                                   int64_t ldi, const float* lam, float c, const float* h0, void* h,
-                                   float* hT, int32_t train, void* ws, int64_t ws_bytes, void* stream) {
+                                   const void* x, const void* r, const void* i, int64_t ld, const float* lam,
+                                   float c, const float* h0, void* h, float* hT, int32_t train, void* ws,
+                                   int64_t ws_bytes, void* stream) {
   am::GatedRecurrence a{};
   GatedLayout l;
   AM_TRY(check_gated(T, B, H, dtype, lengths, lam, c, train != 0, ws, ws_bytes, a, l));
-  AM_TRY(check_rows(a.N, H, dtype, x, ldx, "x"));
-  AM_TRY(check_rows(a.N, H, dtype, r, ldr, "r"));
-  AM_TRY(check_rows(a.N, H, dtype, i, ldi, "i"));
-  AM_TRY(check_rows(a.N, H, dtype, h, H, "h"));
+  AM_TRY(check_rows(a.N, H, dtype, x, ld, "x", B));
+  AM_TRY(check_rows(a.N, H, dtype, r, ld, "r", B));
+  AM_TRY(check_rows(a.N, H, dtype, i, ld, "i", B));
+  AM_TRY(check_rows(a.N, H, dtype, h, H, "h", B));
   if (!aligned(h0, 4) || !aligned(hT, 4)) return fail(AM_EINVAL, "h0 and hT must be 4-byte aligned");
   a.x = x; a.r = r; a.i = i;
-  a.ldx = ldx; a.ldr = ldr; a.ldi = ldi;
+  a.ld = ld;
   a.h0 = h0;
   a.h = h;
   a.hT = hT;
@@ -1459,28 +1469,28 @@ am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtyp
 }
 
 am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dtype, const int32_t* lengths,
-                                    const void* x, int64_t ldx, const void* r, int64_t ldr, const void* i,
-                                    int64_t ldi, const float* lam, float c, const void* dh, int64_t lddh,
-                                    const float* dhT, void* dx, int64_t lddx, void* dr, int64_t lddr,
-                                    void* di, int64_t lddi, float* dlam, float* dh0, void* ws,
+                                    const void* x, const void* r, const void* i, int64_t ld, const float* lam,
+                                    float c, const void* dh, int64_t lddh, const float* dhT, void* dx, void* dr,
+                                    void* di, int64_t ldd, float* dlam, float* dh0, void* ws,
                                     int64_t ws_bytes, void* stream) {
   am::GatedRecurrence a{};
   GatedLayout l;
   AM_TRY(check_gated(T, B, H, dtype, lengths, lam, c, true, ws, ws_bytes, a, l));
-  AM_TRY(check_rows(a.N, H, dtype, x, ldx, "x"));
-  AM_TRY(check_rows(a.N, H, dtype, r, ldr, "r"));
-  AM_TRY(check_rows(a.N, H, dtype, i, ldi, "i"));
-  AM_TRY(check_rows(a.N, H, dtype, dh, lddh, "dh"));
-  AM_TRY(check_rows(a.N, H, dtype, dx, lddx, "dx"));
-  AM_TRY(check_rows(a.N, H, dtype, dr, lddr, "dr"));
-  AM_TRY(check_rows(a.N, H, dtype, di, lddi, "di"));
+  AM_TRY(check_rows(a.N, H, dtype, x, ld, "x", B));
+  AM_TRY(check_rows(a.N, H, dtype, r, ld, "r", B));
+  AM_TRY(check_rows(a.N, H, dtype, i, ld, "i", B));
+  AM_TRY(check_rows(a.N, H, dtype, dh, lddh, "dh", B));
+  AM_TRY(check_rows(a.N, H, dtype, dx, ldd, "dx", B));
+  AM_TRY(check_rows(a.N, H, dtype, dr, ldd, "dr", B));
+  AM_TRY(check_rows(a.N, H, dtype, di, ldd, "di", B));
   if (!dlam) return fail(AM_EINVAL, "NULL dlam");
   if (!aligned(dhT, 4) || !aligned(dh0, 4) || !aligned(dlam, 4))
     return fail(AM_EINVAL, "dhT, dh0 and dlam must be 4-byte aligned");
   a.x = x; a.r = r; a.i = i; a.dh = dh;
   a.dx = dx; a.dr = dr; a.di = di;
-  a.ldx = ldx; a.ldr = ldr; a.ldi = ldi; a.lddh = lddh;
-  a.lddx = lddx; a.lddr = lddr; a.lddi = lddi;
+  a.ld = ld;
+  a.lddh = lddh;
+  a.ldd = ldd;
   a.dhT = dhT;
   a.dh0 = dh0;
   a.dlam = dlam;

@@ -267,19 +267,13 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(GatedNorm a) {
   }
 }
 
-// Column sums of parts [rows][2][H] in order: 16 columns a workgroup, 16 threads
-// each.
-__global__ __launch_bounds__(256) void norm_weights_kernel(const float* __restrict__ parts, int rows,
-                                                           GatedNorm a) {
-  __shared__ float sum[16][17];
-  const int c = blockIdx.x * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4;
-  float s = 0.f;
-  if (c < 2 * a.H)
-    for (int k = q; k < rows; k += 16) s += parts[(int64_t)k * 2 * a.H + c];
-  sum[q][threadIdx.x & 15] = s;
-  __syncthreads();
-  if (q != 0 || c >= 2 * a.H) return;
-  for (int k = 1; k < 16; ++k) s += sum[k][threadIdx.x & 15];
+// The factors' gradients from the column sums of parts [rows][2][H].
+__global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restrict__ parts, int rows,
+                                                            GatedNorm a) {
+  __shared__ float sum[32][33];
+  const float s = column_sum(parts, rows, 2 * a.H, sum);
+  const int c = blockIdx.x * 32 + threadIdx.x;
+  if (threadIdx.x >= 32 || c >= 2 * a.H) return;
   if (c >= a.H) {
     if (a.dw_next) a.dw_next[c - a.H] = s;
   } else {
@@ -296,7 +290,7 @@ hipError_t launch(const GatedNorm& a, bool forward, hipStream_t s) {
     hipLaunchKernelGGL((norm_forward_kernel<T, R, NV, WPR>), dim3(grid), dim3(256), 0, s, a);
   } else {
     if (grid > 0) hipLaunchKernelGGL((norm_backward_kernel<T, R, NV, WPR>), dim3(grid), dim3(256), 0, s, a);
-    hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2 * a.H + 15) / 16)), dim3(256), 0, s, a.parts,
+    hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2 * a.H + 31) / 32)), dim3(1024), 0, s, a.parts,
                        (int)grid, a);
   }
   return hipGetLastError();

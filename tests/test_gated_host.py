@@ -21,10 +21,10 @@ def _lens(*v):
     return (ctypes.c_int32 * len(v))(*v)
 
 
-def _forward(L, T=5, B=2, H=64, dtype=am.BF16, lengths=None, x=P, ldx=64, r=P, ldr=64, i=P, ldi=64, lam=P,
-             c=8.0, h0=None, h=P, hT=None, train=0, ws=None, ws_bytes=0):
-    st = L.gated_recurrence_forward(T, B, H, dtype, lengths, x, ldx, r, ldr, i, ldi, lam, c, h0, h, hT,
-                                    train, ws, ws_bytes, None)
+def _forward(L, T=5, B=2, H=64, dtype=am.BF16, lengths=None, x=P, r=P, i=P, ld=64, lam=P, c=8.0, h0=None,
+             h=P, hT=None, train=0, ws=None, ws_bytes=0):
+    st = L.gated_recurrence_forward(T, B, H, dtype, lengths, x, r, i, ld, lam, c, h0, h, hT, train, ws,
+                                    ws_bytes, None)
     return st, L.am_last_error().decode()
 
 
@@ -33,13 +33,14 @@ def _forward(L, T=5, B=2, H=64, dtype=am.BF16, lengths=None, x=P, ldx=64, r=P, l
     (dict(dtype=2), am.EINVAL, "dtype"), (dict(lam=None), am.EINVAL, "lam"), (dict(c=0.0), am.EINVAL, "c must"),
     (dict(c=float("nan")), am.EINVAL, "c must"), (dict(c=float("inf")), am.EINVAL, "c must"),
     (dict(x=None), am.EINVAL, "x"), (dict(r=None), am.EINVAL, "r"), (dict(i=None), am.EINVAL, "i"),
-    (dict(h=None), am.EINVAL, "h"), (dict(ldx=63), am.EINVAL, "row stride"), (dict(r=ODD), am.EINVAL, "aligned"),
+    (dict(h=None), am.EINVAL, "h"), (dict(ld=63), am.EINVAL, "row stride"), (dict(r=ODD), am.EINVAL, "aligned"),
     (dict(h0=ODD), am.EINVAL, "aligned"), (dict(lengths=_lens(2, 5)), am.EINVAL, "non-increasing"),
     (dict(lengths=_lens(6, 5)), am.EINVAL, "outside"), (dict(lengths=_lens(5, -1)), am.EINVAL, "outside"),
     (dict(lengths=_lens(5, 4)), am.EWORKSPACE, "workspace"), (dict(train=1), am.EWORKSPACE, "workspace"),
     (dict(train=1, ws=P, ws_bytes=100), am.EWORKSPACE, "workspace"),
     (dict(train=1, ws=ODD, ws_bytes=1 << 30), am.EWORKSPACE, "256"),
     (dict(T=1 << 20, B=1 << 12), am.EUNSUPPORTED, "frames"),
+    (dict(ld=(1 << 29) + 1), am.EUNSUPPORTED, "beyond"),
 ])
 def test_recurrence_refusals(L, bad, status, word):
     st, msg = _forward(L, **bad)
@@ -53,10 +54,9 @@ def test_recurrence_batches_of_lengths_are_bounded(L):
 
 def test_recurrence_backward_refusals(L):
     need = L.am_gated_recurrence_workspace_bytes(5, 2, 64, 0, 1)
-    good = dict(T=5, B=2, H=64, dtype=am.BF16, lengths=None, x=P, ldx=64, r=P, ldr=64, i=P, ldi=64, lam=P,
-                c=8.0, dh=P, lddh=64, dhT=None, dx=P, lddx=64, dr=P, lddr=64, di=P, lddi=64, dlam=P, dh0=None,
-                ws=P, ws_bytes=need)
-    for bad, status in ((dict(dh=None), am.EINVAL), (dict(dx=None), am.EINVAL), (dict(lddi=10), am.EINVAL),
+    good = dict(T=5, B=2, H=64, dtype=am.BF16, lengths=None, x=P, r=P, i=P, ld=64, lam=P, c=8.0, dh=P, lddh=64,
+                dhT=None, dx=P, dr=P, di=P, ldd=64, dlam=P, dh0=None, ws=P, ws_bytes=need)
+    for bad, status in ((dict(dh=None), am.EINVAL), (dict(dx=None), am.EINVAL), (dict(ldd=10), am.EINVAL),
                         (dict(dlam=None), am.EINVAL), (dict(dlam=ODD), am.EINVAL), (dict(ws=None), am.EWORKSPACE),
                         (dict(ws_bytes=need - 1), am.EWORKSPACE), (dict(lddh=0), am.EINVAL)):
         st = L.gated_recurrence_backward(*{**good, **bad}.values(), None)
