@@ -393,7 +393,7 @@ am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtyp
  * dtype, lengths, x, r, i, lam and c are given again:
  *   dh  [N] rows: dL/dh;  dhT [B][H] fp32 or NULL: dL/dhT
  *   dx, dr, di [N] rows (written);  dlam [H] fp32 (written)
- *   dh0 [B][H] fp32 or NULL (written)
+ *   dh0 [B][H] fp32 or NULL (written; may be dhT itself)
  * No atomics: the same inputs give the same bits.                           */
 am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dtype,
                                     const int32_t* lengths, const void* x, const void* r, const void* i,

@@ -312,6 +312,7 @@ struct GatedRecurrence {
   float* saved;                // [tiles][B][H] (written forward if not null)
   float* parts;                // backward: [spans][B][H] scratch
   float *spans_a, *spans_s;    // [spans][B][H] scratch
+  float* start;                // [B][H] scratch (of several spans)
   const int32_t *offs, *lens;  // [T + 1], [B], or null (every sequence has T frames)
   int64_t N;
   int T, B, H;                 // (T: the longest length)

@@ -626,7 +626,7 @@ am_status check_rows(int64_t N, int32_t H, int32_t dtype, const void* p, int64_t
 }
 
 struct GatedLayout {
-  int64_t offs, lens, tails, saved, parts, spans_a, spans_s, total;
+  int64_t offs, lens, tails, saved, parts, spans_a, spans_s, start, total;
 };
 GatedLayout gated_layout(int64_t T, int64_t B, int64_t H, bool varlen, bool train) {
   GatedLayout l{};
@@ -650,6 +650,7 @@ GatedLayout gated_layout(int64_t T, int64_t B, int64_t H, bool varlen, bool trai
   if (spans > 1) {
     l.spans_a = take(spans * B * H * 4);
     l.spans_s = take(spans * B * H * 4);
+    l.start = take(B * H * 4);
   }
   l.total = at;
   return l;
@@ -687,6 +688,7 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
   a.c = c;
   a.spans_a = at<float>(ws, l.spans_a);
   a.spans_s = at<float>(ws, l.spans_s);
+  a.start = at<float>(ws, l.start);
   if (lengths) {
     a.offs = at<int32_t>(ws, l.offs);
     a.lens = at<int32_t>(ws, l.lens);

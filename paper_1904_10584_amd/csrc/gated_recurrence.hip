@@ -67,10 +67,9 @@ template <> struct Vec<bf16_t, 2> {
 };
 
 // What a frame's gates come to.  1 - a^2 is 1 - e^-y of y = 2L, from its series
-// where the difference would cancel (the seven terms leave 2e-8 of it at 0.35).
-// With L = 0 (a shut gate, or a frame past the sequence's end) the state passes
-// unchanged, and L / q takes its limit 0; so it does where 1 - a^2 is subnormal
-// (the reciprocal root takes those for zero).
+// where the difference would cancel (five terms leave 4e-8 of it at 0.125, where
+// the difference keeps 5e-7).  With L = 0 (a shut gate, or a frame past the
+// sequence's end) the state passes unchanged, and L / q takes its limit 0.
 struct Gates {
   float sr, a, q, Lq;  // sigm(r) (0 past the end), a, q and L / q
 };
@@ -79,22 +78,30 @@ __device__ __forceinline__ Gates gates(float r, float rate, bool live) {
   g.sr = live ? sigm(r) : 0.f;
   const float L = rate * g.sr, y = 2.f * L;
   g.a = __builtin_amdgcn_exp2f(-1.44269504f * L);
-  float p = 1.f / 5040.f;
-  p = fmaf(p, -y, 1.f / 720.f);
-  p = fmaf(p, -y, 1.f / 120.f);
+  float p = 1.f / 120.f;
   p = fmaf(p, -y, 1.f / 24.f);
   p = fmaf(p, -y, 1.f / 6.f);
   p = fmaf(p, -y, 0.5f);
   p = fmaf(p, -y, 1.f);
-  const float q2 = y < 0.35f ? p * y : fmaf(-g.a, g.a, 1.f);
-  const float rq = q2 >= 1.17549435e-38f ? __builtin_amdgcn_rsqf(q2) : 0.f;
+  const float q2 = y < 0.125f ? p * y : fmaf(-g.a, g.a, 1.f);
+  const float rq = __builtin_amdgcn_rsqf(fmaxf(q2, 1.17549435e-38f));
   g.q = q2 * rq;
   g.Lq = L * rq;
   return g;
 }
 
-__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.f) + log1pf(expf(-fabsf(v))); }
-
+// max(v, 0) + log(1 + e), e = e^-|v|, the logarithm as 2 artanh(e / (2 + e)), whose
+// series ends below 2^-24 of it (e / (2 + e) is at most 1 / 3).
+__device__ __forceinline__ float softplus(float v) {
+  const float e = __expf(-fabsf(v)), s = e / (2.f + e), z = s * s;
+  float p = 1.f / 13.f;
+  p = fmaf(p, z, 1.f / 11.f);
+  p = fmaf(p, z, 1.f / 9.f);
+  p = fmaf(p, z, 1.f / 7.f);
+  p = fmaf(p, z, 1.f / 5.f);
+  p = fmaf(p, z, 1.f / 3.f);
+  return fmaxf(v, 0.f) + 2.f * fmaf(p * z, s, s);
+}
 
 // The schedule's tables, written by an earlier launch, for scalar loads.
 typedef const __attribute__((address_space(4))) int32_t* Table;
@@ -108,15 +115,14 @@ template <int V, bool RAGGED> struct Columns {
   int tiles;     // of the workgroup's longest sequence (its first: they are sorted)
   int64_t st;    // place in a [B][H] matrix
   __device__ Columns(const GatedRecurrence& a, int lane) {
-    const int per_row = a.H / V;
-    const int64_t groups = (int64_t)a.B * per_row, g0 = (int64_t)blockIdx.x * 64;
+    const uint32_t per_row = (uint32_t)a.H / V, groups = a.B * per_row, g0 = blockIdx.x * 64;
     on = g0 + lane < groups;
-    const int64_t g = on ? g0 + lane : groups - 1;
+    const uint32_t g = on ? g0 + lane : groups - 1;
     b = (int)(g / per_row);
-    d = (int)(g % per_row) * V;
+    d = (int)(g - b * per_row) * V;
     st = (int64_t)b * a.H + d;
     len = on ? RAGGED ? a.lens[b] : a.T : 0;
-    const int most = RAGGED ? table(a.lens)[(int)(g0 / per_row)] : a.T;
+    const int most = RAGGED ? table(a.lens)[g0 / per_row] : a.T;
     tiles = (most + GR_TILE - 1) / GR_TILE;
   }
 };
@@ -164,31 +170,44 @@ __device__ __forceinline__ void span_start(const GatedRecurrence& a, const Colum
   }
 }
 
-template <typename T, int V, bool RAGGED, int STRETCH, int WAVES>
+// The composition of the stretches (A, S) of waves from, from + by, ... (count of
+// them, wave-uniform) applied to a state.
+template <int V, int N>
+__device__ __forceinline__ void pass(const float (&A)[N][64][V], const float (&S)[N][64][V], int from, int by,
+                                     int count, int lane, float (&state)[V]) {
+#pragma unroll
+  for (int n = 0; n < N - 1; ++n) {
+    if (n >= count) break;
+    const int s = from + n * by;
+#pragma unroll
+    for (int v = 0; v < V; ++v) state[v] = fmaf(A[s][lane][v], state[v], S[s][lane][v]);
+    if (n & 1) asm volatile("" ::: "memory");  // (the later reads stay behind: registers)
+  }
+}
+
+// AHEAD: several tiles, the next one's loads under the end of this one.
+template <typename T, int V, bool RAGGED, bool AHEAD, int STRETCH, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurrence a) {
   __shared__ float agg[2][2][WAVES][64][V];  // of tiles taken in turn: A, S of each stretch
+  __shared__ float end[2][64][V];            // and the state at the tile's end
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Columns<V, RAGGED> c(a, lane);
   const int first = blockIdx.y * a.span_tiles;
   const int last = first + a.span_tiles < c.tiles ? first + a.span_tiles : c.tiles;
   if (first >= c.tiles && first > 0) return;
-  float rate[V], carry[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) rate[v] = a.c * softplus(a.lam[c.d + v]);
-  span_start(a, c, a.h0, 0, 1, (int)blockIdx.y, carry);
   Vec<T, V> x[STRETCH], r[STRETCH], i[STRETCH];
   auto take = [&](int k) {
-    const int t0 = k * GR_TILE + w * STRETCH;
-    fetch<RAGGED, T, V, STRETCH, 3>(a, {a.r, a.i, a.x}, a.ld, t0, c, {&r, &i, &x});
+    fetch<RAGGED, T, V, STRETCH, 3>(a, {a.r, a.i, a.x}, a.ld, k * GR_TILE + w * STRETCH, c, {&r, &i, &x});
   };
-  const uint32_t mine = lane_offset<T>(c, a.H);
   if (first < last) take(first);
+  float rate[V], h[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) rate[v] = a.c * softplus(a.lam[c.d + v]);
+  span_start(a, c, a.h0, 0, 1, (int)blockIdx.y, h);
+  const uint32_t mine = lane_offset<T>(c, a.H);
   for (int k = first; k < last; ++k) {
     const int t0 = k * GR_TILE + w * STRETCH;
-    if (a.saved && c.on && w == 0)
-#pragma unroll
-      for (int v = 0; v < V; ++v) a.saved[(int64_t)k * a.B * a.H + c.st + v] = carry[v];
-    float av[STRETCH][V], u[STRETCH][V], A[V], S[V], h[V];
+    float av[STRETCH][V], u[STRETCH][V], A[V], S[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       A[v] = 1.f;
@@ -204,14 +223,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
         A[v] *= g.a;
         S[v] = fmaf(g.a, S[v], u[j][v]);
       }
-    if (k + 1 < last) take(k + 1);  // (the next tile's loads under the rest of this one)
-    if constexpr (WAVES == 1) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        h[v] = carry[v];
-        carry[v] = fmaf(A[v], carry[v], S[v]);
-      }
-    } else {
+    if (AHEAD && k + 1 < last) take(k + 1);
+    if constexpr (WAVES > 1) {
       float (&g)[2][WAVES][64][V] = agg[k & 1];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
@@ -219,15 +232,13 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
         g[1][w][lane][v] = S[v];
       }
       lds_barrier();
+      if (AHEAD && k > first)
 #pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = carry[v];
+        for (int v = 0; v < V; ++v) h[v] = end[(k & 1) ^ 1][lane][v];
+      if (a.saved && c.on && w == 0)
 #pragma unroll
-      for (int s = 0; s < WAVES; ++s)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          carry[v] = fmaf(g[0][s][lane][v], carry[v], g[1][s][lane][v]);
-          h[v] = s + 1 == w ? carry[v] : h[v];
-        }
+        for (int v = 0; v < V; ++v) a.saved[(int64_t)k * a.B * a.H + c.st + v] = h[v];
+      pass<V, WAVES>(g[0], g[1], 0, 1, w, lane, h);
     }
 #pragma unroll
     for (int j = 0; j < STRETCH; ++j) {
@@ -236,15 +247,19 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
       Vec<T, V>::store(frame(a.h, first_row<RAGGED>(a, t0 + j) * a.H * (int)sizeof(T)),
                        t0 + j < c.len ? mine : NONE, h);
     }
-  }
-  if (a.hT && c.on && w == 0 && last == c.tiles)
+    if (AHEAD && w == WAVES - 1)
 #pragma unroll
-    for (int v = 0; v < V; ++v) a.hT[c.st + v] = carry[v];
+      for (int v = 0; v < V; ++v) end[k & 1][lane][v] = h[v];
+  }
+  if (a.hT && c.on && w == WAVES - 1 && last == c.tiles)
+#pragma unroll
+    for (int v = 0; v < V; ++v) a.hT[c.st + v] = h[v];
 }
 
 template <typename T, int V, bool RAGGED>
 __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence a) {
   __shared__ float agg[2][3][W][64][V];  // A, S and the carry's end from zero
+  __shared__ float end[2][64][V];        // the carry at the tile's start
   __shared__ float lsum[W][64][V];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Columns<V, RAGGED> c(a, lane);
@@ -278,7 +293,7 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
       S[v] = D[v] = 0.f;
     }
 #pragma unroll
-    for (int j = 0; j < TC; ++j)
+    for (int j = 0; j < TC; ++j) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const Gates g = gates(r[j].at(v), rate[v], t0 + j < c.len);
@@ -293,6 +308,16 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
         D[v] = fmaf(A[v], dh[j].at(v), D[v]);
         S[v] = fmaf(g.a, S[v], qs[j][v] * xv);
       }
+    }
+    // (these and no others pass the barrier: what else would be kept, or moved
+    // behind it, does not fit the registers)
+#pragma unroll
+    for (int j = 0; j < TC; ++j) {
+      asm volatile("" : "+v"(dh[j].raw));
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        asm volatile("" : "+v"(av[j][v]), "+v"(sr[j][v]), "+v"(qs[j][v]), "+v"(xs[j][v]), "+v"(m[j][v]));
+    }
     float (&g)[3][W][64][V] = agg[k & 1];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -301,22 +326,11 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
       g[2][w][lane][v] = D[v];
     }
     lds_barrier();
-    float mine[V];
+    if (k + 1 < last)
 #pragma unroll
-    for (int v = 0; v < V; ++v) mine[v] = carry[v];
-    // (two at a time: all of them loaded at once would not fit the registers)
-#pragma unroll
-    for (int s = 0; s < W; ++s) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int z = W - 1 - s;
-        const float next = fmaf(g[0][s][lane][v], h[v], g[1][s][lane][v]);
-        h[v] = s < w ? next : h[v];
-        carry[v] = fmaf(g[0][z][lane][v], carry[v], g[2][z][lane][v]);
-        mine[v] = z - 1 == w ? carry[v] : mine[v];
-      }
-      if (s & 1) __builtin_amdgcn_sched_barrier(0);
-    }
+      for (int v = 0; v < V; ++v) carry[v] = end[(k & 1) ^ 1][lane][v];
+    pass<V, W>(g[0], g[1], 0, 1, w, lane, h);
+    pass<V, W>(g[0], g[2], W - 1, -1, W - 1 - w, lane, carry);
 #pragma unroll
     for (int j = 0; j < TC; ++j)  // (h: what the state at the stretch's start has come to)
 #pragma unroll
@@ -330,9 +344,9 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
       float dx[V], dr[V], di[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const float d = dh[j].at(v) + mine[v];
-        mine[v] = av[j][v] * d;
-        const float e = mine[v] * m[j][v];
+        const float d = dh[j].at(v) + carry[v];
+        carry[v] = av[j][v] * d;
+        const float e = carry[v] * m[j][v];
         dlam[v] += e;
         dr[v] = fmaf(-e, sr[j][v], e);
         dx[v] = d * qs[j][v];
@@ -344,6 +358,9 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
       Vec<T, V>::store(frame(a.dr, at), o, dr);
       Vec<T, V>::store(frame(a.di, at), o, di);
     }
+    if (w == 0)
+#pragma unroll
+      for (int v = 0; v < V; ++v) end[k & 1][lane][v] = carry[v];
   }
   if (a.dh0 && c.on && w == 0 && first == 0)
 #pragma unroll
@@ -369,6 +386,12 @@ __global__ __launch_bounds__(64 * W) void gr_span_kernel(GatedRecurrence a) {
   __shared__ float agg[2][W][64][V];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Columns<V, RAGGED> c(a, lane);
+  // what all spans start from, where no span's end (which may go to its place)
+  // overwrites it before the others have read it
+  const float* from = BACK ? a.dhT : a.h0;
+  if (from && blockIdx.y == 0 && c.on && w == 0)
+#pragma unroll
+    for (int v = 0; v < V; ++v) a.start[c.st + v] = from[c.st + v];
   const int span = blockIdx.y + (BACK ? 1 : 0);  // (the first one's backward is not needed)
   const int first = span * a.span_tiles;
   const int last = first + a.span_tiles < c.tiles ? first + a.span_tiles : c.tiles;
@@ -381,9 +404,9 @@ __global__ __launch_bounds__(64 * W) void gr_span_kernel(GatedRecurrence a) {
     A[v] = 1.f;
     S[v] = 0.f;
   }
-  const int from = first * GR_TILE + w * mine * TC;
+  const int begin = first * GR_TILE + w * mine * TC;
   for (int k = 0; k < mine; ++k) {
-    const int t0 = from + k * TC;
+    const int t0 = begin + k * TC;
     Vec<T, V> x[TC], r[TC], i[TC], dh[TC];
     if constexpr (BACK) {
       fetch<RAGGED, T, V, TC, 1>(a, {a.r}, a.ld, t0, c, {&r});
@@ -466,7 +489,7 @@ hipError_t launch(GatedRecurrence a, bool forward, hipStream_t s) {
   // one frame and nothing to keep of it: a wave does without a tile
   if (forward && a.T == 1 && !a.saved) {
     a.span_tiles = 1;
-    hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, 1, 1>), dim3((unsigned)groups), dim3(64), 0, s, a);
+    hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, false, 1, 1>), dim3((unsigned)groups), dim3(64), 0, s, a);
     return hipGetLastError();
   }
   const int spans = gated_spans(a.T, groups);
@@ -476,9 +499,12 @@ hipError_t launch(GatedRecurrence a, bool forward, hipStream_t s) {
     const dim3 most(grid.x, grid.y - 1);
     if (forward) hipLaunchKernelGGL((gr_span_kernel<T, V, RAGGED, false>), most, dim3(64 * W), 0, s, a);
     else hipLaunchKernelGGL((gr_span_kernel<T, V, RAGGED, true>), most, dim3(64 * W), 0, s, a);
+    if (a.h0) a.h0 = a.start;
+    if (a.dhT) a.dhT = a.start;
   }
   if (forward) {
-    hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, TC, W>), grid, dim3(64 * W), 0, s, a);
+    if (a.span_tiles > 1) hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, true, TC, W>), grid, dim3(64 * W), 0, s, a);
+    else hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, false, TC, W>), grid, dim3(64 * W), 0, s, a);
     return hipGetLastError();
   }
   hipLaunchKernelGGL((gr_backward_kernel<T, V, RAGGED>), grid, dim3(64 * W), 0, s, a);

@@ -138,6 +138,22 @@ def test_frame_by_frame_is_the_whole(B, H):
     assert_close("h", got.float().cpu().numpy(), want.float().cpu().numpy(), 2 * BF16_TOL)
 
 
+@pytest.mark.parametrize("T,B,H,lengths", [(64, 3, 96, None), (5000, 2, 96, None), (20000, 1, 64, None),
+                                           (5000, 3, 96, [5000, 700, 0])])
+def test_states_in_place(T, B, H, lengths):
+    """hT over h0 and dh0 over dhT, however time is cut up."""
+    c = Case(T, B, H, lengths=lengths, seed=16)
+    want = [t.clone() for t in c.forward() + c.backward()]
+    h, state = torch.empty_like(want[0]), c.h0.clone()
+    am.gated_recurrence_forward(*c.cols(c.proj), c.lam, T, B, h, c.ws, lengths=lengths, h0=state, hT=state,
+                                train=True)
+    dproj, dlam, dstate = torch.empty_like(c.proj), torch.empty(H, device="cuda"), c.dhT.clone()
+    am.gated_recurrence_backward(*c.cols(c.proj), c.lam, T, B, c.dh, c.ws, *c.cols(dproj), dlam,
+                                 lengths=lengths, dhT=dstate, dh0=dstate)
+    got = (h, state, *c.cols(dproj), dlam, dstate)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_extreme_gates():
     """Shut and open gates, and rates that vanish or that forget at once: every
     output finite and the oracle's."""
