@@ -152,8 +152,11 @@ def _dev(t, name, dtype=None):
 
 
 def _stream(stream):
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    if torch.cuda.is_initialized():  # (without making a Stream: a microsecond, not three)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
 def _host_i32(a):
@@ -397,45 +400,48 @@ def _dtype(t, name):
     return BF16 if t.dtype == torch.bfloat16 else F32
 
 
+def _refuse(t, name, shape, dtype, how):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise AmError(f"{name} must be a GPU tensor")
+    if t.dtype is not dtype or tuple(t.shape) != shape:
+        raise AmError(f"{name} must be {dtype} of shape {shape}, got {t.dtype} of shape {tuple(t.shape)}")
+    raise AmError(f"{name} must {how}")
+
+
 def _shaped(t, name, shape, dtype=torch.float32):
     """Device pointer of a contiguous GPU tensor of this shape, or None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise AmError(f"{name} must be a GPU tensor")
-    if t.shape != shape:
-        raise AmError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype is not dtype or not t.is_contiguous():
-        raise AmError(f"{name} must be contiguous {dtype}, got {t.dtype}")
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == shape
+            and t.is_contiguous()):
+        _refuse(t, name, shape, dtype, "be contiguous")
     return t.data_ptr()
 
 
-def _rows(N, H, dtype, **named):
-    """Device pointers and the row stride of [N][H] rows (None for None), which
-    may be columns of a wider matrix; they share one stride."""
-    ld, out = None, []
-    for name, t in named.items():
-        if t is None:
-            out.append(None)
-            continue
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise AmError(f"{name} must be a GPU tensor")
-        if t.dtype is not dtype:
-            raise AmError(f"{name} must be {dtype}, got {t.dtype}")
-        if t.shape != (N, H):
-            raise AmError(f"{name} must have shape {(N, H)}, got {tuple(t.shape)}")
-        if N > 1:
-            s0, s1 = t.stride()
-            if (s1 != 1 and H > 1) or s0 < H:
-                raise AmError(f"{name} must have rows of unit stride that do not overlap")
-            if ld is None:
-                ld = s0
-            elif ld != s0:
-                raise AmError(f"{name} must have the same row stride as {next(iter(named))}")
-        elif N == 1 and H > 1 and t.stride(1) != 1:
-            raise AmError(f"{name} must have rows of unit stride")
-        out.append(t.data_ptr())
-    return (*out, H if ld is None else ld)
+def _row(t, name, N, H, dtype):
+    """Device pointer and row stride of [N][H] rows, which may be columns of a
+    wider matrix; (None, H) for None."""
+    if t is None:
+        return None, H
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == (N, H)):
+        _refuse(t, name, (N, H), dtype, "")
+    s0, s1 = t.stride()
+    if s1 != 1 and H > 1 and N > 0:
+        _refuse(t, name, (N, H), dtype, "have rows of unit stride")
+    if N < 2:
+        return t.data_ptr(), H
+    if s0 < H:
+        _refuse(t, name, (N, H), dtype, "have rows that do not overlap")
+    return t.data_ptr(), s0
+
+
+def _rows3(x, r, i, names, N, H, dtype):
+    """Device pointers and the one row stride of three matrices."""
+    (xp, ld), (rp, lr), (ip, li) = (_row(x, names[0], N, H, dtype), _row(r, names[1], N, H, dtype),
+                                    _row(i, names[2], N, H, dtype))
+    if lr != ld or li != ld:
+        raise AmError(f"{', '.join(names)} must have one row stride, got {ld}, {lr} and {li}")
+    return xp, rp, ip, ld
 
 
 def _packed_rows(T, B, lengths):
@@ -444,7 +450,7 @@ def _packed_rows(T, B, lengths):
     arr, lp = _host_i32(lengths)
     if arr.shape != (B,):
         raise AmError(f"lengths must hold B = {B} values")
-    return arr, lp, int(arr.sum())
+    return arr, lp, sum(lengths) if isinstance(lengths, list) else int(arr.sum())
 
 
 def _workspace(ws):
@@ -468,7 +474,7 @@ def gated_recurrence_forward(x, r, i, lam, T, B, h, ws=None, lengths=None, h0=No
     arr, lp, rows = _packed_rows(T, B, lengths)
     if rows != N:
         raise AmError(f"h must have {rows} rows, got {N}")
-    xp, rp, ip, ld = _rows(N, H, x.dtype, x=x, r=r, i=i)
+    xp, rp, ip, ld = _rows3(x, r, i, "xri", N, H, x.dtype)
     wp, wn = _workspace(ws)
     _check(lib().gated_recurrence_forward(
         T, B, H, dt, lp, xp, rp, ip, ld, _shaped(lam, "lam", (H,)), c, _shaped(h0, "h0", (B, H)),
@@ -484,9 +490,9 @@ def gated_recurrence_backward(x, r, i, lam, T, B, dh, ws, dx, dr, di, dlam, leng
     arr, lp, rows = _packed_rows(T, B, lengths)
     if rows != N:
         raise AmError(f"x must have {rows} rows, got {N}")
-    xp, rp, ip, ld = _rows(N, H, x.dtype, x=x, r=r, i=i)
-    dhp, lddh = _rows(N, H, x.dtype, dh=dh)
-    dxp, drp, dip, ldd = _rows(N, H, x.dtype, dx=dx, dr=dr, di=di)
+    xp, rp, ip, ld = _rows3(x, r, i, "xri", N, H, x.dtype)
+    dhp, lddh = _row(dh, "dh", N, H, x.dtype)
+    dxp, drp, dip, ldd = _rows3(dx, dr, di, ("dx", "dr", "di"), N, H, x.dtype)
     wp, wn = _workspace(ws)
     _check(lib().gated_recurrence_backward(
         T, B, H, dt, lp, xp, rp, ip, ld, _shaped(lam, "lam", (H,)), c, dhp, lddh,
@@ -506,7 +512,7 @@ def gated_norm_forward(res, o=None, gate=None, w_post=None, scale=None, w_next=N
     """res, res_out: the residual stream, [N][H] fp32 or bf16; o, gate: [N][H]
     rows; y: [N][H] of their type.  Every part may be left out (see the C ABI)."""
     (N, H), act = res.shape, o if o is not None else y if y is not None else res
-    (op, ldo), (gp, ldg) = _rows(N, H, act.dtype, o=o), _rows(N, H, act.dtype, gate=gate)
+    (op, ldo), (gp, ldg) = _row(o, "o", N, H, act.dtype), _row(gate, "gate", N, H, act.dtype)
     _check(lib().gated_norm_forward(
         N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
         _shaped(scale, "scale", (H,)), _shaped(res, "res", (N, H), res.dtype),
@@ -520,8 +526,8 @@ def gated_norm_backward(res, rstd, dres, ws, o=None, gate=None, w_post=None, sca
     """The gradient of gated_norm_forward with the same res (as it was before),
     o, gate and factors, and the rstd it wrote."""
     (N, H), act = res.shape, o if o is not None else dy if dy is not None else res
-    (op, ldo), (gp, ldg) = _rows(N, H, act.dtype, o=o), _rows(N, H, act.dtype, gate=gate)
-    (dop, lddo), (dgp, lddg) = _rows(N, H, act.dtype, do=do), _rows(N, H, act.dtype, dgate=dgate)
+    (op, ldo), (gp, ldg) = _row(o, "o", N, H, act.dtype), _row(gate, "gate", N, H, act.dtype)
+    (dop, lddo), (dgp, lddg) = _row(do, "do", N, H, act.dtype), _row(dgate, "dgate", N, H, act.dtype)
     wp, wn = _workspace(ws)
     _check(lib().gated_norm_backward(
         N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),

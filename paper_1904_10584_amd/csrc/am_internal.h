@@ -310,27 +310,37 @@ struct GatedRecurrence {
   float* dh0;                  // backward: [B][H] or null
   float* dlam;                 // backward: [H]
   float* saved;                // [tiles][B][H] (written forward if not null)
-  float* parts;                // backward: [spans][B][H] scratch
-  float *spans_a, *spans_s;    // [spans][B][H] scratch
-  float* start;                // [B][H] scratch (of several spans)
-  const int32_t *offs, *lens;  // [T + 1], [B], or null (every sequence has T frames)
+  float* parts;                // backward: [tiles][B][H] scratch (linked tiles; else [B][H])
+  uint32_t *tickets, *flags;   // linked tiles: a word per group, and one per tile of each
+  uint64_t *stretches, *states;  // linked tiles: [tiles][B][H], [blocks][B][H]
+  // [T + 1], [B], [B] (written forward, from the lengths), or null: every sequence
+  // has T frames
+  const int32_t *offs, *lens;
+  int32_t* tails;
   int64_t N;
   int T, B, H;                 // (T: the longest length)
-  int span_tiles;              // (set by the launcher)
+  int most_tiles;              // (set by the launcher)
   float c;
 };
-// Spans that time is cut into for `groups` workgroups' worth of channels.
-int gated_spans(int T, int64_t groups);
-hipError_t gated_forward(const GatedRecurrence& a, bool bf16, hipStream_t s);
+// Whether tiles are workgroups of their own for `groups` workgroups' worth of
+// channels, and the scratch that this takes at most.
+bool gated_linked(int T, int64_t groups);
+struct GatedLinks { int64_t words, stretches, states; };
+GatedLinks gated_links(int64_t T, int64_t B, int64_t H);
+// lengths [host]: those of a.lens, or null
+hipError_t gated_forward(const GatedRecurrence& a, const int32_t* lengths, bool bf16, hipStream_t s);
 hipError_t gated_backward(const GatedRecurrence& a, bool bf16, hipStream_t s);
-// The tables of a batch of sorted lengths, MAX sequences a launch.
+// The tables of a batch of sorted lengths, MAX sequences a launch; the last one
+// clears words and states besides.
 struct GatedSchedule {
   static constexpr int MAX = 400;
   int32_t *offs, *lens, *tails;  // [T + 1], [B], [B] (written)
+  uint32_t* clear_words;
+  uint64_t* clear_states;
+  int64_t words, states;
   int T, B, first, count, last;
   int32_t len[MAX], tail[MAX];   // tail: frames of this sequence and those after it
 };
-hipError_t gated_schedule(GatedSchedule a, const int32_t* lengths, hipStream_t s);
 
 // Gate, norm, residual and next norm (see gated_norm_forward in the C ABI); at
 // most GATED_NORM_BLOCKS workgroups, a row of parts each.

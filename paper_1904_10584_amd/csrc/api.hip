@@ -626,7 +626,7 @@ am_status check_rows(int64_t N, int32_t H, int32_t dtype, const void* p, int64_t
 }
 
 struct GatedLayout {
-  int64_t offs, lens, tails, saved, parts, spans_a, spans_s, start, total;
+  int64_t offs, lens, tails, saved, parts, tickets, stretches, states, total;
 };
 GatedLayout gated_layout(int64_t T, int64_t B, int64_t H, bool varlen, bool train) {
   GatedLayout l{};
@@ -641,16 +641,15 @@ GatedLayout gated_layout(int64_t T, int64_t B, int64_t H, bool varlen, bool trai
     l.lens = take(B * 4);
     l.tails = take(B * 4);
   }
-  // (two channels a lane make the fewest groups, and so the most spans)
-  const int64_t spans = am::gated_spans((int)T, (B * (H / 2) + 63) / 64 > 0 ? (B * (H / 2) + 63) / 64 : 1);
+  const am::GatedLinks k = am::gated_links(T, B, H);
   if (train) {
     l.saved = take((T + am::GR_TILE - 1) / am::GR_TILE * B * H * 4);
-    l.parts = take(spans * B * H * 4);
+    l.parts = take((k.words > 0 ? k.stretches : B * H) * 4);
   }
-  if (spans > 1) {
-    l.spans_a = take(spans * B * H * 4);
-    l.spans_s = take(spans * B * H * 4);
-    l.start = take(B * H * 4);
+  if (k.words > 0) {
+    l.tickets = take(k.words * 4);
+    l.stretches = take(k.stretches * 8);
+    l.states = take(k.states * 8);
   }
   l.total = at;
   return l;
@@ -686,12 +685,13 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
   a.H = H;
   a.lam = lam;
   a.c = c;
-  a.spans_a = at<float>(ws, l.spans_a);
-  a.spans_s = at<float>(ws, l.spans_s);
-  a.start = at<float>(ws, l.start);
+  a.tickets = at<uint32_t>(ws, l.tickets);
+  a.stretches = at<uint64_t>(ws, l.stretches);
+  a.states = at<uint64_t>(ws, l.states);
   if (lengths) {
     a.offs = at<int32_t>(ws, l.offs);
     a.lens = at<int32_t>(ws, l.lens);
+    a.tails = at<int32_t>(ws, l.tails);
   }
   return AM_OK;
 }
@@ -1456,18 +1456,8 @@ am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtyp
   a.hT = hT;
   if (train) a.saved = at<float>(ws, l.saved);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (lengths) {
-    am::GatedSchedule g;
-    g.offs = at<int32_t>(ws, l.offs);
-    g.lens = at<int32_t>(ws, l.lens);
-    g.tails = at<int32_t>(ws, l.tails);
-    g.T = a.T;
-    g.B = B;
-    Timed tm(AM_K_MISC, s, 0.0, 4.0 * a.T + 8.0 * B);
-    AM_TRY(hip_check(am::gated_schedule(g, lengths, s), "schedule"));
-  }
   Timed tm(AM_K_GATED, s, 20.0 * a.N * H, 4.0 * esz_of(dtype) * a.N * H + 8.0 * B * H);
-  return hip_check(am::gated_forward(a, dtype == AM_BF16, s), "gated recurrence");
+  return hip_check(am::gated_forward(a, lengths, dtype == AM_BF16, s), "gated recurrence");
 }
 
 am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dtype, const int32_t* lengths,

@@ -13,11 +13,13 @@
 // stretch's a_t and inputs once, in registers, leaves (A, S) in LDS, composes
 // those of the waves before it, and walks its stretch from the state so found;
 // then the workgroup goes on to the next tile of W stretches.  Where the channels
-// are too few to fill the chip, time is cut into spans of tiles, a workgroup
-// each: one launch leaves every span's (A, S), the next one composes those of the
-// spans before its own and runs.
+// are too few to fill the chip, every tile is a workgroup of its own and they are
+// linked through memory (see Link).
+#include <cstdlib>
+
 #include "am_device.h"
 #include "am_internal.h"
+#include "poll_budget.h"
 
 namespace am {
 namespace {
@@ -153,21 +155,165 @@ __device__ __forceinline__ void fetch(const GatedRecurrence& a, const void* cons
   }
 }
 
-// The state that a span starts from: `from` (or zero) through the stretches
-// (A, S) of the spans first, first + step, ... before it.
-template <int V, bool RAGGED>
-__device__ __forceinline__ void span_start(const GatedRecurrence& a, const Columns<V, RAGGED>& c, const float* from,
-                                           int first, int step, int count, float (&carry)[V]) {
+// Tiles as workgroups of their own.  A workgroup draws the next tile of its
+// channels from a counter, so it only ever waits for tiles that others have drawn
+// before, whose workgroups run already: no wait depends on what is resident or in
+// which order it was launched.  LINK tiles make a block.  A tile publishes its
+// (A, S) as soon as it is evaluated and composes those of the tiles before it in
+// its block; the block's last tile publishes the state that the next block starts
+// from.  So the chain through memory has a link for LINK tiles, and what is
+// composed with what does not depend on who comes first: the same bits each time.
+// All of it is stored and loaded past the caches that XCDs do not share
+// (agent-scope atomics).  A tile's (A, S) are followed by its flag; a state carries
+// its flag in its upper half.  Polls are bounded; one that runs out (a stalled
+// device) goes on with NaN.
+constexpr int LINK = 16;
+constexpr unsigned POLLS = 1u << 22;
+
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  return (uint64_t)__float_as_uint(lo) | ((uint64_t)__float_as_uint(hi) << 32);
+}
+template <typename U> __device__ __forceinline__ U peek(const U* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename U> __device__ __forceinline__ void post(U* p, U v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The state that tile n (of `tiles`, in the order of the recurrence) starts from.
+// (A, S): its stretches', `start` what tile 0 starts from, pre and first LDS.  Each
+// wave composes two of the block's tiles before this one.
+template <bool BACK, int V, bool RAGGED>
+__device__ __forceinline__ void linked(const GatedRecurrence& a, const Columns<V, RAGGED>& c, int lane, int w,
+                                       int n, int tiles, const float (&A)[W][64][V], const float (&S)[W][64][V],
+                                       const float (&start)[V], float (&pre)[2][W][64][V], float (&first)[64][V],
+                                       float (&state)[V]) {
+  static_assert(LINK <= 2 * W, "two tiles a wave");
   const int64_t BH = (int64_t)a.B * a.H;
+  const int block = n / LINK, place = n % LINK;
+  const bool more = n + 1 < tiles;
+  uint32_t* flags = a.flags + (int64_t)blockIdx.x * a.most_tiles + (n - place);
+  uint64_t* parts = a.stretches + (int64_t)(n - place) * BH + c.st;
+  float ta[V], ts[V];
+  if (w == 0 && more) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) carry[v] = from ? from[c.st + v] : 0.f;
-#pragma unroll 8
-  for (int n = 0; n < count; ++n) {
-    const float* p = a.spans_a + (first + n * step) * BH + c.st;
-    const float* q = a.spans_s + (first + n * step) * BH + c.st;
+    for (int v = 0; v < V; ++v) {
+      ta[v] = 1.f;
+      ts[v] = 0.f;
+    }
 #pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = fmaf(p[v], carry[v], q[v]);
+    for (int q = 0; q < W; ++q)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int s = BACK ? W - 1 - q : q;
+        ts[v] = fmaf(A[s][lane][v], ts[v], S[s][lane][v]);
+        ta[v] *= A[s][lane][v];
+        if (v + 1 == V && (q & 1)) asm volatile("" ::: "memory");
+      }
+    if (place + 1 < LINK) {
+      if (c.on)
+#pragma unroll
+        for (int v = 0; v < V; ++v) post(parts + place * BH + v, pair(ta[v], ts[v]));
+      // (the stores have arrived, and `start` has been read: its place may be given
+      // to the state at the sequence's end)
+#pragma unroll
+      for (int v = 0; v < V; ++v) asm volatile("" ::"v"(start[v]));
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      __builtin_amdgcn_s_waitcnt(0);
+      if (lane == 0) post(flags + place, 1u);
+    }
   }
+  float pa[V], ps[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    pa[v] = 1.f;
+    ps[v] = 0.f;
+  }
+  PollBudget<POLLS> budget;
+  const int j0 = 2 * w, j1 = 2 * w + 1 < place ? 2 * w + 1 : 2 * w;
+  if (j0 < place) {
+    bool lost = false;
+    while (!__all(peek(flags + (lane & 1 ? j1 : j0)) != 0)) {
+      if (budget.spent()) {
+        lost = true;
+        break;
+      }
+      __builtin_amdgcn_s_sleep(1);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    uint64_t p0[V], p1[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      p0[v] = peek(parts + j0 * BH + v);
+      p1[v] = peek(parts + j1 * BH + v);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      pa[v] = lost ? __builtin_nanf("") : __uint_as_float((uint32_t)p0[v]);
+      ps[v] = __uint_as_float((uint32_t)(p0[v] >> 32));
+      if (j1 > j0) {
+        const float a1 = __uint_as_float((uint32_t)p1[v]), s1 = __uint_as_float((uint32_t)(p1[v] >> 32));
+        ps[v] = fmaf(a1, ps[v], s1);
+        pa[v] *= a1;
+      }
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    pre[0][w][lane][v] = pa[v];
+    pre[1][w][lane][v] = ps[v];
+  }
+  if (w == 0) {
+    float from[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) from[v] = start[v];
+    if (block > 0) {
+      const uint64_t* at = a.states + (int64_t)block * BH + c.st;
+      budget.begin();
+      for (;;) {
+        bool here = true;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const uint64_t p = peek(at + v);
+          from[v] = __uint_as_float((uint32_t)p);
+          here = here && (p >> 32) != 0;
+        }
+        if (__all(here)) break;
+        if (budget.spent()) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) from[v] = __builtin_nanf("");
+          break;
+        }
+        __builtin_amdgcn_s_sleep(1);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) first[lane][v] = from[v];
+  }
+  lds_barrier();
+#pragma unroll
+  for (int v = 0; v < V; ++v) state[v] = first[lane][v];
+#pragma unroll
+  for (int s = 0; s < LINK / 2; ++s) {
+    if (2 * s >= place) break;
+#pragma unroll
+    for (int v = 0; v < V; ++v) state[v] = fmaf(pre[0][s][lane][v], state[v], pre[1][s][lane][v]);
+    if (s & 1) asm volatile("" ::: "memory");
+  }
+  if (w == 0 && more && place + 1 == LINK && c.on)
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      post(a.states + (int64_t)(block + 1) * BH + c.st + v,
+           (uint64_t)__float_as_uint(fmaf(ta[v], state[v], ts[v])) | ((uint64_t)1 << 32));
+}
+
+// The tile that this workgroup draws (every wave calls this).
+__device__ __forceinline__ int draw_tile(const GatedRecurrence& a) {
+  __shared__ int drawn;
+  if (threadIdx.x == 0)
+    drawn = (int)__hip_atomic_fetch_add(a.tickets + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(drawn);
 }
 
 // The composition of the stretches (A, S) of waves from, from + by, ... (count of
@@ -185,16 +331,20 @@ __device__ __forceinline__ void pass(const float (&A)[N][64][V], const float (&S
   }
 }
 
-// AHEAD: several tiles, the next one's loads under the end of this one.
-template <typename T, int V, bool RAGGED, bool AHEAD, int STRETCH, int WAVES>
+// How a workgroup takes tiles: the one there is, all of its channels' in turn (the
+// next one's loads under the end of this one), or one that it draws.
+enum Tiles { ONE, IN_TURN, LINKED };
+
+template <typename T, int V, bool RAGGED, Tiles MODE, int STRETCH, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurrence a) {
   __shared__ float agg[2][2][WAVES][64][V];  // of tiles taken in turn: A, S of each stretch
-  __shared__ float end[2][64][V];            // and the state at the tile's end
+  __shared__ float end[2][64][V];            // and the state at the tile's end, or its block's start (LINKED)
+  __shared__ float pre[MODE == LINKED ? 2 : 1][MODE == LINKED ? W : 1][64][V];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Columns<V, RAGGED> c(a, lane);
-  const int first = blockIdx.y * a.span_tiles;
-  const int last = first + a.span_tiles < c.tiles ? first + a.span_tiles : c.tiles;
-  if (first >= c.tiles && first > 0) return;
+  const int first = MODE == LINKED ? draw_tile(a) : 0;
+  if (MODE == LINKED && first >= c.tiles && first > 0) return;
+  const int last = MODE == IN_TURN ? c.tiles : c.tiles > first ? first + 1 : first;
   Vec<T, V> x[STRETCH], r[STRETCH], i[STRETCH];
   auto take = [&](int k) {
     fetch<RAGGED, T, V, STRETCH, 3>(a, {a.r, a.i, a.x}, a.ld, k * GR_TILE + w * STRETCH, c, {&r, &i, &x});
@@ -202,10 +352,12 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
   if (first < last) take(first);
   float rate[V], h[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) rate[v] = a.c * softplus(a.lam[c.d + v]);
-  span_start(a, c, a.h0, 0, 1, (int)blockIdx.y, h);
+  for (int v = 0; v < V; ++v) {
+    rate[v] = a.c * softplus(a.lam[c.d + v]);
+    h[v] = a.h0 && (MODE != LINKED || first < LINK) ? a.h0[c.st + v] : 0.f;
+  }
   const uint32_t mine = lane_offset<T>(c, a.H);
-  for (int k = first; k < last; ++k) {
+  auto tile = [&](int k) {
     const int t0 = k * GR_TILE + w * STRETCH;
     float av[STRETCH][V], u[STRETCH][V], A[V], S[V];
 #pragma unroll
@@ -214,7 +366,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
       S[v] = 0.f;
     }
 #pragma unroll
-    for (int j = 0; j < STRETCH; ++j)
+    for (int j = 0; j < STRETCH; ++j) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const Gates g = gates(r[j].at(v), rate[v], t0 + j < c.len);
@@ -223,7 +375,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
         A[v] *= g.a;
         S[v] = fmaf(g.a, S[v], u[j][v]);
       }
-    if (AHEAD && k + 1 < last) take(k + 1);
+    }
+    if (MODE == IN_TURN && k + 1 < last) take(k + 1);
     if constexpr (WAVES > 1) {
       float (&g)[2][WAVES][64][V] = agg[k & 1];
 #pragma unroll
@@ -232,9 +385,15 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
         g[1][w][lane][v] = S[v];
       }
       lds_barrier();
-      if (AHEAD && k > first)
+      if constexpr (MODE == LINKED) {
+        float start[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) start[v] = h[v];
+        linked<false>(a, c, lane, w, k, c.tiles, g[0], g[1], start, pre, end[0], h);
+      } else if (MODE == IN_TURN && k > first) {
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = end[(k & 1) ^ 1][lane][v];
+      }
       if (a.saved && c.on && w == 0)
 #pragma unroll
         for (int v = 0; v < V; ++v) a.saved[(int64_t)k * a.B * a.H + c.st + v] = h[v];
@@ -247,34 +406,39 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
       Vec<T, V>::store(frame(a.h, first_row<RAGGED>(a, t0 + j) * a.H * (int)sizeof(T)),
                        t0 + j < c.len ? mine : NONE, h);
     }
-    if (AHEAD && w == WAVES - 1)
+    if (MODE == IN_TURN && w == WAVES - 1)
 #pragma unroll
       for (int v = 0; v < V; ++v) end[k & 1][lane][v] = h[v];
-  }
+  };
+  if constexpr (MODE == IN_TURN)
+    for (int k = first; k < last; ++k) tile(k);
+  else if (first < last)
+    tile(first);
   if (a.hT && c.on && w == WAVES - 1 && last == c.tiles)
 #pragma unroll
     for (int v = 0; v < V; ++v) a.hT[c.st + v] = h[v];
 }
 
-template <typename T, int V, bool RAGGED>
+template <typename T, int V, bool RAGGED, Tiles MODE>
 __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence a) {
   __shared__ float agg[2][3][W][64][V];  // A, S and the carry's end from zero
-  __shared__ float end[2][64][V];        // the carry at the tile's start
+  __shared__ float end[2][64][V];        // the carry at the tile's start, or at its block's end (LINKED)
+  __shared__ float pre[MODE == LINKED ? 2 : 1][MODE == LINKED ? W : 1][64][V];
   __shared__ float lsum[W][64][V];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Columns<V, RAGGED> c(a, lane);
   const int64_t BH = (int64_t)a.B * a.H;
-  const int first = blockIdx.y * a.span_tiles;
-  const int last = first + a.span_tiles < c.tiles ? first + a.span_tiles : c.tiles;
+  const int drawn = MODE == LINKED ? draw_tile(a) : 0;  // (from the last tile down)
+  const int last = MODE == LINKED ? (drawn < c.tiles ? c.tiles - drawn : 0) : c.tiles;
+  const int first = MODE == LINKED ? (last > 0 ? last - 1 : 0) : 0;
   float rate[V], carry[V], dlam[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     rate[v] = a.c * softplus(a.lam[c.d + v]);
+    carry[v] = a.dhT && (MODE != LINKED || drawn < LINK) ? a.dhT[c.st + v] : 0.f;
     dlam[v] = 0.f;
   }
-  const int spans = (c.tiles + a.span_tiles - 1) / a.span_tiles;
-  span_start(a, c, a.dhT, spans - 1, -1, spans - 1 - (int)blockIdx.y, carry);
-  for (int k = last - 1; k >= first; --k) {
+  auto tile = [&](int k) {
     const int t0 = k * GR_TILE + w * TC;
     Vec<T, V> x[TC], r[TC], i[TC], dh[TC];
     fetch<RAGGED, T, V, TC, 3>(a, {a.r, a.i, a.x}, a.ld, t0, c, {&r, &i, &x});
@@ -326,9 +490,15 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
       g[2][w][lane][v] = D[v];
     }
     lds_barrier();
-    if (k + 1 < last)
+    if constexpr (MODE == LINKED) {
+      float start[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) start[v] = carry[v];
+      linked<true>(a, c, lane, w, drawn, c.tiles, g[0], g[2], start, pre, end[0], carry);
+    } else if (k + 1 < last) {
 #pragma unroll
       for (int v = 0; v < V; ++v) carry[v] = end[(k & 1) ^ 1][lane][v];
+    }
     pass<V, W>(g[0], g[1], 0, 1, w, lane, h);
     pass<V, W>(g[0], g[2], W - 1, -1, W - 1 - w, lane, carry);
 #pragma unroll
@@ -358,11 +528,17 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
       Vec<T, V>::store(frame(a.dr, at), o, dr);
       Vec<T, V>::store(frame(a.di, at), o, di);
     }
-    if (w == 0)
+    if (MODE != LINKED && w == 0)
 #pragma unroll
       for (int v = 0; v < V; ++v) end[k & 1][lane][v] = carry[v];
-  }
-  if (a.dh0 && c.on && w == 0 && first == 0)
+  };
+  if constexpr (MODE != LINKED)
+    for (int k = last - 1; k >= first; --k) tile(k);
+  else if (first < last)
+    tile(first);
+  // (every drawn number has its row of parts, and number c.tiles - 1, or 0 where
+  // there are none, ends at the first frame)
+  if (a.dh0 && c.on && w == 0 && first == 0 && (MODE != LINKED || drawn + 1 == c.tiles || (c.tiles == 0 && drawn == 0)))
 #pragma unroll
     for (int v = 0; v < V; ++v) a.dh0[c.st + v] = carry[v];
 #pragma unroll
@@ -374,76 +550,8 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
       float s = lsum[0][lane][v];
 #pragma unroll
       for (int k = 1; k < W; ++k) s += lsum[k][lane][v];
-      a.parts[blockIdx.y * BH + c.st + v] = s;
+      a.parts[drawn * BH + c.st + v] = s;
     }
-}
-
-// What a span does to the state that it starts from: (A, S) forward, (A, the
-// carry's end) backward (BACK).  Each wave composes stretches that follow one
-// another, then the waves' in order.
-template <typename T, int V, bool RAGGED, bool BACK>
-__global__ __launch_bounds__(64 * W) void gr_span_kernel(GatedRecurrence a) {
-  __shared__ float agg[2][W][64][V];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Columns<V, RAGGED> c(a, lane);
-  // what all spans start from, where no span's end (which may go to its place)
-  // overwrites it before the others have read it
-  const float* from = BACK ? a.dhT : a.h0;
-  if (from && blockIdx.y == 0 && c.on && w == 0)
-#pragma unroll
-    for (int v = 0; v < V; ++v) a.start[c.st + v] = from[c.st + v];
-  const int span = blockIdx.y + (BACK ? 1 : 0);  // (the first one's backward is not needed)
-  const int first = span * a.span_tiles;
-  const int last = first + a.span_tiles < c.tiles ? first + a.span_tiles : c.tiles;
-  if (first >= last) return;
-  const int mine = last - first;  // stretches a wave
-  float rate[V], A[V], S[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    rate[v] = a.c * softplus(a.lam[c.d + v]);
-    A[v] = 1.f;
-    S[v] = 0.f;
-  }
-  const int begin = first * GR_TILE + w * mine * TC;
-  for (int k = 0; k < mine; ++k) {
-    const int t0 = begin + k * TC;
-    Vec<T, V> x[TC], r[TC], i[TC], dh[TC];
-    if constexpr (BACK) {
-      fetch<RAGGED, T, V, TC, 1>(a, {a.r}, a.ld, t0, c, {&r});
-      fetch<RAGGED, T, V, TC, 1>(a, {a.dh}, a.lddh, t0, c, {&dh});
-    } else {
-      fetch<RAGGED, T, V, TC, 3>(a, {a.r, a.i, a.x}, a.ld, t0, c, {&r, &i, &x});
-    }
-#pragma unroll
-    for (int j = 0; j < TC; ++j)
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const Gates g = gates(r[j].at(v), rate[v], t0 + j < c.len);
-        if constexpr (BACK) S[v] = fmaf(A[v] * g.a, dh[j].at(v), S[v]);
-        else S[v] = fmaf(g.a, S[v], g.q * sigm(i[j].at(v)) * x[j].at(v));
-        A[v] *= g.a;
-      }
-  }
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    agg[0][w][lane][v] = A[v];
-    agg[1][w][lane][v] = S[v];
-  }
-  __syncthreads();
-  if (w != 0 || !c.on) return;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    float at = 1.f, st = 0.f;
-#pragma unroll
-    for (int k = 0; k < W; ++k) {
-      const int s = BACK ? W - 1 - k : k;
-      st = fmaf(agg[0][s][lane][v], st, agg[1][s][lane][v]);
-      at *= agg[0][s][lane][v];
-    }
-    const int64_t o = (int64_t)span * a.B * a.H + c.st + v;
-    a.spans_a[o] = at;
-    a.spans_s[o] = st;
-  }
 }
 
 // dlam[d] = sigm(lam) / softplus(lam) times the sum of the rows of parts; their
@@ -460,7 +568,8 @@ __global__ __launch_bounds__(1024) void gr_dlam_kernel(const float* __restrict__
 }
 
 // The packed offset of every frame, off_t = B_t t + (the sum of the lengths from
-// sequence B_t on), and the lengths, where the kernels read them.
+// sequence B_t on), and the lengths, where the kernels read them; and the words of
+// linked tiles that start from zero.
 __global__ __launch_bounds__(256) void gr_schedule_kernel(GatedSchedule a) {
   const int t = blockIdx.x * 256 + threadIdx.x;
   if (t <= a.T && a.last) {
@@ -477,37 +586,78 @@ __global__ __launch_bounds__(256) void gr_schedule_kernel(GatedSchedule a) {
     a.lens[a.first + t] = a.len[t];
     a.tails[a.first + t] = a.tail[t];
   }
+  if (a.last)
+    for (int64_t k = t; k < a.words + a.states; k += (int64_t)gridDim.x * 256) {
+      if (k < a.words) a.clear_words[k] = 0;
+      else a.clear_states[k - a.words] = 0;
+    }
 }
 
-// Workgroups that fill the chip: three of 8 waves a CU.
-constexpr int64_t FULL = 768;
+hipError_t schedule(GatedSchedule a, const int32_t* lengths, hipStream_t s) {
+  int64_t after = 0;  // frames of the sequences from a place on
+  for (int b = 0; b < a.B; ++b) after += lengths[b];
+  for (a.first = 0; a.first < a.B; a.first += a.count) {
+    a.count = a.B - a.first < GatedSchedule::MAX ? a.B - a.first : GatedSchedule::MAX;
+    for (int k = 0; k < a.count; ++k) {
+      a.len[k] = lengths[a.first + k];
+      a.tail[k] = (int32_t)after;
+      after -= lengths[a.first + k];
+    }
+    a.last = a.first + a.count == a.B;
+    int64_t n = a.count;
+    if (a.last) {
+      if (a.T + 1 > n) n = a.T + 1;
+      const int64_t clear = a.words + a.states < 65536 ? a.words + a.states : 65536;
+      if (clear > n) n = clear;
+    }
+    hipLaunchKernelGGL(gr_schedule_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
+  }
+  return hipGetLastError();
+}
 
 template <typename T, int V, bool RAGGED>
-hipError_t launch(GatedRecurrence a, bool forward, hipStream_t s) {
-  const int64_t groups = ((int64_t)a.B * (a.H / V) + 63) / 64;
-  const int tiles = (a.T + GR_TILE - 1) / GR_TILE;
+hipError_t launch(GatedRecurrence a, const int32_t* lengths, bool forward, hipStream_t s) {
+  const unsigned groups = (unsigned)(((int64_t)a.B * (a.H / V) + 63) / 64);
+  a.most_tiles = (a.T + GR_TILE - 1) / GR_TILE;
+  const bool link = gated_linked(a.T, groups);
+  int64_t words = 0, states = 0;  // (tickets, flags and states start from zero)
+  if (link) {
+    a.flags = a.tickets + groups;
+    words = (int64_t)(1 + a.most_tiles) * groups;
+    states = (int64_t)((a.most_tiles - 1) / LINK + 1) * a.B * a.H;
+  }
+  if (RAGGED && forward) {
+    GatedSchedule g;
+    g.offs = const_cast<int32_t*>(a.offs);
+    g.lens = const_cast<int32_t*>(a.lens);
+    g.tails = a.tails;
+    g.T = a.T;
+    g.B = a.B;
+    g.clear_words = a.tickets;
+    g.clear_states = a.states;
+    g.words = words;
+    g.states = states;
+    const hipError_t e = schedule(g, lengths, s);
+    if (e != hipSuccess) return e;
+  } else if (link) {
+    const hipError_t e = fill_zero2(reinterpret_cast<float*>(a.tickets), words,
+                                    reinterpret_cast<float*>(a.states), 2 * states, s);
+    if (e != hipSuccess) return e;
+  }
   // one frame and nothing to keep of it: a wave does without a tile
   if (forward && a.T == 1 && !a.saved) {
-    a.span_tiles = 1;
-    hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, false, 1, 1>), dim3((unsigned)groups), dim3(64), 0, s, a);
+    hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, ONE, 1, 1>), dim3(groups), dim3(64), 0, s, a);
     return hipGetLastError();
   }
-  const int spans = gated_spans(a.T, groups);
-  a.span_tiles = tiles > 0 ? (tiles + spans - 1) / spans : 1;
-  const dim3 grid((unsigned)groups, (unsigned)(tiles > 0 ? (tiles + a.span_tiles - 1) / a.span_tiles : 1));
-  if (grid.y > 1) {
-    const dim3 most(grid.x, grid.y - 1);
-    if (forward) hipLaunchKernelGGL((gr_span_kernel<T, V, RAGGED, false>), most, dim3(64 * W), 0, s, a);
-    else hipLaunchKernelGGL((gr_span_kernel<T, V, RAGGED, true>), most, dim3(64 * W), 0, s, a);
-    if (a.h0) a.h0 = a.start;
-    if (a.dhT) a.dhT = a.start;
-  }
+  const dim3 grid(groups, link ? a.most_tiles : 1), block(64 * W);
   if (forward) {
-    if (a.span_tiles > 1) hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, true, TC, W>), grid, dim3(64 * W), 0, s, a);
-    else hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, false, TC, W>), grid, dim3(64 * W), 0, s, a);
+    if (link) hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, LINKED, TC, W>), grid, block, 0, s, a);
+    else if (a.most_tiles > 1) hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, IN_TURN, TC, W>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, ONE, TC, W>), grid, block, 0, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((gr_backward_kernel<T, V, RAGGED>), grid, dim3(64 * W), 0, s, a);
+  if (link) hipLaunchKernelGGL((gr_backward_kernel<T, V, RAGGED, LINKED>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((gr_backward_kernel<T, V, RAGGED, IN_TURN>), grid, block, 0, s, a);
   hipLaunchKernelGGL(gr_dlam_kernel, dim3((unsigned)((a.H + 31) / 32)), dim3(1024), 0, s, a.parts,
                      (int64_t)a.B * grid.y, a.H, a.lam, a.dlam);
   return hipGetLastError();
@@ -523,46 +673,38 @@ bool paired(const GatedRecurrence& a) {
 }
 
 template <typename T, int V>
-hipError_t shaped(const GatedRecurrence& a, bool forward, hipStream_t s) {
-  return a.lens ? launch<T, V, true>(a, forward, s) : launch<T, V, false>(a, forward, s);
+hipError_t shaped(const GatedRecurrence& a, const int32_t* lengths, bool forward, hipStream_t s) {
+  return a.lens ? launch<T, V, true>(a, lengths, forward, s) : launch<T, V, false>(a, lengths, forward, s);
 }
 
-hipError_t route(const GatedRecurrence& a, bool bf16, bool forward, hipStream_t s) {
-  if (!bf16) return shaped<float, 1>(a, forward, s);
-  return paired(a) ? shaped<bf16_t, 2>(a, forward, s) : shaped<bf16_t, 1>(a, forward, s);
+hipError_t route(const GatedRecurrence& a, const int32_t* lengths, bool bf16, bool forward, hipStream_t s) {
+  if (!bf16) return shaped<float, 1>(a, lengths, forward, s);
+  return paired(a) ? shaped<bf16_t, 2>(a, lengths, forward, s) : shaped<bf16_t, 1>(a, lengths, forward, s);
 }
 
 }  // namespace
 
-hipError_t gated_schedule(GatedSchedule a, const int32_t* lengths, hipStream_t s) {
-  int64_t after = 0;  // frames of the sequences from a place on
-  for (int b = 0; b < a.B; ++b) after += lengths[b];
-  for (a.first = 0; a.first < a.B; a.first += a.count) {
-    a.count = a.B - a.first < GatedSchedule::MAX ? a.B - a.first : GatedSchedule::MAX;
-    for (int k = 0; k < a.count; ++k) {
-      a.len[k] = lengths[a.first + k];
-      a.tail[k] = (int32_t)after;
-      after -= lengths[a.first + k];
-    }
-    a.last = a.first + a.count == a.B;
-    const int n = a.last && a.T + 1 > a.count ? a.T + 1 : a.count;
-    hipLaunchKernelGGL(gr_schedule_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
-  }
-  return hipGetLastError();
+hipError_t gated_forward(const GatedRecurrence& a, const int32_t* lengths, bool bf16, hipStream_t s) {
+  return route(a, lengths, bf16, true, s);
 }
-
-hipError_t gated_forward(const GatedRecurrence& a, bool bf16, hipStream_t s) {
-  return route(a, bf16, true, s);
-}
-
 hipError_t gated_backward(const GatedRecurrence& a, bool bf16, hipStream_t s) {
-  return route(a, bf16, false, s);
+  return route(a, nullptr, bf16, false, s);
 }
 
-int gated_spans(int T, int64_t groups) {
-  const int tiles = (T + GR_TILE - 1) / GR_TILE;
-  const int64_t want = groups * 2 > FULL ? 1 : FULL / groups;
-  return (int)(want < tiles ? want : tiles > 0 ? tiles : 1);
+bool gated_linked(int T, int64_t groups) {
+  static const char* v = getenv("AM_GR_LINK");
+  return T > GR_TILE && groups < (v ? atoi(v) : 512);
+}
+GatedLinks gated_links(int64_t T, int64_t B, int64_t H) {
+  GatedLinks l{0, 0, 0};
+  const int64_t tiles = (T + GR_TILE - 1) / GR_TILE;
+  // two channels a lane make the fewest groups, one a lane the most
+  const int64_t fewest = (B * (H / 2) + 63) / 64, most = (B * H + 63) / 64;
+  if (!gated_linked((int)T, fewest)) return l;
+  l.words = (1 + tiles) * most;
+  l.stretches = tiles * B * H;
+  l.states = ((tiles - 1) / LINK + 1) * B * H;
+  return l;
 }
 
 }  // namespace am
