@@ -112,7 +112,7 @@ __device__ __forceinline__ uint32_t encode4(f32x4_t v, const uint32_t (&bits)[4]
     const float m = fabsf(v[k]);
     top = fmaxf(top, m < __builtin_inff() ? m : 0.f);
   }
-  top = wave_max(top);
+  top = wave_max_uniform(top);
   const int e = (int)(__float_as_uint(top) >> 23) - 7;
   const uint32_t ex = e < 1 ? 1u : (uint32_t)e;
   *scale = __uint_as_float(ex << 23);

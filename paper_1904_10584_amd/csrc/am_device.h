@@ -217,6 +217,30 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// Sum and maximum over a wave by lane moves (no LDS): xor 1, xor 2, then the mirror
+// images of 8 and of 16 lanes, then the four rows of 16.  The same order in every
+// lane, and the result is wave-uniform.
+template <int CTRL> __device__ __forceinline__ float lanes_moved(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+__device__ __forceinline__ float wave_sum_uniform(float v) {
+  v += lanes_moved<0xB1>(v);
+  v += lanes_moved<0x4E>(v);
+  v += lanes_moved<0x141>(v);
+  v += lanes_moved<0x140>(v);
+  return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+}
+__device__ __forceinline__ float wave_max_uniform(float v) {
+  v = fmaxf(v, lanes_moved<0xB1>(v));
+  v = fmaxf(v, lanes_moved<0x4E>(v));
+  v = fmaxf(v, lanes_moved<0x141>(v));
+  v = fmaxf(v, lanes_moved<0x140>(v));
+  return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+
 // The sum of column 32 blockIdx.x + threadIdx.x % 32 of parts [rows][width], by a
 // workgroup of 1024: 32 threads take every 32nd row each, eight loads ahead of
 // their adds, and the first 32 threads return the sums (in a fixed order).

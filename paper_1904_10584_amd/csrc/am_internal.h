@@ -344,7 +344,7 @@ struct GatedSchedule {
 
 // Gate, norm, residual and next norm (see gated_norm_forward in the C ABI); at
 // most GATED_NORM_BLOCKS workgroups, a row of parts each.
-constexpr int GATED_NORM_BLOCKS = 1024, GATED_NORM_MAX_H = 8192;
+constexpr int GATED_NORM_BLOCKS = 768, GATED_NORM_MAX_H = 8192;
 struct GatedNorm {
   int64_t N;
   int H;

@@ -16,8 +16,6 @@ typedef f32x4_t f32x4_u __attribute__((aligned(4)));
 typedef uint16_t u16x4_t __attribute__((ext_vector_type(4)));
 typedef u16x4_t u16x4_u __attribute__((aligned(2)));
 
-// Four elements from a place of a row of H, those past its end as zeros; rows of
-// odd lengths start at any element, which the memory instructions take.
 __device__ __forceinline__ f32x4_t wide(f32x4_t v) { return v; }
 __device__ __forceinline__ f32x4_t wide(u16x4_t v) {
   f32x4_t o;
@@ -29,24 +27,43 @@ template <typename T> struct Four;
 template <> struct Four<float> { typedef f32x4_t type; typedef f32x4_u at; };
 template <> struct Four<bf16_t> { typedef u16x4_t type; typedef u16x4_u at; };
 
+__device__ __forceinline__ f32x4_t narrow(f32x4_t v, f32x4_t*) { return v; }
+__device__ __forceinline__ u16x4_t narrow(f32x4_t v, u16x4_t*) {  // (to nearest even)
+  typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(u16x4_t, __builtin_convertvector(v, bf16x4_t));
+}
+
+// Four elements from place e of a row of H, those past its end as zeros; rows of
+// odd lengths start at any element, which the memory instructions take.  `inside`
+// (a constant where it is called): none are past it.  Else the load is the same for every lane (a branch for each
+// would keep the loads of a row apart): where fewer than four are left, the row's
+// last four, moved down.
 template <typename T>
-__device__ __forceinline__ typename Four<T>::type load4(const T* row, int e, int H) {
+__device__ __forceinline__ typename Four<T>::type load4(const T* row, int e, int H, bool inside) {
+  typedef typename Four<T>::at At;
+  if (inside) return *reinterpret_cast<const At*>(row + e);
   typename Four<T>::type v = {0, 0, 0, 0};
-  if (e + 4 <= H) {
-    v = *reinterpret_cast<const typename Four<T>::at*>(row + e);
-  } else {
+  if (H < 4) {
 #pragma unroll
     for (int k = 0; k < 3; ++k)
       if (e + k < H) v[k] = row[e + k];
+    return v;
   }
+  const int from = e < H - 4 ? e : H - 4, past = e - from;
+  v = *reinterpret_cast<const At*>(row + from);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = past & 1 ? (k < 3 ? v[k < 3 ? k + 1 : 3] : (T)0) : v[k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = past & 2 ? (k < 2 ? v[k < 2 ? k + 2 : 3] : (T)0) : v[k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = past > 3 ? (T)0 : v[k];
   return v;
 }
 template <typename T>
-__device__ __forceinline__ void store4(T* row, int e, int H, f32x4_t v) {
-  typename Four<T>::type o;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) o[k] = from_f32<T>(v[k]);
-  if (e + 4 <= H) {
+__device__ __forceinline__ void store4(T* row, int e, int H, bool inside, f32x4_t v) {
+  typedef typename Four<T>::type Type;
+  const Type o = narrow(v, (Type*)nullptr);
+  if (inside || e + 4 <= H) {
     *reinterpret_cast<typename Four<T>::at*>(row + e) = o;
   } else {
 #pragma unroll
@@ -57,49 +74,73 @@ __device__ __forceinline__ void store4(T* row, int e, int H, f32x4_t v) {
 
 constexpr int WAVES = 4;  // waves of a workgroup
 
-// The sum over the row's WPR waves (1, or all of the workgroup), in each of them.
+// Place of this thread's elements: WPR waves have a row, NV times four elements a
+// lane; WAVES / WPR rows of a workgroup side by side.
+template <int WPR> struct Place {
+  static constexpr int ROWS = WAVES / WPR, STEP = 256 * WPR;
+  int row, e0;  // row of the workgroup's, first element
+  __device__ Place() {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    row = w / WPR;
+    e0 = 4 * ((w % WPR) * 64 + (threadIdx.x & 63));
+  }
+};
+
+// The sum over the row's WPR waves, in each of them; red: LDS, of sums taken in
+// turn (`turn` alternates, so that one barrier a sum is enough).
 template <int WPR>
-__device__ __forceinline__ float row_sum(float v, float* red) {
-  v = wave_sum(v);
+__device__ __forceinline__ float row_sum(float v, float (&red)[2][WAVES], int& turn) {
+  v = wave_sum_uniform(v);
   if constexpr (WPR == 1) return v;
-  const int w = threadIdx.x >> 6;
-  __syncthreads();  // the last sum has been read
-  if ((threadIdx.x & 63) == 0) red[w] = v;
+  const int w = threadIdx.x >> 6, w0 = w / WPR * WPR;
+  if ((threadIdx.x & 63) == 0) red[turn][w] = v;
   __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
+  float s = red[turn][w0];
+#pragma unroll
+  for (int k = 1; k < WPR; ++k) s += red[turn][w0 + k];
+  turn ^= 1;
+  return s;
 }
 
-template <typename T, typename R, int NV, int WPR>
+// Of a lane's NV fours those that lie in every row of the lengths that NV stands
+// for (see `sized`).
+constexpr int whole_fours(int nv) { return nv <= 4 ? nv - 1 : 4; }
+
+template <typename T, typename R, int NV, int WPR, bool EXACT>
 __global__ __launch_bounds__(256) void norm_forward_kernel(GatedNorm a) {
-  __shared__ float red[WAVES];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int H = a.H, e0 = 4 * (WPR == 1 ? lane : (int)threadIdx.x);
+  __shared__ float red[2][WAVES];
+  int turn = 0;
+  const Place<WPR> at;
+  auto inside = [](int k) { return EXACT || k < whole_fours(NV); };
+  const int H = a.H;
   const float inv = 1.f / (float)H;
   f32x4_t add[NV], next[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int e = e0 + k * 256 * WPR;
+    const int e = at.e0 + k * at.STEP;
     const f32x4_t one = {1.f, 1.f, 1.f, 1.f};
-    add[k] = (a.w_post ? load4(a.w_post, e, H) : one) * (a.scale ? load4(a.scale, e, H) : one);
-    next[k] = a.w_next ? load4(a.w_next, e, H) : one;
+    add[k] = (a.w_post ? load4(a.w_post, e, H, inside(k)) : one) * (a.scale ? load4(a.scale, e, H, inside(k)) : one);
+    next[k] = a.w_next ? load4(a.w_next, e, H, inside(k)) : one;
   }
-  constexpr int ROWS = WAVES / WPR;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + (WPR == 1 ? w : 0); row < a.N;
-       row += (int64_t)gridDim.x * ROWS) {
+  // (every wave takes as many turns: the sums of several waves have barriers; a row
+  // past the last is the last one again, and not stored)
+  for (int64_t first = (int64_t)blockIdx.x * at.ROWS; first < a.N; first += (int64_t)gridDim.x * at.ROWS) {
+    const bool on = first + at.row < a.N;
+    const int64_t row = on ? first + at.row : a.N - 1;
     f32x4_t u[NV], t[NV];
     const R* res = static_cast<const R*>(a.res) + row * H;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) t[k] = wide(load4(res, e0 + k * 256 * WPR, H));
+    for (int k = 0; k < NV; ++k) t[k] = wide(load4(res, at.e0 + k * at.STEP, H, inside(k)));
     float rstd_u = 1.f;
     if (a.o) {
       const T* o = static_cast<const T*>(a.o) + row * a.ldo;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) u[k] = wide(load4(o, e0 + k * 256 * WPR, H));
+      for (int k = 0; k < NV; ++k) u[k] = wide(load4(o, at.e0 + k * at.STEP, H, inside(k)));
       if (a.gate) {
         const T* gate = static_cast<const T*>(a.gate) + row * a.ldg;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          const f32x4_t g = wide(load4(gate, e0 + k * 256 * WPR, H));
+          const f32x4_t g = wide(load4(gate, at.e0 + k * at.STEP, H, inside(k)));
 #pragma unroll
           for (int j = 0; j < 4; ++j) u[k][j] *= g[j] * sigm(g[j]);
         }
@@ -110,15 +151,17 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(GatedNorm a) {
         for (int k = 0; k < NV; ++k)
 #pragma unroll
           for (int j = 0; j < 4; ++j) s = fmaf(u[k][j], u[k][j], s);
-        rstd_u = rsqrtf(row_sum<WPR>(s, red) * inv + a.eps);
+        rstd_u = rsqrtf(row_sum<WPR>(s, red, turn) * inv + a.eps);
       }
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int j = 0; j < 4; ++j) t[k][j] = fmaf(u[k][j] * rstd_u, add[k][j], t[k][j]);
-      R* out = static_cast<R*>(a.res_out) + row * H;
+      if (on) {
+        R* out = static_cast<R*>(a.res_out) + row * H;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) store4(out, e0 + k * 256 * WPR, H, t[k]);
+        for (int k = 0; k < NV; ++k) store4(out, at.e0 + k * at.STEP, H, inside(k), t[k]);
+      }
     }
     float rstd_n = 1.f;
     if (a.w_next) {
@@ -127,17 +170,25 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(GatedNorm a) {
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int j = 0; j < 4; ++j) s = fmaf(t[k][j], t[k][j], s);
-      rstd_n = rsqrtf(row_sum<WPR>(s, red) * inv + a.eps);
-      T* y = static_cast<T*>(a.y) + row * H;
+      rstd_n = rsqrtf(row_sum<WPR>(s, red, turn) * inv + a.eps);
+      if (on) {
+        T* y = static_cast<T*>(a.y) + row * H;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) store4(y, e0 + k * 256 * WPR, H, t[k] * rstd_n * next[k]);
+        for (int k = 0; k < NV; ++k) store4(y, at.e0 + k * at.STEP, H, inside(k), t[k] * rstd_n * next[k]);
+      }
     }
-    if (a.rstd && (WPR == 1 ? lane : (int)threadIdx.x) == 0) {
+    if (a.rstd && on && at.e0 == 0) {
       a.rstd[2 * row] = rstd_u;
       a.rstd[2 * row + 1] = rstd_n;
     }
   }
 }
+
+// Wavefronts a SIMD that the backward pass's registers leave room for: as many
+// workgroups a CU make the grid, which then has no last round half empty (32768 x
+// 1536 in bf16: 207 us with 1024 workgroups, 157 with 768; 16384 x 768 with an fp32
+// stream: 61 and 52).
+constexpr int backward_waves(int nv) { return nv <= 3 ? 3 : nv <= 4 ? 2 : 1; }
 
 // With n = R / rms(R), dn = dy w_next:  dR = dres_out + (dn - n mean(dn n)) / rms(R),
 // the gradient of res; dp = dR scale w_post;  du = (dp - p mean(dp p)) / rms(u), and
@@ -146,40 +197,42 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(GatedNorm a) {
 // gradients of w_post and scale are scale and w_post times the same column sum
 // of dR p; the sums run down a wave's rows in its registers and leave as one row
 // per workgroup.
-template <typename T, typename R, int NV, int WPR>
-__global__ __launch_bounds__(256) void norm_backward_kernel(GatedNorm a) {
-  __shared__ float red[WAVES];
-  __shared__ f32x4_t sums[2][WPR == 1 ? NV * 64 : 1];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int H = a.H, e0 = 4 * (WPR == 1 ? lane : (int)threadIdx.x);
+template <typename T, typename R, int NV, int WPR, bool EXACT>
+__global__ __launch_bounds__(256, backward_waves(NV)) void norm_backward_kernel(GatedNorm a) {
+  __shared__ float red[2][WAVES];
+  __shared__ f32x4_t sums[2][WPR < WAVES ? NV * 64 * WPR : 1];
+  int turn = 0;
+  const Place<WPR> at;
+  auto inside = [](int k) { return EXACT || k < whole_fours(NV); };
+  const int H = a.H;
   const float inv = 1.f / (float)H;
   f32x4_t add[NV], next[NV], along[NV], ndy[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int e = e0 + k * 256 * WPR;
+    const int e = at.e0 + k * at.STEP;
     const f32x4_t one = {1.f, 1.f, 1.f, 1.f};
-    add[k] = (a.w_post ? load4(a.w_post, e, H) : one) * (a.scale ? load4(a.scale, e, H) : one);
-    next[k] = a.w_next ? load4(a.w_next, e, H) : one;
+    add[k] = (a.w_post ? load4(a.w_post, e, H, inside(k)) : one) * (a.scale ? load4(a.scale, e, H, inside(k)) : one);
+    next[k] = a.w_next ? load4(a.w_next, e, H, inside(k)) : one;
     along[k] = ndy[k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  constexpr int ROWS = WAVES / WPR;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + (WPR == 1 ? w : 0); row < a.N;
-       row += (int64_t)gridDim.x * ROWS) {
+  for (int64_t first = (int64_t)blockIdx.x * at.ROWS; first < a.N; first += (int64_t)gridDim.x * at.ROWS) {
+    const bool on = first + at.row < a.N;
+    const int64_t row = on ? first + at.row : a.N - 1;
     f32x4_t p[NV], t[NV], d[NV];
     typename Four<T>::type o[NV], g[NV];
     const float rstd_u = a.rstd[2 * row], rstd_n = a.rstd[2 * row + 1];
     const R* res = static_cast<const R*>(a.res) + row * H;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) t[k] = wide(load4(res, e0 + k * 256 * WPR, H));
+    for (int k = 0; k < NV; ++k) t[k] = wide(load4(res, at.e0 + k * at.STEP, H, inside(k)));
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      d[k] = a.dres_out ? wide(load4(static_cast<const R*>(a.dres_out) + row * H, e0 + k * 256 * WPR, H))
+      d[k] = a.dres_out ? wide(load4(static_cast<const R*>(a.dres_out) + row * H, at.e0 + k * at.STEP, H, inside(k)))
                         : f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (a.o) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        o[k] = load4(static_cast<const T*>(a.o) + row * a.ldo, e0 + k * 256 * WPR, H);
-        if (a.gate) g[k] = load4(static_cast<const T*>(a.gate) + row * a.ldg, e0 + k * 256 * WPR, H);
+        o[k] = load4(static_cast<const T*>(a.o) + row * a.ldo, at.e0 + k * at.STEP, H, inside(k));
+        if (a.gate) g[k] = load4(static_cast<const T*>(a.gate) + row * a.ldg, at.e0 + k * at.STEP, H, inside(k));
       }
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
@@ -197,30 +250,31 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(GatedNorm a) {
       float s = 0.f;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        dy[k] = wide(load4(static_cast<const T*>(a.dy) + row * H, e0 + k * 256 * WPR, H));
+        dy[k] = wide(load4(static_cast<const T*>(a.dy) + row * H, at.e0 + k * at.STEP, H, inside(k)));
         t[k] *= rstd_n;
-        ndy[k] += dy[k] * t[k];
+        if (on) ndy[k] += dy[k] * t[k];
         dy[k] *= next[k];
 #pragma unroll
         for (int j = 0; j < 4; ++j) s = fmaf(dy[k][j], t[k][j], s);
       }
-      s = row_sum<WPR>(s, red) * inv;
+      s = row_sum<WPR>(s, red, turn) * inv;
 #pragma unroll
       for (int k = 0; k < NV; ++k) d[k] += (dy[k] - t[k] * s) * rstd_n;
     }
+    if (on)
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-      store4(static_cast<R*>(a.dres) + row * H, e0 + k * 256 * WPR, H, d[k]);
+      for (int k = 0; k < NV; ++k)
+        store4(static_cast<R*>(a.dres) + row * H, at.e0 + k * at.STEP, H, inside(k), d[k]);
     if (a.o) {
       float s = 0.f;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        along[k] += d[k] * p[k];
+        if (on) along[k] += d[k] * p[k];
         d[k] *= add[k];
 #pragma unroll
         for (int j = 0; j < 4; ++j) s = fmaf(d[k][j], p[k][j], s);
       }
-      if (a.w_post) s = row_sum<WPR>(s, red) * inv;
+      if (a.w_post) s = row_sum<WPR>(s, red, turn) * inv;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const f32x4_t ov = wide(o[k]);
@@ -236,34 +290,35 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(GatedNorm a) {
             dov[j] = du[j] * gv[j] * sg;
             dg[j] = du[j] * ov[j] * sg * (1.f + gv[j] * (1.f - sg));
           }
-          store4(static_cast<T*>(a.dgate) + row * a.lddg, e0 + k * 256 * WPR, H, dg);
+          if (on) store4(static_cast<T*>(a.dgate) + row * a.lddg, at.e0 + k * at.STEP, H, inside(k), dg);
         }
-        store4(static_cast<T*>(a.d_o) + row * a.lddo, e0 + k * 256 * WPR, H, dov);
+        if (on) store4(static_cast<T*>(a.d_o) + row * a.lddo, at.e0 + k * at.STEP, H, inside(k), dov);
       }
     }
   }
-  // the column sums of this workgroup's rows, wave after wave
-  if constexpr (WPR == 1) {
-    for (int s = 0; s < WAVES; ++s) {
-      if (w == s)
+  // the column sums of this workgroup's rows, one of them after another
+  if constexpr (WPR < WAVES) {
+    const int place = at.e0 / 4;
+    for (int s = 0; s < at.ROWS; ++s) {
+      if (at.row == s)
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
           if (s > 0) {
-            along[k] += sums[0][k * 64 + lane];
-            ndy[k] += sums[1][k * 64 + lane];
+            along[k] += sums[0][k * 64 * WPR + place];
+            ndy[k] += sums[1][k * 64 * WPR + place];
           }
-          sums[0][k * 64 + lane] = along[k];
-          sums[1][k * 64 + lane] = ndy[k];
+          sums[0][k * 64 * WPR + place] = along[k];
+          sums[1][k * 64 * WPR + place] = ndy[k];
         }
       __syncthreads();
     }
-    if (w != WAVES - 1) return;
+    if (at.row != at.ROWS - 1) return;
   }
   float* parts = a.parts + (int64_t)blockIdx.x * 2 * H;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    store4(parts, e0 + k * 256 * WPR, H, along[k]);
-    store4(parts + H, e0 + k * 256 * WPR, H, ndy[k]);
+    store4(parts, at.e0 + k * at.STEP, H, inside(k), along[k]);
+    store4(parts + H, at.e0 + k * at.STEP, H, inside(k), ndy[k]);
   }
 }
 
@@ -282,29 +337,36 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restr
   }
 }
 
-template <typename T, typename R, int NV, int WPR>
+template <typename T, typename R, int NV, int WPR, bool EXACT>
 hipError_t launch(const GatedNorm& a, bool forward, hipStream_t s) {
-  const int64_t blocks = (a.N * WPR + WAVES - 1) / WAVES;
-  const unsigned grid = (unsigned)(blocks < GATED_NORM_BLOCKS ? blocks : GATED_NORM_BLOCKS);
+  const int64_t blocks = (a.N * WPR + WAVES - 1) / WAVES, most = forward ? 1024 : 256 * backward_waves(NV);
+  const unsigned grid = (unsigned)(blocks < most ? blocks : most);
   if (forward) {
-    hipLaunchKernelGGL((norm_forward_kernel<T, R, NV, WPR>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((norm_forward_kernel<T, R, NV, WPR, EXACT>), dim3(grid), dim3(256), 0, s, a);
   } else {
-    if (grid > 0) hipLaunchKernelGGL((norm_backward_kernel<T, R, NV, WPR>), dim3(grid), dim3(256), 0, s, a);
+    if (grid > 0) hipLaunchKernelGGL((norm_backward_kernel<T, R, NV, WPR, EXACT>), dim3(grid), dim3(256), 0, s, a);
     hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2 * a.H + 31) / 32)), dim3(1024), 0, s, a.parts,
                        (int)grid, a);
   }
   return hipGetLastError();
 }
 
+template <typename T, typename R, int NV, int WPR>
+hipError_t filled(const GatedNorm& a, bool forward, hipStream_t s) {
+  return a.H == NV * 256 * WPR ? launch<T, R, NV, WPR, true>(a, forward, s) : launch<T, R, NV, WPR, false>(a, forward, s);
+}
+
 template <typename T, typename R>
 hipError_t sized(const GatedNorm& a, bool forward, hipStream_t s) {
-  if (a.H <= 256) return launch<T, R, 1, 1>(a, forward, s);
-  if (a.H <= 512) return launch<T, R, 2, 1>(a, forward, s);
-  if (a.H <= 768) return launch<T, R, 3, 1>(a, forward, s);
-  if (a.H <= 1024) return launch<T, R, 4, 1>(a, forward, s);
-  if (a.H <= 2048) return launch<T, R, 2, 4>(a, forward, s);
-  if (a.H <= 4096) return launch<T, R, 4, 4>(a, forward, s);
-  return launch<T, R, 8, 4>(a, forward, s);
+  if (a.H <= 256) return filled<T, R, 1, 1>(a, forward, s);
+  if (a.H <= 512) return filled<T, R, 2, 1>(a, forward, s);
+  if (a.H <= 768) return filled<T, R, 3, 1>(a, forward, s);
+  if (a.H <= 1024) return filled<T, R, 4, 1>(a, forward, s);
+  if (a.H <= 1536) return filled<T, R, 3, 2>(a, forward, s);
+  if (a.H <= 2048) return filled<T, R, 4, 2>(a, forward, s);
+  if (a.H <= 3 * 1024) return filled<T, R, 3, 4>(a, forward, s);
+  if (a.H <= 4096) return filled<T, R, 4, 4>(a, forward, s);
+  return filled<T, R, 8, 4>(a, forward, s);
 }
 
 hipError_t route(const GatedNorm& a, bool bf16, bool stream_bf16, bool forward, hipStream_t s) {
