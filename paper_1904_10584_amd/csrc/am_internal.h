@@ -383,7 +383,8 @@ struct AdamwBatch {
   float b1, c1, b2, c2, root, eps, step;
   const float* grad_scale;    // device, or null
 };
-hipError_t adamw_launch(const AdamwBatch& a, bool grad_bf16, bool codes, hipStream_t s);
+// bytes: what the whole step reads and writes, in however many launches
+hipError_t adamw_launch(const AdamwBatch& a, bool grad_bf16, bool codes, int64_t bytes, hipStream_t s);
 
 // Elementwise and data-movement helpers.
 hipError_t sgd_apply_f32(int64_t n, float* master, uint16_t* w_bf16, const float* u, float lr,

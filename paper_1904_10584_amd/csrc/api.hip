@@ -1590,7 +1590,8 @@ am_status adamw_apply(int32_t count, const am_adamw_tensor* tensors, int32_t gra
     all += t.n;
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
-  Timed tm(AM_K_ADAMW, s, 14.0 * all, (10.0 + (grad_dtype == AM_BF16 ? 2 : 4) + (codes ? 4 : 16)) * all);
+  const int64_t bytes = (10 + (grad_dtype == AM_BF16 ? 2 : 4) + (codes ? 4 : 16)) * all;
+  Timed tm(AM_K_ADAMW, s, 14.0 * all, (double)bytes);
   am::AdamwBatch a{};
   a.b1 = (float)beta1;
   a.c1 = (float)(1.0 - beta1);
@@ -1606,7 +1607,7 @@ am_status adamw_apply(int32_t count, const am_adamw_tensor* tensors, int32_t gra
     if (t.n > 0) {
       const uint64_t need = (uint64_t)((t.n + am::ADAMW_CHUNK - 1) / am::ADAMW_CHUNK);
       if (a.count == am::AdamwBatch::MAX || (a.count > 0 && groups + need >= (1ull << 31))) {
-        AM_TRY(hip_check(am::adamw_launch(a, grad_dtype == AM_BF16, codes, s), "adamw"));
+        AM_TRY(hip_check(am::adamw_launch(a, grad_dtype == AM_BF16, codes, bytes, s), "adamw"));
         a.count = 0;
         groups = 0;
       }
@@ -1626,7 +1627,7 @@ am_status adamw_apply(int32_t count, const am_adamw_tensor* tensors, int32_t gra
       a.first[++a.count] = (uint32_t)groups;
     }
   }
-  if (a.count > 0) return hip_check(am::adamw_launch(a, grad_dtype == AM_BF16, codes, s), "adamw");
+  if (a.count > 0) return hip_check(am::adamw_launch(a, grad_dtype == AM_BF16, codes, bytes, s), "adamw");
   return AM_OK;
 }
 

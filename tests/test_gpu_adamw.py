@@ -193,6 +193,26 @@ def test_elements_past_32_bits():
         assert torch.equal(d[k][-4096:], s[k]) and not d[k][:8192].any()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_large_step_is_the_small_ones(bits):
+    """More than the caches hold (accesses go past them): the first elements as by
+    themselves."""
+    n, few = 45_000_001, 256 * 300
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    kind = torch.float32 if bits == 32 else torch.uint8
+    d = {k: torch.randn(n, device="cuda", generator=gen) for k in ("master", "grad")}
+    d.update({k: torch.zeros(n, dtype=kind, device="cuda") for k in ("m", "v")})
+    d["weights_bf16"] = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    if bits == 8:
+        d.update({k: torch.zeros(am.adamw_scales(n), device="cuda") for k in ("m_scale", "v_scale")})
+    s = {k: t[:few // 256 if "scale" in k else few].clone() for k, t in d.items()}
+    for step in (1, 2):
+        am.adamw_apply(am.AdamWTensors([d]), step=step, seed=step, **OPT)
+        am.adamw_apply(am.AdamWTensors([s]), step=step, seed=step, **OPT)
+    for k, t in s.items():
+        assert torch.equal(d[k][:t.numel()], t), k
+
+
 def test_from_a_graph_and_on_a_stream():
     t, u = Tensors([300, 70001], 8), Tensors([300, 70001], 8)
     a, b = am.AdamWTensors(t.dev), am.AdamWTensors(u.dev)
