@@ -621,7 +621,8 @@ am_status check_rows(int64_t N, int32_t H, int32_t dtype, const void* p, int64_t
   if (N > 0 && !p) return fail(AM_EINVAL, "NULL %s", name);
   if (!aligned(p, (uintptr_t)esz_of(dtype))) return fail(AM_EINVAL, "%s is not aligned to its elements", name);
   if (ld < H) return fail(AM_EINVAL, "row stride %lld of %s is less than %d", (long long)ld, name, H);
-  if (frame > 0 && ld > (1ll << 30) / frame) return fail(AM_EUNSUPPORTED, "frames of %s beyond 2^30 elements", name);
+  if (frame > 0 && ld > ((1ll << 30) - 8) / frame)
+    return fail(AM_EUNSUPPORTED, "frames of %s beyond 2^30 - 8 elements", name);
   return AM_OK;
 }
 

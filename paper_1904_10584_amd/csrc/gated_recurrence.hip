@@ -15,8 +15,6 @@
 // then the workgroup goes on to the next tile of W stretches.  Where the channels
 // are too few to fill the chip, every tile is a workgroup of its own and they are
 // linked through memory (see Link).
-#include <cstdlib>
-
 #include "am_device.h"
 #include "am_internal.h"
 #include "poll_budget.h"
@@ -167,8 +165,12 @@ __device__ __forceinline__ void fetch(const GatedRecurrence& a, const void* cons
 // (agent-scope atomics).  A tile's (A, S) are followed by its flag; a state carries
 // its flag in its upper half.  Polls are bounded; one that runs out (a stalled
 // device) goes on with NaN.
-constexpr int LINK = 16;
+// (One sequence of 40001 frames x 1536, forward: LINK = 4, 8, 12, 16: 190, 164, 174,
+// 171 us.  Without the links it would take 102, the time of its bytes: the tiles of
+// a group wait for one another at the same time, with nothing left to load.)
+constexpr int LINK = 8;
 constexpr unsigned POLLS = 1u << 22;
+constexpr int TICKET_LINE = 64;  // words: a counter to itself
 
 __device__ __forceinline__ uint64_t pair(float lo, float hi) {
   return (uint64_t)__float_as_uint(lo) | ((uint64_t)__float_as_uint(hi) << 32);
@@ -181,21 +183,24 @@ template <typename U> __device__ __forceinline__ void post(U* p, U v) {
 }
 
 // The state that tile n (of `tiles`, in the order of the recurrence) starts from.
-// (A, S): its stretches', `start` what tile 0 starts from, pre and first LDS.  Each
-// wave composes two of the block's tiles before this one.
+// (A, S): its stretches', `start` what tile 0 starts from, pre and first LDS.  The
+// waves share the work, so that its round trips to memory run side by side: the
+// last one publishes, the one before it waits for the block's start, and each of
+// the first ones composes two of the block's tiles before this one.
 template <bool BACK, int V, bool RAGGED>
 __device__ __forceinline__ void linked(const GatedRecurrence& a, const Columns<V, RAGGED>& c, int lane, int w,
                                        int n, int tiles, const float (&A)[W][64][V], const float (&S)[W][64][V],
                                        const float (&start)[V], float (&pre)[2][W][64][V], float (&first)[64][V],
                                        float (&state)[V]) {
-  static_assert(LINK <= 2 * W, "two tiles a wave");
+  static_assert(LINK <= 2 * (W - 2), "two tiles a wave");
+  constexpr int PUBLISHES = W - 1, WAITS = W - 2;
   const int64_t BH = (int64_t)a.B * a.H;
   const int block = n / LINK, place = n % LINK;
   const bool more = n + 1 < tiles;
   uint32_t* flags = a.flags + (int64_t)blockIdx.x * a.most_tiles + (n - place);
   uint64_t* parts = a.stretches + (int64_t)(n - place) * BH + c.st;
   float ta[V], ts[V];
-  if (w == 0 && more) {
+  if (w == PUBLISHES && more) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       ta[v] = 1.f;
@@ -214,11 +219,7 @@ __device__ __forceinline__ void linked(const GatedRecurrence& a, const Columns<V
       if (c.on)
 #pragma unroll
         for (int v = 0; v < V; ++v) post(parts + place * BH + v, pair(ta[v], ts[v]));
-      // (the stores have arrived, and `start` has been read: its place may be given
-      // to the state at the sequence's end)
-#pragma unroll
-      for (int v = 0; v < V; ++v) asm volatile("" ::"v"(start[v]));
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");  // (the stores have arrived)
       __builtin_amdgcn_s_waitcnt(0);
       if (lane == 0) post(flags + place, 1u);
     }
@@ -231,7 +232,7 @@ __device__ __forceinline__ void linked(const GatedRecurrence& a, const Columns<V
   }
   PollBudget<POLLS> budget;
   const int j0 = 2 * w, j1 = 2 * w + 1 < place ? 2 * w + 1 : 2 * w;
-  if (j0 < place) {
+  if (j0 < place && w < WAITS) {
     bool lost = false;
     while (!__all(peek(flags + (lane & 1 ? j1 : j0)) != 0)) {
       if (budget.spent()) {
@@ -263,7 +264,7 @@ __device__ __forceinline__ void linked(const GatedRecurrence& a, const Columns<V
     pre[0][w][lane][v] = pa[v];
     pre[1][w][lane][v] = ps[v];
   }
-  if (w == 0) {
+  if (w == WAITS) {
     float from[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) from[v] = start[v];
@@ -300,7 +301,7 @@ __device__ __forceinline__ void linked(const GatedRecurrence& a, const Columns<V
     for (int v = 0; v < V; ++v) state[v] = fmaf(pre[0][s][lane][v], state[v], pre[1][s][lane][v]);
     if (s & 1) asm volatile("" ::: "memory");
   }
-  if (w == 0 && more && place + 1 == LINK && c.on)
+  if (w == PUBLISHES && more && place + 1 == LINK && c.on)
 #pragma unroll
     for (int v = 0; v < V; ++v)
       post(a.states + (int64_t)(block + 1) * BH + c.st + v,
@@ -311,7 +312,7 @@ __device__ __forceinline__ void linked(const GatedRecurrence& a, const Columns<V
 __device__ __forceinline__ int draw_tile(const GatedRecurrence& a) {
   __shared__ int drawn;
   if (threadIdx.x == 0)
-    drawn = (int)__hip_atomic_fetch_add(a.tickets + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    drawn = (int)__hip_atomic_fetch_add(a.tickets + (int64_t)blockIdx.x * TICKET_LINE, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(drawn);
 }
@@ -334,7 +335,7 @@ __device__ __forceinline__ void pass(const float (&A)[N][64][V], const float (&S
 // The 64 groups of channels of a workgroup.  Sequences are sorted by length, and
 // workgroups 256 apart tend to share a CU: every second 256 are taken from their
 // end, so that long and short ones meet (128 utterances of 200 to 1500 frames x 768:
-// forward 180 -> XX us).
+// forward 180 -> 171 us).
 template <bool RAGGED> __device__ __forceinline__ uint32_t group_of(uint32_t block, uint32_t blocks) {
   if (!RAGGED || !(block >> 8 & 1)) return block;
   const uint32_t first = block & ~255u, last = first + 255 < blocks ? first + 255 : blocks - 1;
@@ -394,6 +395,11 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
         g[0][w][lane][v] = A[v];
         g[1][w][lane][v] = S[v];
       }
+      // (`h0` has been read when the tile is published: its place may be given to the
+      // state at the sequence's end)
+      if (MODE == LINKED)
+#pragma unroll
+        for (int v = 0; v < V; ++v) asm volatile("" ::"v"(h[v]));
       lds_barrier();
       if constexpr (MODE == LINKED) {
         float start[V];
@@ -499,6 +505,9 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
       g[1][w][lane][v] = S[v];
       g[2][w][lane][v] = D[v];
     }
+    if (MODE == LINKED)  // (dhT has been read when the tile is published)
+#pragma unroll
+      for (int v = 0; v < V; ++v) asm volatile("" ::"v"(carry[v]));
     lds_barrier();
     if constexpr (MODE == LINKED) {
       float start[V];
@@ -632,8 +641,8 @@ hipError_t launch(GatedRecurrence a, const int32_t* lengths, bool forward, hipSt
   const bool link = gated_linked(a.T, groups);
   int64_t words = 0, states = 0;  // (tickets, flags and states start from zero)
   if (link) {
-    a.flags = a.tickets + groups;
-    words = (int64_t)(1 + a.most_tiles) * groups;
+    a.flags = a.tickets + (int64_t)groups * TICKET_LINE;
+    words = (int64_t)(TICKET_LINE + a.most_tiles) * groups;
     states = (int64_t)((a.most_tiles - 1) / LINK + 1) * a.B * a.H;
   }
   if (RAGGED && forward) {
@@ -701,17 +710,20 @@ hipError_t gated_backward(const GatedRecurrence& a, bool bf16, hipStream_t s) {
   return route(a, nullptr, bf16, false, s);
 }
 
-bool gated_linked(int T, int64_t groups) {
-  static const char* v = getenv("AM_GR_LINK");
-  return T > GR_TILE && groups < (v ? atoi(v) : 512);
-}
+// From five tiles on, where at most 400 workgroups' worth of channels leave CUs (or,
+// at 256 and more, the second workgroup of some) without work.  Linked / in turn,
+// us, forward and backward, bf16: 6 groups x 2 tiles 17 26 / 13 21, x 5 18 26 / 18
+// 27, x 7 18 26 / 24 35; 192 x 32 tiles 95 173 / 109 217; 256 x 8 35 49 / 31 49;
+// 384 x 32 177 339 / 203 338 (lengths that differ: 114 218 / 119 234); 480 x 32 219
+// 419 / 209 373.
+bool gated_linked(int T, int64_t groups) { return T > 4 * GR_TILE && groups <= 400; }
 GatedLinks gated_links(int64_t T, int64_t B, int64_t H) {
   GatedLinks l{0, 0, 0};
   const int64_t tiles = (T + GR_TILE - 1) / GR_TILE;
   // two channels a lane make the fewest groups, one a lane the most
   const int64_t fewest = (B * (H / 2) + 63) / 64, most = (B * H + 63) / 64;
   if (!gated_linked((int)T, fewest)) return l;
-  l.words = (1 + tiles) * most;
+  l.words = (TICKET_LINE + tiles) * most;
   l.stretches = tiles * B * H;
   l.states = ((tiles - 1) / LINK + 1) * B * H;
   return l;
