@@ -456,7 +456,9 @@ def _packed_rows(T, B, lengths):
 def _workspace(ws):
     if ws is None:
         return None, 0
-    return _dev(ws, "ws"), ws.numel() * ws.element_size()
+    if not (isinstance(ws, torch.Tensor) and ws.is_cuda and ws.is_contiguous()):
+        raise AmError("ws must be a contiguous GPU tensor")
+    return ws.data_ptr(), ws.nbytes
 
 
 def gated_recurrence_workspace_bytes(T, B, H, lengths=None, train=False) -> int:
@@ -476,10 +478,12 @@ def gated_recurrence_forward(x, r, i, lam, T, B, h, ws=None, lengths=None, h0=No
         raise AmError(f"h must have {rows} rows, got {N}")
     xp, rp, ip, ld = _rows3(x, r, i, "xri", N, H, x.dtype)
     wp, wn = _workspace(ws)
-    _check(lib().gated_recurrence_forward(
+    st = (_lib or lib()).gated_recurrence_forward(
         T, B, H, dt, lp, xp, rp, ip, ld, _shaped(lam, "lam", (H,)), c, _shaped(h0, "h0", (B, H)),
         _shaped(h, "h", (N, H), x.dtype), _shaped(hT, "hT", (B, H)), 1 if train else 0, wp, wn,
-        _stream(stream)))
+        _stream(stream))
+    if st:
+        _check(st)
 
 
 def gated_recurrence_backward(x, r, i, lam, T, B, dh, ws, dx, dr, di, dlam, lengths=None, dhT=None,
@@ -494,10 +498,12 @@ def gated_recurrence_backward(x, r, i, lam, T, B, dh, ws, dx, dr, di, dlam, leng
     dhp, lddh = _row(dh, "dh", N, H, x.dtype)
     dxp, drp, dip, ldd = _rows3(dx, dr, di, ("dx", "dr", "di"), N, H, x.dtype)
     wp, wn = _workspace(ws)
-    _check(lib().gated_recurrence_backward(
+    st = (_lib or lib()).gated_recurrence_backward(
         T, B, H, dt, lp, xp, rp, ip, ld, _shaped(lam, "lam", (H,)), c, dhp, lddh,
         _shaped(dhT, "dhT", (B, H)), dxp, drp, dip, ldd, _shaped(dlam, "dlam", (H,)),
-        _shaped(dh0, "dh0", (B, H)), wp, wn, _stream(stream)))
+        _shaped(dh0, "dh0", (B, H)), wp, wn, _stream(stream))
+    if st:
+        _check(st)
 
 
 def gated_norm_workspace_bytes(N, H) -> int:
@@ -513,11 +519,13 @@ def gated_norm_forward(res, o=None, gate=None, w_post=None, scale=None, w_next=N
     rows; y: [N][H] of their type.  Every part may be left out (see the C ABI)."""
     (N, H), act = res.shape, o if o is not None else y if y is not None else res
     (op, ldo), (gp, ldg) = _row(o, "o", N, H, act.dtype), _row(gate, "gate", N, H, act.dtype)
-    _check(lib().gated_norm_forward(
+    st = (_lib or lib()).gated_norm_forward(
         N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
         _shaped(scale, "scale", (H,)), _shaped(res, "res", (N, H), res.dtype),
         _shaped(w_next, "w_next", (H,)), float(eps), _shaped(res_out, "res_out", (N, H), res.dtype),
-        _shaped(y, "y", (N, H), act.dtype), _shaped(rstd, "rstd", (N, 2)), _stream(stream)))
+        _shaped(y, "y", (N, H), act.dtype), _shaped(rstd, "rstd", (N, 2)), _stream(stream))
+    if st:
+        _check(st)
 
 
 def gated_norm_backward(res, rstd, dres, ws, o=None, gate=None, w_post=None, scale=None, w_next=None,
@@ -529,14 +537,16 @@ def gated_norm_backward(res, rstd, dres, ws, o=None, gate=None, w_post=None, sca
     (op, ldo), (gp, ldg) = _row(o, "o", N, H, act.dtype), _row(gate, "gate", N, H, act.dtype)
     (dop, lddo), (dgp, lddg) = _row(do, "do", N, H, act.dtype), _row(dgate, "dgate", N, H, act.dtype)
     wp, wn = _workspace(ws)
-    _check(lib().gated_norm_backward(
+    st = (_lib or lib()).gated_norm_backward(
         N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
         _shaped(scale, "scale", (H,)), _shaped(res, "res", (N, H), res.dtype),
         _shaped(w_next, "w_next", (H,)), float(eps), _shaped(rstd, "rstd", (N, 2)),
         _shaped(dy, "dy", (N, H), act.dtype), _shaped(dres_out, "dres_out", (N, H), res.dtype),
         dop, lddo, dgp, lddg, _shaped(dres, "dres", (N, H), res.dtype),
         _shaped(dw_post, "dw_post", (H,)), _shaped(dscale, "dscale", (H,)),
-        _shaped(dw_next, "dw_next", (H,)), wp, wn, _stream(stream)))
+        _shaped(dw_next, "dw_next", (H,)), wp, wn, _stream(stream))
+    if st:
+        _check(st)
 
 
 class _AdamWTensor(ctypes.Structure):
@@ -601,10 +611,12 @@ def adamw_apply(tensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=
                 stream=None):
     """One AdamW step of an AdamWTensors; grad_scale: [1] fp32 GPU tensor that the
     gradients are multiplied by; seed: of the rounding of 8-bit moments."""
-    _check(lib().adamw_apply(
+    st = (_lib or lib()).adamw_apply(
         len(tensors), tensors.array, tensors.grad_dtype, tensors.state_bits, float(lr), float(beta1),
         float(beta2), float(eps), int(step), _shaped(grad_scale, "grad_scale", (1,)),
-        int(seed) & 0xFFFFFFFF, _stream(stream)))
+        int(seed) & 0xFFFFFFFF, _stream(stream))
+    if st:
+        _check(st)
 
 
 # ------------------------------------------------------------------ timing --

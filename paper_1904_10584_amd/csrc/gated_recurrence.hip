@@ -14,7 +14,7 @@
 // those of the waves before it, and walks its stretch from the state so found;
 // then the workgroup goes on to the next tile of W stretches.  Where the channels
 // are too few to fill the chip, every tile is a workgroup of its own and they are
-// linked through memory (see Link).
+// linked through memory (see LINK).
 #include "am_device.h"
 #include "am_internal.h"
 #include "poll_budget.h"
@@ -114,7 +114,7 @@ template <int V, bool RAGGED> struct Columns {
   bool on;
   int tiles;     // of the workgroup's longest sequence (its first: they are sorted)
   int64_t st;    // place in a [B][H] matrix
-  __device__ Columns(const GatedRecurrence& a, int lane, uint32_t group) {
+  __device__ Columns(const GatedRecurrence& a, int lane, uint32_t group, int tile) {
     const uint32_t per_row = (uint32_t)a.H / V, groups = a.B * per_row, g0 = group * 64;
     on = g0 + lane < groups;
     const uint32_t g = on ? g0 + lane : groups - 1;
@@ -123,7 +123,7 @@ template <int V, bool RAGGED> struct Columns {
     st = (int64_t)b * a.H + d;
     len = on ? RAGGED ? a.lens[b] : a.T : 0;
     const int most = RAGGED ? table(a.lens)[g0 / per_row] : a.T;
-    tiles = (most + GR_TILE - 1) / GR_TILE;
+    tiles = (most + tile - 1) / tile;
   }
 };
 
@@ -165,9 +165,9 @@ __device__ __forceinline__ void fetch(const GatedRecurrence& a, const void* cons
 // (agent-scope atomics).  A tile's (A, S) are followed by its flag; a state carries
 // its flag in its upper half.  Polls are bounded; one that runs out (a stalled
 // device) goes on with NaN.
-// (One sequence of 40001 frames x 1536, forward: LINK = 4, 8, 12, 16: 190, 164, 174,
-// 171 us.  Without the links it would take 102, the time of its bytes: the tiles of
-// a group wait for one another at the same time, with nothing left to load.)
+// (One sequence of 40001 frames x 1536, forward: LINK = 4, 8, 12: 134, 135, 136 us.
+// Without the links it would take 102, the time of its bytes: the tiles of a group
+// wait for one another at the same time, with nothing left to load.)
 constexpr int LINK = 8;
 constexpr unsigned POLLS = 1u << 22;
 constexpr int TICKET_LINE = 64;  // words: a counter to itself
@@ -348,17 +348,18 @@ enum Tiles { ONE, IN_TURN, LINKED };
 
 template <typename T, int V, bool RAGGED, Tiles MODE, int STRETCH, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurrence a) {
+  constexpr int TILE = STRETCH * WAVES;
   __shared__ float agg[2][2][WAVES][64][V];  // of tiles taken in turn: A, S of each stretch
   __shared__ float end[2][64][V];            // and the state at the tile's end, or its block's start (LINKED)
   __shared__ float pre[MODE == LINKED ? 2 : 1][MODE == LINKED ? W : 1][64][V];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Columns<V, RAGGED> c(a, lane, group_of<RAGGED && MODE == IN_TURN>(blockIdx.x, gridDim.x));
+  const Columns<V, RAGGED> c(a, lane, group_of<RAGGED && MODE == IN_TURN>(blockIdx.x, gridDim.x), TILE);
   const int first = MODE == LINKED ? draw_tile(a) : 0;
   if (MODE == LINKED && first >= c.tiles && first > 0) return;
   const int last = MODE == IN_TURN ? c.tiles : c.tiles > first ? first + 1 : first;
   Vec<T, V> x[STRETCH], r[STRETCH], i[STRETCH];
   auto take = [&](int k) {
-    fetch<RAGGED, T, V, STRETCH, 3>(a, {a.r, a.i, a.x}, a.ld, k * GR_TILE + w * STRETCH, c, {&r, &i, &x});
+    fetch<RAGGED, T, V, STRETCH, 3>(a, {a.r, a.i, a.x}, a.ld, k * TILE + w * STRETCH, c, {&r, &i, &x});
   };
   if (first < last) take(first);
   float rate[V], h[V];
@@ -369,7 +370,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
   }
   const uint32_t mine = lane_offset<T>(c, a.H);
   auto tile = [&](int k) {
-    const int t0 = k * GR_TILE + w * STRETCH;
+    const int t0 = k * TILE + w * STRETCH;
     float av[STRETCH][V], u[STRETCH][V], A[V], S[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -410,10 +411,10 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = end[(k & 1) ^ 1][lane][v];
       }
-      if (a.saved && c.on && w == 0)
-#pragma unroll
-        for (int v = 0; v < V; ++v) a.saved[(int64_t)k * a.B * a.H + c.st + v] = h[v];
       pass<V, WAVES>(g[0], g[1], 0, 1, w, lane, h);
+      if (a.saved && c.on && t0 % GR_TILE == 0 && t0 < a.T)
+#pragma unroll
+        for (int v = 0; v < V; ++v) a.saved[(int64_t)(t0 / GR_TILE) * a.B * a.H + c.st + v] = h[v];
     }
 #pragma unroll
     for (int j = 0; j < STRETCH; ++j) {
@@ -442,7 +443,7 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
   __shared__ float pre[MODE == LINKED ? 2 : 1][MODE == LINKED ? W : 1][64][V];
   __shared__ float lsum[W][64][V];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Columns<V, RAGGED> c(a, lane, group_of<RAGGED && MODE == IN_TURN>(blockIdx.x, gridDim.x));
+  const Columns<V, RAGGED> c(a, lane, group_of<RAGGED && MODE == IN_TURN>(blockIdx.x, gridDim.x), GR_TILE);
   const int64_t BH = (int64_t)a.B * a.H;
   const int drawn = MODE == LINKED ? draw_tile(a) : 0;  // (from the last tile down)
   const int last = MODE == LINKED ? (drawn < c.tiles ? c.tiles - drawn : 0) : c.tiles;
@@ -670,7 +671,11 @@ hipError_t launch(GatedRecurrence a, const int32_t* lengths, bool forward, hipSt
   }
   const dim3 grid(groups, link ? a.most_tiles : 1), block(64 * W);
   if (forward) {
-    if (link) hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, LINKED, TC, W>), grid, block, 0, s, a);
+    // (linked stretches of 16 frames, half as many links: the recording of the
+    // comment at LINK took 163 us with 8; the backward pass has no registers left)
+    constexpr int LONG = 16;
+    const dim3 linked(groups, (unsigned)((a.T + LONG * W - 1) / (LONG * W)));
+    if (link) hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, LINKED, LONG, W>), linked, block, 0, s, a);
     else if (a.most_tiles > 1) hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, IN_TURN, TC, W>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((gr_forward_kernel<T, V, RAGGED, ONE, TC, W>), grid, block, 0, s, a);
     return hipGetLastError();
@@ -710,13 +715,15 @@ hipError_t gated_backward(const GatedRecurrence& a, bool bf16, hipStream_t s) {
   return route(a, nullptr, bf16, false, s);
 }
 
-// From five tiles on, where at most 400 workgroups' worth of channels leave CUs (or,
-// at 256 and more, the second workgroup of some) without work.  Linked / in turn,
-// us, forward and backward, bf16: 6 groups x 2 tiles 17 26 / 13 21, x 5 18 26 / 18
-// 27, x 7 18 26 / 24 35; 192 x 32 tiles 95 173 / 109 217; 256 x 8 35 49 / 31 49;
-// 384 x 32 177 339 / 203 338 (lengths that differ: 114 218 / 119 234); 480 x 32 219
-// 419 / 209 373.
-bool gated_linked(int T, int64_t groups) { return T > 4 * GR_TILE && groups <= 400; }
+// Where at most 400 workgroups' worth of channels leave CUs (or the second workgroup
+// of some) without work, from five tiles on, or seven where the first wave of
+// workgroups is nearly enough.  Linked / in turn, us, forward and backward, bf16: 6
+// groups x 320 frames 16 24 / 18 27, x 2000 15 23 / 96 142; 192 x 320 25 30 / 21 33, x
+// 2000 92 173 / 109 217; 256 x 320 28 36 / 22 35, x 500 35 48 / 31 48 (lengths that
+// differ 29 38 / 36 46); 384 x 2000 174 340 / 209 348; 480 x 2000 212 419 / 213 375.
+bool gated_linked(int T, int64_t groups) {
+  return groups <= 400 && T > (groups <= 192 ? 4 : 6) * GR_TILE;
+}
 GatedLinks gated_links(int64_t T, int64_t B, int64_t H) {
   GatedLinks l{0, 0, 0};
   const int64_t tiles = (T + GR_TILE - 1) / GR_TILE;
