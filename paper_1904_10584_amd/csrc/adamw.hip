@@ -4,7 +4,11 @@
 //   g = grad * grad_scale;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) (g g);
 //   w = w keep - step (m / (sqrt(v) root + eps)).
 // HBM bounds it: 30 bytes an element with 32-bit moments, fp32 gradients and the
-// bf16 copy, 18 with 8-bit moments.
+// bf16 copy, 18 with 8-bit moments (16 with bf16 gradients).  24.1 M elements with
+// 32-bit moments: 120 us (6.0 TB/s); 95.4 M with 8-bit moments and bf16 gradients: 277 us (5.5
+// TB/s), where about 125 vector instruction slots an element are nearly as long.
+// A launch has up to 48 tensors, a workgroup 2048 elements of one: every load of a
+// wave's two blocks comes before the first use.
 //
 // 8-bit moments: blocks of 256 elements of a tensor share a scale, the power of
 // two that puts the block's largest magnitude into [128, 256); m and sqrt(v) are
