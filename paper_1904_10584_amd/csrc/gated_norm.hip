@@ -361,7 +361,10 @@ hipError_t filled(const GatedNorm& a, bool forward, hipStream_t s) {
 
 // Two waves for rows beyond 1024: as many registers of one wave would leave one or
 // two waves a SIMD (32768 x 1536 in bf16, forward and backward: one wave a row 428
-// us, two 249).
+// us, two 249).  No more of them where rows are few: the barriers cost what the
+// shorter rows save (512 x 768 in bf16, forward and backward: one wave 3.6 and 9.0 us,
+// two 4.5 and 9.1, four 4.5 and 9.7; 1237 x 1001 in fp32: 7.3 and 15.9, 6.7 and 16.6,
+// 7.9 and 17.2).
 template <typename T, typename R>
 hipError_t sized(const GatedNorm& a, bool forward, hipStream_t s) {
   if (a.H <= 256) return filled<T, R, 1, 1>(a, forward, s);
