@@ -162,6 +162,18 @@ __device__ __forceinline__ void fetch(const GatedRecurrence& a, const void* cons
   }
 }
 
+// V neighbouring fp32 values.
+template <int V> __device__ __forceinline__ void fetch_state(Frame f, uint32_t o, float (&out)[V]) {
+  static_assert(V == 1 || V == 2, "a word or two");
+  if constexpr (V == 1) {
+    out[0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(f, o, 0, 0));
+  } else {
+    const auto w = __builtin_amdgcn_raw_buffer_load_b64(f, o, 0, 0);
+    out[0] = __uint_as_float(w[0]);
+    out[1] = __uint_as_float(w[1]);
+  }
+}
+
 // Tiles as workgroups of their own.  A workgroup draws the next tile of its
 // channels from a counter, so it only ever waits for tiles that others have drawn
 // before, whose workgroups run already: no wait depends on what is resident or in
@@ -469,9 +481,10 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
     Vec<T, V> x[TC], r[TC], i[TC], dh[TC];
     fetch<RAGGED, T, V, TC, 3>(a, {a.r, a.i, a.x}, a.ld, t0, c, {&r, &i, &x});
     fetch<RAGGED, T, V, TC, 1>(a, {a.dh}, a.lddh, t0, c, {&dh});
+    // (zeros for tiles that the lane's sequence does not have: the forward pass may
+    // have grouped channels otherwise and saved nothing there)
     float h[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = a.saved[(int64_t)k * BH + c.st + v];
+    fetch_state<V>(frame(a.saved, k * BH * 4), k * GR_TILE < c.len ? (uint32_t)c.st * 4 : NONE, h);
     // Of a frame: a, sigm(r), q sigm(i) (dx of its dv), x (1 - sigm(i)) (di of its
     // dx), and what its carry is multiplied by in the gradient of log a times log
     // a: v a L / q - L h_{t-1}, at first with the h of a stretch that starts from
