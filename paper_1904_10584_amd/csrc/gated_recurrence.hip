@@ -586,13 +586,15 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
 #pragma unroll
   for (int v = 0; v < V; ++v) lsum[w][lane][v] = dlam[v];
   __syncthreads();
+  // (a sequence without frames adds nothing, whatever its dhT: 0 times an infinity
+  // is none)
   if (c.on && w == 0)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float s = lsum[0][lane][v];
 #pragma unroll
       for (int k = 1; k < W; ++k) s += lsum[k][lane][v];
-      a.parts[drawn * BH + c.st + v] = s;
+      a.parts[drawn * BH + c.st + v] = c.len > 0 ? s : 0.f;
     }
 }
 

@@ -40,3 +40,23 @@ def test_one_pass_on_odd_addresses(H, lengths, odd_forward, odd_backward):
     names = ("h", "hT", "dx", "dr", "di", "dlam", "dh0")
     for name, g, ref in zip(names, (h, hT, dx, dr, di, dlam, dh0), c.oracle()):
         assert_close(name, g.float().cpu().numpy(), ref, BF16_TOL if g.dtype == torch.bfloat16 else F32_TOL)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lengths", [[70, 20, 0], [700, 0, 0], [5, 0]])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_states_of_a_sequence_without_frames_stay_its_own(value, lengths, dtype):
+    """The last sequence has no frames: whatever its states hold leaves as they
+    are, and nothing else sees them."""
+    T, B, H = max(lengths), len(lengths), 40
+    c = Case(T, B, H, dtype, lengths, seed=21)
+    ref = c.oracle()
+    c.h0[-1], c.dhT[-1] = value, value
+    got = c.forward() + c.backward()
+    names = ("h", "hT", "dx", "dr", "di", "dlam", "dh0")
+    for name, g, r in zip(names, got, ref):
+        g = g.float().cpu().numpy()
+        if name in ("hT", "dh0"):
+            assert np.array_equal(g[-1], np.full(H, value, np.float32), equal_nan=True), name
+            g, r = g[:-1], r[:-1]
+        assert_close(name, g, r, BF16_TOL if dtype == torch.bfloat16 and name in ("h", "dx", "dr", "di") else F32_TOL)
