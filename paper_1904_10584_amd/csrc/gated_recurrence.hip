@@ -417,11 +417,11 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
         g[0][w][lane][v] = A[v];
         g[1][w][lane][v] = S[v];
       }
-      // (`h0` has been read when the tile is published: its place may be given to the
-      // state at the sequence's end)
-      if (MODE == LINKED)
+      // (hT may be h0: every wave has read its start before any wave of the workgroup,
+      // or one that waits for this tile, can be done.  The barrier itself waits for LDS
+      // alone; using the register here waits for the load.)
 #pragma unroll
-        for (int v = 0; v < V; ++v) asm volatile("" ::"v"(h[v]));
+      for (int v = 0; v < V; ++v) asm volatile("" ::"v"(h[v]));
       lds_barrier();
       if constexpr (MODE == LINKED) {
         float start[V];
@@ -528,9 +528,9 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
       g[1][w][lane][v] = S[v];
       g[2][w][lane][v] = D[v];
     }
-    if (MODE == LINKED)  // (dhT has been read when the tile is published)
+    // (dh0 may be dhT: as for h0 in the forward pass)
 #pragma unroll
-      for (int v = 0; v < V; ++v) asm volatile("" ::"v"(carry[v]));
+    for (int v = 0; v < V; ++v) asm volatile("" ::"v"(carry[v]));
     lds_barrier();
     if constexpr (MODE == LINKED) {
       float start[V];
