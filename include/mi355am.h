@@ -381,10 +381,10 @@ am_status am_cast_f32_to_bf16(int64_t n, const float* src, void* dst_bf16, void*
  *   ws      workspace of am_gated_recurrence_workspace_bytes (256-byte aligned;
  *           may be NULL where that is 0).  train = 1 keeps in it what
  *           gated_recurrence_backward reads; it must not be modified between.
- * B times a row stride is at most 2^30 - 8.  A batch of one frame per sequence
- * with train = 0 and without lengths is one launch.  Long sequences of few channels
- * run as workgroups that wait for one another; every wait is bounded, and what
- * follows one that runs out (a stalled device) is NaN. */
+ * B times a row stride is at most 2^30 - 8, N less than 2^31 - 256.  A batch of
+ * one frame per sequence with train = 0 and without lengths is one launch.  Long
+ * sequences of few channels run as workgroups that wait for one another; every
+ * wait is bounded, and what follows one that runs out (a stalled device) is NaN. */
 int64_t am_gated_recurrence_workspace_bytes(int32_t T, int32_t B, int32_t H, int32_t varlen,
                                             int32_t train);
 am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtype,

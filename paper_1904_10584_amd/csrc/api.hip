@@ -678,7 +678,9 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
     }
     a.T = lengths[0];
   }
-  if (a.N >= (1ll << 31)) return fail(AM_EUNSUPPORTED, "too many frames");
+  // (the kernels count frames in 32 bits, up to the end of a tile or a workgroup of
+  // 256 past the last)
+  if (a.N >= (1ll << 31) - 256) return fail(AM_EUNSUPPORTED, "too many frames");
   l = gated_layout(T, B, H, lengths != nullptr, train);
   if (l.total > 0 && (!ws || !aligned(ws, 256) || ws_bytes < l.total))
     return fail(AM_EWORKSPACE, "needs %lld workspace bytes, 256-byte aligned", (long long)l.total);
