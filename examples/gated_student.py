@@ -57,7 +57,7 @@ class GatedStudent:
         self.rec_ws = [new(max(need, 1), torch.uint8) for _ in range(layers)]
         self.norm_ws = new(am.gated_norm_workspace_bytes(N, H), torch.uint8)
         self.ce_ws = new(am.ce_workspace_bytes(N), torch.uint8)
-        self.loss, self.dlogits = new(1, F32), new((N, classes))
+        self.loss, self.dlogits, self.guard = new(1, F32), new((N, classes)), new(1, F32)
         self.optimizer = self._optimizer(bits, weight_decay)
 
     def _add(self, name, value, kind=F32):
@@ -124,14 +124,23 @@ class GatedStudent:
         torch.mm(below.to(self.dtype).t(), self.x, out=g["Win"])
 
     def step(self, x, idx, prob):
-        """One training step; the loss stays on the GPU."""
+        """One training step; the loss stays on the GPU.  A loss that is not finite
+        leaves weights and moments as they were (so does a forward pass that timed
+        out: its outputs are NaN)."""
         logits = self.forward(x)
         am.sparse_soft_ce(logits, idx, prob, self.loss, self.dlogits, self.ce_ws)
         self.backward(self.dlogits)
         self.steps += 1
+        torch.mul(self.loss, 0.0, out=self.guard).add_(1.0)  # 1, or NaN
         for tensors in self.optimizer:
-            am.adamw_apply(tensors, lr=self.lr, step=self.steps, beta2=0.99, seed=self.steps)
+            am.adamw_apply(tensors, lr=self.lr, step=self.steps, beta2=0.99, seed=self.steps,
+                           grad_scale=self.guard)
         return self.loss
+
+    def check(self):
+        """Synchronise; raise if a wait of the last step's recurrences timed out."""
+        for ws in self.rec_ws:
+            am.workspace_check(ws)
 
     def stream(self, states, x):
         """Logits of the next frame of each stream (x [B][D]); states [layers][B][H]
@@ -164,6 +173,7 @@ def main():
     for k in range(a.steps):
         loss = student.step(x, idx, prob)
         if k % 10 == 0 or k + 1 == a.steps:
+            student.check()
             print(f"step {k}: loss {float(loss):.4f}", flush=True)
 
 

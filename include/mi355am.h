@@ -61,7 +61,7 @@ typedef enum {
   AM_EUNSUPPORTED = -3,  /* valid but outside what the kernels handle */
   AM_EHIP = -4,          /* a HIP call failed (launch error, ...) */
   AM_EWORKSPACE = -5,    /* workspace missing or too small */
-  AM_ETIMEOUT = -6       /* a step barrier timed out; the pass's results are invalid */
+  AM_ETIMEOUT = -6       /* a wait of a recurrence timed out; the pass's results are invalid */
 } am_status;
 
 typedef enum { AM_F32 = 0, AM_BF16 = 1 } am_dtype;
@@ -177,7 +177,8 @@ am_status lstm_am_backward(const am_model* m, const void* params, const void* x,
  * lstm_am_backward reads the flag on the device as its last step and, when
  * it is set, overwrites `grads` with zeros, so that a caller that encodes
  * and applies the gradient before this check adds nothing to its residual
- * or weights. */
+ * or weights.  The same holds for gated_recurrence_forward and _backward and
+ * the gradients that the latter writes. */
 am_status am_workspace_check(const void* ws, int64_t ws_bytes, void* stream);
 
 /* Gradient Threshold Compression encode (§VI-A), exact fp32:
@@ -383,8 +384,10 @@ am_status am_cast_f32_to_bf16(int64_t n, const float* src, void* dst_bf16, void*
  *           gated_recurrence_backward reads; it must not be modified between.
  * B times a row stride is at most 2^30 - 8, N less than 2^31 - 256.  A batch of
  * one frame per sequence with train = 0 and without lengths is one launch.  Long
- * sequences of few channels run as workgroups that wait for one another; every
- * wait is bounded, and what follows one that runs out (a stalled device) is NaN. */
+ * sequences of few channels run as workgroups that wait for one another.  Every
+ * wait is bounded; one that runs out (a stalled device) sets a flag in `ws`, and
+ * what follows it in h and hT is NaN.  am_workspace_check of any workspace that is
+ * not empty then reports AM_ETIMEOUT; the next forward call clears the flag. */
 int64_t am_gated_recurrence_workspace_bytes(int32_t T, int32_t B, int32_t H, int32_t varlen,
                                             int32_t train);
 am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtype,
@@ -396,6 +399,8 @@ am_status gated_recurrence_forward(int32_t T, int32_t B, int32_t H, int32_t dtyp
  *   dh  [N] rows: dL/dh;  dhT [B][H] fp32 or NULL: dL/dhT
  *   dx, dr, di [N] rows (written);  dlam [H] fp32 (written)
  *   dh0 [B][H] fp32 or NULL (written; may be dhT itself)
+ * Where a wait of this call or of the forward call ran out, dx, dr, di, dlam and
+ * dh0 are zeros (see am_workspace_check).
  * No atomics: the same inputs give the same bits.                           */
 am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dtype,
                                     const int32_t* lengths, const void* x, const void* r, const void* i,

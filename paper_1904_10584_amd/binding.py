@@ -242,8 +242,9 @@ def sparse_soft_ce(logits, idx, prob, loss, dlogits, ws, mask=None, reduction=ME
 
 
 def workspace_check(ws, stream=None):
-    """Synchronise the stream; raise AmError if a step barrier of the last
-    forward/backward pass on `ws` timed out (its outputs are then invalid)."""
+    """Synchronise the stream; raise AmError if a wait of the last forward/backward
+    pass on `ws` (the LSTM's, or a gated recurrence's that is not empty) timed out:
+    its outputs are then invalid."""
     _check(lib().am_workspace_check(_dev(ws, "ws"), ws.numel() * ws.element_size(),
                                     _stream(stream)))
 

@@ -311,7 +311,10 @@ struct GatedRecurrence {
   float* dlam;                 // backward: [H]
   float* saved;                // [tiles][B][H] (written forward if not null)
   float* parts;                // backward: [tiles][B][H] scratch (linked tiles; else [B][H])
-  uint32_t *tickets, *flags;   // linked tiles: a word per group, and one per tile of each
+  int* err;                    // the time-out flag: cleared forward, set by a link's wait
+                               // that runs out; null without a workspace
+  uint32_t *tickets, *flags;   // linked tiles: a word per group, and one per tile of each;
+                               // tickets follow err in memory
   uint64_t *stretches, *states;  // linked tiles: [tiles][B][H], [blocks][B][H]
   // [T + 1], [B], [B] (written forward, from the lengths), or null: every sequence
   // has T frames

@@ -626,8 +626,10 @@ am_status check_rows(int64_t N, int32_t H, int32_t dtype, const void* p, int64_t
   return AM_OK;
 }
 
+// The time-out flag is the last word of a first slot, where am_workspace_check
+// looks; the words of linked tiles follow it, so that one clear serves both.
 struct GatedLayout {
-  int64_t offs, lens, tails, saved, parts, tickets, stretches, states, total;
+  int64_t sync, offs, lens, tails, saved, parts, tickets, stretches, states, total;
 };
 GatedLayout gated_layout(int64_t T, int64_t B, int64_t H, bool varlen, bool train) {
   GatedLayout l{};
@@ -637,20 +639,21 @@ GatedLayout gated_layout(int64_t T, int64_t B, int64_t H, bool varlen, bool trai
     at += align256(bytes);
     return here;
   };
+  const am::GatedLinks k = am::gated_links(T, B, H);
+  if (varlen || train || k.words > 0) l.sync = take(SYNC_BYTES);
+  if (k.words > 0) {
+    l.tickets = take(k.words * 4);
+    l.stretches = take(k.stretches * 8);
+    l.states = take(k.states * 8);
+  }
   if (varlen) {
     l.offs = take((T + 1) * 4);
     l.lens = take(B * 4);
     l.tails = take(B * 4);
   }
-  const am::GatedLinks k = am::gated_links(T, B, H);
   if (train) {
     l.saved = take((T + am::GR_TILE - 1) / am::GR_TILE * B * H * 4);
     l.parts = take((k.words > 0 ? k.stretches : B * H) * 4);
-  }
-  if (k.words > 0) {
-    l.tickets = take(k.words * 4);
-    l.stretches = take(k.stretches * 8);
-    l.states = take(k.states * 8);
   }
   l.total = at;
   return l;
@@ -688,6 +691,7 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
   a.H = H;
   a.lam = lam;
   a.c = c;
+  if (l.total > 0) a.err = sync_err(at<void>(ws, l.sync));
   a.tickets = at<uint32_t>(ws, l.tickets);
   a.stretches = at<uint64_t>(ws, l.stretches);
   a.states = at<uint64_t>(ws, l.states);

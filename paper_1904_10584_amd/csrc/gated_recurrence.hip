@@ -185,7 +185,7 @@ template <int V> __device__ __forceinline__ void fetch_state(Frame f, uint32_t o
 // All of it is stored and loaded past the caches that XCDs do not share
 // (agent-scope atomics).  A tile's (A, S) are followed by its flag; a state carries
 // its flag in its upper half.  Polls are bounded; one that runs out (a stalled
-// device) goes on with NaN.
+// device) sets the workspace's time-out flag and goes on with NaN.
 // (One sequence of 40001 frames x 1536, forward: LINK = 4, 8, 12: 134, 135, 136 us.
 // Without the links it would take 102, the time of its bytes: the tiles of a group
 // wait for one another at the same time, with nothing left to load.)
@@ -258,6 +258,7 @@ __device__ __forceinline__ void linked(const GatedRecurrence& a, const Columns<V
     while (!__all(peek(flags + (lane & 1 ? j1 : j0)) != 0)) {
       if (budget.spent()) {
         lost = true;
+        *a.err = 1;
         break;
       }
       __builtin_amdgcn_s_sleep(1);
@@ -302,6 +303,7 @@ __device__ __forceinline__ void linked(const GatedRecurrence& a, const Columns<V
         }
         if (__all(here)) break;
         if (budget.spent()) {
+          *a.err = 1;
 #pragma unroll
           for (int v = 0; v < V; ++v) from[v] = __builtin_nanf("");
           break;
@@ -375,6 +377,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void gr_forward_kernel(GatedRecurren
   __shared__ float pre[MODE == LINKED ? 2 : 1][MODE == LINKED ? W : 1][64][V];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Columns<V, RAGGED> c(a, lane, group_of<RAGGED && MODE == IN_TURN>(blockIdx.x, gridDim.x), TILE);
+  if (MODE != LINKED && a.err && blockIdx.x == 0 && threadIdx.x == 0) *a.err = 0;
   const int first = MODE == LINKED ? draw_tile(a) : 0;
   if (MODE == LINKED && first >= c.tiles && first > 0) return;
   const int last = MODE == IN_TURN ? c.tiles : c.tiles > first ? first + 1 : first;
@@ -598,23 +601,38 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
     }
 }
 
+// Zeros in place of the gradients of a pass whose wait ran out (every thread of the
+// grid calls this).
+template <typename T> __device__ void discard_gradients(const GatedRecurrence& a) {
+  const int64_t i0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t i = i0; i < a.N * a.H; i += step) {
+    const int64_t row = i / a.H, at = row * a.ldd + (i - row * a.H);
+    static_cast<T*>(a.dx)[at] = static_cast<T*>(a.dr)[at] = static_cast<T*>(a.di)[at] = (T)0;
+  }
+  if (a.dh0)
+    for (int64_t i = i0; i < (int64_t)a.B * a.H; i += step) a.dh0[i] = 0.f;
+}
+
 // dlam[d] = sigm(lam) / softplus(lam) times the sum of the rows of parts; their
 // quotient tends to 1 where both vanish.  (256 rows of 768: 4.9 us, the latency of
-// eight rows in turn, a barrier and a launch.)
-__global__ __launch_bounds__(1024) void gr_dlam_kernel(const float* __restrict__ parts, int64_t rows, int H,
-                                                       const float* __restrict__ lam,
-                                                       float* __restrict__ dlam) {
+// eight rows in turn, a barrier and a launch.)  The last launch of a backward call:
+// where a wait of it or of its forward call ran out, it leaves zeros.
+template <typename T>
+__global__ __launch_bounds__(1024) void gr_dlam_kernel(GatedRecurrence a, int64_t rows) {
   __shared__ float sum[32][33];
-  const float s = column_sum(parts, rows, H, sum);
+  const bool lost = *a.err != 0;
+  if (lost) discard_gradients<T>(a);
+  const float s = column_sum(a.parts, rows, a.H, sum);
   const int d = blockIdx.x * 32 + threadIdx.x;
-  if (threadIdx.x >= 32 || d >= H) return;
-  const float l = lam[d];
-  dlam[d] = l < -20.f ? s : s * (1.f / (1.f + expf(-l))) / softplus(l);
+  if (threadIdx.x >= 32 || d >= a.H) return;
+  const float l = a.lam[d];
+  const float g = l < -20.f ? s : s * (1.f / (1.f + expf(-l))) / softplus(l);
+  a.dlam[d] = lost ? 0.f : g;
 }
 
 // The packed offset of every frame, off_t = B_t t + (the sum of the lengths from
-// sequence B_t on), and the lengths, where the kernels read them; and the words of
-// linked tiles that start from zero.  (1500 frames of 128 sequences: 5.2 us, the
+// sequence B_t on), and the lengths, where the kernels read them; and the words that
+// linked tiles start from as zeros.  (1500 frames of 128 sequences: 5.2 us, the
 // latency of the search.)
 __global__ __launch_bounds__(256) void gr_schedule_kernel(GatedSchedule a) {
   const int t = blockIdx.x * 256 + threadIdx.x;
@@ -666,7 +684,7 @@ hipError_t launch(GatedRecurrence a, const int32_t* lengths, bool forward, hipSt
   const unsigned groups = (unsigned)(((int64_t)a.B * (a.H / V) + 63) / 64);
   a.most_tiles = (a.T + GR_TILE - 1) / GR_TILE;
   const bool link = gated_linked(a.T, groups);
-  int64_t words = 0, states = 0;  // (tickets, flags and states start from zero)
+  int64_t words = 0, states = 0;  // (tickets, flags and states start from zero, and the time-out flag)
   if (link) {
     a.flags = a.tickets + (int64_t)groups * TICKET_LINE;
     words = (int64_t)(TICKET_LINE + a.most_tiles) * groups;
@@ -679,15 +697,16 @@ hipError_t launch(GatedRecurrence a, const int32_t* lengths, bool forward, hipSt
     g.tails = a.tails;
     g.T = a.T;
     g.B = a.B;
-    g.clear_words = a.tickets;
+    g.clear_words = reinterpret_cast<uint32_t*>(a.err);
     g.clear_states = a.states;
-    g.words = words;
+    g.words = link ? words + 1 : 0;
     g.states = states;
     const hipError_t e = schedule(g, lengths, s);
     if (e != hipSuccess) return e;
   } else if (link) {
-    const hipError_t e = fill_zero2(reinterpret_cast<float*>(a.tickets), words,
-                                    reinterpret_cast<float*>(a.states), 2 * states, s);
+    // (a backward pass leaves the time-out flag as its forward pass did)
+    float* const from = forward ? reinterpret_cast<float*>(a.err) : reinterpret_cast<float*>(a.tickets);
+    const hipError_t e = fill_zero2(from, forward ? words + 1 : words, reinterpret_cast<float*>(a.states), 2 * states, s);
     if (e != hipSuccess) return e;
   }
   // one frame and nothing to keep of it: a wave does without a tile
@@ -708,8 +727,8 @@ hipError_t launch(GatedRecurrence a, const int32_t* lengths, bool forward, hipSt
   }
   if (link) hipLaunchKernelGGL((gr_backward_kernel<T, V, RAGGED, LINKED>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((gr_backward_kernel<T, V, RAGGED, IN_TURN>), grid, block, 0, s, a);
-  hipLaunchKernelGGL(gr_dlam_kernel, dim3((unsigned)((a.H + 31) / 32)), dim3(1024), 0, s, a.parts,
-                     (int64_t)a.B * grid.y, a.H, a.lam, a.dlam);
+  hipLaunchKernelGGL(gr_dlam_kernel<T>, dim3((unsigned)((a.H + 31) / 32)), dim3(1024), 0, s, a,
+                     (int64_t)a.B * grid.y);
   return hipGetLastError();
 }
 
