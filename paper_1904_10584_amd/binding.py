@@ -151,11 +151,17 @@ def _dev(t, name, dtype=None):
     return ctypes.c_void_p(t.data_ptr())
 
 
+# torch's own way to a stream's handle without making a Stream object (a microsecond,
+# not three); a torch without it takes the public way.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream):
     if stream is not None:
         return ctypes.c_void_p(stream.cuda_stream)
-    if torch.cuda.is_initialized():  # (without making a Stream: a microsecond, not three)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
+        return _raw_stream(_raw_device())
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
