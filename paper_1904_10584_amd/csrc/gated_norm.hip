@@ -36,6 +36,29 @@ __device__ __forceinline__ u16x4_t narrow(f32x4_t v, u16x4_t*) {  // (to nearest
   return __builtin_bit_cast(u16x4_t, __builtin_convertvector(v, bf16x4_t));
 }
 
+// v moved down by `past` elements (0 to 3; more: all zeros), zeros moving in.
+__device__ __forceinline__ f32x4_t moved_down(f32x4_t v, int past) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = past & 1 ? (k < 3 ? v[k < 3 ? k + 1 : 3] : 0.f) : v[k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = past & 2 ? (k < 2 ? v[k < 2 ? k + 2 : 3] : 0.f) : v[k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = past > 3 ? 0.f : v[k];
+  return v;
+}
+// Four bf16 in two words: constant shifts of words.  (Picked one by one, the elements
+// became 64-bit shifts by a register.  Where that was the last register of a wave's
+// allocation, 40 of 40 in the forward kernel of rows up to 256 in bf16, the results were
+// wrong wherever waves shared a SIMD.)
+__device__ __forceinline__ u16x4_t moved_down(u16x4_t v, int past) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+  uint32_t lo = past & 2 ? w[1] : w[0], hi = past & 2 ? 0u : w[1];
+  lo = past & 1 ? __builtin_amdgcn_alignbit(hi, lo, 16) : lo;
+  hi = past & 1 ? hi >> 16 : hi;
+  return __builtin_bit_cast(u16x4_t, u32x2_t{past > 3 ? 0u : lo, past > 3 ? 0u : hi});
+}
+
 // Four elements from place e of a row of H, those past its end as zeros; rows of
 // odd lengths start at any element, which the memory instructions take.  `inside`
 // (a constant where it is called): none are past it.  Else the load is the same for
@@ -52,15 +75,9 @@ __device__ __forceinline__ typename Four<T>::type load4(const T* row, int e, int
       if (e + k < H) v[k] = row[e + k];
     return v;
   }
-  const int from = e < H - 4 ? e : H - 4, past = e - from;
+  const int from = e < H - 4 ? e : H - 4;
   v = *reinterpret_cast<const At*>(row + from);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = past & 1 ? (k < 3 ? v[k < 3 ? k + 1 : 3] : (T)0) : v[k];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = past & 2 ? (k < 2 ? v[k < 2 ? k + 2 : 3] : (T)0) : v[k];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = past > 3 ? (T)0 : v[k];
-  return v;
+  return moved_down(v, e - from);
 }
 template <typename T>
 __device__ __forceinline__ void store4(T* row, int e, int H, bool inside, f32x4_t v) {
