@@ -575,7 +575,10 @@ class AdamWTensors:
     in all of them), `m` and `v` (fp32, or 8-bit: torch.float8_e4m3fn or uint8,
     then with fp32 `m_scale` and `v_scale` of adamw_scales(n) elements),
     optionally `weights_bf16`, and a number `weight_decay`.  The list keeps the
-    tensors alive and passes their addresses; it holds nothing of a step."""
+    tensors alive and passes the addresses that they have when it is made; it holds
+    nothing of a step.  Making it costs some microseconds a tensor, more than a small
+    step itself, so a program makes it once and writes its gradients into the same
+    tensors each step; gradients allocated anew need a new list."""
 
     def __init__(self, tensors):
         self.tensors = [dict(t) for t in tensors]

@@ -6,7 +6,7 @@
 // HBM bounds it: 30 bytes an element with 32-bit moments, fp32 gradients and the
 // bf16 copy, 18 with 8-bit moments (16 with bf16 gradients).  24.1 M elements with
 // 32-bit moments: 120 us (6.0 TB/s); 95.4 M with 8-bit moments and bf16 gradients: 277 us (5.5
-// TB/s), where about 125 vector instruction slots an element are nearly as long.
+// TB/s), where 111 vector instruction slots an element are as long (269 us counted).
 // A launch has up to 48 tensors, a workgroup 2048 elements of one: every load of a
 // wave's two blocks comes before the first use.
 //
@@ -120,6 +120,8 @@ __device__ __forceinline__ f32x4_t decode(uint32_t c, float scale) {
   return f32x4_t{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
 }
 
+// (Two multipliers and shifts of 15: published constants, from a search for hashes of
+// 32 bits of little bias, hash-prospector.)
 __device__ __forceinline__ uint32_t hash(uint32_t i, uint32_t key) {
   uint32_t x = i * 0x85EBCA6Bu + key;
   x = (x ^ (x >> 15)) * 0xD168AAADu;

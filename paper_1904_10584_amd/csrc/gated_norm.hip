@@ -6,7 +6,7 @@
 // rms(z) = sqrt(mean z^2 + eps), and the gradient of it all.  HBM bounds it:
 // every input is read once and every output written once, so a row stays in the
 // registers of its wave (of its two or four waves if it is long) across both norms.
-// 16384 x 768 with an fp32 stream: forward 36 us (4.9 TB/s), backward 52 us (5.3
+// 16384 x 768 with an fp32 stream: forward 35 us (5.0 TB/s), backward 52 us (5.3
 // TB/s) and 5 us for the factors' gradients; 32768 x 1536 in bf16: 91 us (5.5 TB/s)
 // and 162 us (5.0 TB/s).  64 x 768 forward: 3.6 us, a launch and one row's latency.
 #include "am_device.h"
@@ -206,8 +206,8 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(GatedNorm a) {
 
 // Wavefronts a SIMD that the backward pass's registers leave room for: as many
 // workgroups a CU make the grid, which then has no last round half empty (32768 x
-// 1536 in bf16: 207 us with 1024 workgroups, 157 with 768; 16384 x 768 with an fp32
-// stream: 61 and 52).
+// 1536 in bf16: 207 us with 1024 workgroups, 162 with 768; 16384 x 768 with an fp32
+// stream: 63 and 52).
 constexpr int backward_waves(int nv) { return nv <= 3 ? 3 : nv <= 4 ? 2 : 1; }
 
 // With n = R / rms(R), dn = dy w_next:  dR = dres_out + (dn - n mean(dn n)) / rms(R),

@@ -16,14 +16,15 @@
 // are too few to fill the chip, every tile is a workgroup of its own and they are
 // linked through memory (see LINK).
 //
-// Bounds, bf16: 8 bytes an element forward and 14 backward against about 50 and 90
-// vector instruction slots (three exponentials, two reciprocals and a root at a
-// quarter rate), which take a little less time than the bytes and overlap them in
-// part.  16384 frames x 768 (64 a sequence): forward 27 us (3.8 TB/s, 16 us of vector
-// instructions), backward 43 us (4.1 TB/s, 23 us).  128 utterances of 200 to 1500
-// frames x 768: 174 us (3.9 TB/s) and 271 us (4.4 TB/s).  Stores past the caches
-// make these 5 % faster by themselves and what reads their results next slower by
-// more (forward with the norm after it: 58 -> 60 us): not taken.
+// Bounds, bf16: 8 bytes an element forward and 14 backward against 42 and 63 vector
+// instructions (three exponentials, two reciprocals and a root among them: 48 and 69
+// issue slots counted), which take less time than the bytes and overlap them in part.
+// 16384 frames x 768 (64 a sequence): forward 26 us (3.9 TB/s, 15 us of vector
+// instructions), backward 42 us (4.2 TB/s, 22 us).  128 utterances of 200 to 1500
+// frames x 768: 170 us (4.0 TB/s, 97 us of vector instructions) and 266 us (4.5 TB/s,
+// 140 us).  Stores past the caches make these 5 % faster by themselves and what reads
+// their results next slower by more (forward with the norm after it: 58 -> 60 us): not
+// taken.
 #include "am_device.h"
 #include "am_internal.h"
 #include "poll_budget.h"
@@ -358,7 +359,7 @@ __device__ __forceinline__ void pass(const float (&A)[N][64][V], const float (&S
 // The 64 groups of channels of a workgroup.  Sequences are sorted by length, and
 // workgroups 256 apart tend to share a CU: every second 256 are taken from their
 // end, so that long and short ones meet (128 utterances of 200 to 1500 frames x 768:
-// forward 180 -> 171 us).
+// forward 180 -> 170 us).
 template <bool RAGGED> __device__ __forceinline__ uint32_t group_of(uint32_t block, uint32_t blocks) {
   if (!RAGGED || !(block >> 8 & 1)) return block;
   const uint32_t first = block & ~255u, last = first + 255 < blocks ? first + 255 : blocks - 1;
@@ -765,9 +766,11 @@ hipError_t gated_backward(const GatedRecurrence& a, bool bf16, hipStream_t s) {
 // Where at most 400 workgroups' worth of channels leave CUs (or the second workgroup
 // of some) without work, from five tiles on, or seven where the first wave of
 // workgroups is nearly enough.  Linked / in turn, us, forward and backward, bf16: 6
-// groups x 320 frames 16 24 / 18 27, x 2000 15 23 / 96 142; 192 x 320 25 30 / 21 33, x
-// 2000 92 173 / 109 217; 256 x 320 28 36 / 22 35, x 500 35 48 / 31 48 (lengths that
-// differ 29 38 / 36 46); 384 x 2000 174 340 / 209 348; 480 x 2000 212 419 / 213 375.
+// groups x 320 frames 12 13 / 17 25, x 2000 14 18 / 95 139; 192 x 320 25 30 / 21 31, x
+// 2000 94 176 / 108 222; 256 x 320 28 35 / 22 33, x 500 35 48 / 30 47 (lengths that
+// differ 29 40 / 34 46); 384 x 500 46 91 / 46 89, x 2000 172 348 / 201 340; 480 x 2000
+// 216 435 / 209 374.  One rule serves both passes and all lengths: a forward call near
+// its edge (192 x 320, 256 x 500 of equal lengths) is 4 to 5 us slower for it.
 bool gated_linked(int T, int64_t groups) {
   return groups <= 400 && T > (groups <= 192 ? 4 : 6) * GR_TILE;
 }
