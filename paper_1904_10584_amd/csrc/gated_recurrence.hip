@@ -20,7 +20,7 @@
 // instructions (three exponentials, two reciprocals and a root among them: 48 and 69
 // issue slots counted), which take less time than the bytes and overlap them in part.
 // 16384 frames x 768 (64 a sequence): forward 26 us (3.9 TB/s, 15 us of vector
-// instructions), backward 42 us (4.2 TB/s, 22 us).  128 utterances of 200 to 1500
+// instructions), backward 41 us (4.3 TB/s, 22 us).  128 utterances of 200 to 1500
 // frames x 768: 170 us (4.0 TB/s, 97 us of vector instructions) and 266 us (4.5 TB/s,
 // 140 us).  Stores past the caches make these 5 % faster by themselves and what reads
 // their results next slower by more (forward with the norm after it: 58 -> 60 us): not
@@ -486,9 +486,15 @@ __global__ __launch_bounds__(64 * W, 4) void gr_backward_kernel(GatedRecurrence 
     fetch<RAGGED, T, V, TC, 3>(a, {a.r, a.i, a.x}, a.ld, t0, c, {&r, &i, &x});
     fetch<RAGGED, T, V, TC, 1>(a, {a.dh}, a.lddh, t0, c, {&dh});
     // (zeros for tiles that the lane's sequence does not have: the forward pass may
-    // have grouped channels otherwise and saved nothing there)
+    // have grouped channels otherwise and saved nothing there.  Sequences of one length
+    // have the same tiles.)
     float h[V];
-    fetch_state<V>(frame(a.saved, k * BH * 4), k * GR_TILE < c.len ? (uint32_t)c.st * 4 : NONE, h);
+    if constexpr (RAGGED) {
+      fetch_state<V>(frame(a.saved, k * BH * 4), k * GR_TILE < c.len ? (uint32_t)c.st * 4 : NONE, h);
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) h[v] = a.saved[(int64_t)k * BH + c.st + v];
+    }
     // Of a frame: a, sigm(r), q sigm(i) (dx of its dv), x (1 - sigm(i)) (di of its
     // dx), and what its carry is multiplied by in the gradient of log a times log
     // a: v a L / q - L h_{t-1}, at first with the h of a stretch that starts from
