@@ -14,7 +14,7 @@ A case is a dict of plain values; its "kind" says which operator it calls:
   quantise  a matrix as 8-bit floats (4 bits of exponent, 3 of fraction) with a
             power of two for each 128 elements of a row or each tile of 128 x 128:
             as it lies, and transposed for the products of the backward pass.
-  product   out = a b^T of two such matrices.
+  product   out = a b^T of two such matrices, in bf16.
   norm      a block's output gated, normed, scaled and added to the residual
             stream, and the next block's norm as such a matrix.
 
@@ -54,9 +54,9 @@ def _quantise(name, R, C, tiles, dtype="bf16"):
     return dict(c, name=name) if name else c
 
 
-def _product(name, M, N, K, tiles=True, bias=False, out="bf16"):
+def _product(name, M, N, K, tiles=True, bias=False):
     """tiles: b has a scale for each tile (weights), else for each 128 of a row."""
-    c = dict(kind="product", M=M, N=N, K=K, tiles=tiles, bias=bias, out=out)
+    c = dict(kind="product", M=M, N=N, K=K, tiles=tiles, bias=bias)
     return dict(c, name=name) if name else c
 
 
@@ -89,7 +89,7 @@ def listed():
         # the wide student's projection of a batch
         _product("product wide", 32768, 4608, 1536, bias=True),
         # a weight gradient: few outputs, a sum over a ragged number of frames
-        _product("product over frames", 2304, 768, 16283, tiles=False, out="f32"),
+        _product("product over frames", 2304, 768, 16283, tiles=False),
         # one new frame of each of 64 streams
         _norm("norm token", 64, 768),
         # the chunked batch, kept for the backward pass too
@@ -122,10 +122,9 @@ def draw(rng):
         elif kind == "quantise":
             c = _quantise(None, _size(rng, 1, 40000), _size(rng, 16, 6000), rng.random() < 0.4, dtype)
         elif kind == "product":
-            out = rng.choice(["bf16", "bf16", "f32"])
             long = rng.random() < 0.3
             c = _product(None, _size(rng, 1, 3000 if long else 40000), _size(rng, 16, 5000),
-                         _size(rng, 16, 40000 if long else 5000), rng.random() < 0.6, rng.random() < 0.3, out)
+                         _size(rng, 16, 40000 if long else 5000), rng.random() < 0.6, rng.random() < 0.3)
         else:
             c = _norm(None, _log(rng, 1, 60000), _size(rng, 64, 2560), dtype, rng.choice(["f32", "bf16"]),
                       rng.random() < 0.5)
@@ -169,7 +168,7 @@ def work(c):
         return {"bytes": n * (size(c["dtype"]) + 2), "flops": 4 * n}
     if c["kind"] == "product":
         M, N, K = c["M"], c["N"], c["K"]
-        return {"bytes": (M + N) * K + size(c["out"]) * M * N, "flops": 2 * M * N * K}
+        return {"bytes": (M + N) * K + 2 * M * N, "flops": 2 * M * N * K}
     e, f, n = size(c["dtype"]), size(c["stream"]), c["N"] * c["H"]
     # o, gate; the stream in and out; codes, y
     return {"bytes": (2 * e + 2 * f + 1 + (e if c["keep"] else 0)) * n + 12 * c["H"], "flops": 18 * n}
@@ -245,7 +244,7 @@ def _prepare_product(c, rnd):
     b, b_scale = _coded(rnd.normal(N, K, std=K ** -0.5), c["tiles"])
     return dict(case=c, a=a, a_scale=a_scale, b=b, b_scale=b_scale,
                 bias=rnd.normal(N, std=0.1) if c["bias"] else None,
-                out=torch.empty((M, N), dtype=DTYPES[c["out"]], device=DEV))
+                out=torch.empty((M, N), dtype=BF16, device=DEV))
 
 
 def _prepare_norm(c, rnd):
@@ -292,7 +291,7 @@ def _plain_quantise(s):
 
 def _plain_product(s):
     out = _values8(s["a"], s["a_scale"], False) @ _values8(s["b"], s["b_scale"], s["case"]["tiles"]).t()
-    return {"out": (out if s["bias"] is None else out + s["bias"]).to(s["out"].dtype)}
+    return {"out": (out if s["bias"] is None else out + s["bias"]).to(BF16)}
 
 
 def _plain_norm(s):
