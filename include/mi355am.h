@@ -442,6 +442,56 @@ am_status gated_norm_backward(int64_t N, int32_t H, int32_t dtype, int32_t res_d
                               int64_t lddo, void* dgate, int64_t lddg, void* dres, float* dw_post,
                               float* dscale, float* dw_next, void* ws, int64_t ws_bytes, void* stream);
 
+/* ---- matrices in 8 bits --------------------------------------------------- */
+
+/* A matrix [rows][cols] in 8 bits is held as codes and scales:
+ *   codes   8-bit floats (4 exponent bits of bias 7, 3 fraction bits, as
+ *           torch.float8_e4m3fn), rows of `cols` codes, a multiple of 16 bytes
+ *           apart, on 16 bytes; what follows a row's end up to a multiple of 16
+ *           codes is zero
+ *   scales  a byte e for each 128 elements of a row (row r, elements 128 k to
+ *           128 k + 127: byte k of row r), or, in tiles, for each 128 x 128 (rows
+ *           128 j to 128 j + 127: byte k of row j), which stands for 2^(e - 127) (as
+ *           torch.float8_e8m0fnu).  Rows of scales are a multiple of 4 bytes apart,
+ *           on 4 bytes, and have room for a multiple of 4 of them
+ * q8_quantise writes x [rows] of cols (`ld` elements apart) in this form: codes and
+ * scales as x lies (or both NULL), codes_t and scales_t of its transpose (or both
+ * NULL), which in tiles are the same codes.  A scale is the power of two (2^-126 at
+ * least) that puts the largest finite magnitude it serves into [128, 256); codes are
+ * rounded to nearest even; what is not finite has the code NaN.  Zeros are written
+ * behind the rows' ends; bytes of scales that serve nothing are left as they are.
+ * dtype: of x. */
+am_status q8_quantise(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ld, int32_t tiles,
+                      void* codes, int64_t ldc, void* scales, int64_t lds, void* codes_t, int64_t ldct,
+                      void* scales_t, int64_t ldst, void* stream);
+
+/* out[m][n] = sum_k a[m][k] b[n][k] (+ bias[n]) (+ out[m][n]), in bf16, rounded once:
+ * a projection where b holds its weights, the gradient of its input where b holds
+ * their transpose, the weights' gradient where a and b hold the transposes of the
+ * output's gradient and of the input.
+ *   a   [M] rows of K in 8 bits, a scale for each 128 of a row
+ *   b   [N] rows of K, a scale for each 128 of a row, or each tile (b_tiles = 1)
+ *   bias [N] fp32 or NULL;  out [M] rows of N, ldo elements apart;  accumulate = 1
+ *   adds to what out holds
+ * The matrix cores form products of 8-bit floats exactly and their sums to about 16
+ * bits of their size, in fixed order.  ws: workspace of am_q8_matmul_workspace_bytes
+ * (256-byte aligned; may be NULL where that is 0).  M, N and K below 2^31. */
+int64_t am_q8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
+am_status q8_matmul(int64_t M, int64_t N, int64_t K, const void* a, int64_t lda, const void* a_scales,
+                    int64_t ldas, const void* b, int64_t ldb, const void* b_scales, int64_t ldbs,
+                    int32_t b_tiles, const float* bias, void* out, int64_t ldo, int32_t accumulate,
+                    void* ws, int64_t ws_bytes, void* stream);
+
+/* gated_norm_forward whose norm y leaves in 8 bits, a scale for each 128 of a row: the
+ * operand of the next block's projections.  Its codes are made from the values before
+ * they are rounded.  y may be NULL, or is written besides (a backward pass reads it
+ * through the weights' gradient); w_next is not NULL. */
+am_status gated_norm_forward_q8(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, const void* o,
+                                int64_t ldo, const void* gate, int64_t ldg, const float* w_post,
+                                const float* scale, const void* res, const float* w_next, float eps,
+                                void* res_out, void* y, float* rstd, void* codes, int64_t ldc, void* scales,
+                                int64_t lds, void* stream);
+
 /* One tensor of an AdamW step.  Any element alignment. */
 typedef struct {
   int64_t n;              /* elements */
@@ -497,7 +547,8 @@ typedef enum {
   AM_K_GATED = 11,        /* gated linear recurrence, forward and backward */
   AM_K_NORM = 12,         /* gate, norm, residual and next norm, and their gradient */
   AM_K_ADAMW = 13,        /* AdamW step */
-  AM_K_NCLASSES = 14
+  AM_K_Q8 = 14,           /* matrices in 8 bits: quantising and products */
+  AM_K_NCLASSES = 15
 } am_kernel_class;
 
 /* Starts recording: every later launch of a class whose bit is set in

@@ -20,9 +20,9 @@ F32, BF16 = 0, 1
 MEAN_VALID, SUM = 0, 1
 K_GEMM_FWD, K_GEMM_BWD_DATA, K_GEMM_BWD_WGT, K_LSTM_FWD, K_LSTM_BWD = 0, 1, 2, 3, 4
 K_CE, K_ENCODE, K_DECODE, K_SGD, K_MISC, K_BMUF = 5, 6, 7, 8, 9, 10
-K_GATED, K_NORM, K_ADAMW = 11, 12, 13
+K_GATED, K_NORM, K_ADAMW, K_Q8 = 11, 12, 13, 14
 KERNEL_CLASSES = ["gemm_fwd", "gemm_bwd_data", "gemm_bwd_wgt", "lstm_fwd", "lstm_bwd",
-                  "soft_ce", "encode", "decode", "sgd", "misc", "bmuf", "gated", "norm", "adamw"]
+                  "soft_ce", "encode", "decode", "sgd", "misc", "bmuf", "gated", "norm", "adamw", "q8"]
 
 
 OK, EINVAL, ECAPACITY, EUNSUPPORTED, EHIP, EWORKSPACE, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6
@@ -101,6 +101,12 @@ _PROTOS = {
                                   _P, _P, _P]),
     "gated_norm_backward": (_I32, [_I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _F32, _P,
                                    _P, _P, _P, _I64, _P, _I64, _P, _P, _P, _P, _P, _I64, _P]),
+    "gated_norm_forward_q8": (_I32, [_I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _F32, _P,
+                                     _P, _P, _P, _I64, _P, _I64, _P]),
+    "q8_quantise": (_I32, [_I64, _I64, _I32, _P, _I64, _I32, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
+    "am_q8_matmul_workspace_bytes": (_I64, [_I64, _I64, _I64]),
+    "q8_matmul": (_I32, [_I64, _I64, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _I32, _P, _P, _I64, _I32,
+                         _P, _I64, _P]),
     "adamw_apply": (_I32, [_I32, _P, _I32, _I32, _F64, _F64, _F64, _F64, _I64, _P, _U32, _P]),
     "am_cast_f32_to_bf16": (_I32, [_I64, _P, _P, _P]),
     "am_workspace_check": (_I32, [_P, _I64, _P]),
@@ -552,6 +558,96 @@ def gated_norm_backward(res, rstd, dres, ws, o=None, gate=None, w_post=None, sca
         dop, lddo, dgp, lddg, _shaped(dres, "dres", (N, H), res.dtype),
         _shaped(dw_post, "dw_post", (H,)), _shaped(dscale, "dscale", (H,)),
         _shaped(dw_next, "dw_next", (H,)), wp, wn, _stream(stream))
+    if st:
+        _check(st)
+
+
+# ------------------------------------------------------ matrices in 8 bits --
+
+Q8_BLOCK = 128  # elements that share a scale
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+_SCALES = (torch.float8_e8m0fnu, torch.uint8)
+
+
+def q8_empty(rows, cols, tiles=False, device="cuda"):
+    """Room for a matrix [rows][cols] in 8 bits: its codes, a view [rows][cols] of rows
+    that start on 16 bytes, and its scales, in rows of a multiple of 4 (unused ones are
+    zeros).  `tiles`: a scale for each 128 x 128, else for each 128 of a row."""
+    codes = torch.zeros((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device)
+    scales = torch.zeros((-(-rows // Q8_BLOCK) if tiles else rows, -(-cols // (4 * Q8_BLOCK)) * 4),
+                         dtype=torch.uint8, device=device)
+    return codes.view(torch.float8_e4m3fn)[:, :cols], scales.view(torch.float8_e8m0fnu)
+
+
+def _q8(codes, scales, name, rows, cols, tiles=False):
+    """Pointers and row strides of a matrix in 8 bits; Nones for None."""
+    if codes is None and scales is None:
+        return None, 0, None, 0
+    for t, what, kinds, n, least in (
+            (codes, "codes", _CODES, rows, cols),
+            (scales, "scales", _SCALES, -(-rows // Q8_BLOCK) if tiles else rows, -(-cols // (4 * Q8_BLOCK)) * 4)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise AmError(f"{what} of {name} must be a GPU tensor")
+        if t.dtype not in kinds:
+            raise AmError(f"{what} of {name} must be {kinds[0]} or uint8, got {t.dtype}")
+        if t.dim() != 2 or t.shape[0] != n or (t.shape[1] != cols if what == "codes" else t.shape[1] < least):
+            raise AmError(f"{what} of {name} must be of shape ({n}, {least}), got {tuple(t.shape)}")
+        if t.stride(1) != 1 and t.shape[1] > 1:
+            raise AmError(f"{what} of {name} must have rows of unit stride")
+    # (a row's end: what is allocated behind the last one too)
+    ldc = codes.stride(0) if rows > 1 else max(codes.stride(0), -(-cols // 16) * 16)
+    behind = codes.untyped_storage().nbytes() - codes.storage_offset() - (rows - 1) * ldc
+    if rows and cols and behind < -(-cols // 16) * 16:
+        raise AmError(f"codes of {name} must have room for a multiple of 16 codes in every row")
+    lds = scales.stride(0) if scales.shape[0] > 1 else max(scales.stride(0), scales.shape[1])
+    return codes.data_ptr(), ldc, scales.data_ptr(), lds
+
+
+def q8_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, tiles=False, stream=None):
+    """x [rows][cols] fp32 or bf16 (rows may be columns of a wider matrix) in 8 bits, as
+    it lies and, with codes_t and scales_t, transposed; see q8_empty."""
+    dt, (rows, cols) = _dtype(x, "x"), x.shape
+    xp, ld = _row(x, "x", rows, cols, x.dtype)
+    st = (_lib or lib()).q8_quantise(
+        rows, cols, dt, xp, ld, 1 if tiles else 0, *_q8(codes, scales, "x", rows, cols, tiles),
+        *_q8(codes_t, scales_t, "x transposed", cols, rows, tiles), _stream(stream))
+    if st:
+        _check(st)
+
+
+def q8_matmul_workspace_bytes(M, N, K) -> int:
+    n = lib().am_q8_matmul_workspace_bytes(M, N, K)
+    if n < 0:
+        raise AmError("invalid sizes for workspace query", EINVAL)
+    return int(n)
+
+
+def q8_matmul(a, a_scales, b, b_scales, out, tiles=False, bias=None, accumulate=False, ws=None, stream=None):
+    """out [M][N] bf16 = a [M][K] b [N][K]^T of matrices in 8 bits (+ bias [N] fp32) (+
+    out); tiles: b has a scale for each 128 x 128."""
+    if a.dim() != 2 or b.dim() != 2 or a.shape[1] != b.shape[1]:
+        raise AmError(f"a and b must be [M][K] and [N][K], got {tuple(a.shape)} and {tuple(b.shape)}")
+    (M, K), N = a.shape, b.shape[0]
+    op, ldo = _row(out, "out", M, N, torch.bfloat16)
+    wp, wn = _workspace(ws)
+    st = (_lib or lib()).q8_matmul(
+        M, N, K, *_q8(a, a_scales, "a", M, K), *_q8(b, b_scales, "b", N, K, tiles), 1 if tiles else 0,
+        _shaped(bias, "bias", (N,)), op, ldo, 1 if accumulate else 0, wp, wn, _stream(stream))
+    if st:
+        _check(st)
+
+
+def gated_norm_forward_q8(res, codes, scales, o=None, gate=None, w_post=None, scale=None, w_next=None,
+                          res_out=None, y=None, rstd=None, eps=1e-6, stream=None):
+    """gated_norm_forward whose norm leaves in 8 bits, and in y if that is given."""
+    (N, H), act = res.shape, o if o is not None else y if y is not None else res
+    (op, ldo), (gp, ldg) = _row(o, "o", N, H, act.dtype), _row(gate, "gate", N, H, act.dtype)
+    st = (_lib or lib()).gated_norm_forward_q8(
+        N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
+        _shaped(scale, "scale", (H,)), _shaped(res, "res", (N, H), res.dtype),
+        _shaped(w_next, "w_next", (H,)), float(eps), _shaped(res_out, "res_out", (N, H), res.dtype),
+        _shaped(y, "y", (N, H), act.dtype), _shaped(rstd, "rstd", (N, 2)),
+        *_q8(codes, scales, "y", N, H), _stream(stream))
     if st:
         _check(st)
 

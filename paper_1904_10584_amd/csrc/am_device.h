@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace am {
 
 typedef uint16_t bf16_t;  // bf16 storage: upper half of an IEEE binary32
@@ -239,6 +241,33 @@ __device__ __forceinline__ float wave_max_uniform(float v) {
   v = fmaxf(v, lanes_moved<0x141>(v));
   v = fmaxf(v, lanes_moved<0x140>(v));
   return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+
+// The maximum over each 16 lanes, in every one of them.
+__device__ __forceinline__ uint32_t lanes16_max(uint32_t v) {
+  auto moved = [](uint32_t u, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)u, decltype(ctrl)::value, 0xf, 0xf, true);
+  };
+  auto most = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+  v = most(v, moved(v, std::integral_constant<int, 0xB1>()));
+  v = most(v, moved(v, std::integral_constant<int, 0x4E>()));
+  v = most(v, moved(v, std::integral_constant<int, 0x141>()));
+  return most(v, moved(v, std::integral_constant<int, 0x140>()));
+}
+
+// 8-bit floats in units of a power of two.  `top`: the bits of a block's largest
+// finite magnitude; the exponent byte of the power that puts it into [128, 256)
+// (2^-126 at least, which 0 has too).
+__device__ __forceinline__ uint32_t q8_exponent(uint32_t top) {
+  const uint32_t e = top >> 23;
+  return e > 8 ? e - 7 : 1;
+}
+__device__ __forceinline__ float q8_inverse(uint32_t e) { return __uint_as_float((254 - e) << 23); }
+// Four codes, rounded to nearest even; what is not finite becomes NaN.
+__device__ __forceinline__ uint32_t q8_codes4(float a, float b, float c, float d, float inv) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+  return (uint32_t)w;
 }
 
 // The sum of column 32 blockIdx.x + threadIdx.x % 32 of parts [rows][width], by a

@@ -364,9 +364,37 @@ struct GatedNorm {
   void* dres;            // backward: [N][H] (written)
   float *dw_post, *dscale, *dw_next;  // backward: [H] or null (written)
   float* parts;          // backward: [GATED_NORM_BLOCKS][2][H] scratch
+  uint8_t *codes, *scales;  // forward: y in 8 bits (written), or null
+  int64_t ldc, lds;
 };
 hipError_t gated_norm_forward(const GatedNorm& a, bool bf16, bool stream_bf16, hipStream_t s);
 hipError_t gated_norm_backward(const GatedNorm& a, bool bf16, bool stream_bf16, hipStream_t s);
+
+// A matrix as 8-bit codes and their scales' exponents (see q8_quantise in the C ABI).
+struct Q8Quantise {
+  int64_t rows, cols, ld;
+  const void* x;                // [rows] of cols, ld apart
+  bool tiles, wide;             // wide: rows of x start on 16 bytes
+  uint8_t *codes, *scales;      // or null
+  int64_t ldc, lds;
+  uint8_t *codes_t, *scales_t;  // or null
+  int64_t ldct, ldst;
+  uint32_t across;              // (set by the launcher: tiles side by side)
+};
+hipError_t q8_quantise(Q8Quantise a, bool bf16, hipStream_t s);
+// out = a b^T (see q8_matmul in the C ABI).
+struct Q8Matmul {
+  int64_t M, N, K, lda, ldas, ldb, ldbs, ldo;
+  const uint8_t *a, *a_scale, *b, *b_scale;
+  bool b_tiles, accumulate, wide;  // wide: rows of out start on 16 bytes
+  const float* bias;
+  uint16_t* out;
+  float* parts;                    // scratch of q8_plan().bytes, if any
+  int tiles_m, tiles_n, blocks, steps, splits;  // (set by the launcher)
+};
+struct Q8Plan { int kind, steps, splits; int64_t bytes; };
+Q8Plan q8_plan(int64_t M, int64_t N, int64_t K);
+hipError_t q8_matmul(const Q8Matmul& a, hipStream_t s);
 
 // AdamW step of up to MAX tensors, a workgroup for ADAMW_CHUNK elements of one.
 constexpr int ADAMW_CHUNK = 2048;

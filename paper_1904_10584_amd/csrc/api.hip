@@ -733,6 +733,25 @@ am_status check_norm(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, con
   return AM_OK;
 }
 
+// Codes and scales of a matrix in 8 bits.
+am_status check_q8(int64_t rows, int64_t cols, const void* codes, int64_t ldc, const void* scales, int64_t lds,
+                   const char* name) {
+  if (rows > 0 && cols > 0 && (!codes || !scales)) return fail(AM_EINVAL, "NULL codes or scales of %s", name);
+  if (!aligned(codes, 16) || ldc % 16 != 0)
+    return fail(AM_EINVAL, "rows of codes of %s must start on 16 bytes (row stride %lld)", name, (long long)ldc);
+  if (ldc < (cols + 15) / 16 * 16)
+    return fail(AM_EINVAL, "codes of %s need rows of %lld bytes, got %lld", name, (long long)((cols + 15) / 16 * 16),
+                (long long)ldc);
+  if (!aligned(scales, 4) || lds % 4 != 0)
+    return fail(AM_EINVAL, "rows of scales of %s must start on 4 bytes (row stride %lld)", name, (long long)lds);
+  if (lds < (cols + 511) / 512 * 4)
+    return fail(AM_EINVAL, "scales of %s need rows of %lld bytes, got %lld", name, (long long)((cols + 511) / 512 * 4),
+                (long long)lds);
+  const int64_t most = int64_t(1) << 62;
+  if (rows > 0 && (ldc > most / rows || lds > most / rows)) return fail(AM_EINVAL, "%s is too large", name);
+  return AM_OK;
+}
+
 double norm_bytes(const am::GatedNorm& a, int dtype, int res_dtype, bool backward) {
   const double e = esz_of(dtype), f = esz_of(res_dtype);
   const double act = (a.o ? 1 : 0) + (a.gate ? 1 : 0);
@@ -1566,6 +1585,109 @@ am_status gated_norm_backward(int64_t N, int32_t H, int32_t dtype, int32_t res_d
   hipStream_t s = static_cast<hipStream_t>(stream);
   Timed tm(AM_K_NORM, s, 44.0 * N * H, norm_bytes(a, dtype, res_dtype, true));
   return hip_check(am::gated_norm_backward(a, dtype == AM_BF16, res_dtype == AM_BF16, s), "gated norm backward");
+}
+
+am_status gated_norm_forward_q8(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, const void* o,
+                                int64_t ldo, const void* gate, int64_t ldg, const float* w_post,
+                                const float* scale, const void* res, const float* w_next, float eps,
+                                void* res_out, void* y, float* rstd, void* codes, int64_t ldc, void* scales,
+                                int64_t lds, void* stream) {
+  am::GatedNorm a{};
+  AM_TRY(check_norm(N, H, dtype, res_dtype, o, ldo, gate, ldg, w_post, scale, res, w_next, eps, a));
+  if (!w_next) return fail(AM_EINVAL, "NULL w_next");
+  if (o) AM_TRY(check_rows(N, H, res_dtype, res_out, H, "res_out"));
+  else if (N > 0 && res_out) return fail(AM_EINVAL, "res_out without o");
+  if (y) AM_TRY(check_rows(N, H, dtype, y, H, "y"));
+  if (!aligned(rstd, 4)) return fail(AM_EINVAL, "rstd must be 4-byte aligned");
+  AM_TRY(check_q8(N, H, codes, ldc, scales, lds, "y"));
+  if (N == 0) return AM_OK;
+  a.res_out = res_out;
+  a.y = y;
+  a.rstd = rstd;
+  a.codes = static_cast<uint8_t*>(codes);
+  a.scales = static_cast<uint8_t*>(scales);
+  a.ldc = ldc;
+  a.lds = lds;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Timed tm(AM_K_NORM, s, 18.0 * N * H,
+           norm_bytes(a, dtype, res_dtype, false) + (double)N * H * (1.0 - (y ? 0 : esz_of(dtype))));
+  return hip_check(am::gated_norm_forward(a, dtype == AM_BF16, res_dtype == AM_BF16, s), "gated norm");
+}
+
+am_status q8_quantise(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ld, int32_t tiles,
+                      void* codes, int64_t ldc, void* scales, int64_t lds, void* codes_t, int64_t ldct,
+                      void* scales_t, int64_t ldst, void* stream) {
+  if (rows < 0 || cols < 0 || rows >= (1ll << 31) || cols >= (1ll << 31))
+    return fail(AM_EINVAL, "need 0 <= rows, cols < 2^31 (rows=%lld, cols=%lld)", (long long)rows, (long long)cols);
+  if (dtype != AM_F32 && dtype != AM_BF16) return fail(AM_EINVAL, "dtype %d unknown", dtype);
+  if (tiles != 0 && tiles != 1) return fail(AM_EINVAL, "tiles must be 0 or 1");
+  if (!codes != !scales || !codes_t != !scales_t) return fail(AM_EINVAL, "codes without scales, or scales without codes");
+  if (rows == 0 || cols == 0) return AM_OK;
+  if (!codes && !codes_t) return fail(AM_EINVAL, "neither codes nor codes_t: nothing to do");
+  AM_TRY(check_rows(cols > 0 ? rows : 0, (int32_t)cols, dtype, x, ld, "x"));
+  if (codes) AM_TRY(check_q8(rows, cols, codes, ldc, scales, lds, "x"));
+  if (codes_t) AM_TRY(check_q8(cols, rows, codes_t, ldct, scales_t, ldst, "x transposed"));
+  if ((rows + 127) / 128 * ((cols + 127) / 128) >= (1ll << 31)) return fail(AM_EUNSUPPORTED, "matrix too large");
+  am::Q8Quantise a{};
+  a.rows = rows;
+  a.cols = cols;
+  a.ld = ld;
+  a.x = x;
+  a.tiles = tiles != 0;
+  a.wide = aligned(x, 16) && ld * esz_of(dtype) % 16 == 0;
+  a.codes = static_cast<uint8_t*>(codes);
+  a.scales = static_cast<uint8_t*>(scales);
+  a.ldc = ldc;
+  a.lds = lds;
+  a.codes_t = static_cast<uint8_t*>(codes_t);
+  a.scales_t = static_cast<uint8_t*>(scales_t);
+  a.ldct = ldct;
+  a.ldst = ldst;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Timed tm(AM_K_Q8, s, 4.0 * rows * cols,
+           (double)rows * cols * (esz_of(dtype) + (codes ? 1 : 0) + (codes_t ? 1 : 0)));
+  return hip_check(am::q8_quantise(a, dtype == AM_BF16, s), "q8 quantise");
+}
+
+int64_t am_q8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+  const int64_t most = 1ll << 31;
+  if (M < 0 || N < 0 || K < 0 || M >= most || N >= most || K >= most) return -1;
+  return M == 0 || N == 0 ? 0 : align256(am::q8_plan(M, N, K).bytes);
+}
+
+am_status q8_matmul(int64_t M, int64_t N, int64_t K, const void* a, int64_t lda, const void* a_scales,
+                    int64_t ldas, const void* b, int64_t ldb, const void* b_scales, int64_t ldbs,
+                    int32_t b_tiles, const float* bias, void* out, int64_t ldo, int32_t accumulate,
+                    void* ws, int64_t ws_bytes, void* stream) {
+  const int64_t need = am_q8_matmul_workspace_bytes(M, N, K);
+  if (need < 0)
+    return fail(AM_EINVAL, "need 0 <= M, N, K < 2^31 (M=%lld, N=%lld, K=%lld)", (long long)M, (long long)N, (long long)K);
+  if ((b_tiles != 0 && b_tiles != 1) || (accumulate != 0 && accumulate != 1))
+    return fail(AM_EINVAL, "b_tiles and accumulate must be 0 or 1");
+  if (M == 0 || N == 0) return AM_OK;
+  AM_TRY(check_q8(M, K, a, lda, a_scales, ldas, "a"));
+  AM_TRY(check_q8(N, K, b, ldb, b_scales, ldbs, "b"));
+  AM_TRY(check_rows(M, (int32_t)N, AM_BF16, out, ldo, "out"));
+  if (!aligned(bias, 4)) return fail(AM_EINVAL, "bias must be 4-byte aligned");
+  if ((M + 63) / 64 * ((N + 63) / 64) >= (1ll << 24)) return fail(AM_EUNSUPPORTED, "product too large");
+  if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need))
+    return fail(AM_EWORKSPACE, "needs %lld workspace bytes, 256-byte aligned", (long long)need);
+  am::Q8Matmul m{};
+  m.M = M; m.N = N; m.K = K;
+  m.a = static_cast<const uint8_t*>(a);
+  m.a_scale = static_cast<const uint8_t*>(a_scales);
+  m.b = static_cast<const uint8_t*>(b);
+  m.b_scale = static_cast<const uint8_t*>(b_scales);
+  m.lda = lda; m.ldas = ldas; m.ldb = ldb; m.ldbs = ldbs; m.ldo = ldo;
+  m.b_tiles = b_tiles != 0;
+  m.accumulate = accumulate != 0;
+  m.wide = aligned(out, 16) && ldo % 8 == 0;
+  m.bias = bias;
+  m.out = static_cast<uint16_t*>(out);
+  m.parts = static_cast<float*>(ws);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Timed tm(AM_K_Q8, s, 2.0 * M * N * K, (double)(M + N) * K + 2.0 * M * N * (accumulate ? 2 : 1));
+  return hip_check(am::q8_matmul(m, s), "q8 product");
 }
 
 am_status adamw_apply(int32_t count, const am_adamw_tensor* tensors, int32_t grad_dtype, int32_t state_bits,

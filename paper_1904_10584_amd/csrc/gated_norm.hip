@@ -126,7 +126,9 @@ __device__ __forceinline__ float row_sum(float v, float (&red)[2][WAVES], int& t
 // for (see `sized`).
 constexpr int whole_fours(int nv) { return nv <= 4 ? nv - 1 : 4; }
 
-template <typename T, typename R, int NV, int WPR, bool EXACT>
+// Q8: y as 8-bit codes too (or only), in units of a power of two for each 128 elements
+// of a row: 32 lanes have those, so their largest costs five moves between lanes.
+template <typename T, typename R, int NV, int WPR, bool EXACT, bool Q8>
 __global__ __launch_bounds__(256) void norm_forward_kernel(GatedNorm a) {
   __shared__ float red[2][WAVES];
   int turn = 0;
@@ -191,10 +193,30 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(GatedNorm a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) s = fmaf(t[k][j], t[k][j], s);
       rstd_n = rsqrtf(row_sum<WPR>(s, red, turn) * inv + a.eps);
-      if (on) {
+      if (on && (!Q8 || a.y)) {
         T* y = static_cast<T*>(a.y) + row * H;
 #pragma unroll
         for (int k = 0; k < NV; ++k) store4(y, at.e0 + k * at.STEP, H, inside(k), t[k] * rstd_n * next[k]);
+      }
+      if constexpr (Q8) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int e = at.e0 + k * at.STEP;
+          const f32x4_t v = t[k] * rstd_n * next[k];
+          uint32_t top = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
+            top = m < 0x7f800000u && m > top ? m : top;
+          }
+          top = lanes16_max(top);
+          const uint32_t other = (uint32_t)__shfl_xor((int)top, 16, 64);
+          const uint32_t ex = q8_exponent(top > other ? top : other);
+          if (on && e < ((H + 15) & ~15)) {  // (zeros behind the row's end)
+            *reinterpret_cast<uint32_t*>(a.codes + row * a.ldc + e) = q8_codes4(v[0], v[1], v[2], v[3], q8_inverse(ex));
+            if ((threadIdx.x & 31) == 0) a.scales[row * a.lds + (e >> 7)] = (uint8_t)ex;
+          }
+        }
       }
     }
     if (a.rstd && on && at.e0 == 0) {
@@ -362,7 +384,8 @@ hipError_t launch(const GatedNorm& a, bool forward, hipStream_t s) {
   const int64_t blocks = (a.N * WPR + WAVES - 1) / WAVES, most = forward ? 1024 : 256 * backward_waves(NV);
   const unsigned grid = (unsigned)(blocks < most ? blocks : most);
   if (forward) {
-    hipLaunchKernelGGL((norm_forward_kernel<T, R, NV, WPR, EXACT>), dim3(grid), dim3(256), 0, s, a);
+    if (a.codes) hipLaunchKernelGGL((norm_forward_kernel<T, R, NV, WPR, EXACT, true>), dim3(grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((norm_forward_kernel<T, R, NV, WPR, EXACT, false>), dim3(grid), dim3(256), 0, s, a);
   } else {
     if (grid > 0) hipLaunchKernelGGL((norm_backward_kernel<T, R, NV, WPR, EXACT>), dim3(grid), dim3(256), 0, s, a);
     hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2 * a.H + 31) / 32)), dim3(1024), 0, s, a.parts,

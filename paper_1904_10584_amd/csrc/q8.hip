@@ -1,0 +1,442 @@
+// Matrices as 8-bit floats and their products.
+//
+// A matrix is held as codes (4 bits of exponent of bias 7, 3 of fraction) with a
+// power of two for each 128 elements of a row, or for each tile of 128 x 128, that
+// puts the largest of them into [128, 256).  Powers of two make the scaling exact,
+// and the matrix cores apply them inside the product: an instruction of 128 elements
+// of the sum takes one exponent byte for each row of either operand.
+#include "am_device.h"
+#include "am_internal.h"
+#include "per_device.h"
+
+namespace am {
+namespace {
+
+// ------------------------------------------------------------- quantising --
+//
+// One workgroup takes a tile of 128 x 128: a thread has 8 x 8 elements of it, so its
+// rows leave as words and its columns, through LDS, as 16-byte pieces.  The matrix is
+// read once for both layouts; HBM bounds it.
+
+constexpr int QT = 128;           // rows and columns of a tile, elements of a scale
+constexpr int QPITCH = QT + 16;   // bytes between the transposed tile's rows in LDS
+
+// The bits of |v|, or 0 where v is not finite: what is not a number sets no scale.
+__device__ __forceinline__ uint32_t magnitude(float v) {
+  const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
+  return u < 0x7f800000u ? u : 0u;
+}
+__device__ __forceinline__ uint32_t umax32(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// Eight elements from column c of a row of `cols`, zeros past its end.
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, bool wide, float (&v)[8]) {
+  if (wide && c + 8 <= cols) {
+    if constexpr (sizeof(T) == 2) {
+      const uint4 u = *reinterpret_cast<const uint4*>(row + c);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = __uint_as_float(w[k] << 16);
+        v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+      }
+    } else {
+      const float4 a = *reinterpret_cast<const float4*>(row + c), b = *reinterpret_cast<const float4*>(row + c + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? to_f32(row[c + k]) : 0.f;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void q8_quantise_kernel(Q8Quantise a) {
+  __shared__ __attribute__((aligned(16))) uint8_t turned[QT * QPITCH];
+  __shared__ uint32_t tops[16][QT + 4];
+  const int t = threadIdx.x, cx = t & 15, ry = t >> 4;
+  const int64_t ty = blockIdx.x / a.across, tx = blockIdx.x % a.across, r0 = ty * QT, c0 = tx * QT;
+  const int64_t rows = a.rows, cols = a.cols, c = c0 + 8 * cx;
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = r0 + 8 * ry + i;
+    if (r < rows) {
+      load8(static_cast<const T*>(a.x) + r * a.ld, c, cols, a.wide, v[i]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+    }
+  }
+  uint32_t row_top[8], col_top[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) row_top[i] = col_top[i] = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t m = magnitude(v[i][k]);
+      row_top[i] = umax32(row_top[i], m);
+      col_top[k] = umax32(col_top[k], m);
+    }
+  // along a row: the 16 threads of it are 16 lanes
+#pragma unroll
+  for (int i = 0; i < 8; ++i) row_top[i] = lanes16_max(row_top[i]);
+  if (a.tiles) {
+    uint32_t top = row_top[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = umax32(top, row_top[i]);
+    if (cx == 0) tops[ry][0] = top;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) top = umax32(top, tops[k][0]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) row_top[i] = col_top[i] = top;
+  } else if (a.codes_t) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) tops[ry][8 * cx + k] = col_top[k];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 16; ++q)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) col_top[k] = umax32(col_top[k], tops[q][8 * cx + k]);
+  }
+  if (a.codes) {
+    const int64_t pad = (cols + 15) & ~(int64_t)15;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = r0 + 8 * ry + i;
+      const uint32_t e = q8_exponent(row_top[i]);
+      const float inv = q8_inverse(e);
+      if (r < rows) {
+        if (c < pad)
+          *reinterpret_cast<uint2*>(a.codes + r * a.ldc + c) =
+              make_uint2(q8_codes4(v[i][0], v[i][1], v[i][2], v[i][3], inv), q8_codes4(v[i][4], v[i][5], v[i][6], v[i][7], inv));
+        if (!a.tiles && cx == 0) a.scales[r * a.lds + tx] = (uint8_t)e;
+      }
+    }
+    if (a.tiles && t == 0) a.scales[ty * a.lds + tx] = (uint8_t)q8_exponent(row_top[0]);
+  }
+  if (!a.codes_t) return;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t e = q8_exponent(col_top[k]);
+    const float inv = q8_inverse(e);
+    *reinterpret_cast<uint2*>(turned + (8 * cx + k) * QPITCH + 8 * ry) =
+        make_uint2(q8_codes4(v[0][k], v[1][k], v[2][k], v[3][k], inv), q8_codes4(v[4][k], v[5][k], v[6][k], v[7][k], inv));
+    if (!a.tiles && ry == 0 && c + k < cols) a.scales_t[(c + k) * a.ldst + ty] = (uint8_t)e;
+  }
+  if (a.tiles && t == 0) a.scales_t[tx * a.ldst + ty] = (uint8_t)q8_exponent(col_top[0]);
+  __syncthreads();
+  const int64_t pad = (rows + 15) & ~(int64_t)15;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int col = p * 32 + (t >> 3), piece = 16 * (t & 7);
+    if (c0 + col < cols && r0 + piece < pad)
+      *reinterpret_cast<uint4*>(a.codes_t + (c0 + col) * a.ldct + r0 + piece) =
+          *reinterpret_cast<const uint4*>(turned + col * QPITCH + piece);
+  }
+}
+
+// --------------------------------------------------------------- products --
+//
+// out = a b^T over k.  The matrix instruction forms 16 columns of out (rows of b) by
+// 16 rows (of a): a lane then has columns of one row, and with the rows of b dealt to
+// the instructions in fours it has 4 FN of them side by side, which leave as 16-byte
+// stores.  Operand tiles of 128 elements of the sum go from global memory straight to
+// LDS, NS stages deep, with their scales: a word of a row's scales serves four of
+// them, and an instruction picks its byte.
+
+__device__ uint4 g_none[1];  // zeros: what lies outside an operand
+
+constexpr int BK = 128;     // elements of the sum a stage
+constexpr int XCDS = 8;
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+// Four bytes a lane from global memory to LDS at lds_base + 4 * lane.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma4(const void* src, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds_base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int OP>
+__device__ __forceinline__ void mma8(f32x4_t& acc, const i32x8_t& a, const i32x8_t& b, int sa, int sb) {
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, OP, sa, OP, sb);
+}
+
+template <int BM_, int BN_, int WM_, int WN_, int NS_> struct Shape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NS = NS_;
+  static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+  static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
+  static constexpr int A_BYTES = BM * BK, B_BYTES = BN * BK, STAGE = A_BYTES + B_BYTES;
+  static constexpr int LOADS = (BM + BN) / 8 / WAVES;             // 16-byte loads a stage of each wave
+  static constexpr int SCALE_ROWS = BM + BN, SCALE_WAVES = SCALE_ROWS / 64;
+  static constexpr int SETS = (NS + 6) / 4;                       // sets of scales alive at once
+  static constexpr int LDS = NS * STAGE + SETS * SCALE_ROWS * 4;
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && (BM + BN) % (8 * WAVES) == 0, "whole loads");
+  static_assert(SCALE_WAVES <= WAVES, "one load of scales a wave");
+  static_assert(FN == 2 || FN == 4, "columns of a lane in 16-byte pieces");
+};
+
+// Which 16-byte piece of a row of 128 bytes lies in which slot: lanes that are served
+// together read rows whose keys differ.
+__device__ __forceinline__ int key_a(int row) { return row & 7; }
+template <int FN> __device__ __forceinline__ int key_b(int row) { return (row & 3) | ((row / (4 * FN)) & 1) << 2; }
+
+// One row's 4 FN columns: + bias, + what out holds, rounded once.
+template <int FN>
+__device__ __forceinline__ void q8_store(const Q8Matmul& a, int64_t row, int64_t col, const f32x4_t (&v)[FN]) {
+  if (row >= a.M || col >= a.N) return;
+  bf16_t* p = a.out + row * a.ldo + col;
+  float x[4 * FN];
+#pragma unroll
+  for (int j = 0; j < 4 * FN; ++j) x[j] = v[j / 4][j % 4];
+  if (a.bias) {
+#pragma unroll
+    for (int j = 0; j < 4 * FN; ++j)
+      if (col + j < a.N) x[j] += a.bias[col + j];
+  }
+  if (a.wide && col + 4 * FN <= a.N) {
+#pragma unroll
+    for (int h = 0; h < FN / 2; ++h) {
+      typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+      typedef float f8 __attribute__((ext_vector_type(8)));
+      f8 w;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = x[8 * h + j];
+      if (a.accumulate) {
+        const uint4 u = reinterpret_cast<const uint4*>(p)[h];
+        const uint32_t o[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[2 * j] += __uint_as_float(o[j] << 16);
+          w[2 * j + 1] += __uint_as_float(o[j] & 0xffff0000u);
+        }
+      }
+      reinterpret_cast<uint4*>(p)[h] = __builtin_bit_cast(uint4, __builtin_convertvector(w, b8));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4 * FN; ++j)
+      if (col + j < a.N) p[j] = f32_to_bf16(a.accumulate ? x[j] + bf16_to_f32(p[j]) : x[j]);
+  }
+}
+
+// The tile that a workgroup of a launch takes: each XCD has a run of them, so that
+// tiles with the same rows of a share its L2.
+__device__ __forceinline__ int tile_of(int b, int tiles) {
+  const int x = b % XCDS, q = tiles / XCDS, rem = tiles % XCDS;
+  return x * q + min(x, rem) + b / XCDS;
+}
+
+template <typename S>
+__global__ __launch_bounds__(S::THREADS) void q8_matmul_kernel(Q8Matmul a) {
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  constexpr int FM = S::FM, FN = S::FN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tile = tile_of(blockIdx.x, a.tiles_m * a.tiles_n);
+  const int64_t m0 = (int64_t)(tile / a.tiles_n) * S::BM, n0 = (int64_t)(tile % a.tiles_n) * S::BN;
+  const int split = blockIdx.y, k0 = split * a.steps, nk = min(a.blocks - k0, a.steps);  // (blocks of BK)
+  const uint32_t base = lds_address(lds), scales = base + S::NS * S::STAGE;
+  const uint8_t* scale_lds = lds + S::NS * S::STAGE;
+
+  // where this lane's loads come from; pieces outside an operand come from zeros
+  const uint8_t* src[S::LOADS];
+  bool in[S::LOADS];
+  int piece[S::LOADS];
+#pragma unroll
+  for (int i = 0; i < S::LOADS; ++i) {
+    const int row = (wave * S::LOADS + i) * 8 + (lane >> 3);  // of both operands' tiles
+    const bool is_a = (wave * S::LOADS + i) * 8 < S::BM;
+    const int r = is_a ? row : row - S::BM;
+    piece[i] = 16 * ((lane & 7) ^ (is_a ? key_a(r) : key_b<FN>(r)));
+    const int64_t g = (is_a ? m0 : n0) + r;
+    in[i] = g < (is_a ? a.M : a.N);
+    src[i] = (is_a ? a.a + g * a.lda : a.b + g * a.ldb) + piece[i];
+  }
+  // and one row's scales
+  const uint8_t* scale_src = nullptr;
+  if (wave < S::SCALE_WAVES) {
+    const int row = wave * 64 + lane;
+    if (row < S::BM) {
+      scale_src = a.a_scale + min(m0 + row, a.M - 1) * a.ldas;
+    } else {
+      const int64_t g = min(n0 + row - S::BM, a.N - 1);
+      scale_src = a.b_scale + (a.b_tiles ? g / QT : g) * a.ldbs;
+    }
+  }
+  auto load = [&](int t) {  // stage t of this workgroup's (a constant number of loads but for scales)
+    const int64_t at = (int64_t)(k0 + t) * BK;
+    const uint32_t to = base + (t % S::NS) * S::STAGE + wave * S::LOADS * 1024;
+    if (t % 4 == 0 && wave < S::SCALE_WAVES)
+      dma4(scale_src + at / BK, scales + (t / 4 % S::SETS) * S::SCALE_ROWS * 4 + wave * 256);
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i) {
+      const void* p = in[i] && at + piece[i] < a.K ? (const void*)(src[i] + at) : (const void*)g_none;
+      dma16(p, to + i * 1024);
+    }
+  };
+#pragma unroll
+  for (int t = 0; t < S::NS - 1; ++t)
+    if (t < nk) load(t);
+
+  const int wm = wave / S::WN, wn = wave % S::WN, i16 = lane & 15, g4 = lane >> 4;
+  f32x4_t acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  int sa[FM], sb[FN];
+
+  auto step = [&](int t, auto op) {
+    constexpr int OP = decltype(op)::value;
+    // stage t is here once at most the later stages' loads are in flight
+    const int later = min(nk - 1 - t, S::NS - 2);
+    wait_vm_n<S::LOADS * (S::NS - 2)>(later * S::LOADS);
+    lds_barrier();
+    if (t + S::NS - 1 < nk) load(t + S::NS - 1);  // (into the stage that was read before the barrier)
+    const uint8_t* st = lds + (t % S::NS) * S::STAGE;
+    if constexpr (OP == 0) {
+      const uint8_t* sc = scale_lds + (t / 4 % S::SETS) * S::SCALE_ROWS * 4;
+#pragma unroll
+      for (int i = 0; i < FM; ++i) sa[i] = *reinterpret_cast<const int*>(sc + 4 * (wm * S::TM + 16 * i + i16));
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        sb[j] = *reinterpret_cast<const int*>(sc + 4 * (S::BM + wn * S::TN + (i16 >> 2) * 4 * FN + 4 * j + (i16 & 3)));
+    }
+    auto fragment = [&](const uint8_t* row, int key) {
+      i32x8_t f;
+      const uint4 lo = *reinterpret_cast<const uint4*>(row + 16 * ((2 * g4) ^ key));
+      const uint4 hi = *reinterpret_cast<const uint4*>(row + 16 * ((2 * g4 + 1) ^ key));
+      f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w;
+      f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
+      return f;
+    };
+    i32x8_t fb[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const int r = wn * S::TN + (i16 >> 2) * 4 * FN + 4 * j + (i16 & 3);
+      fb[j] = fragment(st + S::A_BYTES + r * BK, key_b<FN>(r));
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int r = wm * S::TM + 16 * i + i16;
+      const i32x8_t fa = fragment(st + r * BK, key_a(r));
+#pragma unroll
+      for (int j = 0; j < FN; ++j) mma8<OP>(acc[i][j], fb[j], fa, sb[j], sa[i]);
+    }
+  };
+  for (int t = 0; t < nk; t += 4) {
+    step(t, std::integral_constant<int, 0>());
+    if (t + 1 < nk) step(t + 1, std::integral_constant<int, 1>());
+    if (t + 2 < nk) step(t + 2, std::integral_constant<int, 2>());
+    if (t + 3 < nk) step(t + 3, std::integral_constant<int, 3>());
+  }
+
+  if (a.parts) {  // one of several sums: in the order of the registers
+    float4* p = reinterpret_cast<float4*>(a.parts) +
+                (((int64_t)split * a.tiles_m * a.tiles_n + tile) * FM * FN) * S::THREADS + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        p[(int64_t)(i * FN + j) * S::THREADS] = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+    q8_store<FN>(a, m0 + wm * S::TM + 16 * i + i16, n0 + wn * S::TN + g4 * 4 * FN, acc[i]);
+}
+
+// The sums of a split product, added in the order of the splits.
+template <typename S>
+__global__ __launch_bounds__(S::THREADS) void q8_join_kernel(Q8Matmul a) {
+  constexpr int FM = S::FM, FN = S::FN;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int tile = blockIdx.x / FM, i = blockIdx.x % FM;
+  const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
+  const float4* p = reinterpret_cast<const float4*>(a.parts) + ((int64_t)tile * FM + i) * FN * S::THREADS + threadIdx.x;
+  f32x4_t v[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) v[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.splits; ++s, p += tiles * FM * FN * S::THREADS)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const float4 u = p[j * S::THREADS];
+      v[j] += f32x4_t{u.x, u.y, u.z, u.w};
+    }
+  const int64_t m0 = (int64_t)(tile / a.tiles_n) * S::BM, n0 = (int64_t)(tile % a.tiles_n) * S::BN;
+  q8_store<FN>(a, m0 + wave / S::WN * S::TM + 16 * i + (lane & 15), n0 + wave % S::WN * S::TN + (lane >> 4) * 4 * FN, v);
+}
+
+typedef Shape<256, 256, 2, 4, 2> Large;
+typedef Shape<128, 128, 2, 2, 2> Medium;
+typedef Shape<64, 64, 2, 2, 4> Small;
+
+template <typename S> void plan_of(Q8Plan& p, int64_t M, int64_t N, int64_t K) {
+  const int64_t tiles = ((M + S::BM - 1) / S::BM) * ((N + S::BN - 1) / S::BN), blocks = (K + BK - 1) / BK;
+  // split where the tiles leave CUs idle and the sum is long: each part has eight
+  // steps at least, in whole words of scales
+  int64_t splits = 1;
+  const int64_t room = 512 / tiles;
+  if (room >= 2 && blocks >= 16) splits = std::min<int64_t>(room, blocks / 8);
+  const int64_t steps = ((blocks + splits - 1) / splits + 3) / 4 * 4;
+  splits = blocks ? (blocks + steps - 1) / steps : 1;
+  p.steps = (int)steps;
+  p.splits = (int)splits;
+  p.bytes = splits > 1 ? splits * tiles * S::BM * S::BN * 4 : 0;
+}
+
+template <typename S> hipError_t run(Q8Matmul a, const Q8Plan& p, hipStream_t s) {
+  static PerDevice ready;
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e == hipSuccess)
+    e = ready.once(device, [] {
+      return hipFuncSetAttribute(reinterpret_cast<const void*>(&q8_matmul_kernel<S>),
+                                 hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+    });
+  if (e != hipSuccess) return e;
+  a.tiles_m = (int)((a.M + S::BM - 1) / S::BM);
+  a.tiles_n = (int)((a.N + S::BN - 1) / S::BN);
+  a.blocks = (int)((a.K + BK - 1) / BK);
+  a.steps = p.steps;
+  a.splits = p.splits;
+  if (p.splits == 1) a.parts = nullptr;
+  const unsigned tiles = (unsigned)((int64_t)a.tiles_m * a.tiles_n);
+  hipLaunchKernelGGL((q8_matmul_kernel<S>), dim3(tiles, p.splits), dim3(S::THREADS), S::LDS, s, a);
+  if (p.splits > 1)
+    hipLaunchKernelGGL((q8_join_kernel<S>), dim3(tiles * S::FM), dim3(S::THREADS), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t q8_quantise(Q8Quantise a, bool bf16, hipStream_t s) {
+  a.across = (unsigned)((a.cols + QT - 1) / QT);
+  const dim3 grid((unsigned)(a.across * ((a.rows + QT - 1) / QT)));
+  if (bf16) hipLaunchKernelGGL((q8_quantise_kernel<bf16_t>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((q8_quantise_kernel<float>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+Q8Plan q8_plan(int64_t M, int64_t N, int64_t K) {
+  Q8Plan p{};
+  const int64_t large = ((M + 255) / 256) * ((N + 255) / 256), medium = ((M + 127) / 128) * ((N + 127) / 128);
+  p.kind = large >= 1024 ? 2 : M > 64 && (medium >= 96 || K >= 4096) ? 1 : 0;
+  if (p.kind == 2) plan_of<Large>(p, M, N, K);
+  else if (p.kind == 1) plan_of<Medium>(p, M, N, K);
+  else plan_of<Small>(p, M, N, K);
+  return p;
+}
+
+hipError_t q8_matmul(const Q8Matmul& a, hipStream_t s) {
+  const Q8Plan p = q8_plan(a.M, a.N, a.K);
+  return p.kind == 2 ? run<Large>(a, p, s) : p.kind == 1 ? run<Medium>(a, p, s) : run<Small>(a, p, s);
+}
+
+}  // namespace am
