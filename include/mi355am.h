@@ -408,6 +408,50 @@ am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dty
                                     const float* dhT, void* dx, void* dr, void* di, int64_t ldd,
                                     float* dlam, float* dh0, void* ws, int64_t ws_bytes, void* stream);
 
+/* A recurrent layer whose state is a matrix: the gated delta rule over packed frames
+ * (layout and lengths as in lstm_am_forward).  Per head, S [dk][dv]:
+ *   q = q / sqrt(q q + eps),  k = k / sqrt(k k + eps),
+ *   a_t = exp(-c softplus(lam) sigm(r_t)),  beta_t = sigm(b_t),
+ *   S_t = a_t S_{t-1} + beta_t k_t (v_t - a_t S_{t-1}^T k_t)^T,   o_t = S_t^T q_t:
+ * the state forgets by a_t, and what it holds under the key k_t moves to v_t by
+ * beta_t.  `heads` heads share `key_heads` pairs of q and k, heads / key_heads of them
+ * (neighbours) one pair.  Sums and states are in 32 bits, each output is rounded once.
+ *   dtype    AM_F32 or AM_BF16: type of q, k, v, r, b, o and their gradients
+ *   q, k     [N] rows of key_heads dk;  v, o [N] rows of heads dv;  r, b [N] rows of
+ *            heads; each with its row stride (columns of one projection, say)
+ *   lam      [heads] fp32, finite;  c > 0;  eps > 0
+ *   lengths  [host] [B] or NULL; variable-length batches allow B <= 1024
+ *   s0       [B][heads][dk][dv] fp32 or NULL (zero);  sT the same or NULL: states after
+ *            each sequence's last frame (s0 where it has none; may be s0 itself)
+ *   ws       workspace of am_gated_delta_workspace_bytes (256-byte aligned; may be NULL
+ *            where that is 0).  train = 1 keeps in it what gated_delta_backward reads;
+ *            it must not be modified between.
+ * 1 <= dk, dv <= 128; key_heads divides heads; N less than 2^31 - 256.  A batch of one
+ * frame a sequence with train = 0 and without lengths is one launch that reads and
+ * writes the states once.  No atomics and no waits between workgroups: the same inputs
+ * give the same bits. */
+int64_t am_gated_delta_workspace_bytes(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk,
+                                       int32_t dv, int32_t dtype, int32_t varlen, int32_t train);
+am_status gated_delta_forward(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv,
+                              int32_t dtype, const int32_t* lengths, const void* q, int64_t ldq, const void* k,
+                              int64_t ldk, const void* v, int64_t ldv, const void* r, int64_t ldr,
+                              const void* b, int64_t ldb, const float* lam, float c, float eps,
+                              const float* s0, void* o, int64_t ldo, float* sT, int32_t train, void* ws,
+                              int64_t ws_bytes, void* stream);
+/* The gradient of the forward call (train = 1) that filled `ws`, whose sizes, lengths,
+ * q, k, v, r, b, lam, c, eps and s0 (as it was before that call) are given again:
+ *   d_o   [N] rows: dL/do;  dsT [B][heads][dk][dv] fp32 or NULL: dL/dsT
+ *   dq, dk_, dv_, dr, db  rows as of q, k, v, r, b (written)
+ *   dlam  [heads] fp32 (written);  ds0 as s0 or NULL (written; may be dsT itself) */
+am_status gated_delta_backward(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv,
+                               int32_t dtype, const int32_t* lengths, const void* q, int64_t ldq, const void* k,
+                               int64_t ldk, const void* v, int64_t ldv, const void* r, int64_t ldr,
+                               const void* b, int64_t ldb, const float* lam, float c, float eps,
+                               const float* s0, const void* d_o, int64_t lddo, const float* dsT, void* dq,
+                               int64_t lddq, void* dk_, int64_t lddk, void* dv_, int64_t lddv, void* dr,
+                               int64_t lddr, void* db, int64_t lddb, float* dlam, float* ds0, void* ws,
+                               int64_t ws_bytes, void* stream);
+
 /* Between two blocks of a residual stack, per row of H:
  *   u = o * gate * sigm(gate)                         (gate NULL: u = o)
  *   p = u / sqrt(mean(u^2) + eps)                     (w_post NULL: p = u)
@@ -544,7 +588,7 @@ typedef enum {
   AM_K_SGD = 8,
   AM_K_MISC = 9,          /* casts, transposes, bias reductions, gathers */
   AM_K_BMUF = 10,         /* BMUF-NBM global step */
-  AM_K_GATED = 11,        /* gated linear recurrence, forward and backward */
+  AM_K_GATED = 11,        /* gated linear recurrence, gated delta rule, forward and backward */
   AM_K_NORM = 12,         /* gate, norm, residual and next norm, and their gradient */
   AM_K_ADAMW = 13,        /* AdamW step */
   AM_K_Q8 = 14,           /* matrices in 8 bits: quantising and products */

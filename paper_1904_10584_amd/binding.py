@@ -96,6 +96,11 @@ _PROTOS = {
                                         _P, _I32, _P, _I64, _P]),
     "gated_recurrence_backward": (_I32, [_I32, _I32, _I32, _I32, _P, _P, _P, _P, _I64, _P, _F32, _P, _I64,
                                          _P, _P, _P, _P, _I64, _P, _P, _P, _I64, _P]),
+    "am_gated_delta_workspace_bytes": (_I64, [_I32] * 9),
+    "gated_delta_forward": (_I32, [_I32] * 7 + [_P] + [_P, _I64] * 5 + [_P, _F32, _F32, _P, _P, _I64, _P, _I32, _P,
+                                   _I64, _P]),
+    "gated_delta_backward": (_I32, [_I32] * 7 + [_P] + [_P, _I64] * 5 + [_P, _F32, _F32, _P, _P, _I64, _P]
+                             + [_P, _I64] * 5 + [_P, _P, _P, _I64, _P]),
     "am_gated_norm_workspace_bytes": (_I64, [_I64, _I32]),
     "gated_norm_forward": (_I32, [_I64, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _F32, _P,
                                   _P, _P, _P]),
@@ -515,6 +520,62 @@ def gated_recurrence_backward(x, r, i, lam, T, B, dh, ws, dx, dr, di, dlam, leng
         T, B, H, dt, lp, xp, rp, ip, ld, _shaped(lam, "lam", (H,)), c, dhp, lddh,
         _shaped(dhT, "dhT", (B, H)), dxp, drp, dip, ldd, _shaped(dlam, "dlam", (H,)),
         _shaped(dh0, "dh0", (B, H)), wp, wn, _stream(stream))
+    if st:
+        _check(st)
+
+
+def gated_delta_workspace_bytes(T, B, heads, dk, dv, key_heads=None, dtype=torch.bfloat16, lengths=None,
+                                train=False) -> int:
+    kinds = {torch.float32: F32, torch.bfloat16: BF16}
+    n = lib().am_gated_delta_workspace_bytes(T, B, heads, heads if key_heads is None else key_heads, dk, dv,
+                                             kinds.get(dtype, -1), int(lengths is not None), int(bool(train)))
+    if n < 0:
+        raise AmError("invalid sizes for workspace query", EINVAL)
+    return int(n)
+
+
+def _delta(q, k, v, r, b, lam, T, B, heads, key_heads, lengths, s0):
+    """What both passes share: sizes, states' shape and the arguments up to b."""
+    key_heads = heads if key_heads is None else key_heads
+    arr, lp, N = _packed_rows(T, B, lengths)
+    if heads < 1 or key_heads < 1 or heads % key_heads:
+        raise AmError(f"key_heads = {key_heads} must divide heads = {heads}")
+    dt = _dtype(q, "q")
+    for t, name, n in ((q, "q", key_heads), (v, "v", heads)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[1] % n:
+            raise AmError(f"{name} must be [{N}] rows of {n} heads")
+    dk, dv, kind = q.shape[1] // key_heads, v.shape[1] // heads, q.dtype
+    rows = [x for t, name, n in ((q, "q", key_heads * dk), (k, "k", key_heads * dk), (v, "v", heads * dv),
+                                 (r, "r", heads), (b, "b", heads)) for x in _row(t, name, N, n, kind)]
+    return dk, dv, N, kind, (B, heads, dk, dv), arr, [T, B, heads, key_heads, dk, dv, dt, lp] + rows
+
+
+def gated_delta_forward(q, k, v, r, b, lam, T, B, o, ws=None, heads=1, key_heads=None, lengths=None, s0=None,
+                        sT=None, c=8.0, eps=1e-6, train=False, stream=None):
+    """q, k: [N][key_heads dk], v and o: [N][heads dv], r, b: [N][heads] rows (columns of
+    one projection, say); lam: [heads]; s0, sT: [B][heads][dk][dv] fp32 (sT may be s0)."""
+    dk, dv, N, kind, state, arr, args = _delta(q, k, v, r, b, lam, T, B, heads, key_heads, lengths, s0)
+    wp, wn = _workspace(ws)
+    st = (_lib or lib()).gated_delta_forward(
+        *args, _shaped(lam, "lam", (heads,)), c, eps, _shaped(s0, "s0", state), *_row(o, "o", N, heads * dv, kind),
+        _shaped(sT, "sT", state), 1 if train else 0, wp, wn, _stream(stream))
+    if st:
+        _check(st)
+
+
+def gated_delta_backward(q, k, v, r, b, lam, T, B, do, ws, dq, dk, dv, dr, db, dlam, heads=1, key_heads=None,
+                         lengths=None, s0=None, dsT=None, ds0=None, c=8.0, eps=1e-6, stream=None):
+    """The gradient of the forward call (train=True) that filled `ws`, with the s0 that
+    it had; dq, dk, dv, dr, db: rows as of q, k, v, r, b."""
+    nk, nv, N, kind, state, arr, args = _delta(q, k, v, r, b, lam, T, B, heads, key_heads, lengths, s0)
+    keys = heads if key_heads is None else key_heads
+    wp, wn = _workspace(ws)
+    st = (_lib or lib()).gated_delta_backward(
+        *args, _shaped(lam, "lam", (heads,)), c, eps, _shaped(s0, "s0", state),
+        *_row(do, "do", N, heads * nv, kind), _shaped(dsT, "dsT", state),
+        *_row(dq, "dq", N, keys * nk, kind), *_row(dk, "dk", N, keys * nk, kind),
+        *_row(dv, "dv", N, heads * nv, kind), *_row(dr, "dr", N, heads, kind), *_row(db, "db", N, heads, kind),
+        _shaped(dlam, "dlam", (heads,)), _shaped(ds0, "ds0", state), wp, wn, _stream(stream))
     if st:
         _check(st)
 

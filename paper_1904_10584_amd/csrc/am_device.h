@@ -120,6 +120,19 @@ __device__ __forceinline__ float sigm(float x) {
 }
 __device__ __forceinline__ float tanh_f(float x) { return 2.0f * sigm(2.0f * x) - 1.0f; }
 
+// max(v, 0) + log(1 + e), e = e^-|v|, the logarithm as 2 artanh(e / (2 + e)), whose
+// series ends below 2^-24 of it (e / (2 + e) is at most 1 / 3).
+__device__ __forceinline__ float softplus(float v) {
+  const float e = __expf(-fabsf(v)), s = e / (2.f + e), z = s * s;
+  float p = 1.f / 13.f;
+  p = fmaf(p, z, 1.f / 11.f);
+  p = fmaf(p, z, 1.f / 9.f);
+  p = fmaf(p, z, 1.f / 7.f);
+  p = fmaf(p, z, 1.f / 5.f);
+  p = fmaf(p, z, 1.f / 3.f);
+  return fmaxf(v, 0.f) + 2.f * fmaf(p * z, s, s);
+}
+
 // One LSTM cell step of one unit (bf16 per-step paths) from its gate
 // pre-activations (i, f, g, o) and c_{t-1}: the gates, c_t and h_t.  The
 // products are rounded separately (no multiply-add contraction), so every

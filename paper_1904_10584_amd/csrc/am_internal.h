@@ -344,6 +344,42 @@ struct GatedSchedule {
   int T, B, first, count, last;
   int32_t len[MAX], tail[MAX];   // tail: frames of this sequence and those after it
 };
+hipError_t gated_schedule(const GatedSchedule& a, const int32_t* lengths, hipStream_t s);
+
+// Gated delta rule (see gated_delta_forward in the C ABI).  A chunk of GD_CHUNK
+// frames is evaluated at once; a training forward pass saves the state each starts
+// from.
+constexpr int GD_CHUNK = 64, GD_MAX_DIM = 128;
+struct GatedDelta {
+  const void *q, *k, *v, *r, *b;     // [N] rows of G dk, G dk, H dv, H and H
+  int64_t ldq, ldk, ldv, ldr, ldb;
+  const float* lam;                  // [H]
+  const float* s0;                   // [B][H][dk][dv] or null (zero)
+  float* sT;                         // forward: the same, or null
+  void* o;                           // forward: [N] rows of H dv (written)
+  int64_t ldo;
+  const void* d_o;                   // backward: [N] rows of H dv
+  int64_t lddo;
+  const float* dsT;                  // backward: [B][H][dk][dv] or null (zero)
+  float* ds0;                        // backward: the same, or null
+  void *dq, *dk_, *dv_, *dr, *db;    // backward: rows as of q, k, v, r, b (written)
+  int64_t lddq, lddk, lddv, lddr, lddb;
+  float* dlam;                       // backward: [H]
+  float* saved;                      // [chunks - 1][B][H][dk][dv]: states that the second chunk
+                                     // and on start from (written by a training forward)
+  float* dsaved;                     // backward: [chunks][B][H][dk][dv], the gradients of
+                                     // the chunks' last states
+  float *u, *dr_rows;                // backward: [N] rows of H dv
+  float* parts;                      // backward: [B][H]
+  const int32_t *offs, *lens;        // [T + 1], [B], or null: every sequence has T frames
+  int64_t N;
+  int T, B, H, G, dk, dv;
+  float c, eps;
+  bool train;                        // forward: keep the states
+  bool keep_end;                     // backward: ds0 is dsT, which is kept in dsaved
+};
+hipError_t gated_delta_forward(GatedDelta a, bool bf16, hipStream_t s);
+hipError_t gated_delta_backward(GatedDelta a, bool bf16, hipStream_t s);
 
 // Gate, norm, residual and next norm (see gated_norm_forward in the C ABI); at
 // most GATED_NORM_BLOCKS workgroups, a row of parts each.

@@ -703,6 +703,92 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
   return AM_OK;
 }
 
+struct DeltaLayout { int64_t offs, lens, tails, saved, dsaved, u, dr, parts, total; };
+DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int64_t dk, int64_t dv, bool varlen, bool train) {
+  DeltaLayout l{};
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += align256(bytes);
+    return here;
+  };
+  if (varlen) {
+    l.offs = take((T + 1) * 4);
+    l.lens = take(B * 4);
+    l.tails = take(B * 4);
+  }
+  if (train) {  // (the first chunk starts from s0, the last one's gradient from dsT)
+    const int64_t links = T > am::GD_CHUNK ? (T - 1) / am::GD_CHUNK : 0;
+    l.saved = take(links * B * H * dk * dv * 4);
+    l.dsaved = take((links + 1) * B * H * dk * dv * 4);
+    l.u = take(T * B * H * dv * 4);
+    l.dr = take(T * B * H * dv * 4);
+    l.parts = take(B * H * 4);
+  }
+  l.total = at;
+  return l;
+}
+
+bool delta_sizes(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv) {
+  return T >= 0 && B >= 1 && heads >= 1 && key_heads >= 1 && heads % key_heads == 0 && dk >= 1 && dv >= 1;
+}
+
+// The arguments that forward and backward share; fills in a.
+am_status check_delta(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv,
+                      int32_t dtype, const int32_t* lengths, const void* q, int64_t ldq, const void* k,
+                      int64_t ldk, const void* v, int64_t ldv, const void* r, int64_t ldr, const void* b,
+                      int64_t ldb, const float* lam, float c, float eps, const float* s0, bool train, void* ws,
+                      int64_t ws_bytes, am::GatedDelta& a, DeltaLayout& l) {
+  if (!delta_sizes(T, B, heads, key_heads, dk, dv))
+    return fail(AM_EINVAL, "need T >= 0, B, dk, dv >= 1 and key_heads a divisor of heads (T=%d, B=%d, dk=%d, dv=%d, heads=%d, key_heads=%d)",
+                T, B, dk, dv, heads, key_heads);
+  if (dk > am::GD_MAX_DIM || dv > am::GD_MAX_DIM)
+    return fail(AM_EUNSUPPORTED, "heads of at most %d x %d", am::GD_MAX_DIM, am::GD_MAX_DIM);
+  if (dtype != AM_F32 && dtype != AM_BF16) return fail(AM_EINVAL, "dtype %d unknown", dtype);
+  if (!lam || !aligned(lam, 4)) return fail(AM_EINVAL, "NULL or unaligned lam");
+  if (!(c > 0.f && c <= 3.4e38f)) return fail(AM_EINVAL, "c must be positive and finite");
+  if (!(eps > 0.f && eps <= 3.4e38f)) return fail(AM_EINVAL, "eps must be positive and finite");
+  if (!aligned(s0, 4)) return fail(AM_EINVAL, "states must be 4-byte aligned");
+  a.N = (int64_t)T * B;
+  a.T = T;
+  if (lengths) {
+    if (B > 1024) return fail(AM_EUNSUPPORTED, "variable-length batches allow B <= 1024");
+    a.N = 0;
+    for (int n = 0; n < B; ++n) {
+      if (lengths[n] < 0 || lengths[n] > T)
+        return fail(AM_EINVAL, "lengths[%d] = %d outside [0, %d]", n, lengths[n], T);
+      if (n > 0 && lengths[n] > lengths[n - 1])
+        return fail(AM_EINVAL, "lengths must be non-increasing (lengths[%d] > lengths[%d])", n, n - 1);
+      a.N += lengths[n];
+    }
+    a.T = lengths[0];
+  }
+  if (a.N >= (1ll << 31) - 256 || T > (1 << 30)) return fail(AM_EUNSUPPORTED, "too many frames");
+  if (((int64_t)T / am::GD_CHUNK + 1) * B * heads >= (1ll << 31) || (int64_t)heads * am::GD_MAX_DIM >= (1ll << 31))
+    return fail(AM_EUNSUPPORTED, "too many heads");
+  AM_TRY(check_rows(a.N, key_heads * dk, dtype, q, ldq, "q"));
+  AM_TRY(check_rows(a.N, key_heads * dk, dtype, k, ldk, "k"));
+  AM_TRY(check_rows(a.N, heads * dv, dtype, v, ldv, "v"));
+  AM_TRY(check_rows(a.N, heads, dtype, r, ldr, "r"));
+  AM_TRY(check_rows(a.N, heads, dtype, b, ldb, "b"));
+  l = delta_layout(T, B, heads, dk, dv, lengths != nullptr, train);
+  if (l.total > 0 && (!ws || !aligned(ws, 256) || ws_bytes < l.total))
+    return fail(AM_EWORKSPACE, "needs %lld workspace bytes, 256-byte aligned", (long long)l.total);
+  a.q = q; a.k = k; a.v = v; a.r = r; a.b = b;
+  a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldr = ldr; a.ldb = ldb;
+  a.B = B; a.H = heads; a.G = key_heads;
+  a.dk = dk; a.dv = dv;
+  a.lam = lam;
+  a.c = c;
+  a.eps = eps;
+  a.s0 = s0;
+  if (lengths) {
+    a.offs = at<int32_t>(ws, l.offs);
+    a.lens = at<int32_t>(ws, l.lens);
+  }
+  return AM_OK;
+}
+
 am_status check_norm(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, const void* o, int64_t ldo,
                      const void* gate, int64_t ldg, const float* w_post, const float* scale, const void* res,
                      const float* w_next, float eps, am::GatedNorm& a) {
@@ -1517,6 +1603,84 @@ am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dty
   hipStream_t s = static_cast<hipStream_t>(stream);
   Timed tm(AM_K_GATED, s, 40.0 * a.N * H, 7.0 * esz_of(dtype) * a.N * H + 8.0 * B * H);
   return hip_check(am::gated_backward(a, dtype == AM_BF16, s), "gated recurrence backward");
+}
+
+int64_t am_gated_delta_workspace_bytes(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk,
+                                       int32_t dv, int32_t dtype, int32_t varlen, int32_t train) {
+  if (!delta_sizes(T, B, heads, key_heads, dk, dv) || dk > am::GD_MAX_DIM || dv > am::GD_MAX_DIM) return -1;
+  if ((dtype != AM_F32 && dtype != AM_BF16) || (int64_t)T * B >= (1ll << 32) || (int64_t)B * heads >= (1ll << 31)) return -1;
+  return delta_layout(T, B, heads, dk, dv, varlen != 0, train != 0).total;
+}
+
+am_status gated_delta_forward(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv,
+                              int32_t dtype, const int32_t* lengths, const void* q, int64_t ldq, const void* k,
+                              int64_t ldk, const void* v, int64_t ldv, const void* r, int64_t ldr,
+                              const void* b, int64_t ldb, const float* lam, float c, float eps,
+                              const float* s0, void* o, int64_t ldo, float* sT, int32_t train, void* ws,
+                              int64_t ws_bytes, void* stream) {
+  am::GatedDelta a{};
+  DeltaLayout l;
+  AM_TRY(check_delta(T, B, heads, key_heads, dk, dv, dtype, lengths, q, ldq, k, ldk, v, ldv, r, ldr, b, ldb,
+                     lam, c, eps, s0, train != 0, ws, ws_bytes, a, l));
+  AM_TRY(check_rows(a.N, heads * dv, dtype, o, ldo, "o"));
+  if (!aligned(sT, 4)) return fail(AM_EINVAL, "states must be 4-byte aligned");
+  a.o = o;
+  a.ldo = ldo;
+  a.sT = sT;
+  a.train = train != 0;
+  if (train) a.saved = at<float>(ws, l.saved);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Timed tm(AM_K_GATED, s, 6.0 * a.N * heads * dk * dv,
+           (double)esz_of(dtype) * a.N * (2.0 * key_heads * dk + 2.0 * heads * dv + 2.0 * heads) + 8.0 * B * heads * dk * dv);
+  if (lengths) {
+    am::GatedSchedule g{};
+    g.offs = at<int32_t>(ws, l.offs);
+    g.lens = at<int32_t>(ws, l.lens);
+    g.tails = at<int32_t>(ws, l.tails);
+    g.T = a.T;
+    g.B = B;
+    AM_TRY(hip_check(am::gated_schedule(g, lengths, s), "gated delta schedule"));
+  }
+  return hip_check(am::gated_delta_forward(a, dtype == AM_BF16, s), "gated delta rule");
+}
+
+am_status gated_delta_backward(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv,
+                               int32_t dtype, const int32_t* lengths, const void* q, int64_t ldq, const void* k,
+                               int64_t ldk, const void* v, int64_t ldv, const void* r, int64_t ldr,
+                               const void* b, int64_t ldb, const float* lam, float c, float eps,
+                               const float* s0, const void* d_o, int64_t lddo, const float* dsT, void* dq,
+                               int64_t lddq, void* dk_, int64_t lddk, void* dv_, int64_t lddv, void* dr,
+                               int64_t lddr, void* db, int64_t lddb, float* dlam, float* ds0, void* ws,
+                               int64_t ws_bytes, void* stream) {
+  am::GatedDelta a{};
+  DeltaLayout l;
+  AM_TRY(check_delta(T, B, heads, key_heads, dk, dv, dtype, lengths, q, ldq, k, ldk, v, ldv, r, ldr, b, ldb,
+                     lam, c, eps, s0, true, ws, ws_bytes, a, l));
+  AM_TRY(check_rows(a.N, heads * dv, dtype, d_o, lddo, "d_o"));
+  AM_TRY(check_rows(a.N, key_heads * dk, dtype, dq, lddq, "dq"));
+  AM_TRY(check_rows(a.N, key_heads * dk, dtype, dk_, lddk, "dk"));
+  AM_TRY(check_rows(a.N, heads * dv, dtype, dv_, lddv, "dv"));
+  AM_TRY(check_rows(a.N, heads, dtype, dr, lddr, "dr"));
+  AM_TRY(check_rows(a.N, heads, dtype, db, lddb, "db"));
+  if (!dlam || !aligned(dlam, 4)) return fail(AM_EINVAL, "NULL or unaligned dlam");
+  if (!aligned(dsT, 4) || !aligned(ds0, 4)) return fail(AM_EINVAL, "states must be 4-byte aligned");
+  a.train = true;
+  a.d_o = d_o; a.lddo = lddo;
+  a.dq = dq; a.dk_ = dk_; a.dv_ = dv_; a.dr = dr; a.db = db;
+  a.lddq = lddq; a.lddk = lddk; a.lddv = lddv; a.lddr = lddr; a.lddb = lddb;
+  a.dsT = dsT;
+  a.ds0 = ds0;
+  a.keep_end = dsT && ds0 == dsT;
+  a.dlam = dlam;
+  a.saved = at<float>(ws, l.saved);
+  a.dsaved = at<float>(ws, l.dsaved);
+  a.u = at<float>(ws, l.u);
+  a.dr_rows = at<float>(ws, l.dr);
+  a.parts = at<float>(ws, l.parts);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Timed tm(AM_K_GATED, s, 12.0 * a.N * heads * dk * dv,
+           (double)esz_of(dtype) * a.N * (4.0 * key_heads * dk + 3.0 * heads * dv + 4.0 * heads) + 8.0 * B * heads * dk * dv);
+  return hip_check(am::gated_delta_backward(a, dtype == AM_BF16, s), "gated delta rule backward");
 }
 
 am_status gated_norm_forward(int64_t N, int32_t H, int32_t dtype, int32_t res_dtype, const void* o,

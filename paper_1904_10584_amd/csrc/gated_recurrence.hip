@@ -100,19 +100,6 @@ __device__ __forceinline__ Gates gates(float r, float rate, bool live) {
   return g;
 }
 
-// max(v, 0) + log(1 + e), e = e^-|v|, the logarithm as 2 artanh(e / (2 + e)), whose
-// series ends below 2^-24 of it (e / (2 + e) is at most 1 / 3).
-__device__ __forceinline__ float softplus(float v) {
-  const float e = __expf(-fabsf(v)), s = e / (2.f + e), z = s * s;
-  float p = 1.f / 13.f;
-  p = fmaf(p, z, 1.f / 11.f);
-  p = fmaf(p, z, 1.f / 9.f);
-  p = fmaf(p, z, 1.f / 7.f);
-  p = fmaf(p, z, 1.f / 5.f);
-  p = fmaf(p, z, 1.f / 3.f);
-  return fmaxf(v, 0.f) + 2.f * fmaf(p * z, s, s);
-}
-
 // The schedule's tables, written by an earlier launch, for scalar loads.
 typedef const __attribute__((address_space(4))) int32_t* Table;
 __device__ __forceinline__ Table table(const int32_t* p) { return (Table)(uintptr_t)p; }
@@ -761,6 +748,10 @@ hipError_t route(const GatedRecurrence& a, const int32_t* lengths, bool bf16, bo
 }
 
 }  // namespace
+
+hipError_t gated_schedule(const GatedSchedule& a, const int32_t* lengths, hipStream_t s) {
+  return schedule(a, lengths, s);
+}
 
 hipError_t gated_forward(const GatedRecurrence& a, const int32_t* lengths, bool bf16, hipStream_t s) {
   return route(a, lengths, bf16, true, s);
