@@ -365,19 +365,20 @@ struct GatedDelta {
   void *dq, *dk_, *dv_, *dr, *db;    // backward: rows as of q, k, v, r, b (written)
   int64_t lddq, lddk, lddv, lddr, lddb;
   float* dlam;                       // backward: [H]
-  float* saved;                      // [chunks - 1][B][H][dk][dv]: states that the second chunk
+  // what the passes leave for one another, of heads padded to 64 or 128
+  float* saved;                      // [chunks - 1][B][H][dv][dk]: states that the second chunk
                                      // and on start from (written by a training forward)
-  float* dsaved;                     // backward: [chunks][B][H][dk][dv], the gradients of
-                                     // the chunks' last states
-  float *u, *dr_rows;                // backward: [N] rows of H dv
+  float* dsaved;                     // [chunks][B][H][dv][dk]: gradients of the chunks' last states
+  uint16_t *u, *dr_rows;             // [chunks][B][H][terms][dv][GD_CHUNK], terms as of gd_kept_terms
   float* parts;                      // backward: [B][H]
   const int32_t *offs, *lens;        // [T + 1], [B], or null: every sequence has T frames
   int64_t N;
   int T, B, H, G, dk, dv;
   float c, eps;
   bool train;                        // forward: keep the states
-  bool keep_end;                     // backward: ds0 is dsT, which is kept in dsaved
 };
+constexpr int gd_padded(int dim) { return dim <= 64 ? 64 : 128; }
+constexpr int gd_kept_terms(bool bf16) { return bf16 ? 2 : 3; }
 hipError_t gated_delta_forward(GatedDelta a, bool bf16, hipStream_t s);
 hipError_t gated_delta_backward(GatedDelta a, bool bf16, hipStream_t s);
 

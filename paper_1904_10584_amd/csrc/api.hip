@@ -704,7 +704,8 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
 }
 
 struct DeltaLayout { int64_t offs, lens, tails, saved, dsaved, u, dr, parts, total; };
-DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int64_t dk, int64_t dv, bool varlen, bool train) {
+DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int32_t dk, int32_t dv, bool bf16, bool varlen,
+                         bool train) {
   DeltaLayout l{};
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -718,11 +719,12 @@ DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int64_t dk, int64_t dv
     l.tails = take(B * 4);
   }
   if (train) {  // (the first chunk starts from s0, the last one's gradient from dsT)
-    const int64_t links = T > am::GD_CHUNK ? (T - 1) / am::GD_CHUNK : 0;
-    l.saved = take(links * B * H * dk * dv * 4);
-    l.dsaved = take((links + 1) * B * H * dk * dv * 4);
-    l.u = take(T * B * H * dv * 4);
-    l.dr = take(T * B * H * dv * 4);
+    const int64_t chunks = T > 0 ? (T - 1) / am::GD_CHUNK + 1 : 0;
+    const int64_t columns = B * H * am::gd_padded(dv);
+    l.saved = take(chunks ? (chunks - 1) * columns * am::gd_padded(dk) * 4 : 0);
+    l.dsaved = take(chunks * columns * am::gd_padded(dk) * 4);
+    l.u = take(chunks * columns * am::GD_CHUNK * am::gd_kept_terms(bf16) * 2);
+    l.dr = take(chunks * columns * am::GD_CHUNK * am::gd_kept_terms(bf16) * 2);
     l.parts = take(B * H * 4);
   }
   l.total = at;
@@ -771,7 +773,7 @@ am_status check_delta(int32_t T, int32_t B, int32_t heads, int32_t key_heads, in
   AM_TRY(check_rows(a.N, heads * dv, dtype, v, ldv, "v"));
   AM_TRY(check_rows(a.N, heads, dtype, r, ldr, "r"));
   AM_TRY(check_rows(a.N, heads, dtype, b, ldb, "b"));
-  l = delta_layout(T, B, heads, dk, dv, lengths != nullptr, train);
+  l = delta_layout(T, B, heads, dk, dv, dtype == AM_BF16, lengths != nullptr, train);
   if (l.total > 0 && (!ws || !aligned(ws, 256) || ws_bytes < l.total))
     return fail(AM_EWORKSPACE, "needs %lld workspace bytes, 256-byte aligned", (long long)l.total);
   a.q = q; a.k = k; a.v = v; a.r = r; a.b = b;
@@ -1609,7 +1611,7 @@ int64_t am_gated_delta_workspace_bytes(int32_t T, int32_t B, int32_t heads, int3
                                        int32_t dv, int32_t dtype, int32_t varlen, int32_t train) {
   if (!delta_sizes(T, B, heads, key_heads, dk, dv) || dk > am::GD_MAX_DIM || dv > am::GD_MAX_DIM) return -1;
   if ((dtype != AM_F32 && dtype != AM_BF16) || (int64_t)T * B >= (1ll << 32) || (int64_t)B * heads >= (1ll << 31)) return -1;
-  return delta_layout(T, B, heads, dk, dv, varlen != 0, train != 0).total;
+  return delta_layout(T, B, heads, dk, dv, dtype == AM_BF16, varlen != 0, train != 0).total;
 }
 
 am_status gated_delta_forward(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv,
@@ -1670,12 +1672,11 @@ am_status gated_delta_backward(int32_t T, int32_t B, int32_t heads, int32_t key_
   a.lddq = lddq; a.lddk = lddk; a.lddv = lddv; a.lddr = lddr; a.lddb = lddb;
   a.dsT = dsT;
   a.ds0 = ds0;
-  a.keep_end = dsT && ds0 == dsT;
   a.dlam = dlam;
   a.saved = at<float>(ws, l.saved);
   a.dsaved = at<float>(ws, l.dsaved);
-  a.u = at<float>(ws, l.u);
-  a.dr_rows = at<float>(ws, l.dr);
+  a.u = at<uint16_t>(ws, l.u);
+  a.dr_rows = at<uint16_t>(ws, l.dr);
   a.parts = at<float>(ws, l.parts);
   hipStream_t s = static_cast<hipStream_t>(stream);
   Timed tm(AM_K_GATED, s, 12.0 * a.N * heads * dk * dv,

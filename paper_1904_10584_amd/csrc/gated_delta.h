@@ -9,11 +9,13 @@
 //   (I + L) U = R,  L_ij = beta_i M_ij (k_i k_j), j < i,
 //   O = diag(g) Q S + P U,  P_ij = M_ij (q_i k_j), j <= i,
 //   S' = g_end S + K^T diag(M_end) U.
-// Every column of S, R, U and O goes its way alone, so a wave keeps its columns of
-// them in registers from one product to the next: what a 16 x 16 product leaves in a
-// lane (column lane % 16, rows 4 (lane / 16) + 0..3) is, as it is, the right operand of
-// the next one.  The left operands (K, Q, their transposes, L, P) are the same for all
-// columns and lie in LDS.  (I + L) U = R is solved block after block of 16 rows with
+// Every column of S, R, U and O goes its way alone, so a wave keeps 16 columns of them in
+// registers from one product to the next: what a 16 x 16 product leaves in a lane
+// (column lane % 16, rows 4 (lane / 16) + 0..3) is, as it is, an operand of the next
+// one.  As its right operand the columns stay with their lanes; as its left one they
+// come out transposed, a frame a lane and four columns side by side, which is how rows
+// leave for memory.  The other operands (K, Q, their transposes, L, P) are the same for
+// all columns and lie in LDS.  (I + L) U = R is solved block after block of 16 rows with
 // the inverses of I + L's diagonal blocks, which come from substitution: frames that
 // repeat a key make the powers of L grow, but not its inverse.
 //
@@ -42,7 +44,6 @@ template <int BYTES> hipError_t allow_lds(const void* kernel, PerDevice& ready) 
 }
 
 constexpr int C = GD_CHUNK, NB = C / 16;  // frames of a chunk, blocks of 16
-constexpr int THREADS = 256, WAVES = 4;
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
@@ -50,7 +51,9 @@ template <typename T> struct Terms;
 template <> struct Terms<bf16_t> { static constexpr int IN = 1, X = 3, OUT = 2; };
 template <> struct Terms<float> { static constexpr int IN = 3, X = 3, OUT = 3; };
 
-template <int N> struct Piece { uint2 t[N]; };  // four elements in N terms
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+template <int N> struct Piece { u32x2_t t[N]; };  // four elements in N terms
 template <int M, int N> __device__ __forceinline__ Piece<M> first(const Piece<N>& p) {
   Piece<M> q;
 #pragma unroll
@@ -73,7 +76,7 @@ template <int N> __device__ __forceinline__ Piece<N> split(f32x4_t v) {
   Piece<N> p;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    p.t[i] = make_uint2(pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]));
+    p.t[i] = u32x2_t{pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3])};
     if (i + 1 < N) {
       v[0] -= __uint_as_float(p.t[i].x << 16);
       v[1] -= __uint_as_float(p.t[i].x & 0xffff0000u);
@@ -84,8 +87,8 @@ template <int N> __device__ __forceinline__ Piece<N> split(f32x4_t v) {
   return p;
 }
 
-__device__ __forceinline__ bf16x8_t join(uint2 a, uint2 b) {
-  return __builtin_bit_cast(bf16x8_t, make_uint4(a.x, a.y, b.x, b.y));
+__device__ __forceinline__ bf16x8_t join(u32x2_t a, u32x2_t b) {
+  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3));
 }
 // acc += A B over 16, or over two blocks of 16, of the inner axis; small terms first.
 // Over 16, an instruction of 32 takes two products of terms.  (Instructions of 16 are
@@ -94,7 +97,7 @@ __device__ __forceinline__ bf16x8_t join(uint2 a, uint2 b) {
 template <int TA, int TB>
 __device__ __forceinline__ void mma(f32x4_t& acc, const Piece<TA>& a, const Piece<TB>& b) {
   constexpr int N = TA > TB ? TA : TB;
-  uint2 wa = make_uint2(0, 0), wb = wa;
+  u32x2_t wa = u32x2_t{0, 0}, wb = wa;
   int held = 0;
 #pragma unroll
   for (int s = N - 1; s >= 0; --s)
@@ -110,7 +113,7 @@ __device__ __forceinline__ void mma(f32x4_t& acc, const Piece<TA>& a, const Piec
           held = 1;
         }
       }
-  if (held) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join(wa, make_uint2(0, 0)), join(wb, make_uint2(0, 0)), acc, 0, 0, 0);
+  if (held) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join(wa, u32x2_t{0, 0}), join(wb, u32x2_t{0, 0}), acc, 0, 0, 0);
 }
 template <int TA, int TB>
 __device__ __forceinline__ void mma(f32x4_t& acc, const Piece<TA>& a0, const Piece<TA>& a1, const Piece<TB>& b0,
@@ -126,67 +129,112 @@ __device__ __forceinline__ void mma(f32x4_t& acc, const Piece<TA>& a0, const Pie
 
 // Rows of any element alignment, in pieces.
 typedef uint32_t u32x4_u __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_u __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f32x4_a __attribute__((ext_vector_type(4), aligned(4)));
-typedef float f32x2_a __attribute__((ext_vector_type(2), aligned(4)));
-typedef uint32_t u32_u __attribute__((aligned(2)));
 
-// A chunk of a head in LDS.  A row of K or Q has its pieces of four columns, of each 32,
-// in the order 0 4 1 5 2 6 3 7: the two that a lane takes for a step of 32 lie together.
-template <typename T, int DKP> struct Staged {
-  static constexpr int TI = Terms<T>::IN, TX = Terms<T>::X;
-  static constexpr int PITCH = DKP * 2 + 16;  // bytes of a row
-  uint8_t k[TI][C * PITCH], q[TI][C * PITCH];
-  float ch[C], cl[C];          // c, and what is left of it behind 24 bits
+// A workgroup of W waves has 16 W columns of v: 64 or 128, as the padded heads have.
+template <int W> constexpr int threads_of = 64 * W;
+constexpr int pitch_of(int columns) { return columns * 2 + 16; }  // bytes of a row in LDS
+
+// A chunk of a head in LDS.  A row has its pieces of four columns, of each 32, in the
+// order 0 4 1 5 2 6 3 7: the two that a lane takes for a step of 32 lie together.
+// Frames past a sequence's end are its last one again, whose row can be read, with
+// beta, rk and rq 0: everything that they touch is multiplied by one of those.
+struct Gates {
+  float ch[C], cl[C];          // c log2(e), and what is left of it behind 24 bits
   float g[C], end[C], beta[C], rk[C], rq[C];  // e^c, e^(c_end - c), gates, 1 / lengths
   float bgk[C], gq[C], gk[C];  // beta g rk, g rq, end rk
+  int32_t row[2][C];           // the frames' rows, of this chunk and of the next one
 };
-// PT: terms of P.
-template <typename T, int DKP, int PT> struct Chunk : Staged<T, DKP> {
-  static constexpr int TX = Terms<T>::X;
+template <int N, int COLS> struct Matrix { uint8_t at[N][C * pitch_of(COLS)]; };  // in N terms
+// PT: terms of P; R: matrices like v (v, and in the backward pass dO).
+// (Inputs in fp32 would not leave room for those: they stay in memory.)
+template <typename T, int DKP, int W, int PT, int R> struct Chunk {
+  static constexpr int TI = Terms<T>::IN, TX = Terms<T>::X;
+  Matrix<TI, DKP> k, q;
+  Matrix<1, 16 * W> v[TI == 1 ? R : 0];
   uint8_t l[6][TX][512], d[NB][TX][512], p[10][PT][512];  // blocks of 16 x 16: -L below the diagonal,
                                                           // (I + L)^-1 on it, P
-  float n[NB][260];            // L on the diagonal, transposed
+  float n[NB][16][20];         // L on the diagonal, transposed
+  Gates s;
 };
 
-// Eight columns of a row, zeros past `cols`.
-__device__ __forceinline__ void load8(const bf16_t* p, int left, float (&v)[8]) {
-  if (left >= 8) {
+// Eight columns of a row as they lie in memory.
+template <typename T> struct Eight;
+template <> struct Eight<bf16_t> {
+  uint32_t w[4];
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+  __device__ __forceinline__ Piece<1> piece(int half) const { return {{u32x2_t{w[2 * half], w[2 * half + 1]}}}; }
+  __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
+  __device__ __forceinline__ void load(const bf16_t* p) {
     const u32x4_u u = *reinterpret_cast<const u32x4_u*>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(u[i] << 16);
-      v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-  } else {
+    for (int i = 0; i < 4; ++i) w[i] = u[i];
+  }
+  __device__ __forceinline__ void load(const bf16_t* p, int left) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_to_f32(p[i]) : 0.f;
+    for (int i = 0; i < 4; ++i)
+      w[i] = (2 * i < left ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+  }
+};
+template <> struct Eight<float> {
+  f32x4_t v[2];
+  __device__ __forceinline__ float at(int i) const { return v[i >> 2][i & 3]; }
+  __device__ __forceinline__ Piece<3> piece(int half) const { return split<3>(v[half]); }
+  __device__ __forceinline__ void zero() { v[0] = v[1] = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ void load(const float* p) {
+    v[0] = *reinterpret_cast<const f32x4_a*>(p);
+    v[1] = *reinterpret_cast<const f32x4_a*>(p + 4);
+  }
+  __device__ __forceinline__ void load(const float* p, int left) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = i < left ? p[i] : 0.f;
+  }
+};
+// What terms stand for.
+template <int N> __device__ __forceinline__ f32x4_t values(const Piece<N>& p) {
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = N - 1; e >= 0; --e)
+    v += f32x4_t{__uint_as_float(p.t[e].x << 16), __uint_as_float(p.t[e].x & 0xffff0000u),
+                 __uint_as_float(p.t[e].y << 16), __uint_as_float(p.t[e].y & 0xffff0000u)};
+  return v;
+}
+// Four columns of a row to memory, `left` of them where that is less.
+__device__ __forceinline__ void put4(bf16_t* p, int left, f32x4_t v) {
+  const uint32_t lo = pair_bf16(v[0], v[1]), hi = pair_bf16(v[2], v[3]);
+  if (left >= 4) {
+    *reinterpret_cast<u32x2_u*>(p) = u32x2_u{lo, hi};
+  } else {
+    if (left > 0) p[0] = (uint16_t)lo;
+    if (left > 1) p[1] = (uint16_t)(lo >> 16);
+    if (left > 2) p[2] = (uint16_t)hi;
   }
 }
-__device__ __forceinline__ void load8(const float* p, int left, float (&v)[8]) {
-  if (left >= 8) {
-    const f32x4_a a = *reinterpret_cast<const f32x4_a*>(p), b = *reinterpret_cast<const f32x4_a*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+__device__ __forceinline__ void put4(float* p, int left, f32x4_t v) {
+  if (left >= 4) {
+    *reinterpret_cast<f32x4_a*>(p) = v;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
+    for (int j = 0; j < 3; ++j)
+      if (j < left) p[j] = v[j];
   }
 }
 
-// The sequence and head of a workgroup, and where its frames' rows are.
+// The sequence and head of a workgroup.
 struct Head {
   int b, h, kh, len;  // sequence, head, key head, frames
-  const int32_t* offs;
-  int B;
   __device__ Head(const GatedDelta& a, int bh) {
     b = bh / a.H;
     h = bh % a.H;
     kh = h / (a.H / a.G);
     len = a.lens ? a.lens[b] : a.T;
-    offs = a.offs;
-    B = a.B;
   }
-  __device__ int64_t row(int t) const { return offs ? (int64_t)offs[t] + b : (int64_t)t * B + b; }
+  // the row of frame t, or of the last one
+  __device__ __forceinline__ int row(const GatedDelta& a, int t) const {
+    t = min(t, len - 1);
+    return (a.offs ? a.offs[t] : t * a.B) + b;
+  }
 };
 
 // The sum over each group of 8 or 16 lanes, in every one of them.
@@ -197,117 +245,191 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
   if constexpr (LANES == 16) v += lanes_moved<0x140>(v);
   return v;
 }
+// The sums of a wave's lanes up to each of them, in 64 bits: lane moves by 1, 2, 4 and 8
+// within rows of 16, then the ends of rows (of two rows) to those behind them.
+template <int CTRL, int ROWS> __device__ __forceinline__ double lanes_before(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double sums_before(double c) {
+  c += lanes_before<0x111, 0xf>(c);
+  c += lanes_before<0x112, 0xf>(c);
+  c += lanes_before<0x114, 0xf>(c);
+  c += lanes_before<0x118, 0xf>(c);
+  c += lanes_before<0x142, 0xa>(c);
+  c += lanes_before<0x143, 0xc>(c);
+  return c;
+}
 
-// K, Q and the gates of a chunk on their way from memory.
-template <typename T, int DKP> struct Fetched {
-  static constexpr int PER_ROW = DKP / 8, PIECES = C * PER_ROW / THREADS;
-  float k[PIECES][8], q[PIECES][8];
-  float r, b;
-  __device__ __forceinline__ void from(const GatedDelta& a, const Head& hd, int t0) {
+// Rows of COLS columns (`dim` of them there) of a chunk on their way from memory to LDS.
+template <typename T, int COLS, int W> struct Rows {
+  static constexpr int PER_ROW = COLS / 8, PIECES = C * PER_ROW / threads_of<W>;
+  static_assert(PIECES >= 1, "every thread has a piece");
+  Eight<T> v[PIECES];
+  __device__ __forceinline__ void from(const void* m, int64_t ld, int head, int dim, const int32_t (&rows)[C]) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int at = threadIdx.x + i * THREADS, t = t0 + at / PER_ROW, u = at % PER_ROW, left = a.dk - 8 * u;
-      if (t < hd.len && left > 0) {
-        const int64_t row = hd.row(t), col = (int64_t)hd.kh * a.dk + 8 * u;
-        load8(static_cast<const T*>(a.k) + row * a.ldk + col, left, k[i]);
-        load8(static_cast<const T*>(a.q) + row * a.ldq + col, left, q[i]);
-      } else {
+      const int at = threadIdx.x + i * threads_of<W>, u = at % PER_ROW, left = dim - 8 * u;
+      const T* p = static_cast<const T*>(m) + rows[at / PER_ROW] * ld + (int64_t)head * dim + 8 * u;
+      if (dim == COLS || left >= 8) v[i].load(p);
+      else if (left > 0) v[i].load(p, left);
+      else v[i].zero();
+    }
+  }
+  __device__ __forceinline__ void store(Matrix<Terms<T>::IN, COLS>& m) const {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) k[i][j] = q[i][j] = 0.f;
+    for (int i = 0; i < PIECES; ++i) {
+      const int at = threadIdx.x + i * threads_of<W>, u = at % PER_ROW;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int p = 2 * (u & 3) + half, slot = (p & 3) * 2 + (p >> 2);  // of the eight pieces of 32 columns
+        const Piece<Terms<T>::IN> w = v[i].piece(half);
+#pragma unroll
+        for (int e = 0; e < Terms<T>::IN; ++e)
+          *reinterpret_cast<u32x2_t*>(m.at[e] + at / PER_ROW * pitch_of(COLS) + (u >> 2) * 64 + slot * 8) = w.t[e];
       }
     }
-    if (threadIdx.x < C) {
-      const int t = t0 + threadIdx.x;
-      if (t < hd.len) {
-        const int64_t row = hd.row(t);
-        r = to_f32(static_cast<const T*>(a.r)[row * a.ldr + hd.h]);
-        b = to_f32(static_cast<const T*>(a.b)[row * a.ldb + hd.h]);
-      }
+  }
+  // 1 / sqrt(sum of squares + eps) of each row; 0 from row `left` on
+  __device__ __forceinline__ void lengths(float (&out)[C], float eps, int left) const {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int at = threadIdx.x + i * threads_of<W>, row = at / PER_ROW;
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s = fmaf(v[i].at(j), v[i].at(j), s);
+      s = lanes_sum<PER_ROW>(s);
+      if (at % PER_ROW == 0) out[row] = row < left ? rsqrtf(s + eps) : 0.f;
     }
   }
 };
-
-// Writes a chunk's K, Q, lengths and gates.  (Ends without a barrier.)
-template <typename T, int DKP>
-__device__ __forceinline__ void stage(Staged<T, DKP>& s, const Fetched<T, DKP>& f, float eps, float rate, int left) {
-  typedef Fetched<T, DKP> F;
-  constexpr int TI = Terms<T>::IN;
-#pragma unroll
-  for (int i = 0; i < F::PIECES; ++i) {
-    const int at = threadIdx.x + i * THREADS, row = at / F::PER_ROW, u = at % F::PER_ROW;
-    float sk = 0.f, sq = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sk = fmaf(f.k[i][j], f.k[i][j], sk), sq = fmaf(f.q[i][j], f.q[i][j], sq);
-    sk = lanes_sum<F::PER_ROW>(sk);
-    sq = lanes_sum<F::PER_ROW>(sq);
-    if (u == 0) {
-      s.rk[row] = 1.f / sqrtf(sk + eps);
-      s.rq[row] = 1.f / sqrtf(sq + eps);
-    }
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int p = 2 * (u & 3) + half, slot = (p & 3) * 2 + (p >> 2);  // of the eight pieces of 32 columns
-      const int to = row * Staged<T, DKP>::PITCH + (u >> 2) * 64 + slot * 8;
-      const f32x4_t kv = {f.k[i][4 * half], f.k[i][4 * half + 1], f.k[i][4 * half + 2], f.k[i][4 * half + 3]};
-      const f32x4_t qv = {f.q[i][4 * half], f.q[i][4 * half + 1], f.q[i][4 * half + 2], f.q[i][4 * half + 3]};
-      const Piece<TI> kp = split<TI>(kv), qp = split<TI>(qv);
-#pragma unroll
-      for (int e = 0; e < TI; ++e) {
-        *reinterpret_cast<uint2*>(s.k[e] + to) = kp.t[e];
-        *reinterpret_cast<uint2*>(s.q[e] + to) = qp.t[e];
-      }
-    }
+// Rows of a matrix like v, 16 W columns of it: in LDS if they are bf16, which arrive
+// while the chunk before is in hand; in memory if they are fp32.
+template <typename T, int W> struct Values;
+template <int W> struct Values<bf16_t, W> {
+  Rows<bf16_t, 16 * W, W> v;
+  const Matrix<1, 16 * W>* m;
+  __device__ __forceinline__ void from(const void* p, int64_t ld, const Head& hd, int dv, const int32_t (&rows)[C]) {
+    v.from(p, ld, hd.h, dv, rows);
   }
-  if (threadIdx.x < C) {  // one wave: the decays' sums in 64 bits
-    const int t = threadIdx.x;
-    const bool live = t < left;
-    double c = live ? (double)(-rate * sigm(f.r)) : 0.0;
+  __device__ __forceinline__ void store(Matrix<1, 16 * W>* to, const int32_t (&)[C]) {
+    v.store(*to);
+    m = to;
+  }
+  // columns 16 t + lane % 16 over frames of block I; row 16 I + lane % 16, columns 16 t + 4 (lane / 16) and on
+  __device__ __forceinline__ Piece<1> column(int t, int I, int lane) const;
+  __device__ __forceinline__ f32x4_t column_values(int t, int I, int lane) const;
+  __device__ __forceinline__ f32x4_t row_values(int I, int t, int lane) const;
+};
+template <int W> struct Values<float, W> {
+  const float* p;
+  int64_t ld;
+  int dv;
+  const int32_t* rows;
+  __device__ __forceinline__ void from(const void* m, int64_t stride, const Head& hd, int cols, const int32_t (&)[C]) {
+    p = static_cast<const float*>(m) + (int64_t)hd.h * cols;
+    ld = stride;
+    dv = cols;
+  }
+  __device__ __forceinline__ void store(Matrix<1, 16 * W>*, const int32_t (&at)[C]) { rows = at; }
+  __device__ __forceinline__ f32x4_t column_values(int t, int I, int lane) const {
+    const int col = 16 * t + (lane & 15);
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+    if (col < dv)
 #pragma unroll
-    for (int o = 1; o < C; o <<= 1) {
-      const double below = __shfl_up(c, o, 64);
-      if (t >= o) c += below;
-    }
+      for (int r = 0; r < 4; ++r) v[r] = p[rows[16 * I + 4 * (lane >> 4) + r] * ld + col];
+    return v;
+  }
+  __device__ __forceinline__ Piece<3> column(int t, int I, int lane) const { return split<3>(column_values(t, I, lane)); }
+  __device__ __forceinline__ f32x4_t row_values(int I, int t, int lane) const {
+    const int col = 16 * t + 4 * (lane >> 4);
+    const float* const at = p + rows[16 * I + (lane & 15)] * ld + col;
+    if (col + 4 <= dv) return *reinterpret_cast<const f32x4_a*>(at);
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (col + j < dv) v[j] = at[j];
+    return v;
+  }
+};
+// The gates of a chunk and the rows of another one; the last wave's.
+template <typename T, int W> struct GateRows {
+  T r, b;
+  int next;
+  __device__ __forceinline__ static bool mine() { return threadIdx.x >= threads_of<W> - C; }
+  __device__ __forceinline__ void from(const GatedDelta& a, const Head& hd, const int32_t (&rows)[C], int next0) {
+    if (!mine()) return;
+    const int t = threadIdx.x & 63;
+    const int64_t row = rows[t];
+    r = static_cast<const T*>(a.r)[row * a.ldr + hd.h];
+    b = static_cast<const T*>(a.b)[row * a.ldb + hd.h];
+    next = hd.row(a, next0 + t);
+  }
+  // `left`: frames that the sequence has from here on
+  __device__ __forceinline__ void store(Gates& s, float rate, int left, int turn) const {
+    if (!mine()) return;
+    const int t = threadIdx.x & 63;
+    const bool live = t < left;
+    const double c = sums_before(live ? (double)(-rate * sigm(to_f32(r))) * 1.4426950408889634 : 0.0);
     const double last = __shfl(c, C - 1, 64);
     const float hi = (float)c;
     s.ch[t] = hi;
     s.cl[t] = (float)(c - (double)hi);
-    s.g[t] = expf(hi);
-    s.end[t] = expf((float)(last - c));
-    s.beta[t] = live ? sigm(f.b) : 0.f;
+    s.g[t] = __builtin_amdgcn_exp2f(hi);
+    s.end[t] = __builtin_amdgcn_exp2f((float)(last - c));
+    s.beta[t] = live ? sigm(to_f32(b)) : 0.f;
+    s.row[turn ^ 1][t] = next;
   }
-}
+};
 
-// Left operands: rows 16 I + lane % 16 of K or Q over columns 32 t and on ...
-template <typename T, int DKP>
-__device__ __forceinline__ void rows_of(const uint8_t (&m)[Terms<T>::IN][C * Staged<T, DKP>::PITCH], int I, int t, int lane,
-                                        Piece<Terms<T>::IN>& a0, Piece<Terms<T>::IN>& a1) {
+// Operands from LDS: rows 16 I + lane % 16 over columns 32 t and on ...
+template <int N, int COLS>
+__device__ __forceinline__ void rows_of(const Matrix<N, COLS>& m, int I, int t, int lane, Piece<N>& a0, Piece<N>& a1) {
 #pragma unroll
-  for (int e = 0; e < Terms<T>::IN; ++e) {
-    const uint4 u = *reinterpret_cast<const uint4*>(m[e] + (16 * I + (lane & 15)) * Staged<T, DKP>::PITCH + t * 64 + (lane >> 4) * 16);
-    a0.t[e] = make_uint2(u.x, u.y);
-    a1.t[e] = make_uint2(u.z, u.w);
+  for (int e = 0; e < N; ++e) {
+    const u32x4_t u = *reinterpret_cast<const u32x4_t*>(m.at[e] + (16 * I + (lane & 15)) * pitch_of(COLS) + t * 64 + (lane >> 4) * 16);
+    a0.t[e] = u.xy;
+    a1.t[e] = u.zw;
   }
 }
-// ... and of their transposes: columns 16 t + lane % 16 over frames of block I.  A
-// group of 16 lanes reads 4 rows of 16 columns, and each lane gets a column's four.
-__device__ __forceinline__ uint2 turned(const uint8_t* p) {
-  typedef __attribute__((address_space(3))) s16x4_t* At;
-  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p)));
+// (four of them: columns 16 t + 4 (lane / 16) and on)
+template <int N, int COLS> __device__ __forceinline__ Piece<N> row4_of(const Matrix<N, COLS>& m, int I, int t, int lane) {
+  Piece<N> a;
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    a.t[e] = *reinterpret_cast<const u32x2_t*>(m.at[e] + (16 * I + (lane & 15)) * pitch_of(COLS) + (t >> 1) * 64 +
+                                             ((lane >> 4) * 2 + (t & 1)) * 8);
+  return a;
 }
-template <typename T, int DKP>
-__device__ __forceinline__ Piece<Terms<T>::IN> columns_of(const uint8_t (&m)[Terms<T>::IN][C * Staged<T, DKP>::PITCH], int t, int I,
-                                                          int lane) {
-  Piece<Terms<T>::IN> a;
+// ... and columns 16 t + lane % 16 over frames of block I.  A group of 16 lanes reads 4
+// rows of 16 columns, and each lane gets a column's four.
+__device__ __forceinline__ u32x2_t turned(const uint8_t* p) {
+  typedef __attribute__((address_space(3))) s16x4_t* At;
+  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p)));
+}
+template <int N, int COLS> __device__ __forceinline__ Piece<N> columns_of(const Matrix<N, COLS>& m, int t, int I, int lane) {
+  Piece<N> a;
   const int row = 16 * I + (lane >> 4) * 4 + ((lane & 15) >> 2), slot = (lane & 3) * 2 + (t & 1);
 #pragma unroll
-  for (int e = 0; e < Terms<T>::IN; ++e) a.t[e] = turned(m[e] + row * Staged<T, DKP>::PITCH + (t >> 1) * 64 + slot * 8);
+  for (int e = 0; e < N; ++e) a.t[e] = turned(m.at[e] + row * pitch_of(COLS) + (t >> 1) * 64 + slot * 8);
   return a;
+}
+template <int W> __device__ __forceinline__ Piece<1> Values<bf16_t, W>::column(int t, int I, int lane) const {
+  return columns_of(*m, t, I, lane);
+}
+template <int W> __device__ __forceinline__ f32x4_t Values<bf16_t, W>::column_values(int t, int I, int lane) const {
+  return values(columns_of(*m, t, I, lane));
+}
+template <int W> __device__ __forceinline__ f32x4_t Values<bf16_t, W>::row_values(int I, int t, int lane) const {
+  return values(row4_of(*m, I, t, lane));
 }
 // A block of 16 x 16, and its transpose.
 template <int TX> __device__ __forceinline__ Piece<TX> block_of(const uint8_t (&m)[TX][512], int lane) {
   Piece<TX> a;
 #pragma unroll
-  for (int e = 0; e < TX; ++e) a.t[e] = *reinterpret_cast<const uint2*>(m[e] + (lane & 15) * 32 + (lane >> 4) * 8);
+  for (int e = 0; e < TX; ++e) a.t[e] = *reinterpret_cast<const u32x2_t*>(m[e] + (lane & 15) * 32 + (lane >> 4) * 8);
   return a;
 }
 template <int TX> __device__ __forceinline__ Piece<TX> block_turned(const uint8_t (&m)[TX][512], int lane) {
@@ -321,76 +443,85 @@ __device__ __forceinline__ f32x4_t rows4(const float (&v)[C], int I, int lane) {
 }
 constexpr int below(int I, int J) { return I * (I - 1) / 2 + J; }   // block of l
 constexpr int lower(int I, int J) { return I * (I + 1) / 2 + J; }   // block of p
+__device__ __forceinline__ int block_row(int at) { return at >= 6 ? 3 : at >= 3 ? 2 : at >= 1 ? 1 : 0; }
+
+__device__ __forceinline__ void combine(Gates& s, int t) {
+  s.bgk[t] = s.beta[t] * s.g[t] * s.rk[t];
+  s.gq[t] = s.g[t] * s.rq[t];
+  s.gk[t] = s.end[t] * s.rk[t];
+}
+
+// x_i -= n_i of lane J, x_J, for every i below J; and so on from column J + 1.
+template <int J> __device__ __forceinline__ void substitute(float (&x)[16], const float (&n)[16]) {
+  if constexpr (J < 15) {
+#pragma unroll
+    for (int i = J + 1; i < 16; ++i) x[i] = fmaf(-lanes_moved<0x150 + J>(n[i]), x[J], x[i]);
+    substitute<J + 1>(x, n);
+  }
+}
 
 // L, P and the inverses of I + L's diagonal blocks from a staged chunk (behind a
 // barrier; ends with one).
-template <typename T, int DKP, int PT> __device__ __forceinline__ void triangles(Chunk<T, DKP, PT>& s) {
+template <typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ void triangles(Chunk<T, DKP, W, PT, R>& c) {
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
-  if (wave == 1) {
-    const int t = lane;
-    s.bgk[t] = s.beta[t] * s.g[t] * s.rk[t];
-    s.gq[t] = s.g[t] * s.rq[t];
-    s.gk[t] = s.end[t] * s.rk[t];
-  }
+  Gates& s = c.s;
+  if (wave == W - 1) combine(s, lane);
 #pragma unroll
-  for (int m = 0; m < 5; ++m) {  // ten tiles of K K^T, ten of Q K^T
-    const int job = wave + WAVES * m, at = job < 10 ? job : job - 10;
-    const int I = at >= 6 ? 3 : at >= 3 ? 2 : at >= 1 ? 1 : 0, J = at - lower(I, 0);
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  for (int at0 = 0; at0 < 10; at0 += W) {  // ten tiles of K K^T and of Q K^T
+    const int at = at0 + wave;
+    if (at >= 10) break;
+    const int I = block_row(at), J = at - lower(I, 0);
+    f32x4_t kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
 #pragma unroll
     for (int t = 0; t < DKP / 32; ++t) {
       Piece<TI> a0, a1, b0, b1;
-      rows_of<T, DKP>(s.k, J, t, lane, a0, a1);
-      if (job < 10) rows_of<T, DKP>(s.k, I, t, lane, b0, b1);
-      else rows_of<T, DKP>(s.q, I, t, lane, b0, b1);
-      mma<TI, TI>(acc, a0, a1, b0, b1);
+      rows_of(c.k, J, t, lane, a0, a1);
+      rows_of(c.k, I, t, lane, b0, b1);
+      mma<TI, TI>(kk, a0, a1, b0, b1);
+      rows_of(c.q, I, t, lane, b0, b1);
+      mma<TI, TI>(qk, a0, a1, b0, b1);
     }
     // a lane has row i and columns j, j + 1, ... of the tile
     const int i = 16 * I + l16;
     const f32x4_t ch = rows4(s.ch, J, lane), cl = rows4(s.cl, J, lane), rk = rows4(s.rk, J, lane);
-    const float hi = s.ch[i], lo = s.cl[i], f = job < 10 ? s.beta[i] * s.rk[i] : s.rq[i];
-    f32x4_t v;
+    const float hi = s.ch[i], lo = s.cl[i], fk = s.beta[i] * s.rk[i], fq = s.rq[i];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int j = 16 * J + 4 * g4 + r;
-      const bool on = job < 10 ? j < i : j <= i;
-      v[r] = on ? f * rk[r] * acc[r] * expf((hi - ch[r]) + (lo - cl[r])) : 0.f;
+      const float m = rk[r] * __builtin_amdgcn_exp2f((hi - ch[r]) + (lo - cl[r]));
+      kk[r] = j < i ? fk * kk[r] * m : 0.f;
+      qk[r] = j <= i ? fq * qk[r] * m : 0.f;
     }
-    if (job >= 10) {
-      const Piece<PT> p = split<PT>(v);
+    const Piece<PT> p = split<PT>(qk);
 #pragma unroll
-      for (int e = 0; e < PT; ++e) *reinterpret_cast<uint2*>(s.p[at][e] + l16 * 32 + g4 * 8) = p.t[e];
-    } else if (I == J) {
+    for (int e = 0; e < PT; ++e) *reinterpret_cast<u32x2_t*>(c.p[at][e] + l16 * 32 + g4 * 8) = p.t[e];
+    if (I == J) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s.n[I][(4 * g4 + r) * 16 + l16] = v[r];
+      for (int r = 0; r < 4; ++r) c.n[I][4 * g4 + r][l16] = kk[r];
     } else {
-      const Piece<TX> p = split<TX>(-v);
+      const Piece<TX> w = split<TX>(-kk);
 #pragma unroll
-      for (int e = 0; e < TX; ++e) *reinterpret_cast<uint2*>(s.l[at - I][e] + l16 * 32 + g4 * 8) = p.t[e];
+      for (int e = 0; e < TX; ++e) *reinterpret_cast<u32x2_t*>(c.l[at - I][e] + l16 * 32 + g4 * 8) = w.t[e];
     }
   }
   __syncthreads();
   if (wave == 0) {  // 16 lanes a block, a column each: substitution
-    float x[16];
+    // (lane j of the 16 has column j of L, and gives its elements to the others)
+    float x[16], n[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i == l16 ? 1.f : 0.f;
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>(&c.n[g4][l16][4 * i4]);
 #pragma unroll
-    for (int j = 0; j < 15; ++j) {
-#pragma unroll
-      for (int i4 = (j + 1) / 4; i4 < 4; ++i4) {
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(&s.n[g4][j * 16 + 4 * i4]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (4 * i4 + r > j) x[4 * i4 + r] = fmaf(-v[r], x[j], x[4 * i4 + r]);
-      }
+      for (int r = 0; r < 4; ++r) n[4 * i4 + r] = v[r], x[4 * i4 + r] = 4 * i4 + r == l16 ? 1.f : 0.f;
     }
+    substitute<0>(x, n);
 #pragma unroll
     for (int i4 = 0; i4 < 4; ++i4) {
       const Piece<TX> p = split<TX>(f32x4_t{x[4 * i4], x[4 * i4 + 1], x[4 * i4 + 2], x[4 * i4 + 3]});
 #pragma unroll
       for (int e = 0; e < TX; ++e) {
-        uint16_t* to = reinterpret_cast<uint16_t*>(s.d[g4][e]) + 4 * i4 * 16 + l16;
+        uint16_t* to = reinterpret_cast<uint16_t*>(c.d[g4][e]) + 4 * i4 * 16 + l16;
         to[0] = (uint16_t)p.t[e].x;
         to[16] = (uint16_t)(p.t[e].x >> 16);
         to[32] = (uint16_t)p.t[e].y;
@@ -401,148 +532,61 @@ template <typename T, int DKP, int PT> __device__ __forceinline__ void triangles
   __syncthreads();
 }
 
-// U from R, in place, and U's terms: (I + L) U = R, block after block.
-template <typename T, int DKP, int PT, int NT>
-__device__ __forceinline__ void solve(const Chunk<T, DKP, PT>& s, int lane, f32x4_t (&u)[NB][NT], Piece<Terms<T>::X> (&up)[NB][NT]) {
-  constexpr int TX = Terms<T>::X;
+// U's terms from R, block after block: (I + L) U = R.  R is left where U is made from:
+// R_I - sum L_IJ U_J, whose terms stay in r.
+template <typename Ch, int TX>
+__device__ __forceinline__ void solve(const Ch& c, int lane, f32x4_t (&u)[NB], Piece<TX> (&r)[NB], Piece<TX> (&up)[NB]) {
 #pragma unroll
   for (int I = 0; I < NB; ++I) {
-    if (I >= 2) {
-      const Piece<TX> a0 = block_of(s.l[below(I, 0)], lane), a1 = block_of(s.l[below(I, 1)], lane);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) mma<TX, TX>(u[I][n], a0, a1, up[0][n], up[1][n]);
-    }
-    if (I == 1 || I == 3) {
-      const Piece<TX> a = block_of(s.l[below(I, I - 1)], lane);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) mma<TX, TX>(u[I][n], a, up[I - 1][n]);
-    }
-    const Piece<TX> d = block_of(s.d[I], lane);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const Piece<TX> r = split<TX>(u[I][n]);
-      u[I][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      mma<TX, TX>(u[I][n], d, r);
-      up[I][n] = split<TX>(u[I][n]);
-    }
+    if (I >= 2) mma<TX, TX>(u[I], block_of(c.l[below(I, 0)], lane), block_of(c.l[below(I, 1)], lane), up[0], up[1]);
+    if (I == 1 || I == 3) mma<TX, TX>(u[I], block_of(c.l[below(I, I - 1)], lane), up[I - 1]);
+    r[I] = split<TX>(u[I]);
+    u[I] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    mma<TX, TX>(u[I], block_of(c.d[I], lane), r[I]);
+    up[I] = split<TX>(u[I]);
   }
 }
 
-// The columns of v (or of a matrix like it) that a wave has: NT a lane, side by side.
-template <int NT> struct Columns {
-  int first;  // this lane's first column
-  int count;  // how many of its columns there are
-  __device__ Columns(int dv) {
-    first = NT * ((threadIdx.x >> 6) * 16 + (threadIdx.x & 15));
-    count = dv - first < 0 ? 0 : dv - first < NT ? dv - first : NT;
-  }
-  __device__ __forceinline__ void load(const bf16_t* p, float (&v)[NT]) const {
-    if (NT == 2 && count == 2) {
-      const uint32_t u = *reinterpret_cast<const u32_u*>(p);
-      v[0] = __uint_as_float(u << 16);
-      v[NT - 1] = __uint_as_float(u & 0xffff0000u);
-    } else {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) v[n] = n < count ? bf16_to_f32(p[n]) : 0.f;
-    }
-  }
-  __device__ __forceinline__ void load(const float* p, float (&v)[NT]) const {
-    if (NT == 2 && count == 2) {
-      const f32x2_a u = *reinterpret_cast<const f32x2_a*>(p);
-      v[0] = u[0];
-      v[NT - 1] = u[1];
-    } else {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) v[n] = n < count ? p[n] : 0.f;
-    }
-  }
-  __device__ __forceinline__ void store(bf16_t* p, const float (&v)[NT]) const {
-    if (NT == 2 && count == 2) {
-      *reinterpret_cast<u32_u*>(p) = pair_bf16(v[0], v[NT - 1]);
-    } else {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (n < count) p[n] = f32_to_bf16(v[n]);
-    }
-  }
-  __device__ __forceinline__ void store(float* p, const float (&v)[NT]) const {
-    if (NT == 2 && count == 2) {
-      *reinterpret_cast<f32x2_a*>(p) = f32x2_a{v[0], v[NT - 1]};
-    } else {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (n < count) p[n] = v[n];
-    }
-  }
-};
-
-// A state's columns from memory [dk][dv] (null: zero), and to it.
-template <int DKP, int NT>
-__device__ __forceinline__ void load_state(const float* m, const GatedDelta& a, const Columns<NT>& cols, int lane,
-                                           f32x4_t (&S)[DKP / 16][NT]) {
+// A state's 16 columns of a wave: from memory [dk][dv] (null: zero), and to it ...
+template <int DKP>
+__device__ __forceinline__ void load_state(const float* m, const GatedDelta& a, int col, int lane, f32x4_t (&S)[DKP / 16]) {
 #pragma unroll
   for (int t = 0; t < DKP / 16; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = 16 * t + 4 * (lane >> 4) + r;
-      float v[NT];
-      if (m && row < a.dk) {
-        cols.load(m + (int64_t)row * a.dv + cols.first, v);
-      } else {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) v[n] = 0.f;
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) S[t][n][r] = v[n];
+      S[t][r] = m && row < a.dk && col < a.dv ? m[row * a.dv + col] : 0.f;
     }
 }
-template <int DKP, int NT>
-__device__ __forceinline__ void store_state(float* m, const GatedDelta& a, const Columns<NT>& cols, int lane,
-                                            const f32x4_t (&S)[DKP / 16][NT]) {
+template <int DKP>
+__device__ __forceinline__ void store_state(float* m, const GatedDelta& a, int col, int lane, const f32x4_t (&S)[DKP / 16]) {
 #pragma unroll
   for (int t = 0; t < DKP / 16; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = 16 * t + 4 * (lane >> 4) + r;
-      float v[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) v[n] = S[t][n][r];
-      if (row < a.dk) cols.store(m + (int64_t)row * a.dv + cols.first, v);
+      if (row < a.dk && col < a.dv) m[row * a.dv + col] = S[t][r];
     }
 }
-// Rows of v, frames t0 and on: this lane's of each block of 16, zeros past the end.
-template <typename T, int NT>
-__device__ __forceinline__ void load_rows(const void* m, int64_t ld, const GatedDelta& a, const Head& hd, int t0,
-                                          const Columns<NT>& cols, int lane, f32x4_t (&v)[NB][NT]) {
+// ... and where the passes keep it, a padded column after another.
+template <int DKP> __device__ __forceinline__ void load_kept(const float* m, int col, int lane, f32x4_t (&S)[DKP / 16]) {
 #pragma unroll
-  for (int I = 0; I < NB; ++I)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = t0 + 16 * I + 4 * (lane >> 4) + r;
-      float x[NT];
-      if (t < hd.len) {
-        cols.load(static_cast<const T*>(m) + hd.row(t) * ld + (int64_t)hd.h * a.dv + cols.first, x);
-      } else {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) x[n] = 0.f;
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) v[I][n][r] = x[n];
-    }
+  for (int t = 0; t < DKP / 16; ++t) S[t] = *reinterpret_cast<const f32x4_t*>(m + col * DKP + 16 * t + 4 * (lane >> 4));
 }
-template <typename T, int NT>
-__device__ __forceinline__ void store_rows(void* m, int64_t ld, const GatedDelta& a, const Head& hd, int t0,
-                                           const Columns<NT>& cols, int lane, const f32x4_t (&v)[NB][NT]) {
+template <int DKP> __device__ __forceinline__ void store_kept(float* m, int col, int lane, const f32x4_t (&S)[DKP / 16]) {
 #pragma unroll
-  for (int I = 0; I < NB; ++I)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = t0 + 16 * I + 4 * (lane >> 4) + r;
-      float x[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) x[n] = v[I][n][r];
-      if (t < hd.len) cols.store(static_cast<T*>(m) + hd.row(t) * ld + (int64_t)hd.h * a.dv + cols.first, x);
-    }
+  for (int t = 0; t < DKP / 16; ++t) *reinterpret_cast<f32x4_t*>(m + col * DKP + 16 * t + 4 * (lane >> 4)) = S[t];
+}
+// Where chunk n of a head keeps what: the state that it starts from (n >= 1) ...
+template <int DKP, int W> __device__ __forceinline__ float* kept_before(const GatedDelta& a, int n, int64_t bh) {
+  return a.saved + ((int64_t)(n - 1) * a.B * a.H + bh) * (DKP * 16 * W);
+}
+// ... the gradient of the one that it ends in, and columns of U and dR, 64 frames each.
+template <int DKP, int W> __device__ __forceinline__ float* kept_after(const GatedDelta& a, int n, int64_t bh) {
+  return a.dsaved + ((int64_t)n * a.B * a.H + bh) * (DKP * 16 * W);
+}
+template <int N, int W> __device__ __forceinline__ uint16_t* kept_columns(uint16_t* m, const GatedDelta& a, int n, int64_t bh) {
+  return m + ((int64_t)n * a.B * a.H + bh) * (N * 16 * W * C);
 }
 
 }  // namespace gd

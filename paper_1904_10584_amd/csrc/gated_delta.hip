@@ -8,96 +8,95 @@ namespace {
 
 using namespace gd;
 
-template <typename T, int DKP, int NT>
-__global__ __launch_bounds__(THREADS) void gd_forward_kernel(GatedDelta a) {
+constexpr int THREADS = 256, WAVES = 4;  // of a frame's kernel
+
+template <typename T, int DKP, int W>
+__global__ __launch_bounds__(threads_of<W>, 2) void gd_forward_kernel(GatedDelta a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT, KT = DKP / 16;
-  Chunk<T, DKP, TO>& s = *reinterpret_cast<Chunk<T, DKP, TO>*>(lds);
-  const int lane = threadIdx.x & 63;
+  Chunk<T, DKP, W, TO, 1>& c = *reinterpret_cast<Chunk<T, DKP, W, TO, 1>*>(lds);
+  Gates& s = c.s;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4, col = 16 * wave + l16;
   const Head hd(a, blockIdx.x);
-  const Columns<NT> cols(a.dv);
   const float rate = a.c * softplus(a.lam[hd.h]);
-  const int64_t state = (int64_t)a.dk * a.dv, mine = blockIdx.x * state;
-  f32x4_t S[KT][NT];
-  load_state<DKP, NT>(a.s0 ? a.s0 + mine : nullptr, a, cols, lane, S);
-  for (int t0 = 0; t0 < hd.len; t0 += C) {
-    Fetched<T, DKP> f;
-    f.from(a, hd, t0);
-    f32x4_t u[NB][NT];
-    load_rows<T, NT>(a.v, a.ldv, a, hd, t0, cols, lane, u);
-    if (a.train && t0 > 0) store_state<DKP, NT>(a.saved + (int64_t)(t0 / C - 1) * gridDim.x * state + mine, a, cols, lane, S);
-    stage<T, DKP>(s, f, a.eps, rate, hd.len - t0);
+  const int64_t mine = (int64_t)blockIdx.x * a.dk * a.dv;
+  const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+  f32x4_t S[KT];
+  load_state<DKP>(a.s0 ? a.s0 + mine : nullptr, a, col, lane, S);
+  Rows<T, DKP, W> fk, fq;
+  Values<T, W> fv;
+  GateRows<T, W> fg;
+  auto fetch = [&](const int32_t (&rows)[C], int next0) {
+    fk.from(a.k, a.ldk, hd.kh, a.dk, rows);
+    fq.from(a.q, a.ldq, hd.kh, a.dk, rows);
+    fv.from(a.v, a.ldv, hd, a.dv, rows);
+    fg.from(a, hd, rows, next0);
+  };
+  if (hd.len > 0) {
+    if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, threadIdx.x);
     __syncthreads();
-    triangles(s);
+    fetch(s.row[0], C);
+  }
+  int turn = 0;
+  for (int t0 = 0; t0 < hd.len; t0 += C, turn ^= 1) {
+    const int left = hd.len - t0;
+    if (a.train && t0 > 0) store_kept<DKP>(kept_before<DKP, W>(a, t0 / C, blockIdx.x), col, lane, S);
+    fk.lengths(s.rk, a.eps, left);
+    fq.lengths(s.rq, a.eps, left);
+    fk.store(c.k);
+    fq.store(c.q);
+    fv.store(&c.v[0], s.row[turn]);
+    fg.store(s, rate, left, turn);
+    __syncthreads();
+    if (left > C) fetch(s.row[turn ^ 1], t0 + 2 * C);  // the next chunk's, which arrive during this one
+    triangles(c);
 
-    f32x4_t ks[NB][NT], o[NB][NT];
+    f32x4_t u[NB], o[NB];
 #pragma unroll
-    for (int I = 0; I < NB; ++I)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) ks[I][n] = o[I][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int I = 0; I < NB; ++I) u[I] = o[I] = zero;
 #pragma unroll
     for (int t = 0; t < DKP / 32; ++t) {
-      Piece<TX> s0[NT], s1[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) s0[n] = split<TX>(S[2 * t][n]), s1[n] = split<TX>(S[2 * t + 1][n]);
+      const Piece<TX> s0 = split<TX>(S[2 * t]), s1 = split<TX>(S[2 * t + 1]);
 #pragma unroll
       for (int I = 0; I < NB; ++I) {
         Piece<TI> a0, a1;
-        rows_of<T, DKP>(s.k, I, t, lane, a0, a1);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma<TI, TX>(ks[I][n], a0, a1, s0[n], s1[n]);
-        rows_of<T, DKP>(s.q, I, t, lane, a0, a1);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma<TI, TO>(o[I][n], a0, a1, first<TO>(s0[n]), first<TO>(s1[n]));
+        rows_of(c.k, I, t, lane, a0, a1);
+        mma<TI, TX>(u[I], a0, a1, s0, s1);
+        rows_of(c.q, I, t, lane, a0, a1);
+        mma<TO, TI>(o[I], first<TO>(s0), first<TO>(s1), a0, a1);
       }
     }
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
-      const f32x4_t beta = rows4(s.beta, I, lane), bgk = rows4(s.bgk, I, lane), gq = rows4(s.gq, I, lane);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        u[I][n] = u[I][n] * beta - ks[I][n] * bgk;
-        o[I][n] *= gq;
-      }
+      u[I] = fv.column_values(wave, I, lane) * rows4(s.beta, I, lane) - u[I] * rows4(s.bgk, I, lane);
+      o[I] *= s.gq[16 * I + l16];
     }
-    Piece<TX> up[NB][NT];
-    solve(s, lane, u, up);
+    Piece<TX> r[NB], up[NB];
+    solve(c, lane, u, r, up);
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
 #pragma unroll
-      for (int J = 0; J + 1 <= I; J += 2) {
-        const Piece<TO> a0 = block_of(s.p[lower(I, J)], lane), a1 = block_of(s.p[lower(I, J + 1)], lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma<TO, TO>(o[I][n], a0, a1, first<TO>(up[J][n]), first<TO>(up[J + 1][n]));
-      }
-      if (I % 2 == 0) {
-        const Piece<TO> a0 = block_of(s.p[lower(I, I)], lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma<TO, TO>(o[I][n], a0, first<TO>(up[I][n]));
-      }
+      for (int J = 0; J + 1 <= I; J += 2)
+        mma<TO, TO>(o[I], first<TO>(up[J]), first<TO>(up[J + 1]), block_of(c.p[lower(I, J)], lane), block_of(c.p[lower(I, J + 1)], lane));
+      if (I % 2 == 0) mma<TO, TO>(o[I], first<TO>(up[I]), block_of(c.p[lower(I, I)], lane));
     }
-    store_rows<T, NT>(a.o, a.ldo, a, hd, t0, cols, lane, o);
 #pragma unroll
-    for (int I = 0; I < NB; ++I) {
-      const f32x4_t gk = rows4(s.gk, I, lane);
+    for (int I = 0; I < NB; ++I)
+      if (16 * I + l16 < left)
+        put4(static_cast<T*>(a.o) + s.row[turn][16 * I + l16] * a.ldo + (int64_t)hd.h * a.dv + 16 * wave + 4 * g4,
+             a.dv - 16 * wave - 4 * g4, o[I]);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) up[I][n] = split<TX>(u[I][n] * gk);
-    }
+    for (int I = 0; I < NB; ++I) up[I] = split<TX>(u[I] * rows4(s.gk, I, lane));
     const float g_end = s.g[C - 1];
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
+      S[t] *= g_end;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) S[t][n] *= g_end;
-#pragma unroll
-      for (int I = 0; I < NB; I += 2) {
-        const Piece<TI> a0 = columns_of<T, DKP>(s.k, t, I, lane), a1 = columns_of<T, DKP>(s.k, t, I + 1, lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma<TI, TX>(S[t][n], a0, a1, up[I][n], up[I + 1][n]);
-      }
+      for (int I = 0; I < NB; I += 2) mma<TI, TX>(S[t], columns_of(c.k, t, I, lane), columns_of(c.k, t, I + 1, lane), up[I], up[I + 1]);
     }
     __syncthreads();
   }
-  if (a.sT) store_state<DKP, NT>(a.sT + mine, a, cols, lane, S);
+  if (a.sT) store_state<DKP>(a.sT + mine, a, col, lane, S);
 }
 
 // One frame of each sequence: a state is read once, kept in registers, and written
@@ -135,7 +134,7 @@ __global__ __launch_bounds__(THREADS) void gd_token_kernel(GatedDelta a) {
             if (j < left) a.sT[mine + (int64_t)(rg + i * RG) * a.dv + c0 + j] = S[i][j];
     return;
   }
-  const int64_t row0 = hd.row(0);
+  const int64_t row0 = hd.row(a, 0);
   if (wave < 2) {  // k, then q: its elements and 1 / its length
     const T* p = wave == 0 ? static_cast<const T*>(a.k) + row0 * a.ldk : static_cast<const T*>(a.q) + row0 * a.ldq;
     float x[2], sum = 0.f;
@@ -195,13 +194,13 @@ __global__ __launch_bounds__(THREADS) void gd_token_kernel(GatedDelta a) {
     }
 }
 
-template <typename T, int DKP, int NT> hipError_t chunks(const GatedDelta& a, hipStream_t s) {
-  constexpr int LDS = sizeof(Chunk<T, DKP, Terms<T>::OUT>);
+template <typename T, int DKP, int W> hipError_t chunks(const GatedDelta& a, hipStream_t s) {
+  constexpr int LDS = sizeof(Chunk<T, DKP, W, Terms<T>::OUT, 1>);
   static_assert(LDS <= 160 * 1024, "a workgroup's LDS");
   static PerDevice ready;
-  const hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_forward_kernel<T, DKP, NT>), ready);
+  const hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_forward_kernel<T, DKP, W>), ready);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((gd_forward_kernel<T, DKP, NT>), dim3((unsigned)(a.B * a.H)), dim3(THREADS), LDS, s, a);
+  hipLaunchKernelGGL((gd_forward_kernel<T, DKP, W>), dim3((unsigned)(a.B * a.H)), dim3(threads_of<W>), LDS, s, a);
   return hipGetLastError();
 }
 
@@ -219,8 +218,8 @@ template <typename T> hipError_t forward(const GatedDelta& a, hipStream_t s) {
     if (a.dv <= 64) return token<T, 16>(a, s);
     return token<T, 32>(a, s);
   }
-  if (a.dk <= 64) return a.dv <= 64 ? chunks<T, 64, 1>(a, s) : chunks<T, 64, 2>(a, s);
-  return a.dv <= 64 ? chunks<T, 128, 1>(a, s) : chunks<T, 128, 2>(a, s);
+  if (a.dk <= 64) return a.dv <= 64 ? chunks<T, 64, 4>(a, s) : chunks<T, 64, 8>(a, s);
+  return a.dv <= 64 ? chunks<T, 128, 4>(a, s) : chunks<T, 128, 8>(a, s);
 }
 
 }  // namespace

@@ -20,224 +20,194 @@ namespace {
 
 using namespace gd;
 
-// The state that chunk n of a head starts from, and the gradient of the one it ends in.
-__device__ __forceinline__ const float* state_before(const GatedDelta& a, int n, int64_t bh) {
-  const int64_t state = (int64_t)a.dk * a.dv;
-  if (n == 0) return a.s0 ? a.s0 + bh * state : nullptr;
-  return a.saved + ((int64_t)(n - 1) * a.B * a.H + bh) * state;
-}
-__device__ __forceinline__ float* gradient_after(const GatedDelta& a, int n, int64_t bh) {
-  return a.dsaved + ((int64_t)n * a.B * a.H + bh) * ((int64_t)a.dk * a.dv);
-}
-
-template <typename T, int DKP> struct Backward {
-  Chunk<T, DKP, Terms<T>::X> s;
-  float rows[2][WAVES][C];  // dO . O - dV . V and dR . U, of a wave's columns
-  float end[WAVES];         // <dS', S'>
+template <typename T, int DKP, int W> struct Backward {
+  Chunk<T, DKP, W, Terms<T>::X, 2> c;
+  float rows[2][W][C];  // dO . O - dV . V and dR . U, of a wave's columns
+  float end[W];         // <dS', S'>
 };
 
-template <typename T, int DKP, int NT>
-__global__ __launch_bounds__(THREADS) void gd_backward_kernel(GatedDelta a) {
+template <typename T, int DKP, int W>
+__global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelta a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  Backward<T, DKP>& all = *reinterpret_cast<Backward<T, DKP>*>(lds);
-  Chunk<T, DKP, Terms<T>::X>& s = all.s;
-  constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, KT = DKP / 16;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
-  const int64_t bh = blockIdx.x;
+  constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT, KT = DKP / 16;
+  Backward<T, DKP, W>& all = *reinterpret_cast<Backward<T, DKP, W>*>(lds);
+  auto& c = all.c;
+  Gates& s = c.s;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4, col = 16 * wave + l16;
+  const int64_t bh = blockIdx.x, state = (int64_t)a.dk * a.dv;
   const Head hd(a, blockIdx.x);
-  const Columns<NT> cols(a.dv);
   const float rate = a.c * softplus(a.lam[hd.h]);
-  const int64_t state = (int64_t)a.dk * a.dv, ldu = (int64_t)a.H * a.dv;
   const int chunks = (hd.len + C - 1) / C;
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
-  f32x4_t dS[KT][NT];
-  load_state<DKP, NT>(a.dsT ? a.dsT + bh * state : nullptr, a, cols, lane, dS);
-  float dlam = 0.f;  // (of frame `lane` of every chunk, in the first wave)
-  for (int n = chunks - 1; n >= 0; --n) {
-    const int t0 = n * C;
-    Fetched<T, DKP> f;
-    f.from(a, hd, t0);
-    f32x4_t v[NB][NT], u[NB][NT], dO[NB][NT];
-    load_rows<T, NT>(a.v, a.ldv, a, hd, t0, cols, lane, v);
-    load_rows<T, NT>(a.d_o, a.lddo, a, hd, t0, cols, lane, dO);
-    if (n < chunks - 1 || a.keep_end) store_state<DKP, NT>(gradient_after(a, n, bh), a, cols, lane, dS);
-    stage<T, DKP>(s, f, a.eps, rate, hd.len - t0);
+  f32x4_t dS[KT];
+  load_state<DKP>(a.dsT ? a.dsT + bh * state : nullptr, a, col, lane, dS);
+  Rows<T, DKP, W> fk, fq;
+  Values<T, W> fv, fo;
+  GateRows<T, W> fg;
+  auto fetch = [&](const int32_t (&rows)[C], int next0) {
+    fk.from(a.k, a.ldk, hd.kh, a.dk, rows);
+    fq.from(a.q, a.ldq, hd.kh, a.dk, rows);
+    fv.from(a.v, a.ldv, hd, a.dv, rows);
+    fo.from(a.d_o, a.lddo, hd, a.dv, rows);
+    fg.from(a, hd, rows, next0);
+  };
+  if (chunks) {
+    if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, (chunks - 1) * C + threadIdx.x);
     __syncthreads();
-    triangles(s);
+    fetch(s.row[0], max(chunks - 2, 0) * C);
+  }
+  float dlam = 0.f;  // (of a frame a lane of every chunk, in the last wave)
+  int turn = 0;
+  for (int n = chunks - 1; n >= 0; --n, turn ^= 1) {
+    const int left = hd.len - n * C;
+    const T r_now = fg.r;
+    store_kept<DKP>(kept_after<DKP, W>(a, n, bh), col, lane, dS);
+    fk.lengths(s.rk, a.eps, left);
+    fq.lengths(s.rq, a.eps, left);
+    fk.store(c.k);
+    fq.store(c.q);
+    fv.store(&c.v[0], s.row[turn]);
+    fo.store(&c.v[1], s.row[turn]);
+    fg.store(s, rate, left, turn);
+    __syncthreads();
+    if (n > 0) fetch(s.row[turn ^ 1], max(n - 2, 0) * C);  // the chunk before, which arrives during this one
+    f32x4_t S[KT];
+    if (n > 0) load_kept<DKP>(kept_before<DKP, W>(a, n, bh), col, lane, S);
+    else load_state<DKP>(a.s0 ? a.s0 + bh * state : nullptr, a, col, lane, S);
+    triangles(c);
 
-    f32x4_t ks[NB][NT], o[NB][NT], kd[NB][NT];
+    f32x4_t u[NB], o[NB], kd[NB];
 #pragma unroll
-    for (int I = 0; I < NB; ++I)
-#pragma unroll
-      for (int m = 0; m < NT; ++m) ks[I][m] = o[I][m] = kd[I][m] = zero;
-    const float* const before = state_before(a, n, bh);
+    for (int I = 0; I < NB; ++I) u[I] = o[I] = kd[I] = zero;
     float end = 0.f;
-    {
-      f32x4_t S[KT][NT];
-      load_state<DKP, NT>(before, a, cols, lane, S);
 #pragma unroll
-      for (int t = 0; t < DKP / 32; ++t) {
-        Piece<TX> s0[NT], s1[NT], d0[NT], d1[NT];
+    for (int t = 0; t < DKP / 32; ++t) {
+      const Piece<TX> s0 = split<TX>(S[2 * t]), s1 = split<TX>(S[2 * t + 1]);
+      const Piece<TX> d0 = split<TX>(dS[2 * t]), d1 = split<TX>(dS[2 * t + 1]);
 #pragma unroll
-        for (int m = 0; m < NT; ++m) {
-          s0[m] = split<TX>(S[2 * t][m]);
-          s1[m] = split<TX>(S[2 * t + 1][m]);
-          d0[m] = split<TX>(dS[2 * t][m]);
-          d1[m] = split<TX>(dS[2 * t + 1][m]);
+      for (int r = 0; r < 4; ++r) end = fmaf(S[2 * t][r], dS[2 * t][r], fmaf(S[2 * t + 1][r], dS[2 * t + 1][r], end));
 #pragma unroll
-          for (int r = 0; r < 4; ++r) end = fmaf(S[2 * t][m][r], dS[2 * t][m][r], fmaf(S[2 * t + 1][m][r], dS[2 * t + 1][m][r], end));
-        }
-#pragma unroll
-        for (int I = 0; I < NB; ++I) {
-          Piece<TI> a0, a1;
-          rows_of<T, DKP>(s.k, I, t, lane, a0, a1);
-#pragma unroll
-          for (int m = 0; m < NT; ++m) {
-            mma<TI, TX>(ks[I][m], a0, a1, s0[m], s1[m]);
-            mma<TI, TX>(kd[I][m], a0, a1, d0[m], d1[m]);
-          }
-          rows_of<T, DKP>(s.q, I, t, lane, a0, a1);
-#pragma unroll
-          for (int m = 0; m < NT; ++m) mma<TI, TX>(o[I][m], a0, a1, s0[m], s1[m]);
-        }
+      for (int I = 0; I < NB; ++I) {
+        Piece<TI> a0, a1;
+        rows_of(c.k, I, t, lane, a0, a1);
+        mma<TI, TX>(u[I], a0, a1, s0, s1);
+        mma<TI, TX>(kd[I], a0, a1, d0, d1);
+        rows_of(c.q, I, t, lane, a0, a1);
+        mma<TX, TI>(o[I], s0, s1, a0, a1);
       }
     }
     const float g_end = s.g[C - 1];
     end *= g_end;
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
-      const f32x4_t beta = rows4(s.beta, I, lane), bgk = rows4(s.bgk, I, lane), gq = rows4(s.gq, I, lane), gk = rows4(s.gk, I, lane);
-#pragma unroll
-      for (int m = 0; m < NT; ++m) {
-        u[I][m] = v[I][m] * beta - ks[I][m] * bgk;
-        o[I][m] *= gq;
-        kd[I][m] *= gk;
-      }
+      u[I] = fv.column_values(wave, I, lane) * rows4(s.beta, I, lane) - u[I] * rows4(s.bgk, I, lane);
+      o[I] *= s.gq[16 * I + l16];
+      kd[I] *= rows4(s.gk, I, lane);
     }
+    // U; transposed, a frame a lane, it is wanted for dR . U
+    f32x4_t ut[NB];
     {
-      Piece<TX> up[NB][NT];
-      solve(s, lane, u, up);
+      Piece<TX> r[NB], up[NB];
+      solve(c, lane, u, r, up);
 #pragma unroll
       for (int I = 0; I < NB; ++I) {
+        ut[I] = zero;
+        mma<TX, TX>(ut[I], r[I], block_of(c.d[I], lane));
 #pragma unroll
-        for (int J = 0; J + 1 <= I; J += 2) {
-          const Piece<TX> a0 = block_of(s.p[lower(I, J)], lane), a1 = block_of(s.p[lower(I, J + 1)], lane);
+        for (int r4 = 0; r4 < 4; ++r4) end = fmaf(u[I][r4], kd[I][r4], end);
 #pragma unroll
-          for (int m = 0; m < NT; ++m) mma<TX, TX>(o[I][m], a0, a1, up[J][m], up[J + 1][m]);
-        }
-        if (I % 2 == 0) {
-          const Piece<TX> a0 = block_of(s.p[lower(I, I)], lane);
-#pragma unroll
-          for (int m = 0; m < NT; ++m) mma<TX, TX>(o[I][m], a0, up[I][m]);
-        }
+        for (int J = 0; J + 1 <= I; J += 2)
+          mma<TX, TX>(o[I], up[J], up[J + 1], block_of(c.p[lower(I, J)], lane), block_of(c.p[lower(I, J + 1)], lane));
+        if (I % 2 == 0) mma<TX, TX>(o[I], up[I], block_of(c.p[lower(I, I)], lane));
       }
+      uint16_t* const keep = kept_columns<TO, W>(a.u, a, n, bh);
+#pragma unroll
+      for (int e = 0; e < TO; ++e)
+#pragma unroll
+        for (int I = 0; I < NB; ++I)
+          *reinterpret_cast<u32x2_t*>(keep + (e * 16 * W + col) * C + 16 * I + 4 * g4) = up[I].t[e];
     }
-    f32x4_t y1[NB], y2[NB];
+    float y1[NB], y2[NB];
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
-      y1[I] = zero;
-#pragma unroll
-      for (int m = 0; m < NT; ++m) {
-        y1[I] += dO[I][m] * o[I][m];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) end = fmaf(u[I][m][r], kd[I][m][r], end);
-      }
+      const f32x4_t x = fo.row_values(I, wave, lane) * o[I];
+      y1[I] = (x[0] + x[1]) + (x[2] + x[3]);
     }
-    // dU (in kd), then dR (there too)
+    // dU in kd, then dR, block after block from the last
+#pragma unroll
+    for (int J = 0; J < NB; ++J)
+#pragma unroll
+      for (int I = J; I < NB; ++I) mma<TX, TI>(kd[J], block_turned(c.p[lower(I, J)], lane), fo.column(wave, I, lane));
     {
-      Piece<TI> dop[NB][NT];
-#pragma unroll
-      for (int I = 0; I < NB; ++I)
-#pragma unroll
-        for (int m = 0; m < NT; ++m) dop[I][m] = split<TI>(dO[I][m]);
-#pragma unroll
-      for (int J = 0; J < NB; ++J)
-#pragma unroll
-        for (int I = J; I < NB; ++I) {
-          const Piece<TX> p = block_turned(s.p[lower(I, J)], lane);
-#pragma unroll
-          for (int m = 0; m < NT; ++m) mma<TX, TI>(kd[J][m], p, dop[I][m]);
-        }
-    }
-    {
-      Piece<TX> dp[NB][NT];
+      Piece<TX> dp[NB];
 #pragma unroll
       for (int I = NB - 1; I >= 0; --I) {
 #pragma unroll
-        for (int J = NB - 1; J > I; --J) {
-          const Piece<TX> p = block_turned(s.l[below(J, I)], lane);
+        for (int J = NB - 1; J > I; --J) mma<TX, TX>(kd[I], block_turned(c.l[below(J, I)], lane), dp[J]);
+        const Piece<TX> d = block_turned(c.d[I], lane), w = split<TX>(kd[I]);
+        f32x4_t dr = zero;  // (transposed)
+        mma<TX, TX>(dr, w, d);
+        kd[I] = zero;
+        mma<TX, TX>(kd[I], d, w);
+        dp[I] = split<TX>(kd[I]);
+        const f32x4_t dv = dr * s.beta[16 * I + l16], x = dv * fv.row_values(I, wave, lane), y = dr * ut[I];
+        y1[I] -= (x[0] + x[1]) + (x[2] + x[3]);
+        y2[I] = (y[0] + y[1]) + (y[2] + y[3]);
+        if (16 * I + l16 < left)
+          put4(static_cast<T*>(a.dv_) + s.row[turn][16 * I + l16] * a.lddv + (int64_t)hd.h * a.dv + 16 * wave + 4 * g4,
+               a.dv - 16 * wave - 4 * g4, dv);
+      }
+      uint16_t* const keep = kept_columns<TO, W>(a.dr_rows, a, n, bh);
 #pragma unroll
-          for (int m = 0; m < NT; ++m) mma<TX, TX>(kd[I][m], p, dp[J][m]);
-        }
-        const Piece<TX> d = block_turned(s.d[I], lane);
+      for (int e = 0; e < TO; ++e)
 #pragma unroll
-        for (int m = 0; m < NT; ++m) {
-          const Piece<TX> w = split<TX>(kd[I][m]);
-          kd[I][m] = zero;
-          mma<TX, TX>(kd[I][m], d, w);
-          dp[I][m] = split<TX>(kd[I][m]);
+        for (int I = 0; I < NB; ++I)
+          *reinterpret_cast<u32x2_t*>(keep + (e * 16 * W + col) * C + 16 * I + 4 * g4) = dp[I].t[e];
+    }
+    {
+      Piece<TX> w1[NB], w2[NB];
+#pragma unroll
+      for (int I = 0; I < NB; ++I) {
+        w1[I] = split<TX>(fo.column_values(wave, I, lane) * rows4(s.gq, I, lane));
+        w2[I] = split<TX>(-kd[I] * rows4(s.bgk, I, lane));
+      }
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        dS[t] *= g_end;
+#pragma unroll
+        for (int I = 0; I < NB; I += 2) {
+          mma<TI, TX>(dS[t], columns_of(c.q, t, I, lane), columns_of(c.q, t, I + 1, lane), w1[I], w1[I + 1]);
+          mma<TI, TX>(dS[t], columns_of(c.k, t, I, lane), columns_of(c.k, t, I + 1, lane), w2[I], w2[I + 1]);
         }
       }
     }
-    store_rows<float, NT>(a.u, ldu, a, hd, t0, cols, lane, u);
-    store_rows<float, NT>(a.dr_rows, ldu, a, hd, t0, cols, lane, kd);
-    Piece<TX> w1[NB][NT], w2[NB][NT];
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
-      const f32x4_t beta = rows4(s.beta, I, lane), bgk = rows4(s.bgk, I, lane), gq = rows4(s.gq, I, lane);
-      y2[I] = zero;
-#pragma unroll
-      for (int m = 0; m < NT; ++m) {
-        y2[I] += kd[I][m] * u[I][m];
-        const f32x4_t dv = kd[I][m] * beta;
-        y1[I] -= dv * v[I][m];
-        u[I][m] = dv;
-        w1[I][m] = split<TX>(dO[I][m] * gq);
-        w2[I][m] = split<TX>(-kd[I][m] * bgk);
+      y1[I] += __shfl_xor(y1[I], 16, 64);
+      y2[I] += __shfl_xor(y2[I], 16, 64);
+      y1[I] += __shfl_xor(y1[I], 32, 64);
+      y2[I] += __shfl_xor(y2[I], 32, 64);
+      if (g4 == 0) {
+        all.rows[0][wave][16 * I + l16] = y1[I];
+        all.rows[1][wave][16 * I + l16] = y2[I];
       }
     }
-    store_rows<T, NT>(a.dv_, a.lddv, a, hd, t0, cols, lane, u);
-#pragma unroll
-    for (int t = 0; t < KT; ++t) {
-#pragma unroll
-      for (int m = 0; m < NT; ++m) dS[t][m] *= g_end;
-#pragma unroll
-      for (int I = 0; I < NB; I += 2) {
-        const Piece<TI> q0 = columns_of<T, DKP>(s.q, t, I, lane), q1 = columns_of<T, DKP>(s.q, t, I + 1, lane);
-        const Piece<TI> k0 = columns_of<T, DKP>(s.k, t, I, lane), k1 = columns_of<T, DKP>(s.k, t, I + 1, lane);
-#pragma unroll
-        for (int m = 0; m < NT; ++m) {
-          mma<TI, TX>(dS[t][m], q0, q1, w1[I][m], w1[I + 1][m]);
-          mma<TI, TX>(dS[t][m], k0, k1, w2[I][m], w2[I + 1][m]);
-        }
-      }
-    }
-#pragma unroll
-    for (int I = 0; I < NB; ++I)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float s1 = lanes_sum<16>(y1[I][r]), s2 = lanes_sum<16>(y2[I][r]);
-        if (l16 == 0) {
-          all.rows[0][wave][16 * I + 4 * g4 + r] = s1;
-          all.rows[1][wave][16 * I + 4 * g4 + r] = s2;
-        }
-      }
     end = wave_sum_uniform(end);
     if (lane == 0) all.end[wave] = end;
     __syncthreads();
-    if (wave == 0) {  // a frame a lane: the gates' gradients
-      float d = (all.rows[0][0][lane] + all.rows[0][1][lane]) + (all.rows[0][2][lane] + all.rows[0][3][lane]);
-      const float e = (all.rows[1][0][lane] + all.rows[1][1][lane]) + (all.rows[1][2][lane] + all.rows[1][3][lane]);
+    if (wave == W - 1) {  // a frame a lane: the gates' gradients
+      float d = 0.f, e = 0.f, ends = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) d += all.rows[0][w][lane], e += all.rows[1][w][lane], ends += all.end[w];
 #pragma unroll
       for (int k = 1; k < C; k <<= 1) {  // from this frame to the chunk's last
         const float above = __shfl_down(d, k, 64);
         if (lane + k < C) d += above;
       }
-      d += (all.end[0] + all.end[1]) + (all.end[2] + all.end[3]);
-      const int t = t0 + lane;
-      if (t < hd.len) {
-        const float sr = sigm(f.r);
-        const int64_t row = hd.row(t);
+      d += ends;
+      if (lane < left) {
+        const float sr = sigm(to_f32(r_now));
+        const int64_t row = s.row[turn][lane];
         static_cast<T*>(a.dr)[row * a.lddr + hd.h] = from_f32<T>(-rate * d * sr * (1.f - sr));
         static_cast<T*>(a.db)[row * a.lddb + hd.h] = from_f32<T>(e * (1.f - s.beta[lane]));
         dlam -= d * sr;
@@ -245,216 +215,210 @@ __global__ __launch_bounds__(THREADS) void gd_backward_kernel(GatedDelta a) {
     }
     __syncthreads();
   }
-  if (a.ds0) store_state<DKP, NT>(a.ds0 + bh * state, a, cols, lane, dS);
-  if (wave == 0) {
+  if (a.ds0) store_state<DKP>(a.ds0 + bh * state, a, col, lane, dS);
+  if (wave == W - 1) {
     dlam = wave_sum_uniform(dlam);
     if (lane == 0) a.parts[bh] = a.c * dlam;
   }
 }
 
 // The gradients of q and k of a chunk of a key head, summed over its heads: a wave has
-// rows of them (16 columns of q and k at a time), a lane a frame of each block, so that
-// what scales with a frame is a factor of a lane.
+// 16 columns of them, a lane a frame of each block, so that what scales with a frame is
+// a factor of a lane.  It goes through v's columns 32 at a time, then takes the sums
+// over pairs of frames to K and Q, which have the same LDS by then.
 template <typename T, int DKP> struct Keys {
   static constexpr int TI = Terms<T>::IN, TO = Terms<T>::OUT;
-  static constexpr int PITCH = 32 * 2 + 16;  // bytes of a row of a slice of 32 columns of v
-  Staged<T, DKP> s;
+  static constexpr int FRAMES = C * 2 + 16, KEYS = pitch_of(DKP);  // bytes of a row of columns, of states
   union {
-    struct { uint8_t dO[TI][C * PITCH], u[TO][C * PITCH], dR[TO][C * PITCH]; } rows;
-    struct { uint8_t qk[10][TO][512], kk[10][TO][512]; } blocks;
+    struct {
+      Matrix<TI, 32> dO;
+      uint8_t u[TO][32 * FRAMES], dR[TO][32 * FRAMES];  // 32 columns over frames
+      uint8_t S[TO][32 * KEYS], dS[TO][32 * KEYS];      // and over keys
+    } slice;
+    struct {
+      Matrix<TI, DKP> k, q;
+      uint8_t qk[10][TO][512], kk[10][TO][512];
+    } pairs;
   };
-  float dots[2][WAVES][C];
+  float dots[2][DKP / 16][C];
+  Gates s;
 };
 
-template <int N, int PITCH>
-__device__ __forceinline__ void slice_row(const uint8_t (&m)[N][C * PITCH], int I, int lane, Piece<N>& a0, Piece<N>& a1) {
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const uint4 w = *reinterpret_cast<const uint4*>(m[e] + (16 * I + (lane & 15)) * PITCH + (lane >> 4) * 16);
-    a0.t[e] = make_uint2(w.x, w.y);
-    a1.t[e] = make_uint2(w.z, w.w);
-  }
-}
-template <int N, int PITCH>
-__device__ __forceinline__ void slice_store(uint8_t (&m)[N][C * PITCH], int row, int u, const float (&v)[8]) {
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int p = 2 * u + half, slot = (p & 3) * 2 + (p >> 2);
-    const Piece<N> w = split<N>(f32x4_t{v[4 * half], v[4 * half + 1], v[4 * half + 2], v[4 * half + 3]});
-#pragma unroll
-    for (int e = 0; e < N; ++e) *reinterpret_cast<uint2*>(m[e] + row * PITCH + slot * 8) = w.t[e];
-  }
-}
-// Four elements of a state's row from column c on, zeros past its end.
-__device__ __forceinline__ f32x4_t state4(const float* m, int row, int c, const GatedDelta& a) {
-  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-  if (!m || row >= a.dk) return v;
-  const float* p = m + (int64_t)row * a.dv + c;
-  if (c + 4 <= a.dv) return *reinterpret_cast<const f32x4_a*>(p);
-#pragma unroll
-  for (int j = 0; j < 3; ++j)
-    if (c + j < a.dv) v[j] = p[j];
-  return v;
-}
-
-template <typename T, int DKP>
-__global__ __launch_bounds__(THREADS) void gd_keys_kernel(GatedDelta a) {
+template <typename T, int DKP, int VP>
+__global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   Keys<T, DKP>& all = *reinterpret_cast<Keys<T, DKP>*>(lds);
-  Staged<T, DKP>& s = all.s;
-  constexpr int TI = Terms<T>::IN, TO = Terms<T>::OUT, KM = DKP / 64;
+  Gates& s = all.s;
+  constexpr int TI = Terms<T>::IN, TO = Terms<T>::OUT, W = DKP / 16, TH = threads_of<W>, VW = VP / 16;
+  constexpr int FRAMES = Keys<T, DKP>::FRAMES, KEYS = Keys<T, DKP>::KEYS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
   const int group = a.H / a.G, n = blockIdx.x / (a.B * a.G), bg = blockIdx.x % (a.B * a.G), t0 = n * C;
   const int b = bg / a.G, kh = bg % a.G;
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
-  const int64_t ldu = (int64_t)a.H * a.dv;
-  f32x4_t dq[KM][NB], dk[KM][NB];
+  f32x4_t dq[NB], dk[NB];
 #pragma unroll
-  for (int m = 0; m < KM; ++m)
-#pragma unroll
-    for (int I = 0; I < NB; ++I) dq[m][I] = dk[m][I] = zero;
+  for (int I = 0; I < NB; ++I) dq[I] = dk[I] = zero;
+  Rows<T, DKP, W> fk, fq;
+  GateRows<T, W> fg;
   for (int member = 0; member < group; ++member) {
     const int64_t bh = (int64_t)b * a.H + kh * group + member;
     const Head hd(a, (int)bh);
-    if (t0 >= hd.len) return;  // (all heads of a sequence alike)
-    const bool last = t0 + C >= hd.len;
-    const float* const S = state_before(a, n, bh);
-    const float* const dS = !last || a.keep_end ? gradient_after(a, n, bh)
-                            : a.dsT ? a.dsT + bh * ((int64_t)a.dk * a.dv) : nullptr;
-    {
-      Fetched<T, DKP> f;
-      f.from(a, hd, t0);
-      stage<T, DKP>(s, f, a.eps, a.c * softplus(a.lam[hd.h]), hd.len - t0);
+    const int left = hd.len - t0;
+    if (left <= 0) return;  // (all heads of a sequence alike)
+    if (member == 0) {
+      if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, t0 + threadIdx.x);
+      __syncthreads();
     }
-    f32x4_t pair[5], sq[KM][NB], sk[KM][NB], su[KM][NB];
+    fk.from(a.k, a.ldk, kh, a.dk, s.row[0]);
+    fq.from(a.q, a.ldq, kh, a.dk, s.row[0]);
+    fg.from(a, hd, s.row[0], t0);
+    const float* const S = n > 0 ? kept_before<DKP, VW>(a, n, bh) : nullptr;
+    const float* const S0 = a.s0 ? a.s0 + bh * ((int64_t)a.dk * a.dv) : nullptr;
+    const float* const dS = kept_after<DKP, VW>(a, n, bh);
+    const uint16_t *const U = kept_columns<TO, VW>(a.u, a, n, bh), *const dR = kept_columns<TO, VW>(a.dr_rows, a, n, bh);
+    const T* const d_o = static_cast<const T*>(a.d_o) + (int64_t)hd.h * a.dv;
+    f32x4_t pair_q[(10 + W - 1) / W], pair_k[(10 + W - 1) / W], sq[NB], sk[NB], su[NB];
 #pragma unroll
-    for (int k = 0; k < 5; ++k) pair[k] = zero;
+    for (int k = 0; k < (10 + W - 1) / W; ++k) pair_q[k] = pair_k[k] = zero;
 #pragma unroll
-    for (int m = 0; m < KM; ++m)
-#pragma unroll
-      for (int I = 0; I < NB; ++I) sq[m][I] = sk[m][I] = su[m][I] = zero;
+    for (int I = 0; I < NB; ++I) sq[I] = sk[I] = su[I] = zero;
     for (int c0 = 0; c0 < a.dv; c0 += 32) {
-      {
-        const int row = threadIdx.x >> 2, piece = threadIdx.x & 3, col = c0 + 8 * piece, left = a.dv - col, t = t0 + row;
-        float x[3][8];
-        if (t < hd.len && left > 0) {
-          const int64_t at = hd.row(t), h = (int64_t)hd.h * a.dv + col;
-          load8(static_cast<const T*>(a.d_o) + at * a.lddo + h, left, x[0]);
-          load8(a.u + at * ldu + h, left, x[1]);
-          load8(a.dr_rows + at * ldu + h, left, x[2]);
-        } else {
+      if (threadIdx.x < 256) {  // dO: four pieces of eight columns a frame
+        const int row = threadIdx.x >> 2, u = threadIdx.x & 3, more = a.dv - c0 - 8 * u;
+        Eight<T> x;
+        const T* const p = d_o + s.row[0][row] * a.lddo + c0 + 8 * u;
+        if (more >= 8) x.load(p);
+        else if (more > 0) x.load(p, more);
+        else x.zero();
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[0][j] = x[1][j] = x[2][j] = 0.f;
+        for (int half = 0; half < 2; ++half) {
+          const int w = 2 * u + half, slot = (w & 3) * 2 + (w >> 2);
+          const Piece<TI> v = x.piece(half);
+#pragma unroll
+          for (int e = 0; e < TI; ++e) *reinterpret_cast<u32x2_t*>(all.slice.dO.at[e] + row * pitch_of(32) + slot * 8) = v.t[e];
         }
-        slice_store<TI, Keys<T, DKP>::PITCH>(all.rows.dO, row, piece, x[0]);
-        slice_store<TO, Keys<T, DKP>::PITCH>(all.rows.u, row, piece, x[1]);
-        slice_store<TO, Keys<T, DKP>::PITCH>(all.rows.dR, row, piece, x[2]);
+      }
+#pragma unroll
+      for (int i = 0; i < TO * 256; i += TH) {  // U and dR: eight pieces of eight frames a column
+        const int at = i + threadIdx.x, e = at >> 8, row = (at >> 3) & 31, u = at & 7;
+        const int64_t from = (int64_t)(e * VP + c0 + row) * C + 8 * u;
+        if (at < TO * 256) {
+          *reinterpret_cast<u32x4_t*>(all.slice.u[e] + row * FRAMES + 16 * u) = *reinterpret_cast<const u32x4_t*>(U + from);
+          *reinterpret_cast<u32x4_t*>(all.slice.dR[e] + row * FRAMES + 16 * u) = *reinterpret_cast<const u32x4_t*>(dR + from);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 32 * DKP / 4; i += TH) {  // S and dS: pieces of four keys of a column
+        const int at = i + threadIdx.x, row = at / (DKP / 4), u = at % (DKP / 4);
+        f32x4_t v = zero;
+        if (S) {
+          v = *reinterpret_cast<const f32x4_t*>(S + (c0 + row) * DKP + 4 * u);
+        } else if (S0 && c0 + row < a.dv) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (4 * u + r < a.dk) v[r] = S0[(4 * u + r) * a.dv + c0 + row];
+        }
+        const Piece<TO> x = split<TO>(v), y = split<TO>(*reinterpret_cast<const f32x4_t*>(dS + (c0 + row) * DKP + 4 * u));
+#pragma unroll
+        for (int e = 0; e < TO; ++e) {
+          *reinterpret_cast<u32x2_t*>(all.slice.S[e] + row * KEYS + 8 * u) = x.t[e];
+          *reinterpret_cast<u32x2_t*>(all.slice.dS[e] + row * KEYS + 8 * u) = y.t[e];
+        }
       }
       __syncthreads();
-      if (c0 == 0 && wave == 1) {
-        s.bgk[lane] = s.beta[lane] * s.g[lane] * s.rk[lane];
-        s.gq[lane] = s.g[lane] * s.rq[lane];
-        s.gk[lane] = s.end[lane] * s.rk[lane];
+      // column 16 j + lane % 16 of those over rows 4 (lane / 16) and on, of both halves of the 32
+      auto over = [&](const auto& m, int pitch, int j, Piece<TO>& x0, Piece<TO>& x1) {
+        const int at = (4 * g4 + (l16 >> 2)) * pitch + (16 * j + 4 * (lane & 3)) * 2;
+#pragma unroll
+        for (int e = 0; e < TO; ++e) {
+          x0.t[e] = turned(m[e] + at);
+          x1.t[e] = turned(m[e] + at + 16 * pitch);
+        }
+      };
+      Piece<TO> s0, s1, d0, d1;
+      over(all.slice.S, KEYS, wave, s0, s1);
+      over(all.slice.dS, KEYS, wave, d0, d1);
+#pragma unroll
+      for (int I = 0; I < NB; ++I) {
+        Piece<TI> o0, o1;
+        Piece<TO> x0, x1;
+        rows_of(all.slice.dO, I, 0, lane, o0, o1);
+        mma<TO, TI>(sq[I], s0, s1, o0, o1);
+        over(all.slice.dR, FRAMES, I, x0, x1);
+        mma<TO, TO>(sk[I], s0, s1, x0, x1);
+        over(all.slice.u, FRAMES, I, x0, x1);
+        mma<TO, TO>(su[I], d0, d1, x0, x1);
       }
 #pragma unroll
-      for (int k = 0; k < 5; ++k) {  // ten tiles of U dO^T, ten of U dR^T
-        const int job = wave + WAVES * k, at = job < 10 ? job : job - 10;
-        const int I = at >= 6 ? 3 : at >= 3 ? 2 : at >= 1 ? 1 : 0, J = at - lower(I, 0);
-        Piece<TO> u0, u1;
-        slice_row<TO, Keys<T, DKP>::PITCH>(all.rows.u, J, lane, u0, u1);
-        if (job < 10) {
-          Piece<TI> x0, x1;
-          slice_row<TI, Keys<T, DKP>::PITCH>(all.rows.dO, I, lane, x0, x1);
-          mma<TO, TI>(pair[k], u0, u1, x0, x1);
-        } else {
-          Piece<TO> x0, x1;
-          slice_row<TO, Keys<T, DKP>::PITCH>(all.rows.dR, I, lane, x0, x1);
-          mma<TO, TO>(pair[k], u0, u1, x0, x1);
-        }
-      }
-#pragma unroll
-      for (int m = 0; m < KM; ++m) {
-        const int row = 16 * (wave + WAVES * m) + l16, c = c0 + 4 * g4;
-        const Piece<TO> s0 = split<TO>(state4(S, row, c, a)), s1 = split<TO>(state4(S, row, c + 16, a));
-        const Piece<TO> d0 = split<TO>(state4(dS, row, c, a)), d1 = split<TO>(state4(dS, row, c + 16, a));
-#pragma unroll
-        for (int I = 0; I < NB; ++I) {
-          Piece<TI> o0, o1;
-          Piece<TO> x0, x1;
-          slice_row<TI, Keys<T, DKP>::PITCH>(all.rows.dO, I, lane, o0, o1);
-          mma<TO, TI>(sq[m][I], s0, s1, o0, o1);
-          slice_row<TO, Keys<T, DKP>::PITCH>(all.rows.dR, I, lane, x0, x1);
-          mma<TO, TO>(sk[m][I], s0, s1, x0, x1);
-          slice_row<TO, Keys<T, DKP>::PITCH>(all.rows.u, I, lane, x0, x1);
-          mma<TO, TO>(su[m][I], d0, d1, x0, x1);
-        }
+      for (int k = 0; k < (10 + W - 1) / W; ++k) {  // ten tiles of U dO^T and of U dR^T
+        const int at = wave + W * k;
+        if (at >= 10) break;
+        const int I = block_row(at), J = at - lower(I, 0);
+        Piece<TI> o0, o1;
+        Piece<TO> u0, u1, x0, x1;
+        over(all.slice.u, FRAMES, J, u0, u1);
+        rows_of(all.slice.dO, I, 0, lane, o0, o1);
+        mma<TO, TI>(pair_q[k], u0, u1, o0, o1);
+        over(all.slice.dR, FRAMES, I, x0, x1);
+        mma<TO, TO>(pair_k[k], u0, u1, x0, x1);
       }
       __syncthreads();
     }
+    fk.lengths(s.rk, a.eps, left);
+    fq.lengths(s.rq, a.eps, left);
+    fk.store(all.pairs.k);
+    fq.store(all.pairs.q);
+    fg.store(s, a.c * softplus(a.lam[hd.h]), left, 0);
+    __syncthreads();
+    if (wave == W - 1) combine(s, lane);
 #pragma unroll
-    for (int k = 0; k < 5; ++k) {
-      const int job = wave + WAVES * k, at = job < 10 ? job : job - 10;
-      const int I = at >= 6 ? 3 : at >= 3 ? 2 : at >= 1 ? 1 : 0, J = at - lower(I, 0), i = 16 * I + l16;
+    for (int k = 0; k < (10 + W - 1) / W; ++k) {
+      const int at = wave + W * k;
+      if (at >= 10) break;
+      const int I = block_row(at), J = at - lower(I, 0), i = 16 * I + l16;
       const f32x4_t ch = rows4(s.ch, J, lane), cl = rows4(s.cl, J, lane), rk = rows4(s.rk, J, lane);
-      const float hi = s.ch[i], lo = s.cl[i], f = job < 10 ? s.rq[i] : -s.beta[i] * s.rk[i];
-      f32x4_t v;
+      const float hi = s.ch[i], lo = s.cl[i], f = s.rq[i], h = -s.beta[i] * s.rk[i];
+      f32x4_t x, y;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int j = 16 * J + 4 * g4 + r;
-        const bool on = job < 10 ? j <= i : j < i;
-        v[r] = on ? f * rk[r] * pair[k][r] * expf((hi - ch[r]) + (lo - cl[r])) : 0.f;
+        const float m = rk[r] * __builtin_amdgcn_exp2f((hi - ch[r]) + (lo - cl[r]));
+        x[r] = j <= i ? f * m * pair_q[k][r] : 0.f;
+        y[r] = j < i ? h * m * pair_k[k][r] : 0.f;
       }
-      const Piece<TO> p = split<TO>(v);
+      const Piece<TO> p = split<TO>(x), q = split<TO>(y);
 #pragma unroll
-      for (int e = 0; e < TO; ++e)
-        *reinterpret_cast<uint2*>((job < 10 ? all.blocks.qk[at][e] : all.blocks.kk[at][e]) + l16 * 32 + g4 * 8) = p.t[e];
+      for (int e = 0; e < TO; ++e) {
+        *reinterpret_cast<u32x2_t*>(all.pairs.qk[at][e] + l16 * 32 + g4 * 8) = p.t[e];
+        *reinterpret_cast<u32x2_t*>(all.pairs.kk[at][e] + l16 * 32 + g4 * 8) = q.t[e];
+      }
     }
     __syncthreads();
 #pragma unroll
-    for (int m = 0; m < KM; ++m) {
-      const int tile = wave + WAVES * m;
+    for (int I = 0; I < NB; ++I) {
+      const int i = 16 * I + l16;
+      dq[I] += sq[I] * s.gq[i];
+      dk[I] += su[I] * s.gk[i] - sk[I] * s.bgk[i];
+    }
 #pragma unroll
-      for (int I = 0; I < NB; ++I) {
-        const float gq = s.gq[16 * I + l16], bgk = s.bgk[16 * I + l16], gk = s.gk[16 * I + l16];
-        dq[m][I] += sq[m][I] * gq;
-        dk[m][I] += su[m][I] * gk - sk[m][I] * bgk;
-      }
+    for (int I = 0; I < NB; ++I) {
+      const Piece<TI> kI = columns_of(all.pairs.k, wave, I, lane), qI = columns_of(all.pairs.q, wave, I, lane);
 #pragma unroll
-      for (int I = 0; I < NB; ++I) {
-        const Piece<TI> kI = columns_of<T, DKP>(s.k, tile, I, lane), qI = columns_of<T, DKP>(s.q, tile, I, lane);
-#pragma unroll
-        for (int J = 0; J < NB; ++J) {
-          if (J >= I) mma<TI, TO>(dq[m][J], kI, block_of(all.blocks.qk[lower(J, I)], lane));
-          if (J <= I) mma<TI, TO>(dk[m][J], qI, block_turned(all.blocks.qk[lower(I, J)], lane));
-          if (J >= I) mma<TI, TO>(dk[m][J], kI, block_of(all.blocks.kk[lower(J, I)], lane));
-          if (J <= I) mma<TI, TO>(dk[m][J], kI, block_turned(all.blocks.kk[lower(I, J)], lane));
-        }
+      for (int J = 0; J < NB; ++J) {
+        if (J >= I) mma<TI, TO>(dq[J], kI, block_of(all.pairs.qk[lower(J, I)], lane));
+        if (J <= I) mma<TI, TO>(dk[J], qI, block_turned(all.pairs.qk[lower(I, J)], lane));
+        if (J >= I) mma<TI, TO>(dk[J], kI, block_of(all.pairs.kk[lower(J, I)], lane));
+        if (J <= I) mma<TI, TO>(dk[J], kI, block_turned(all.pairs.kk[lower(I, J)], lane));
       }
     }
     if (member + 1 < group) __syncthreads();
   }
   // through the lengths: dq = t - q rq^2 (q . t), t what has been summed
-  const Head hd(a, (int)((int64_t)b * a.H + kh * group));
-  auto elements = [&](const uint8_t (&m)[TI][C * Staged<T, DKP>::PITCH], int tile, int I) {
-    f32x4_t v = zero;
-    const int at = (16 * I + l16) * Staged<T, DKP>::PITCH + (tile >> 1) * 64 + (g4 * 2 + (tile & 1)) * 8;
-#pragma unroll
-    for (int e = TI - 1; e >= 0; --e) {
-      const uint2 w = *reinterpret_cast<const uint2*>(m[e] + at);
-      v += f32x4_t{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                   __uint_as_float(w.y & 0xffff0000u)};
-    }
-    return v;
-  };
+  const int left = (a.lens ? a.lens[b] : a.T) - t0;
 #pragma unroll
   for (int I = 0; I < NB; ++I) {
-    float x = 0.f, y = 0.f;
-#pragma unroll
-    for (int m = 0; m < KM; ++m) {
-      const f32x4_t q = elements(s.q, wave + WAVES * m, I), k = elements(s.k, wave + WAVES * m, I);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x = fmaf(q[r], dq[m][I][r], x), y = fmaf(k[r], dk[m][I][r], y);
-    }
+    const f32x4_t q = values(row4_of(all.pairs.q, I, wave, lane)) * dq[I], k = values(row4_of(all.pairs.k, I, wave, lane)) * dk[I];
+    float x = (q[0] + q[1]) + (q[2] + q[3]), y = (k[0] + k[1]) + (k[2] + k[3]);
     x += __shfl_xor(x, 16, 64);
     y += __shfl_xor(y, 16, 64);
     x += __shfl_xor(x, 32, 64);
@@ -467,36 +431,16 @@ __global__ __launch_bounds__(THREADS) void gd_keys_kernel(GatedDelta a) {
   __syncthreads();
 #pragma unroll
   for (int I = 0; I < NB; ++I) {
-    const int i = 16 * I + l16, t = t0 + i;
-    const float x = (all.dots[0][0][i] + all.dots[0][1][i]) + (all.dots[0][2][i] + all.dots[0][3][i]);
-    const float y = (all.dots[1][0][i] + all.dots[1][1][i]) + (all.dots[1][2][i] + all.dots[1][3][i]);
-    const float fq = s.rq[i] * s.rq[i] * x, fk = s.rk[i] * s.rk[i] * y;
-    if (t >= hd.len) continue;
-    const int64_t row = hd.row(t);
+    const int i = 16 * I + l16, cols = a.dk - 16 * wave - 4 * g4;
+    float x = 0.f, y = 0.f;
 #pragma unroll
-    for (int m = 0; m < KM; ++m) {
-      const int tile = wave + WAVES * m, c = 16 * tile + 4 * g4;
-      const f32x4_t vq = dq[m][I] - elements(s.q, tile, I) * fq, vk = dk[m][I] - elements(s.k, tile, I) * fk;
-      T* const pq = static_cast<T*>(a.dq) + row * a.lddq + (int64_t)kh * a.dk + c;
-      T* const pk = static_cast<T*>(a.dk_) + row * a.lddk + (int64_t)kh * a.dk + c;
-      if (c + 4 <= a.dk) {
-        if constexpr (sizeof(T) == 2) {
-          typedef uint32_t u32x2_u __attribute__((ext_vector_type(2), aligned(2)));
-          *reinterpret_cast<u32x2_u*>(pq) = u32x2_u{pair_bf16(vq[0], vq[1]), pair_bf16(vq[2], vq[3])};
-          *reinterpret_cast<u32x2_u*>(pk) = u32x2_u{pair_bf16(vk[0], vk[1]), pair_bf16(vk[2], vk[3])};
-        } else {
-          *reinterpret_cast<f32x4_a*>(pq) = vq;
-          *reinterpret_cast<f32x4_a*>(pk) = vk;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 3; ++j)
-          if (c + j < a.dk) {
-            pq[j] = from_f32<T>(vq[j]);
-            pk[j] = from_f32<T>(vk[j]);
-          }
-      }
-    }
+    for (int w = 0; w < W; ++w) x += all.dots[0][w][i], y += all.dots[1][w][i];
+    const f32x4_t vq = dq[I] - values(row4_of(all.pairs.q, I, wave, lane)) * (s.rq[i] * s.rq[i] * x);
+    const f32x4_t vk = dk[I] - values(row4_of(all.pairs.k, I, wave, lane)) * (s.rk[i] * s.rk[i] * y);
+    if (i >= left) continue;
+    const int64_t row = s.row[0][i], at = (int64_t)kh * a.dk + 16 * wave + 4 * g4;
+    put4(static_cast<T*>(a.dq) + row * a.lddq + at, cols, vq);
+    put4(static_cast<T*>(a.dk_) + row * a.lddk + at, cols, vk);
   }
 }
 
@@ -508,23 +452,23 @@ __global__ __launch_bounds__(1024) void gd_dlam_kernel(GatedDelta a) {
   if (threadIdx.x < 32 && h < a.H) a.dlam[h] = s / (1.f + expf(-a.lam[h]));
 }
 
-template <typename T, int DKP, int NT> hipError_t backward(const GatedDelta& a, hipStream_t s) {
-  constexpr int LDS = sizeof(Backward<T, DKP>), KEYS = sizeof(Keys<T, DKP>);
+template <typename T, int DKP, int W> hipError_t backward(const GatedDelta& a, hipStream_t s) {
+  constexpr int LDS = sizeof(Backward<T, DKP, W>), KEYS = sizeof(Keys<T, DKP>);
   static_assert(LDS <= 160 * 1024 && KEYS <= 160 * 1024, "a workgroup's LDS");
   static PerDevice ready, ready_keys;
-  hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_backward_kernel<T, DKP, NT>), ready);
-  if (e == hipSuccess) e = allow_lds<KEYS>(reinterpret_cast<const void*>(&gd_keys_kernel<T, DKP>), ready_keys);
+  hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_backward_kernel<T, DKP, W>), ready);
+  if (e == hipSuccess) e = allow_lds<KEYS>(reinterpret_cast<const void*>(&gd_keys_kernel<T, DKP, 16 * W>), ready_keys);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((gd_backward_kernel<T, DKP, NT>), dim3((unsigned)(a.B * a.H)), dim3(THREADS), LDS, s, a);
+  hipLaunchKernelGGL((gd_backward_kernel<T, DKP, W>), dim3((unsigned)(a.B * a.H)), dim3(threads_of<W>), LDS, s, a);
   const unsigned chunks = (unsigned)((a.T + C - 1) / C) * a.B * a.G;
-  if (chunks) hipLaunchKernelGGL((gd_keys_kernel<T, DKP>), dim3(chunks), dim3(THREADS), KEYS, s, a);
+  if (chunks) hipLaunchKernelGGL((gd_keys_kernel<T, DKP, 16 * W>), dim3(chunks), dim3(DKP * 4), KEYS, s, a);
   hipLaunchKernelGGL(gd_dlam_kernel, dim3((unsigned)((a.H + 31) / 32)), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename T> hipError_t sized(const GatedDelta& a, hipStream_t s) {
-  if (a.dk <= 64) return a.dv <= 64 ? backward<T, 64, 1>(a, s) : backward<T, 64, 2>(a, s);
-  return a.dv <= 64 ? backward<T, 128, 1>(a, s) : backward<T, 128, 2>(a, s);
+  if (a.dk <= 64) return a.dv <= 64 ? backward<T, 64, 4>(a, s) : backward<T, 64, 8>(a, s);
+  return a.dv <= 64 ? backward<T, 128, 4>(a, s) : backward<T, 128, 8>(a, s);
 }
 
 }  // namespace
