@@ -159,7 +159,9 @@ template <typename T, int DKP, int W, int PT, int R> struct Chunk {
   Gates s;
 };
 
-// Eight columns of a row as they lie in memory.
+// Eight columns of a row as they lie in memory.  load(p, left): `left` of them are there,
+// which may be none; what lies before the row's end is read in their place, so that
+// lanes without them need no branch.
 template <typename T> struct Eight;
 template <> struct Eight<bf16_t> {
   uint32_t w[4];
@@ -172,9 +174,11 @@ template <> struct Eight<bf16_t> {
     for (int i = 0; i < 4; ++i) w[i] = u[i];
   }
   __device__ __forceinline__ void load(const bf16_t* p, int left) {
+    uint32_t x[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = (2 * i < left ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+    for (int i = 0; i < 8; ++i) x[i] = p[min(i, left - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (2 * i < left ? x[2 * i] : 0u) | (2 * i + 1 < left ? x[2 * i + 1] << 16 : 0u);
   }
 };
 template <> struct Eight<float> {
@@ -188,7 +192,10 @@ template <> struct Eight<float> {
   }
   __device__ __forceinline__ void load(const float* p, int left) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = i < left ? p[i] : 0.f;
+    for (int i = 0; i < 8; ++i) {
+      const float x = p[min(i, left - 1)];
+      v[i >> 2][i & 3] = i < left ? x : 0.f;
+    }
   }
 };
 // What terms stand for.
@@ -220,6 +227,18 @@ __device__ __forceinline__ void put4(float* p, int left, f32x4_t v) {
       if (j < left) p[j] = v[j];
   }
 }
+
+// A thread's number, which the compiler takes for another one in each turn of a loop:
+// what is made from it is made again there, a few instructions, where it would be kept
+// through the loop in more registers than there are.
+__device__ __forceinline__ int this_thread() {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+
+// The column of v that a thread's lane has.
+__device__ __forceinline__ int column_of(int tid) { return (tid >> 6) * 16 + (tid & 15); }
 
 // The sequence and head of a workgroup.
 struct Head {
@@ -268,20 +287,23 @@ template <typename T, int COLS, int W> struct Rows {
   static constexpr int PER_ROW = COLS / 8, PIECES = C * PER_ROW / threads_of<W>;
   static_assert(PIECES >= 1, "every thread has a piece");
   Eight<T> v[PIECES];
-  __device__ __forceinline__ void from(const void* m, int64_t ld, int head, int dim, const int32_t (&rows)[C]) {
+  __device__ __forceinline__ void from(const void* m, int64_t ld, int head, int dim, const int32_t (&rows)[C], int tid) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int at = threadIdx.x + i * threads_of<W>, u = at % PER_ROW, left = dim - 8 * u;
+      const int at = tid + i * threads_of<W>, u = at % PER_ROW, left = dim - 8 * u;
       const T* p = static_cast<const T*>(m) + rows[at / PER_ROW] * ld + (int64_t)head * dim + 8 * u;
-      if (dim == COLS || left >= 8) v[i].load(p);
-      else if (left > 0) v[i].load(p, left);
-      else v[i].zero();
+      if (dim % 8 == 0) {
+        v[i].load(p + min(left - 8, 0));
+        if (dim < COLS && left < 8) v[i].zero();
+      } else {
+        v[i].load(p, left);
+      }
     }
   }
-  __device__ __forceinline__ void store(Matrix<Terms<T>::IN, COLS>& m) const {
+  __device__ __forceinline__ void store(Matrix<Terms<T>::IN, COLS>& m, int tid) const {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int at = threadIdx.x + i * threads_of<W>, u = at % PER_ROW;
+      const int at = tid + i * threads_of<W>, u = at % PER_ROW;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int p = 2 * (u & 3) + half, slot = (p & 3) * 2 + (p >> 2);  // of the eight pieces of 32 columns
@@ -293,10 +315,10 @@ template <typename T, int COLS, int W> struct Rows {
     }
   }
   // 1 / sqrt(sum of squares + eps) of each row; 0 from row `left` on
-  __device__ __forceinline__ void lengths(float (&out)[C], float eps, int left) const {
+  __device__ __forceinline__ void lengths(float (&out)[C], float eps, int left, int tid) const {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int at = threadIdx.x + i * threads_of<W>, row = at / PER_ROW;
+      const int at = tid + i * threads_of<W>, row = at / PER_ROW;
       float s = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) s = fmaf(v[i].at(j), v[i].at(j), s);
@@ -311,11 +333,11 @@ template <typename T, int W> struct Values;
 template <int W> struct Values<bf16_t, W> {
   Rows<bf16_t, 16 * W, W> v;
   const Matrix<1, 16 * W>* m;
-  __device__ __forceinline__ void from(const void* p, int64_t ld, const Head& hd, int dv, const int32_t (&rows)[C]) {
-    v.from(p, ld, hd.h, dv, rows);
+  __device__ __forceinline__ void from(const void* p, int64_t ld, const Head& hd, int dv, const int32_t (&rows)[C], int tid) {
+    v.from(p, ld, hd.h, dv, rows, tid);
   }
-  __device__ __forceinline__ void store(Matrix<1, 16 * W>* to, const int32_t (&)[C]) {
-    v.store(*to);
+  __device__ __forceinline__ void store(Matrix<1, 16 * W>* to, const int32_t (&)[C], int tid) {
+    v.store(*to, tid);
     m = to;
   }
   // columns 16 t + lane % 16 over frames of block I; row 16 I + lane % 16, columns 16 t + 4 (lane / 16) and on
@@ -328,29 +350,36 @@ template <int W> struct Values<float, W> {
   int64_t ld;
   int dv;
   const int32_t* rows;
-  __device__ __forceinline__ void from(const void* m, int64_t stride, const Head& hd, int cols, const int32_t (&)[C]) {
+  __device__ __forceinline__ void from(const void* m, int64_t stride, const Head& hd, int cols, const int32_t (&)[C], int) {
     p = static_cast<const float*>(m) + (int64_t)hd.h * cols;
     ld = stride;
     dv = cols;
   }
-  __device__ __forceinline__ void store(Matrix<1, 16 * W>*, const int32_t (&at)[C]) { rows = at; }
+  __device__ __forceinline__ void store(Matrix<1, 16 * W>*, const int32_t (&at)[C], int) { rows = at; }
   __device__ __forceinline__ f32x4_t column_values(int t, int I, int lane) const {
     const int col = 16 * t + (lane & 15);
-    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-    if (col < dv)
+    f32x4_t v;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = p[rows[16 * I + 4 * (lane >> 4) + r] * ld + col];
+    for (int r = 0; r < 4; ++r) {
+      const float x = p[rows[16 * I + 4 * (lane >> 4) + r] * ld + min(col, dv - 1)];
+      v[r] = col < dv ? x : 0.f;
+    }
     return v;
   }
   __device__ __forceinline__ Piece<3> column(int t, int I, int lane) const { return split<3>(column_values(t, I, lane)); }
   __device__ __forceinline__ f32x4_t row_values(int I, int t, int lane) const {
     const int col = 16 * t + 4 * (lane >> 4);
     const float* const at = p + rows[16 * I + (lane & 15)] * ld + col;
-    if (col + 4 <= dv) return *reinterpret_cast<const f32x4_a*>(at);
-    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+    f32x4_t v;
+    if (dv % 4 == 0) {
+      v = *reinterpret_cast<const f32x4_a*>(at + min(dv - 4 - col, 0));
+      return col < dv ? v : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
 #pragma unroll
-    for (int j = 0; j < 3; ++j)
-      if (col + j < dv) v[j] = at[j];
+    for (int j = 0; j < 4; ++j) {
+      const float x = at[min(j, dv - 1 - col)];
+      v[j] = col + j < dv ? x : 0.f;
+    }
     return v;
   }
 };
@@ -358,19 +387,19 @@ template <int W> struct Values<float, W> {
 template <typename T, int W> struct GateRows {
   T r, b;
   int next;
-  __device__ __forceinline__ static bool mine() { return threadIdx.x >= threads_of<W> - C; }
-  __device__ __forceinline__ void from(const GatedDelta& a, const Head& hd, const int32_t (&rows)[C], int next0) {
-    if (!mine()) return;
-    const int t = threadIdx.x & 63;
+  __device__ __forceinline__ static bool mine(int tid) { return tid >= threads_of<W> - C; }
+  __device__ __forceinline__ void from(const GatedDelta& a, const Head& hd, const int32_t (&rows)[C], int next0, int tid) {
+    if (!mine(tid)) return;
+    const int t = tid & 63;
     const int64_t row = rows[t];
     r = static_cast<const T*>(a.r)[row * a.ldr + hd.h];
     b = static_cast<const T*>(a.b)[row * a.ldb + hd.h];
     next = hd.row(a, next0 + t);
   }
   // `left`: frames that the sequence has from here on
-  __device__ __forceinline__ void store(Gates& s, float rate, int left, int turn) const {
-    if (!mine()) return;
-    const int t = threadIdx.x & 63;
+  __device__ __forceinline__ void store(Gates& s, float rate, int left, int turn, int tid) const {
+    if (!mine(tid)) return;
+    const int t = tid & 63;
     const bool live = t < left;
     const double c = sums_before(live ? (double)(-rate * sigm(to_f32(r))) * 1.4426950408889634 : 0.0);
     const double last = __shfl(c, C - 1, 64);
@@ -462,9 +491,9 @@ template <int J> __device__ __forceinline__ void substitute(float (&x)[16], cons
 
 // L, P and the inverses of I + L's diagonal blocks from a staged chunk (behind a
 // barrier; ends with one).
-template <typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ void triangles(Chunk<T, DKP, W, PT, R>& c) {
+template <typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ void triangles(Chunk<T, DKP, W, PT, R>& c, int tid) {
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
   Gates& s = c.s;
   if (wave == W - 1) combine(s, lane);
 #pragma unroll
@@ -551,21 +580,26 @@ __device__ __forceinline__ void solve(const Ch& c, int lane, f32x4_t (&u)[NB], P
 template <int DKP>
 __device__ __forceinline__ void load_state(const float* m, const GatedDelta& a, int col, int lane, f32x4_t (&S)[DKP / 16]) {
 #pragma unroll
+  for (int t = 0; t < DKP / 16; ++t) S[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  if (!m) return;
+#pragma unroll
   for (int t = 0; t < DKP / 16; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = 16 * t + 4 * (lane >> 4) + r;
-      S[t][r] = m && row < a.dk && col < a.dv ? m[row * a.dv + col] : 0.f;
+      const float x = m[min(row, a.dk - 1) * a.dv + min(col, a.dv - 1)];
+      S[t][r] = row < a.dk && col < a.dv ? x : 0.f;
     }
 }
 template <int DKP>
 __device__ __forceinline__ void store_state(float* m, const GatedDelta& a, int col, int lane, const f32x4_t (&S)[DKP / 16]) {
+  if (col >= a.dv) return;
 #pragma unroll
   for (int t = 0; t < DKP / 16; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = 16 * t + 4 * (lane >> 4) + r;
-      if (row < a.dk && col < a.dv) m[row * a.dv + col] = S[t][r];
+      if (a.dk == DKP || row < a.dk) m[row * a.dv + col] = S[t][r];
     }
 }
 // ... and where the passes keep it, a padded column after another.

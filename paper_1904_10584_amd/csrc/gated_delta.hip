@@ -16,40 +16,40 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_forward_kernel(GatedDelta
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT, KT = DKP / 16;
   Chunk<T, DKP, W, TO, 1>& c = *reinterpret_cast<Chunk<T, DKP, W, TO, 1>*>(lds);
   Gates& s = c.s;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4, col = 16 * wave + l16;
   const Head hd(a, blockIdx.x);
   const float rate = a.c * softplus(a.lam[hd.h]);
   const int64_t mine = (int64_t)blockIdx.x * a.dk * a.dv;
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   f32x4_t S[KT];
-  load_state<DKP>(a.s0 ? a.s0 + mine : nullptr, a, col, lane, S);
+  load_state<DKP>(a.s0 ? a.s0 + mine : nullptr, a, column_of(threadIdx.x), threadIdx.x & 63, S);
   Rows<T, DKP, W> fk, fq;
   Values<T, W> fv;
   GateRows<T, W> fg;
-  auto fetch = [&](const int32_t (&rows)[C], int next0) {
-    fk.from(a.k, a.ldk, hd.kh, a.dk, rows);
-    fq.from(a.q, a.ldq, hd.kh, a.dk, rows);
-    fv.from(a.v, a.ldv, hd, a.dv, rows);
-    fg.from(a, hd, rows, next0);
+  auto fetch = [&](const int32_t (&rows)[C], int next0, int tid) {
+    fk.from(a.k, a.ldk, hd.kh, a.dk, rows, tid);
+    fq.from(a.q, a.ldq, hd.kh, a.dk, rows, tid);
+    fv.from(a.v, a.ldv, hd, a.dv, rows, tid);
+    fg.from(a, hd, rows, next0, tid);
   };
   if (hd.len > 0) {
     if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, threadIdx.x);
     __syncthreads();
-    fetch(s.row[0], C);
+    fetch(s.row[0], C, threadIdx.x);
   }
   int turn = 0;
   for (int t0 = 0; t0 < hd.len; t0 += C, turn ^= 1) {
-    const int left = hd.len - t0;
+    const int left = hd.len - t0, tid = this_thread(), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = 16 * wave + l16;
     if (a.train && t0 > 0) store_kept<DKP>(kept_before<DKP, W>(a, t0 / C, blockIdx.x), col, lane, S);
-    fk.lengths(s.rk, a.eps, left);
-    fq.lengths(s.rq, a.eps, left);
-    fk.store(c.k);
-    fq.store(c.q);
-    fv.store(&c.v[0], s.row[turn]);
-    fg.store(s, rate, left, turn);
+    fk.lengths(s.rk, a.eps, left, tid);
+    fq.lengths(s.rq, a.eps, left, tid);
+    fk.store(c.k, tid);
+    fq.store(c.q, tid);
+    fv.store(&c.v[0], s.row[turn], tid);
+    fg.store(s, rate, left, turn, tid);
     __syncthreads();
-    if (left > C) fetch(s.row[turn ^ 1], t0 + 2 * C);  // the next chunk's, which arrive during this one
-    triangles(c);
+    if (left > C) fetch(s.row[turn ^ 1], t0 + 2 * C, tid);  // the next chunk's, which arrive during this one
+    triangles(c, tid);
 
     f32x4_t u[NB], o[NB];
 #pragma unroll
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_forward_kernel(GatedDelta
     }
     __syncthreads();
   }
-  if (a.sT) store_state<DKP>(a.sT + mine, a, col, lane, S);
+  if (a.sT) store_state<DKP>(a.sT + mine, a, column_of(threadIdx.x), threadIdx.x & 63, S);
 }
 
 // One frame of each sequence: a state is read once, kept in registers, and written

@@ -33,48 +33,48 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
   Backward<T, DKP, W>& all = *reinterpret_cast<Backward<T, DKP, W>*>(lds);
   auto& c = all.c;
   Gates& s = c.s;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4, col = 16 * wave + l16;
   const int64_t bh = blockIdx.x, state = (int64_t)a.dk * a.dv;
   const Head hd(a, blockIdx.x);
   const float rate = a.c * softplus(a.lam[hd.h]);
   const int chunks = (hd.len + C - 1) / C;
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   f32x4_t dS[KT];
-  load_state<DKP>(a.dsT ? a.dsT + bh * state : nullptr, a, col, lane, dS);
+  load_state<DKP>(a.dsT ? a.dsT + bh * state : nullptr, a, column_of(threadIdx.x), threadIdx.x & 63, dS);
   Rows<T, DKP, W> fk, fq;
   Values<T, W> fv, fo;
   GateRows<T, W> fg;
-  auto fetch = [&](const int32_t (&rows)[C], int next0) {
-    fk.from(a.k, a.ldk, hd.kh, a.dk, rows);
-    fq.from(a.q, a.ldq, hd.kh, a.dk, rows);
-    fv.from(a.v, a.ldv, hd, a.dv, rows);
-    fo.from(a.d_o, a.lddo, hd, a.dv, rows);
-    fg.from(a, hd, rows, next0);
+  auto fetch = [&](const int32_t (&rows)[C], int next0, int tid) {
+    fk.from(a.k, a.ldk, hd.kh, a.dk, rows, tid);
+    fq.from(a.q, a.ldq, hd.kh, a.dk, rows, tid);
+    fv.from(a.v, a.ldv, hd, a.dv, rows, tid);
+    fo.from(a.d_o, a.lddo, hd, a.dv, rows, tid);
+    fg.from(a, hd, rows, next0, tid);
   };
   if (chunks) {
     if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, (chunks - 1) * C + threadIdx.x);
     __syncthreads();
-    fetch(s.row[0], max(chunks - 2, 0) * C);
+    fetch(s.row[0], max(chunks - 2, 0) * C, threadIdx.x);
   }
   float dlam = 0.f;  // (of a frame a lane of every chunk, in the last wave)
   int turn = 0;
   for (int n = chunks - 1; n >= 0; --n, turn ^= 1) {
-    const int left = hd.len - n * C;
+    const int left = hd.len - n * C, tid = this_thread(), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = 16 * wave + l16;
     const T r_now = fg.r;
     store_kept<DKP>(kept_after<DKP, W>(a, n, bh), col, lane, dS);
-    fk.lengths(s.rk, a.eps, left);
-    fq.lengths(s.rq, a.eps, left);
-    fk.store(c.k);
-    fq.store(c.q);
-    fv.store(&c.v[0], s.row[turn]);
-    fo.store(&c.v[1], s.row[turn]);
-    fg.store(s, rate, left, turn);
+    fk.lengths(s.rk, a.eps, left, tid);
+    fq.lengths(s.rq, a.eps, left, tid);
+    fk.store(c.k, tid);
+    fq.store(c.q, tid);
+    fv.store(&c.v[0], s.row[turn], tid);
+    fo.store(&c.v[1], s.row[turn], tid);
+    fg.store(s, rate, left, turn, tid);
     __syncthreads();
-    if (n > 0) fetch(s.row[turn ^ 1], max(n - 2, 0) * C);  // the chunk before, which arrives during this one
+    if (n > 0) fetch(s.row[turn ^ 1], max(n - 2, 0) * C, tid);  // the chunk before, which arrives during this one
     f32x4_t S[KT];
     if (n > 0) load_kept<DKP>(kept_before<DKP, W>(a, n, bh), col, lane, S);
     else load_state<DKP>(a.s0 ? a.s0 + bh * state : nullptr, a, col, lane, S);
-    triangles(c);
+    triangles(c, tid);
 
     f32x4_t u[NB], o[NB], kd[NB];
 #pragma unroll
@@ -215,10 +215,10 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
     }
     __syncthreads();
   }
-  if (a.ds0) store_state<DKP>(a.ds0 + bh * state, a, col, lane, dS);
-  if (wave == W - 1) {
+  if (a.ds0) store_state<DKP>(a.ds0 + bh * state, a, column_of(threadIdx.x), threadIdx.x & 63, dS);
+  if (threadIdx.x >= threads_of<W> - 64) {
     dlam = wave_sum_uniform(dlam);
-    if (lane == 0) a.parts[bh] = a.c * dlam;
+    if (threadIdx.x == threads_of<W> - 64) a.parts[bh] = a.c * dlam;
   }
 }
 
@@ -269,9 +269,10 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
       if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, t0 + threadIdx.x);
       __syncthreads();
     }
-    fk.from(a.k, a.ldk, kh, a.dk, s.row[0]);
-    fq.from(a.q, a.ldq, kh, a.dk, s.row[0]);
-    fg.from(a, hd, s.row[0], t0);
+    const int tid = this_thread();
+    fk.from(a.k, a.ldk, kh, a.dk, s.row[0], tid);
+    fq.from(a.q, a.ldq, kh, a.dk, s.row[0], tid);
+    fg.from(a, hd, s.row[0], t0, tid);
     const float* const S = n > 0 ? kept_before<DKP, VW>(a, n, bh) : nullptr;
     const float* const S0 = a.s0 ? a.s0 + bh * ((int64_t)a.dk * a.dv) : nullptr;
     const float* const dS = kept_after<DKP, VW>(a, n, bh);
@@ -288,8 +289,7 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
         Eight<T> x;
         const T* const p = d_o + s.row[0][row] * a.lddo + c0 + 8 * u;
         if (more >= 8) x.load(p);
-        else if (more > 0) x.load(p, more);
-        else x.zero();
+        else x.load(p, more);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const int w = 2 * u + half, slot = (w & 3) * 2 + (w >> 2);
@@ -364,11 +364,11 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
       }
       __syncthreads();
     }
-    fk.lengths(s.rk, a.eps, left);
-    fq.lengths(s.rq, a.eps, left);
-    fk.store(all.pairs.k);
-    fq.store(all.pairs.q);
-    fg.store(s, a.c * softplus(a.lam[hd.h]), left, 0);
+    fk.lengths(s.rk, a.eps, left, tid);
+    fq.lengths(s.rq, a.eps, left, tid);
+    fk.store(all.pairs.k, tid);
+    fq.store(all.pairs.q, tid);
+    fg.store(s, a.c * softplus(a.lam[hd.h]), left, 0, tid);
     __syncthreads();
     if (wave == W - 1) combine(s, lane);
 #pragma unroll
