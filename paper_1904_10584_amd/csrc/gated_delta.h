@@ -147,15 +147,28 @@ struct Gates {
   int32_t row[2][C];           // the frames' rows, of this chunk and of the next one
 };
 template <int N, int COLS> struct Matrix { uint8_t at[N][C * pitch_of(COLS)]; };  // in N terms
-// PT: terms of P; R: matrices like v (v, and in the backward pass dO).
-// (Inputs in fp32 would not leave room for those: they stay in memory.)
-template <typename T, int DKP, int W, int PT, int R> struct Chunk {
+// PT: terms of P; R: matrices like v (v, and in the backward pass dO).  (Inputs in fp32
+// would not leave room for those: they stay in memory.)  In the forward pass v has been
+// read when L is written, and everywhere n when d is: with 46 instead of 60 KiB three
+// workgroups with heads of 64 x 64 share a CU.
+template <int TI, int TX, int W, int R> struct Below {
+  Matrix<1, 16 * W> v[TI == 1 ? R : 0];
+  uint8_t l[6][TX][512];                     // blocks of 16 x 16 of -L below the diagonal
+};
+template <int TX, int W> struct Below<1, TX, W, 1> {
+  union {
+    Matrix<1, 16 * W> v[1];
+    uint8_t l[6][TX][512];
+  };
+};
+template <typename T, int DKP, int W, int PT, int R> struct Chunk : Below<Terms<T>::IN, Terms<T>::X, W, R> {
   static constexpr int TI = Terms<T>::IN, TX = Terms<T>::X;
   Matrix<TI, DKP> k, q;
-  Matrix<1, 16 * W> v[TI == 1 ? R : 0];
-  uint8_t l[6][TX][512], d[NB][TX][512], p[10][PT][512];  // blocks of 16 x 16: -L below the diagonal,
-                                                          // (I + L)^-1 on it, P
-  float n[NB][16][20];         // L on the diagonal, transposed
+  union {
+    float n[NB][16][20];                     // -L on the diagonal, transposed
+    uint8_t d[NB][TX][512];                  // (I + L)^-1 there
+  };
+  uint8_t p[10][PT][512];                    // blocks of P
   Gates s;
 };
 
@@ -480,63 +493,73 @@ __device__ __forceinline__ void combine(Gates& s, int t) {
   s.gk[t] = s.end[t] * s.rk[t];
 }
 
-// x_i -= n_i of lane J, x_J, for every i below J; and so on from column J + 1.
+// x_i += n_i of lane J, x_J, for every i below J; and so on from column J + 1.
 template <int J> __device__ __forceinline__ void substitute(float (&x)[16], const float (&n)[16]) {
   if constexpr (J < 15) {
 #pragma unroll
-    for (int i = J + 1; i < 16; ++i) x[i] = fmaf(-lanes_moved<0x150 + J>(n[i]), x[J], x[i]);
+    for (int i = J + 1; i < 16; ++i) x[i] = fmaf(lanes_moved<0x150 + J>(n[i]), x[J], x[i]);
     substitute<J + 1>(x, n);
   }
 }
 
-// L, P and the inverses of I + L's diagonal blocks from a staged chunk (behind a
-// barrier; ends with one).
-template <typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ void triangles(Chunk<T, DKP, W, PT, R>& c, int tid) {
+// Tile (I, J) of -L and P from K K^T and Q K^T.
+template <typename T, int DKP, int W, int PT, int R>
+__device__ __forceinline__ void tile(Chunk<T, DKP, W, PT, R>& c, int I, int J, int lane) {
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X;
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
-  Gates& s = c.s;
-  if (wave == W - 1) combine(s, lane);
+  const int l16 = lane & 15, g4 = lane >> 4, at = lower(I, J);
+  const Gates& s = c.s;
+  f32x4_t kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
 #pragma unroll
-  for (int at0 = 0; at0 < 10; at0 += W) {  // ten tiles of K K^T and of Q K^T
-    const int at = at0 + wave;
-    if (at >= 10) break;
-    const int I = block_row(at), J = at - lower(I, 0);
-    f32x4_t kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
-#pragma unroll
-    for (int t = 0; t < DKP / 32; ++t) {
-      Piece<TI> a0, a1, b0, b1;
-      rows_of(c.k, J, t, lane, a0, a1);
-      rows_of(c.k, I, t, lane, b0, b1);
-      mma<TI, TI>(kk, a0, a1, b0, b1);
-      rows_of(c.q, I, t, lane, b0, b1);
-      mma<TI, TI>(qk, a0, a1, b0, b1);
-    }
-    // a lane has row i and columns j, j + 1, ... of the tile
-    const int i = 16 * I + l16;
-    const f32x4_t ch = rows4(s.ch, J, lane), cl = rows4(s.cl, J, lane), rk = rows4(s.rk, J, lane);
-    const float hi = s.ch[i], lo = s.cl[i], fk = s.beta[i] * s.rk[i], fq = s.rq[i];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int j = 16 * J + 4 * g4 + r;
-      const float m = rk[r] * __builtin_amdgcn_exp2f((hi - ch[r]) + (lo - cl[r]));
-      kk[r] = j < i ? fk * kk[r] * m : 0.f;
-      qk[r] = j <= i ? fq * qk[r] * m : 0.f;
-    }
-    const Piece<PT> p = split<PT>(qk);
-#pragma unroll
-    for (int e = 0; e < PT; ++e) *reinterpret_cast<u32x2_t*>(c.p[at][e] + l16 * 32 + g4 * 8) = p.t[e];
-    if (I == J) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) c.n[I][4 * g4 + r][l16] = kk[r];
-    } else {
-      const Piece<TX> w = split<TX>(-kk);
-#pragma unroll
-      for (int e = 0; e < TX; ++e) *reinterpret_cast<u32x2_t*>(c.l[at - I][e] + l16 * 32 + g4 * 8) = w.t[e];
-    }
+  for (int t = 0; t < DKP / 32; ++t) {
+    Piece<TI> a0, a1, b0, b1;
+    rows_of(c.k, J, t, lane, a0, a1);
+    rows_of(c.k, I, t, lane, b0, b1);
+    mma<TI, TI>(kk, a0, a1, b0, b1);
+    rows_of(c.q, I, t, lane, b0, b1);
+    mma<TI, TI>(qk, a0, a1, b0, b1);
   }
+  // a lane has row i and columns j, j + 1, ... of the tile
+  const int i = 16 * I + l16;
+  const f32x4_t ch = rows4(s.ch, J, lane), cl = rows4(s.cl, J, lane), rk = rows4(s.rk, J, lane);
+  const float hi = s.ch[i], lo = s.cl[i], fk = -s.beta[i] * s.rk[i], fq = s.rq[i];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int j = 16 * J + 4 * g4 + r;
+    const float m = rk[r] * __builtin_amdgcn_exp2f((hi - ch[r]) + (lo - cl[r]));
+    kk[r] = j < i ? fk * kk[r] * m : 0.f;
+    qk[r] = j <= i ? fq * qk[r] * m : 0.f;
+  }
+  const Piece<PT> p = split<PT>(qk);
+#pragma unroll
+  for (int e = 0; e < PT; ++e) *reinterpret_cast<u32x2_t*>(c.p[at][e] + l16 * 32 + g4 * 8) = p.t[e];
+  if (I == J) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) c.n[I][4 * g4 + r][l16] = kk[r];
+  } else {
+    const Piece<TX> w = split<TX>(kk);
+#pragma unroll
+    for (int e = 0; e < TX; ++e) *reinterpret_cast<u32x2_t*>(c.l[at - I][e] + l16 * 32 + g4 * 8) = w.t[e];
+  }
+}
+
+// L, P and the inverses of I + L's diagonal blocks from a staged chunk (behind a
+// barrier; ends with one).  The first four waves make the tiles on the diagonal; then
+// one wave inverts, and the others make the six tiles below.
+template <typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ void triangles(Chunk<T, DKP, W, PT, R>& c, int tid) {
+  constexpr int TX = Terms<T>::X;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
+  if (wave < NB) tile(c, wave, wave, lane);
+  if (wave == W - 1) combine(c.s, lane);
   __syncthreads();
-  if (wave == 0) {  // 16 lanes a block, a column each: substitution
-    // (lane j of the 16 has column j of L, and gives its elements to the others)
+  if (wave > 0) {
+    constexpr int EACH = (6 + W - 2) / (W - 1);
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int at = min(wave - 1 + (W - 1) * k, 5), I = at >= 3 ? 3 : at >= 1 ? 2 : 1;
+      tile(c, I, at - below(I, 0), lane);
+    }
+  } else {  // 16 lanes a block, a column each: substitution
+    // (lane j of the 16 has column j of -L, and gives its elements to the others)
     float x[16], n[16];
 #pragma unroll
     for (int i4 = 0; i4 < 4; ++i4) {
@@ -561,18 +584,18 @@ template <typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ 
   __syncthreads();
 }
 
-// U's terms from R, block after block: (I + L) U = R.  R is left where U is made from:
-// R_I - sum L_IJ U_J, whose terms stay in r.
+// U's terms from R, block after block: (I + L) U = R; a block of U is taken from those
+// below it as soon as it is there.  What U_I is made from stays in r, as terms.
 template <typename Ch, int TX>
 __device__ __forceinline__ void solve(const Ch& c, int lane, f32x4_t (&u)[NB], Piece<TX> (&r)[NB], Piece<TX> (&up)[NB]) {
 #pragma unroll
   for (int I = 0; I < NB; ++I) {
-    if (I >= 2) mma<TX, TX>(u[I], block_of(c.l[below(I, 0)], lane), block_of(c.l[below(I, 1)], lane), up[0], up[1]);
-    if (I == 1 || I == 3) mma<TX, TX>(u[I], block_of(c.l[below(I, I - 1)], lane), up[I - 1]);
     r[I] = split<TX>(u[I]);
     u[I] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     mma<TX, TX>(u[I], block_of(c.d[I], lane), r[I]);
     up[I] = split<TX>(u[I]);
+#pragma unroll
+    for (int J = I + 1; J < NB; ++J) mma<TX, TX>(u[J], block_of(c.l[below(J, I)], lane), up[I]);
   }
 }
 

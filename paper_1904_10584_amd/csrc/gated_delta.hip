@@ -11,7 +11,7 @@ using namespace gd;
 constexpr int THREADS = 256, WAVES = 4;  // of a frame's kernel
 
 template <typename T, int DKP, int W>
-__global__ __launch_bounds__(threads_of<W>, 2) void gd_forward_kernel(GatedDelta a) {
+__global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2) void gd_forward_kernel(GatedDelta a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT, KT = DKP / 16;
   Chunk<T, DKP, W, TO, 1>& c = *reinterpret_cast<Chunk<T, DKP, W, TO, 1>*>(lds);
@@ -48,6 +48,9 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_forward_kernel(GatedDelta
     fv.store(&c.v[0], s.row[turn], tid);
     fg.store(s, rate, left, turn, tid);
     __syncthreads();
+    f32x4_t v[NB];
+#pragma unroll
+    for (int I = 0; I < NB; ++I) v[I] = fv.column_values(wave, I, lane);
     if (left > C) fetch(s.row[turn ^ 1], t0 + 2 * C, tid);  // the next chunk's, which arrive during this one
     triangles(c, tid);
 
@@ -68,7 +71,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_forward_kernel(GatedDelta
     }
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
-      u[I] = fv.column_values(wave, I, lane) * rows4(s.beta, I, lane) - u[I] * rows4(s.bgk, I, lane);
+      u[I] = v[I] * rows4(s.beta, I, lane) - u[I] * rows4(s.bgk, I, lane);
       o[I] *= s.gq[16 * I + l16];
     }
     Piece<TX> r[NB], up[NB];

@@ -142,14 +142,14 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
       Piece<TX> dp[NB];
 #pragma unroll
       for (int I = NB - 1; I >= 0; --I) {
-#pragma unroll
-        for (int J = NB - 1; J > I; --J) mma<TX, TX>(kd[I], block_turned(c.l[below(J, I)], lane), dp[J]);
         const Piece<TX> d = block_turned(c.d[I], lane), w = split<TX>(kd[I]);
         f32x4_t dr = zero;  // (transposed)
         mma<TX, TX>(dr, w, d);
         kd[I] = zero;
         mma<TX, TX>(kd[I], d, w);
         dp[I] = split<TX>(kd[I]);
+#pragma unroll
+        for (int J = I - 1; J >= 0; --J) mma<TX, TX>(kd[J], block_turned(c.l[below(I, J)], lane), dp[I]);
         const f32x4_t dv = dr * s.beta[16 * I + l16], x = dv * fv.row_values(I, wave, lane), y = dr * ut[I];
         y1[I] -= (x[0] + x[1]) + (x[2] + x[3]);
         y2[I] = (y[0] + y[1]) + (y[2] + y[3]);
@@ -283,42 +283,70 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
     for (int k = 0; k < (10 + W - 1) / W; ++k) pair_q[k] = pair_k[k] = zero;
 #pragma unroll
     for (int I = 0; I < NB; ++I) sq[I] = sk[I] = su[I] = zero;
-    for (int c0 = 0; c0 < a.dv; c0 += 32) {
-      if (threadIdx.x < 256) {  // dO: four pieces of eight columns a frame
-        const int row = threadIdx.x >> 2, u = threadIdx.x & 3, more = a.dv - c0 - 8 * u;
-        Eight<T> x;
+    // a slice on its way: pieces of eight columns of dO, of eight frames of U and dR, of
+    // four keys of S and dS
+    constexpr int NC = (TO * 256 + TH - 1) / TH, NS = 8 * DKP / TH;
+    Eight<T> so;
+    u32x4_t su4[NC], sr4[NC];
+    f32x4_t ss[NS], sd[NS];
+    auto arrive = [&](int c0) {
+      {
+        const int row = (tid >> 2) & 63, u = tid & 3, more = a.dv - c0 - 8 * u;
         const T* const p = d_o + s.row[0][row] * a.lddo + c0 + 8 * u;
-        if (more >= 8) x.load(p);
-        else x.load(p, more);
+        if (a.dv % 8 == 0) {
+          so.load(p + min(more - 8, 0));
+          if (more < 8) so.zero();
+        } else {
+          so.load(p, more);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        const int at = min(i * TH + tid, TO * 256 - 1), e = at >> 8, row = (at >> 3) & 31, u = at & 7;
+        const int from = (e * VP + c0 + row) * C + 8 * u;
+        su4[i] = *reinterpret_cast<const u32x4_t*>(U + from);
+        sr4[i] = *reinterpret_cast<const u32x4_t*>(dR + from);
+      }
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        const int at = i * TH + tid, row = at / (DKP / 4), u = at % (DKP / 4);
+        sd[i] = *reinterpret_cast<const f32x4_t*>(dS + (c0 + row) * DKP + 4 * u);
+        ss[i] = zero;
+        if (S) {
+          ss[i] = *reinterpret_cast<const f32x4_t*>(S + (c0 + row) * DKP + 4 * u);
+        } else if (S0) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float x = S0[min(4 * u + r, a.dk - 1) * a.dv + min(c0 + row, a.dv - 1)];
+            ss[i][r] = 4 * u + r < a.dk && c0 + row < a.dv ? x : 0.f;
+          }
+        }
+      }
+    };
+    arrive(0);
+    for (int c0 = 0; c0 < a.dv; c0 += 32) {
+      if (tid < 256) {
+        const int row = tid >> 2, u = tid & 3;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const int w = 2 * u + half, slot = (w & 3) * 2 + (w >> 2);
-          const Piece<TI> v = x.piece(half);
+          const Piece<TI> v = so.piece(half);
 #pragma unroll
           for (int e = 0; e < TI; ++e) *reinterpret_cast<u32x2_t*>(all.slice.dO.at[e] + row * pitch_of(32) + slot * 8) = v.t[e];
         }
       }
 #pragma unroll
-      for (int i = 0; i < TO * 256; i += TH) {  // U and dR: eight pieces of eight frames a column
-        const int at = i + threadIdx.x, e = at >> 8, row = (at >> 3) & 31, u = at & 7;
-        const int64_t from = (int64_t)(e * VP + c0 + row) * C + 8 * u;
+      for (int i = 0; i < NC; ++i) {
+        const int at = i * TH + tid, e = at >> 8, row = (at >> 3) & 31, u = at & 7;
         if (at < TO * 256) {
-          *reinterpret_cast<u32x4_t*>(all.slice.u[e] + row * FRAMES + 16 * u) = *reinterpret_cast<const u32x4_t*>(U + from);
-          *reinterpret_cast<u32x4_t*>(all.slice.dR[e] + row * FRAMES + 16 * u) = *reinterpret_cast<const u32x4_t*>(dR + from);
+          *reinterpret_cast<u32x4_t*>(all.slice.u[e] + row * FRAMES + 16 * u) = su4[i];
+          *reinterpret_cast<u32x4_t*>(all.slice.dR[e] + row * FRAMES + 16 * u) = sr4[i];
         }
       }
 #pragma unroll
-      for (int i = 0; i < 32 * DKP / 4; i += TH) {  // S and dS: pieces of four keys of a column
-        const int at = i + threadIdx.x, row = at / (DKP / 4), u = at % (DKP / 4);
-        f32x4_t v = zero;
-        if (S) {
-          v = *reinterpret_cast<const f32x4_t*>(S + (c0 + row) * DKP + 4 * u);
-        } else if (S0 && c0 + row < a.dv) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (4 * u + r < a.dk) v[r] = S0[(4 * u + r) * a.dv + c0 + row];
-        }
-        const Piece<TO> x = split<TO>(v), y = split<TO>(*reinterpret_cast<const f32x4_t*>(dS + (c0 + row) * DKP + 4 * u));
+      for (int i = 0; i < NS; ++i) {
+        const int at = i * TH + tid, row = at / (DKP / 4), u = at % (DKP / 4);
+        const Piece<TO> x = split<TO>(ss[i]), y = split<TO>(sd[i]);
 #pragma unroll
         for (int e = 0; e < TO; ++e) {
           *reinterpret_cast<u32x2_t*>(all.slice.S[e] + row * KEYS + 8 * u) = x.t[e];
@@ -326,6 +354,7 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
         }
       }
       __syncthreads();
+      if (c0 + 32 < a.dv) arrive(c0 + 32);
       // column 16 j + lane % 16 of those over rows 4 (lane / 16) and on, of both halves of the 32
       auto over = [&](const auto& m, int pitch, int j, Piece<TO>& x0, Piece<TO>& x1) {
         const int at = (4 * g4 + (l16 >> 2)) * pitch + (16 * j + 4 * (lane & 3)) * 2;
