@@ -134,10 +134,16 @@ typedef float f32x4_a __attribute__((ext_vector_type(4), aligned(4)));
 
 // A workgroup of W waves has 16 W columns of v: 64 or 128, as the padded heads have.
 template <int W> constexpr int threads_of = 64 * W;
-constexpr int pitch_of(int columns) { return columns * 2 + 16; }  // bytes of a row in LDS
+// Where 16 bytes of a row lie in LDS: rows that are read together, 8 next to one another
+// (b128) or 4 by 4 (transposing), then meet in no bank, or in two.
+template <int COLS> constexpr int pitch_of = COLS * 2;  // bytes of a row
+template <int COLS> __device__ __forceinline__ int place(int row, int sixteen) {
+  const int key = COLS == 32 ? (row >> 1) & 3 : (row & 1) << 2 | ((row >> 1) & 3);
+  return row * pitch_of<COLS> + (sixteen ^ key) * 16;
+}
 
 // A chunk of a head in LDS.  A row has its pieces of four columns, of each 32, in the
-// order 0 4 1 5 2 6 3 7: the two that a lane takes for a step of 32 lie together.
+// order 0 4 1 5 2 6 3 7: the two that a lane takes for a step of 32 are 16 bytes.
 // Frames past a sequence's end are its last one again, whose row can be read, with
 // beta, rk and rq 0: everything that they touch is multiplied by one of those.
 struct Gates {
@@ -146,7 +152,7 @@ struct Gates {
   float bgk[C], gq[C], gk[C];  // beta g rk, g rq, end rk
   int32_t row[2][C];           // the frames' rows, of this chunk and of the next one
 };
-template <int N, int COLS> struct Matrix { uint8_t at[N][C * pitch_of(COLS)]; };  // in N terms
+template <int N, int COLS> struct Matrix { uint8_t at[N][C * pitch_of<COLS>]; };  // in N terms
 // PT: terms of P; R: matrices like v (v, and in the backward pass dO).  (Inputs in fp32
 // would not leave room for those: they stay in memory.)  In the forward pass v has been
 // read when L is written, and everywhere n when d is: with 46 instead of 60 KiB three
@@ -166,7 +172,7 @@ template <typename T, int DKP, int W, int PT, int R> struct Chunk : Below<Terms<
   Matrix<TI, DKP> k, q;
   union {
     float n[NB][16][20];                     // -L on the diagonal, transposed
-    uint8_t d[NB][TX][512];                  // (I + L)^-1 there
+    uint8_t d[NB][TX][528];                  // (I + L)^-1 there
   };
   uint8_t p[10][PT][512];                    // blocks of P
   Gates s;
@@ -323,7 +329,7 @@ template <typename T, int COLS, int W> struct Rows {
         const Piece<Terms<T>::IN> w = v[i].piece(half);
 #pragma unroll
         for (int e = 0; e < Terms<T>::IN; ++e)
-          *reinterpret_cast<u32x2_t*>(m.at[e] + at / PER_ROW * pitch_of(COLS) + (u >> 2) * 64 + slot * 8) = w.t[e];
+          *reinterpret_cast<u32x2_t*>(m.at[e] + place<COLS>(at / PER_ROW, (u >> 2) * 4 + (slot >> 1)) + (slot & 1) * 8) = w.t[e];
       }
     }
   }
@@ -431,7 +437,7 @@ template <int N, int COLS>
 __device__ __forceinline__ void rows_of(const Matrix<N, COLS>& m, int I, int t, int lane, Piece<N>& a0, Piece<N>& a1) {
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-    const u32x4_t u = *reinterpret_cast<const u32x4_t*>(m.at[e] + (16 * I + (lane & 15)) * pitch_of(COLS) + t * 64 + (lane >> 4) * 16);
+    const u32x4_t u = *reinterpret_cast<const u32x4_t*>(m.at[e] + place<COLS>(lane & 15, t * 4 + (lane >> 4)) + 16 * I * pitch_of<COLS>);
     a0.t[e] = u.xy;
     a1.t[e] = u.zw;
   }
@@ -441,8 +447,8 @@ template <int N, int COLS> __device__ __forceinline__ Piece<N> row4_of(const Mat
   Piece<N> a;
 #pragma unroll
   for (int e = 0; e < N; ++e)
-    a.t[e] = *reinterpret_cast<const u32x2_t*>(m.at[e] + (16 * I + (lane & 15)) * pitch_of(COLS) + (t >> 1) * 64 +
-                                             ((lane >> 4) * 2 + (t & 1)) * 8);
+    a.t[e] = *reinterpret_cast<const u32x2_t*>(m.at[e] + place<COLS>(lane & 15, (t >> 1) * 4 + (lane >> 4)) +
+                                               16 * I * pitch_of<COLS> + (t & 1) * 8);
   return a;
 }
 // ... and columns 16 t + lane % 16 over frames of block I.  A group of 16 lanes reads 4
@@ -453,9 +459,10 @@ __device__ __forceinline__ u32x2_t turned(const uint8_t* p) {
 }
 template <int N, int COLS> __device__ __forceinline__ Piece<N> columns_of(const Matrix<N, COLS>& m, int t, int I, int lane) {
   Piece<N> a;
-  const int row = 16 * I + (lane >> 4) * 4 + ((lane & 15) >> 2), slot = (lane & 3) * 2 + (t & 1);
+  const int row = (lane >> 4) * 4 + ((lane & 15) >> 2);  // (of a block: its key is that of every block's)
 #pragma unroll
-  for (int e = 0; e < N; ++e) a.t[e] = turned(m.at[e] + row * pitch_of(COLS) + (t >> 1) * 64 + slot * 8);
+  for (int e = 0; e < N; ++e)
+    a.t[e] = turned(m.at[e] + place<COLS>(row, (t >> 1) * 4 + (lane & 3)) + 16 * I * pitch_of<COLS> + (t & 1) * 8);
   return a;
 }
 template <int W> __device__ __forceinline__ Piece<1> Values<bf16_t, W>::column(int t, int I, int lane) const {
@@ -467,17 +474,21 @@ template <int W> __device__ __forceinline__ f32x4_t Values<bf16_t, W>::column_va
 template <int W> __device__ __forceinline__ f32x4_t Values<bf16_t, W>::row_values(int I, int t, int lane) const {
   return values(row4_of(*m, I, t, lane));
 }
-// A block of 16 x 16, and its transpose.
-template <int TX> __device__ __forceinline__ Piece<TX> block_of(const uint8_t (&m)[TX][512], int lane) {
+// A block of 16 x 16 has columns 4 g to 4 g + 3 of all rows in 128 bytes, in an order in
+// which neither the 16 lanes that read a column group nor those that read four rows of
+// all of them (transposing) meet in a bank.
+__device__ __forceinline__ int spot(int row, int g) { return g * 128 + (row ^ (4 * g)) * 8; }
+// Such a block, and its transpose.
+template <int TX, int S> __device__ __forceinline__ Piece<TX> block_of(const uint8_t (&m)[TX][S], int lane) {
   Piece<TX> a;
 #pragma unroll
-  for (int e = 0; e < TX; ++e) a.t[e] = *reinterpret_cast<const u32x2_t*>(m[e] + (lane & 15) * 32 + (lane >> 4) * 8);
+  for (int e = 0; e < TX; ++e) a.t[e] = *reinterpret_cast<const u32x2_t*>(m[e] + spot(lane & 15, lane >> 4));
   return a;
 }
-template <int TX> __device__ __forceinline__ Piece<TX> block_turned(const uint8_t (&m)[TX][512], int lane) {
+template <int TX, int S> __device__ __forceinline__ Piece<TX> block_turned(const uint8_t (&m)[TX][S], int lane) {
   Piece<TX> a;
 #pragma unroll
-  for (int e = 0; e < TX; ++e) a.t[e] = turned(m[e] + ((lane >> 4) * 4 + ((lane & 15) >> 2)) * 32 + (lane & 3) * 8);
+  for (int e = 0; e < TX; ++e) a.t[e] = turned(m[e] + spot((lane >> 4) * 4 + ((lane & 15) >> 2), lane & 3));
   return a;
 }
 __device__ __forceinline__ f32x4_t rows4(const float (&v)[C], int I, int lane) {  // of block I, this lane's
@@ -531,14 +542,14 @@ __device__ __forceinline__ void tile(Chunk<T, DKP, W, PT, R>& c, int I, int J, i
   }
   const Piece<PT> p = split<PT>(qk);
 #pragma unroll
-  for (int e = 0; e < PT; ++e) *reinterpret_cast<u32x2_t*>(c.p[at][e] + l16 * 32 + g4 * 8) = p.t[e];
+  for (int e = 0; e < PT; ++e) *reinterpret_cast<u32x2_t*>(c.p[at][e] + spot(l16, g4)) = p.t[e];
   if (I == J) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) c.n[I][4 * g4 + r][l16] = kk[r];
   } else {
     const Piece<TX> w = split<TX>(kk);
 #pragma unroll
-    for (int e = 0; e < TX; ++e) *reinterpret_cast<u32x2_t*>(c.l[at - I][e] + l16 * 32 + g4 * 8) = w.t[e];
+    for (int e = 0; e < TX; ++e) *reinterpret_cast<u32x2_t*>(c.l[at - I][e] + spot(l16, g4)) = w.t[e];
   }
 }
 
@@ -573,11 +584,11 @@ template <typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ 
       const Piece<TX> p = split<TX>(f32x4_t{x[4 * i4], x[4 * i4 + 1], x[4 * i4 + 2], x[4 * i4 + 3]});
 #pragma unroll
       for (int e = 0; e < TX; ++e) {
-        uint16_t* to = reinterpret_cast<uint16_t*>(c.d[g4][e]) + 4 * i4 * 16 + l16;
+        uint16_t* to = reinterpret_cast<uint16_t*>(c.d[g4][e] + spot(4 * i4, l16 >> 2)) + (l16 & 3);
         to[0] = (uint16_t)p.t[e].x;
-        to[16] = (uint16_t)(p.t[e].x >> 16);
-        to[32] = (uint16_t)p.t[e].y;
-        to[48] = (uint16_t)(p.t[e].y >> 16);
+        to[4] = (uint16_t)(p.t[e].x >> 16);
+        to[8] = (uint16_t)p.t[e].y;
+        to[12] = (uint16_t)(p.t[e].y >> 16);
       }
     }
   }

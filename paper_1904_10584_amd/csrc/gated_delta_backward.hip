@@ -228,7 +228,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
 // over pairs of frames to K and Q, which have the same LDS by then.
 template <typename T, int DKP> struct Keys {
   static constexpr int TI = Terms<T>::IN, TO = Terms<T>::OUT;
-  static constexpr int FRAMES = C * 2 + 16, KEYS = pitch_of(DKP);  // bytes of a row of columns, of states
+  static constexpr int FRAMES = C * 2 + 16, KEYS = DKP * 2 + 16;  // bytes of a row of columns, of states
   union {
     struct {
       Matrix<TI, 32> dO;
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
           const int w = 2 * u + half, slot = (w & 3) * 2 + (w >> 2);
           const Piece<TI> v = so.piece(half);
 #pragma unroll
-          for (int e = 0; e < TI; ++e) *reinterpret_cast<u32x2_t*>(all.slice.dO.at[e] + row * pitch_of(32) + slot * 8) = v.t[e];
+          for (int e = 0; e < TI; ++e) *reinterpret_cast<u32x2_t*>(all.slice.dO.at[e] + place<32>(row, slot >> 1) + (slot & 1) * 8) = v.t[e];
         }
       }
 #pragma unroll
@@ -418,8 +418,8 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
       const Piece<TO> p = split<TO>(x), q = split<TO>(y);
 #pragma unroll
       for (int e = 0; e < TO; ++e) {
-        *reinterpret_cast<u32x2_t*>(all.pairs.qk[at][e] + l16 * 32 + g4 * 8) = p.t[e];
-        *reinterpret_cast<u32x2_t*>(all.pairs.kk[at][e] + l16 * 32 + g4 * 8) = q.t[e];
+        *reinterpret_cast<u32x2_t*>(all.pairs.qk[at][e] + spot(l16, g4)) = p.t[e];
+        *reinterpret_cast<u32x2_t*>(all.pairs.kk[at][e] + spot(l16, g4)) = q.t[e];
       }
     }
     __syncthreads();
