@@ -370,13 +370,20 @@ struct GatedDelta {
                                      // and on start from (written by a training forward)
   float* dsaved;                     // [chunks][B][H][dv][dk]: gradients of the chunks' last states
   uint16_t *u, *dr_rows;             // [chunks][B][H][terms][dv][GD_CHUNK], terms as of gd_kept_terms
-  float* parts;                      // backward: [B][H]
+  float* parts;                      // backward: [segments][B][H]
+  // segments of long sequences (1: none), each of `per` chunks, and padded states of them
+  int segs, per;
+  float *seg_n, *seg_m, *seg_mt;     // [segs][B][H]: ends, maps, maps transposed
+  float* seg_d;                      // backward: gradients of their last states
   const int32_t *offs, *lens;        // [T + 1], [B], or null: every sequence has T frames
   int64_t N;
   int T, B, H, G, dk, dv;
   float c, eps;
   bool train;                        // forward: keep the states
 };
+// How a batch of up to T frames of `heads` heads of all sequences is cut.
+struct DeltaSegments { int count, per; };
+DeltaSegments delta_segments(int64_t T, int64_t heads);
 constexpr int gd_padded(int dim) { return dim <= 64 ? 64 : 128; }
 constexpr int gd_kept_terms(bool bf16) { return bf16 ? 2 : 3; }
 hipError_t gated_delta_forward(GatedDelta a, bool bf16, hipStream_t s);

@@ -703,7 +703,7 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
   return AM_OK;
 }
 
-struct DeltaLayout { int64_t offs, lens, tails, saved, dsaved, u, dr, parts, total; };
+struct DeltaLayout { int64_t offs, lens, tails, saved, dsaved, u, dr, parts, seg_n, seg_m, seg_mt, seg_d, total; };
 DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int32_t dk, int32_t dv, bool bf16, bool varlen,
                          bool train) {
   DeltaLayout l{};
@@ -725,7 +725,15 @@ DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int32_t dk, int32_t dv
     l.dsaved = take(chunks * columns * am::gd_padded(dk) * 4);
     l.u = take(chunks * columns * am::GD_CHUNK * am::gd_kept_terms(bf16) * 2);
     l.dr = take(chunks * columns * am::GD_CHUNK * am::gd_kept_terms(bf16) * 2);
-    l.parts = take(B * H * 4);
+    l.parts = take(B * H * am::delta_segments(T, B * H).count * 4);
+  }
+  const int64_t segs = T > 0 ? am::delta_segments(T, B * H).count : 1;
+  if (segs > 1) {
+    const int64_t key = am::gd_padded(dk), state = segs * B * H * key * 4;
+    l.seg_n = take(state * am::gd_padded(dv));
+    l.seg_m = take(state * key);
+    l.seg_mt = take(state * key);
+    if (train) l.seg_d = take(state * am::gd_padded(dv));
   }
   l.total = at;
   return l;
@@ -788,6 +796,14 @@ am_status check_delta(int32_t T, int32_t B, int32_t heads, int32_t key_heads, in
     a.offs = at<int32_t>(ws, l.offs);
     a.lens = at<int32_t>(ws, l.lens);
   }
+  // (from T, as the workspace is laid out)
+  const am::DeltaSegments cut = am::delta_segments(T, (int64_t)B * heads);
+  a.segs = T > 0 ? cut.count : 1;
+  a.per = T > 0 ? cut.per : 1;
+  a.seg_n = at<float>(ws, l.seg_n);
+  a.seg_m = at<float>(ws, l.seg_m);
+  a.seg_mt = at<float>(ws, l.seg_mt);
+  a.seg_d = at<float>(ws, l.seg_d);
   return AM_OK;
 }
 

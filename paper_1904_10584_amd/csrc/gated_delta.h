@@ -513,8 +513,8 @@ template <int J> __device__ __forceinline__ void substitute(float (&x)[16], cons
   }
 }
 
-// Tile (I, J) of -L and P from K K^T and Q K^T.
-template <typename T, int DKP, int W, int PT, int R>
+// Tile (I, J) of -L and, with OUT, of P from K K^T and Q K^T.
+template <bool OUT, typename T, int DKP, int W, int PT, int R>
 __device__ __forceinline__ void tile(Chunk<T, DKP, W, PT, R>& c, int I, int J, int lane) {
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X;
   const int l16 = lane & 15, g4 = lane >> 4, at = lower(I, J);
@@ -526,8 +526,10 @@ __device__ __forceinline__ void tile(Chunk<T, DKP, W, PT, R>& c, int I, int J, i
     rows_of(c.k, J, t, lane, a0, a1);
     rows_of(c.k, I, t, lane, b0, b1);
     mma<TI, TI>(kk, a0, a1, b0, b1);
-    rows_of(c.q, I, t, lane, b0, b1);
-    mma<TI, TI>(qk, a0, a1, b0, b1);
+    if constexpr (OUT) {
+      rows_of(c.q, I, t, lane, b0, b1);
+      mma<TI, TI>(qk, a0, a1, b0, b1);
+    }
   }
   // a lane has row i and columns j, j + 1, ... of the tile
   const int i = 16 * I + l16;
@@ -540,9 +542,11 @@ __device__ __forceinline__ void tile(Chunk<T, DKP, W, PT, R>& c, int I, int J, i
     kk[r] = j < i ? fk * kk[r] * m : 0.f;
     qk[r] = j <= i ? fq * qk[r] * m : 0.f;
   }
-  const Piece<PT> p = split<PT>(qk);
+  if constexpr (OUT) {
+    const Piece<PT> p = split<PT>(qk);
 #pragma unroll
-  for (int e = 0; e < PT; ++e) *reinterpret_cast<u32x2_t*>(c.p[at][e] + spot(l16, g4)) = p.t[e];
+    for (int e = 0; e < PT; ++e) *reinterpret_cast<u32x2_t*>(c.p[at][e] + spot(l16, g4)) = p.t[e];
+  }
   if (I == J) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) c.n[I][4 * g4 + r][l16] = kk[r];
@@ -556,10 +560,10 @@ __device__ __forceinline__ void tile(Chunk<T, DKP, W, PT, R>& c, int I, int J, i
 // L, P and the inverses of I + L's diagonal blocks from a staged chunk (behind a
 // barrier; ends with one).  The first four waves make the tiles on the diagonal; then
 // one wave inverts, and the others make the six tiles below.
-template <typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ void triangles(Chunk<T, DKP, W, PT, R>& c, int tid) {
+template <bool OUT, typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ void triangles(Chunk<T, DKP, W, PT, R>& c, int tid) {
   constexpr int TX = Terms<T>::X;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
-  if (wave < NB) tile(c, wave, wave, lane);
+  if (wave < NB) tile<OUT>(c, wave, wave, lane);
   if (wave == W - 1) combine(c.s, lane);
   __syncthreads();
   if (wave > 0) {
@@ -567,7 +571,7 @@ template <typename T, int DKP, int W, int PT, int R> __device__ __forceinline__ 
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
       const int at = min(wave - 1 + (W - 1) * k, 5), I = at >= 3 ? 3 : at >= 1 ? 2 : 1;
-      tile(c, I, at - below(I, 0), lane);
+      tile<OUT>(c, I, at - below(I, 0), lane);
     }
   } else {  // 16 lanes a block, a column each: substitution
     // (lane j of the 16 has column j of -L, and gives its elements to the others)
@@ -645,6 +649,32 @@ template <int DKP> __device__ __forceinline__ void store_kept(float* m, int col,
 #pragma unroll
   for (int t = 0; t < DKP / 16; ++t) *reinterpret_cast<f32x4_t*>(m + col * DKP + 16 * t + 4 * (lane >> 4)) = S[t];
 }
+// Long sequences of few heads are cut in segments.  A chunk, and so a segment, acts on
+// the state it starts from as S -> M S + N; N is what it makes of a zero state, and M
+// what it makes of the identity without v.  Those are found for all segments at once,
+// then put together in order (join), then each segment runs from its own state.  So
+// does the gradient, backwards, with M^T.  Segment `seg` of a head keeps a padded state.
+template <int DKP, int W> __device__ __forceinline__ float* segment(float* m, const GatedDelta& a, int seg, int64_t bh) {
+  return m + ((int64_t)seg * a.B * a.H + bh) * (DKP * 16 * W);
+}
+
+// S += M X: a wave's 16 columns of both; M's rows are DKP apart, and four elements of one
+// lie together.
+template <int DKP>
+__device__ __forceinline__ void join(f32x4_t (&S)[DKP / 16], const float* m, const f32x4_t (&X)[DKP / 16], int lane) {
+  Piece<3> x[DKP / 16];
+#pragma unroll
+  for (int t = 0; t < DKP / 16; ++t) x[t] = split<3>(X[t]);
+#pragma unroll
+  for (int t = 0; t < DKP / 16; ++t) {
+    const float* const row = m + (16 * t + (lane & 15)) * DKP + 4 * (lane >> 4);
+#pragma unroll
+    for (int k = 0; k < DKP / 16; k += 2)
+      mma<3, 3>(S[t], split<3>(*reinterpret_cast<const f32x4_t*>(row + 16 * k)),
+                split<3>(*reinterpret_cast<const f32x4_t*>(row + 16 * k + 16)), x[k], x[k + 1]);
+  }
+}
+
 // Where chunk n of a head keeps what: the state that it starts from (n >= 1) ...
 template <int DKP, int W> __device__ __forceinline__ float* kept_before(const GatedDelta& a, int n, int64_t bh) {
   return a.saved + ((int64_t)(n - 1) * a.B * a.H + bh) * (DKP * 16 * W);

@@ -3,6 +3,8 @@
 // sequences, a pass over their states.
 #include "gated_delta.h"
 
+#include <algorithm>
+
 namespace am {
 namespace {
 
@@ -10,49 +12,73 @@ using namespace gd;
 
 constexpr int THREADS = 256, WAVES = 4;  // of a frame's kernel
 
-template <typename T, int DKP, int W>
+// What a launch makes: the outputs, or of each segment but those that nothing follows
+// what it makes of a zero state (ENDS), or of the identity without v (MAPS).
+enum Pass { OUTPUTS, ENDS, MAPS };
+
+template <typename T, int DKP, int W, Pass PASS>
 __global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2) void gd_forward_kernel(GatedDelta a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT, KT = DKP / 16;
+  constexpr bool OUT = PASS == OUTPUTS;
   Chunk<T, DKP, W, TO, 1>& c = *reinterpret_cast<Chunk<T, DKP, W, TO, 1>*>(lds);
   Gates& s = c.s;
   const Head hd(a, blockIdx.x);
+  const int seg = blockIdx.y, begin = seg * a.per * C, end = min(hd.len, begin + a.per * C);
+  if (seg > 0 && begin >= hd.len) return;
   const float rate = a.c * softplus(a.lam[hd.h]);
   const int64_t mine = (int64_t)blockIdx.x * a.dk * a.dv;
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   f32x4_t S[KT];
-  load_state<DKP>(a.s0 ? a.s0 + mine : nullptr, a, column_of(threadIdx.x), threadIdx.x & 63, S);
+  {
+    const int lane = threadIdx.x & 63, col = column_of(threadIdx.x);
+    if (PASS == MAPS) {
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[t][r] = 16 * t + 4 * (lane >> 4) + r == col ? 1.f : 0.f;
+    } else if (OUT && seg > 0) {
+      load_kept<DKP>(segment<DKP, W>(a.seg_n, a, seg - 1, blockIdx.x), col, lane, S);
+    } else {
+      load_state<DKP>(OUT && a.s0 ? a.s0 + mine : nullptr, a, col, lane, S);
+    }
+  }
   Rows<T, DKP, W> fk, fq;
   Values<T, W> fv;
   GateRows<T, W> fg;
   auto fetch = [&](const int32_t (&rows)[C], int next0, int tid) {
     fk.from(a.k, a.ldk, hd.kh, a.dk, rows, tid);
-    fq.from(a.q, a.ldq, hd.kh, a.dk, rows, tid);
-    fv.from(a.v, a.ldv, hd, a.dv, rows, tid);
+    if constexpr (OUT) fq.from(a.q, a.ldq, hd.kh, a.dk, rows, tid);
+    if constexpr (PASS != MAPS) fv.from(a.v, a.ldv, hd, a.dv, rows, tid);
     fg.from(a, hd, rows, next0, tid);
   };
-  if (hd.len > 0) {
-    if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, threadIdx.x);
+  if (begin < end) {
+    if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, begin + threadIdx.x);
     __syncthreads();
-    fetch(s.row[0], C, threadIdx.x);
+    fetch(s.row[0], begin + C, threadIdx.x);
   }
   int turn = 0;
-  for (int t0 = 0; t0 < hd.len; t0 += C, turn ^= 1) {
+  for (int t0 = begin; t0 < end; t0 += C, turn ^= 1) {
     const int left = hd.len - t0, tid = this_thread(), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = 16 * wave + l16;
-    if (a.train && t0 > 0) store_kept<DKP>(kept_before<DKP, W>(a, t0 / C, blockIdx.x), col, lane, S);
+    if (OUT && a.train && t0 > 0) store_kept<DKP>(kept_before<DKP, W>(a, t0 / C, blockIdx.x), col, lane, S);
     fk.lengths(s.rk, a.eps, left, tid);
-    fq.lengths(s.rq, a.eps, left, tid);
     fk.store(c.k, tid);
-    fq.store(c.q, tid);
-    fv.store(&c.v[0], s.row[turn], tid);
+    if constexpr (OUT) {
+      fq.lengths(s.rq, a.eps, left, tid);
+      fq.store(c.q, tid);
+    }
+    if constexpr (PASS != MAPS) fv.store(&c.v[0], s.row[turn], tid);
     fg.store(s, rate, left, turn, tid);
     __syncthreads();
     f32x4_t v[NB];
 #pragma unroll
-    for (int I = 0; I < NB; ++I) v[I] = fv.column_values(wave, I, lane);
-    if (left > C) fetch(s.row[turn ^ 1], t0 + 2 * C, tid);  // the next chunk's, which arrive during this one
-    triangles(c, tid);
+    for (int I = 0; I < NB; ++I) {
+      if constexpr (PASS != MAPS) v[I] = fv.column_values(wave, I, lane);
+      else v[I] = zero;
+    }
+    if (t0 + C < end) fetch(s.row[turn ^ 1], t0 + 2 * C, tid);  // the next chunk's, which arrive during this one
+    triangles<OUT>(c, tid);
 
     f32x4_t u[NB], o[NB];
 #pragma unroll
@@ -65,29 +91,33 @@ __global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2)
         Piece<TI> a0, a1;
         rows_of(c.k, I, t, lane, a0, a1);
         mma<TI, TX>(u[I], a0, a1, s0, s1);
-        rows_of(c.q, I, t, lane, a0, a1);
-        mma<TO, TI>(o[I], first<TO>(s0), first<TO>(s1), a0, a1);
+        if constexpr (OUT) {
+          rows_of(c.q, I, t, lane, a0, a1);
+          mma<TO, TI>(o[I], first<TO>(s0), first<TO>(s1), a0, a1);
+        }
       }
     }
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
       u[I] = v[I] * rows4(s.beta, I, lane) - u[I] * rows4(s.bgk, I, lane);
-      o[I] *= s.gq[16 * I + l16];
+      if constexpr (OUT) o[I] *= s.gq[16 * I + l16];
     }
     Piece<TX> r[NB], up[NB];
     solve(c, lane, u, r, up);
+    if constexpr (OUT) {
 #pragma unroll
-    for (int I = 0; I < NB; ++I) {
+      for (int I = 0; I < NB; ++I) {
 #pragma unroll
-      for (int J = 0; J + 1 <= I; J += 2)
-        mma<TO, TO>(o[I], first<TO>(up[J]), first<TO>(up[J + 1]), block_of(c.p[lower(I, J)], lane), block_of(c.p[lower(I, J + 1)], lane));
-      if (I % 2 == 0) mma<TO, TO>(o[I], first<TO>(up[I]), block_of(c.p[lower(I, I)], lane));
+        for (int J = 0; J + 1 <= I; J += 2)
+          mma<TO, TO>(o[I], first<TO>(up[J]), first<TO>(up[J + 1]), block_of(c.p[lower(I, J)], lane), block_of(c.p[lower(I, J + 1)], lane));
+        if (I % 2 == 0) mma<TO, TO>(o[I], first<TO>(up[I]), block_of(c.p[lower(I, I)], lane));
+      }
+#pragma unroll
+      for (int I = 0; I < NB; ++I)
+        if (16 * I + l16 < left)
+          put4(static_cast<T*>(a.o) + s.row[turn][16 * I + l16] * a.ldo + (int64_t)hd.h * a.dv + 16 * wave + 4 * g4,
+               a.dv - 16 * wave - 4 * g4, o[I]);
     }
-#pragma unroll
-    for (int I = 0; I < NB; ++I)
-      if (16 * I + l16 < left)
-        put4(static_cast<T*>(a.o) + s.row[turn][16 * I + l16] * a.ldo + (int64_t)hd.h * a.dv + 16 * wave + 4 * g4,
-             a.dv - 16 * wave - 4 * g4, o[I]);
 #pragma unroll
     for (int I = 0; I < NB; ++I) up[I] = split<TX>(u[I] * rows4(s.gk, I, lane));
     const float g_end = s.g[C - 1];
@@ -99,7 +129,35 @@ __global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2)
     }
     __syncthreads();
   }
-  if (a.sT) store_state<DKP>(a.sT + mine, a, column_of(threadIdx.x), threadIdx.x & 63, S);
+  const int lane = threadIdx.x & 63, col = column_of(threadIdx.x);
+  if (PASS == ENDS) {
+    store_kept<DKP>(segment<DKP, W>(a.seg_n, a, seg, blockIdx.x), col, lane, S);
+  } else if (PASS == MAPS) {  // by columns, for the backward pass, and by rows
+    store_kept<DKP>(segment<DKP, W>(a.seg_mt, a, seg, blockIdx.x), col, lane, S);
+    float* const m = segment<DKP, W>(a.seg_m, a, seg, blockIdx.x);
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m[(16 * t + 4 * (lane >> 4) + r) * DKP + col] = S[t][r];
+  } else if (a.sT && hd.len <= begin + a.per * C) {
+    store_state<DKP>(a.sT + mine, a, col, lane, S);
+  }
+}
+
+// The states that segments start from, one after another.
+template <int DKP, int W> __global__ __launch_bounds__(threads_of<W>) void gd_join_kernel(GatedDelta a) {
+  const int lane = threadIdx.x & 63, col = column_of(threadIdx.x), len = a.lens ? a.lens[blockIdx.x / a.H] : a.T;
+  f32x4_t S[DKP / 16];
+  load_state<DKP>(a.s0 ? a.s0 + (int64_t)blockIdx.x * a.dk * a.dv : nullptr, a, col, lane, S);
+  for (int seg = 0; seg + 1 < a.segs && (seg + 1) * a.per * C < len; ++seg) {
+    f32x4_t N[DKP / 16];
+    float* const at = segment<DKP, W>(a.seg_n, a, seg, blockIdx.x);
+    load_kept<DKP>(at, col, lane, N);
+    join<DKP>(N, segment<DKP, DKP / 16>(a.seg_m, a, seg, blockIdx.x), S, lane);
+    store_kept<DKP>(at, col, lane, N);
+#pragma unroll
+    for (int t = 0; t < DKP / 16; ++t) S[t] = N[t];
+  }
 }
 
 // One frame of each sequence: a state is read once, kept in registers, and written
@@ -197,14 +255,24 @@ __global__ __launch_bounds__(THREADS) void gd_token_kernel(GatedDelta a) {
     }
 }
 
-template <typename T, int DKP, int W> hipError_t chunks(const GatedDelta& a, hipStream_t s) {
+template <typename T, int DKP, int W, Pass PASS> hipError_t pass(const GatedDelta& a, int segs, hipStream_t s) {
   constexpr int LDS = sizeof(Chunk<T, DKP, W, Terms<T>::OUT, 1>);
   static_assert(LDS <= 160 * 1024, "a workgroup's LDS");
   static PerDevice ready;
-  const hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_forward_kernel<T, DKP, W>), ready);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((gd_forward_kernel<T, DKP, W>), dim3((unsigned)(a.B * a.H)), dim3(threads_of<W>), LDS, s, a);
+  const hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_forward_kernel<T, DKP, W, PASS>), ready);
+  if (e != hipSuccess || segs == 0) return e;
+  hipLaunchKernelGGL((gd_forward_kernel<T, DKP, W, PASS>), dim3((unsigned)(a.B * a.H), segs), dim3(threads_of<W>), LDS, s, a);
   return hipGetLastError();
+}
+template <typename T, int DKP, int W> hipError_t chunks(const GatedDelta& a, hipStream_t s) {
+  if (a.segs > 1) {
+    // (a training pass needs the last segments' maps too, for the gradient)
+    hipError_t e = pass<T, DKP, DKP / 16, MAPS>(a, a.train ? a.segs : a.segs - 1, s);
+    if (e == hipSuccess) e = pass<T, DKP, W, ENDS>(a, a.segs - 1, s);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((gd_join_kernel<DKP, W>), dim3((unsigned)(a.B * a.H)), dim3(threads_of<W>), 0, s, a);
+  }
+  return pass<T, DKP, W, OUTPUTS>(a, a.segs, s);
 }
 
 template <typename T, int CG> hipError_t token(const GatedDelta& a, hipStream_t s) {
@@ -226,6 +294,13 @@ template <typename T> hipError_t forward(const GatedDelta& a, hipStream_t s) {
 }
 
 }  // namespace
+
+DeltaSegments delta_segments(int64_t T, int64_t heads) {
+  const int64_t chunks = (T + GD_CHUNK - 1) / GD_CHUNK, most = std::min<int64_t>(512 / heads, chunks / 8);
+  if (most < 3) return {1, (int)chunks};
+  const int64_t per = (chunks + most - 1) / most;
+  return {(int)((chunks + per - 1) / per), (int)per};
+}
 
 hipError_t gated_delta_forward(GatedDelta a, bool bf16, hipStream_t s) {
   return bf16 ? forward<bf16_t>(a, s) : forward<float>(a, s);

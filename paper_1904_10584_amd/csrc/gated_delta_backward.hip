@@ -26,55 +26,66 @@ template <typename T, int DKP, int W> struct Backward {
   float end[W];         // <dS', S'>
 };
 
-template <typename T, int DKP, int W>
+// ENDS: only what each segment makes of a gradient of zero behind it, at its first state.
+template <typename T, int DKP, int W, bool ENDS>
 __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelta a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT, KT = DKP / 16;
   Backward<T, DKP, W>& all = *reinterpret_cast<Backward<T, DKP, W>*>(lds);
   auto& c = all.c;
   Gates& s = c.s;
+  const int seg = blockIdx.y + (ENDS ? 1 : 0);
   const int64_t bh = blockIdx.x, state = (int64_t)a.dk * a.dv;
   const Head hd(a, blockIdx.x);
   const float rate = a.c * softplus(a.lam[hd.h]);
-  const int chunks = (hd.len + C - 1) / C;
+  const int all_chunks = (hd.len + C - 1) / C, begin = seg * a.per, chunks = min(all_chunks, begin + a.per);
+  if (seg > 0 && begin >= all_chunks) {
+    if (!ENDS && threadIdx.x == 0) a.parts[seg * (int64_t)gridDim.x + bh] = 0.f;
+    return;
+  }
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   f32x4_t dS[KT];
-  load_state<DKP>(a.dsT ? a.dsT + bh * state : nullptr, a, column_of(threadIdx.x), threadIdx.x & 63, dS);
+  if (!ENDS && chunks < all_chunks)
+    load_kept<DKP>(segment<DKP, W>(a.seg_d, a, seg, bh), column_of(threadIdx.x), threadIdx.x & 63, dS);
+  else
+    load_state<DKP>(!ENDS && a.dsT ? a.dsT + bh * state : nullptr, a, column_of(threadIdx.x), threadIdx.x & 63, dS);
   Rows<T, DKP, W> fk, fq;
   Values<T, W> fv, fo;
   GateRows<T, W> fg;
   auto fetch = [&](const int32_t (&rows)[C], int next0, int tid) {
     fk.from(a.k, a.ldk, hd.kh, a.dk, rows, tid);
     fq.from(a.q, a.ldq, hd.kh, a.dk, rows, tid);
-    fv.from(a.v, a.ldv, hd, a.dv, rows, tid);
+    if constexpr (!ENDS) fv.from(a.v, a.ldv, hd, a.dv, rows, tid);
     fo.from(a.d_o, a.lddo, hd, a.dv, rows, tid);
     fg.from(a, hd, rows, next0, tid);
   };
-  if (chunks) {
+  if (begin < chunks) {
     if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, (chunks - 1) * C + threadIdx.x);
     __syncthreads();
     fetch(s.row[0], max(chunks - 2, 0) * C, threadIdx.x);
   }
   float dlam = 0.f;  // (of a frame a lane of every chunk, in the last wave)
   int turn = 0;
-  for (int n = chunks - 1; n >= 0; --n, turn ^= 1) {
+  for (int n = chunks - 1; n >= begin; --n, turn ^= 1) {
     const int left = hd.len - n * C, tid = this_thread(), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = 16 * wave + l16;
     const T r_now = fg.r;
-    store_kept<DKP>(kept_after<DKP, W>(a, n, bh), col, lane, dS);
+    if constexpr (!ENDS) store_kept<DKP>(kept_after<DKP, W>(a, n, bh), col, lane, dS);
     fk.lengths(s.rk, a.eps, left, tid);
     fq.lengths(s.rq, a.eps, left, tid);
     fk.store(c.k, tid);
     fq.store(c.q, tid);
-    fv.store(&c.v[0], s.row[turn], tid);
+    if constexpr (!ENDS) fv.store(&c.v[0], s.row[turn], tid);
     fo.store(&c.v[1], s.row[turn], tid);
     fg.store(s, rate, left, turn, tid);
     __syncthreads();
-    if (n > 0) fetch(s.row[turn ^ 1], max(n - 2, 0) * C, tid);  // the chunk before, which arrives during this one
+    if (n > begin) fetch(s.row[turn ^ 1], max(n - 2, 0) * C, tid);  // the chunk before, which arrives during this one
     f32x4_t S[KT];
-    if (n > 0) load_kept<DKP>(kept_before<DKP, W>(a, n, bh), col, lane, S);
-    else load_state<DKP>(a.s0 ? a.s0 + bh * state : nullptr, a, col, lane, S);
-    triangles(c, tid);
+    if constexpr (!ENDS) {
+      if (n > 0) load_kept<DKP>(kept_before<DKP, W>(a, n, bh), col, lane, S);
+      else load_state<DKP>(a.s0 ? a.s0 + bh * state : nullptr, a, col, lane, S);
+    }
+    triangles<true>(c, tid);
 
     f32x4_t u[NB], o[NB], kd[NB];
 #pragma unroll
@@ -82,31 +93,39 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
     float end = 0.f;
 #pragma unroll
     for (int t = 0; t < DKP / 32; ++t) {
-      const Piece<TX> s0 = split<TX>(S[2 * t]), s1 = split<TX>(S[2 * t + 1]);
       const Piece<TX> d0 = split<TX>(dS[2 * t]), d1 = split<TX>(dS[2 * t + 1]);
+      Piece<TX> s0, s1;
+      if constexpr (!ENDS) {
+        s0 = split<TX>(S[2 * t]);
+        s1 = split<TX>(S[2 * t + 1]);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) end = fmaf(S[2 * t][r], dS[2 * t][r], fmaf(S[2 * t + 1][r], dS[2 * t + 1][r], end));
+        for (int r = 0; r < 4; ++r) end = fmaf(S[2 * t][r], dS[2 * t][r], fmaf(S[2 * t + 1][r], dS[2 * t + 1][r], end));
+      }
 #pragma unroll
       for (int I = 0; I < NB; ++I) {
         Piece<TI> a0, a1;
         rows_of(c.k, I, t, lane, a0, a1);
-        mma<TI, TX>(u[I], a0, a1, s0, s1);
         mma<TI, TX>(kd[I], a0, a1, d0, d1);
-        rows_of(c.q, I, t, lane, a0, a1);
-        mma<TX, TI>(o[I], s0, s1, a0, a1);
+        if constexpr (!ENDS) {
+          mma<TI, TX>(u[I], a0, a1, s0, s1);
+          rows_of(c.q, I, t, lane, a0, a1);
+          mma<TX, TI>(o[I], s0, s1, a0, a1);
+        }
       }
     }
     const float g_end = s.g[C - 1];
     end *= g_end;
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
-      u[I] = fv.column_values(wave, I, lane) * rows4(s.beta, I, lane) - u[I] * rows4(s.bgk, I, lane);
-      o[I] *= s.gq[16 * I + l16];
+      if constexpr (!ENDS) {
+        u[I] = fv.column_values(wave, I, lane) * rows4(s.beta, I, lane) - u[I] * rows4(s.bgk, I, lane);
+        o[I] *= s.gq[16 * I + l16];
+      }
       kd[I] *= rows4(s.gk, I, lane);
     }
     // U; transposed, a frame a lane, it is wanted for dR . U
     f32x4_t ut[NB];
-    {
+    if constexpr (!ENDS) {
       Piece<TX> r[NB], up[NB];
       solve(c, lane, u, r, up);
 #pragma unroll
@@ -130,6 +149,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
     float y1[NB], y2[NB];
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
+      if constexpr (ENDS) break;
       const f32x4_t x = fo.row_values(I, wave, lane) * o[I];
       y1[I] = (x[0] + x[1]) + (x[2] + x[3]);
     }
@@ -144,12 +164,13 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
       for (int I = NB - 1; I >= 0; --I) {
         const Piece<TX> d = block_turned(c.d[I], lane), w = split<TX>(kd[I]);
         f32x4_t dr = zero;  // (transposed)
-        mma<TX, TX>(dr, w, d);
+        if constexpr (!ENDS) mma<TX, TX>(dr, w, d);
         kd[I] = zero;
         mma<TX, TX>(kd[I], d, w);
         dp[I] = split<TX>(kd[I]);
 #pragma unroll
         for (int J = I - 1; J >= 0; --J) mma<TX, TX>(kd[J], block_turned(c.l[below(I, J)], lane), dp[I]);
+        if constexpr (ENDS) continue;
         const f32x4_t dv = dr * s.beta[16 * I + l16], x = dv * fv.row_values(I, wave, lane), y = dr * ut[I];
         y1[I] -= (x[0] + x[1]) + (x[2] + x[3]);
         y2[I] = (y[0] + y[1]) + (y[2] + y[3]);
@@ -158,6 +179,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
                a.dv - 16 * wave - 4 * g4, dv);
       }
       uint16_t* const keep = kept_columns<TO, W>(a.dr_rows, a, n, bh);
+      if constexpr (!ENDS)
 #pragma unroll
       for (int e = 0; e < TO; ++e)
 #pragma unroll
@@ -181,6 +203,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
         }
       }
     }
+    if constexpr (!ENDS) {
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
       y1[I] += __shfl_xor(y1[I], 16, 64);
@@ -213,12 +236,34 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
         dlam -= d * sr;
       }
     }
+    }
     __syncthreads();
   }
-  if (a.ds0) store_state<DKP>(a.ds0 + bh * state, a, column_of(threadIdx.x), threadIdx.x & 63, dS);
+  if constexpr (ENDS) {
+    store_kept<DKP>(segment<DKP, W>(a.seg_d, a, seg - 1, bh), column_of(threadIdx.x), threadIdx.x & 63, dS);
+    return;
+  }
+  if (a.ds0 && seg == 0) store_state<DKP>(a.ds0 + bh * state, a, column_of(threadIdx.x), threadIdx.x & 63, dS);
   if (threadIdx.x >= threads_of<W> - 64) {
     dlam = wave_sum_uniform(dlam);
-    if (threadIdx.x == threads_of<W> - 64) a.parts[bh] = a.c * dlam;
+    if (threadIdx.x == threads_of<W> - 64) a.parts[seg * (int64_t)gridDim.x + bh] = a.c * dlam;
+  }
+}
+
+// The gradients of the states that segments end in, from the last one on.
+template <int DKP, int W> __global__ __launch_bounds__(threads_of<W>) void gd_join_back_kernel(GatedDelta a) {
+  const int lane = threadIdx.x & 63, col = column_of(threadIdx.x), len = a.lens ? a.lens[blockIdx.x / a.H] : a.T;
+  f32x4_t dS[DKP / 16];
+  load_state<DKP>(a.dsT ? a.dsT + (int64_t)blockIdx.x * a.dk * a.dv : nullptr, a, col, lane, dS);
+  const int frames = a.per * C, last = len > 0 ? (len - 1) / frames : 0;
+  for (int seg = last; seg > 0; --seg) {
+    f32x4_t D[DKP / 16];
+    float* const at = segment<DKP, W>(a.seg_d, a, seg - 1, blockIdx.x);
+    load_kept<DKP>(at, col, lane, D);
+    join<DKP>(D, segment<DKP, DKP / 16>(a.seg_mt, a, seg, blockIdx.x), dS, lane);
+    store_kept<DKP>(at, col, lane, D);
+#pragma unroll
+    for (int t = 0; t < DKP / 16; ++t) dS[t] = D[t];
   }
 }
 
@@ -473,22 +518,35 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
   }
 }
 
-// dlam = sigm(lam) times the sum over sequences of parts [B][H].
+// dlam = sigm(lam) times the sum over segments and sequences of parts.
 __global__ __launch_bounds__(1024) void gd_dlam_kernel(GatedDelta a) {
   __shared__ float sum[32][33];
-  const float s = column_sum(a.parts, a.B, a.H, sum);
+  const float s = column_sum(a.parts, (int64_t)a.segs * a.B, a.H, sum);
   const int h = blockIdx.x * 32 + threadIdx.x;
   if (threadIdx.x < 32 && h < a.H) a.dlam[h] = s / (1.f + expf(-a.lam[h]));
 }
 
-template <typename T, int DKP, int W> hipError_t backward(const GatedDelta& a, hipStream_t s) {
-  constexpr int LDS = sizeof(Backward<T, DKP, W>), KEYS = sizeof(Keys<T, DKP>);
-  static_assert(LDS <= 160 * 1024 && KEYS <= 160 * 1024, "a workgroup's LDS");
-  static PerDevice ready, ready_keys;
-  hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_backward_kernel<T, DKP, W>), ready);
-  if (e == hipSuccess) e = allow_lds<KEYS>(reinterpret_cast<const void*>(&gd_keys_kernel<T, DKP, 16 * W>), ready_keys);
+template <typename T, int DKP, int W, bool ENDS> hipError_t pass(const GatedDelta& a, int segs, hipStream_t s) {
+  constexpr int LDS = sizeof(Backward<T, DKP, W>);
+  static_assert(LDS <= 160 * 1024, "a workgroup's LDS");
+  static PerDevice ready;
+  const hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_backward_kernel<T, DKP, W, ENDS>), ready);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((gd_backward_kernel<T, DKP, W>), dim3((unsigned)(a.B * a.H)), dim3(threads_of<W>), LDS, s, a);
+  hipLaunchKernelGGL((gd_backward_kernel<T, DKP, W, ENDS>), dim3((unsigned)(a.B * a.H), segs), dim3(threads_of<W>), LDS, s, a);
+  return hipGetLastError();
+}
+template <typename T, int DKP, int W> hipError_t backward(const GatedDelta& a, hipStream_t s) {
+  constexpr int KEYS = sizeof(Keys<T, DKP>);
+  static_assert(KEYS <= 160 * 1024, "a workgroup's LDS");
+  static PerDevice ready;
+  hipError_t e = allow_lds<KEYS>(reinterpret_cast<const void*>(&gd_keys_kernel<T, DKP, 16 * W>), ready);
+  if (e == hipSuccess && a.segs > 1) {
+    e = pass<T, DKP, W, true>(a, a.segs - 1, s);
+    if (e == hipSuccess)
+      hipLaunchKernelGGL((gd_join_back_kernel<DKP, W>), dim3((unsigned)(a.B * a.H)), dim3(threads_of<W>), 0, s, a);
+  }
+  if (e == hipSuccess) e = pass<T, DKP, W, false>(a, a.segs, s);
+  if (e != hipSuccess) return e;
   const unsigned chunks = (unsigned)((a.T + C - 1) / C) * a.B * a.G;
   if (chunks) hipLaunchKernelGGL((gd_keys_kernel<T, DKP, 16 * W>), dim3(chunks), dim3(DKP * 4), KEYS, s, a);
   hipLaunchKernelGGL(gd_dlam_kernel, dim3((unsigned)((a.H + 31) / 32)), dim3(1024), 0, s, a);
