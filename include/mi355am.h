@@ -519,7 +519,8 @@ am_status q8_quantise(int64_t rows, int64_t cols, int32_t dtype, const void* x, 
  *   adds to what out holds
  * The matrix cores form products of 8-bit floats exactly and their sums to about 16
  * bits of their size, in fixed order.  ws: workspace of am_q8_matmul_workspace_bytes
- * (256-byte aligned; may be NULL where that is 0).  M, N and K below 2^31. */
+ * (256-byte aligned; may be NULL where that is 0).  M and N below 2^31, rows of codes
+ * less than 2^24 apart. */
 int64_t am_q8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
 am_status q8_matmul(int64_t M, int64_t N, int64_t K, const void* a, int64_t lda, const void* a_scales,
                     int64_t ldas, const void* b, int64_t ldb, const void* b_scales, int64_t ldbs,

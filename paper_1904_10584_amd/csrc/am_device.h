@@ -163,6 +163,15 @@ __device__ __forceinline__ float sgd_one(float w, float u, double lr) {
   return (float)((double)w - lr * (double)u);
 }
 
+// A thread's number, which the compiler takes for another one in each turn of a loop:
+// what is made from it is made again there, a few instructions, where it would be kept
+// through the loop in more registers than there are.
+__device__ __forceinline__ int this_thread() {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+
 // Byte address of an LDS object (for instructions that take it in M0).
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;

@@ -1850,6 +1850,7 @@ am_status q8_matmul(int64_t M, int64_t N, int64_t K, const void* a, int64_t lda,
   AM_TRY(check_q8(N, K, b, ldb, b_scales, ldbs, "b"));
   AM_TRY(check_rows(M, (int32_t)N, AM_BF16, out, ldo, "out"));
   if (!aligned(bias, 4)) return fail(AM_EINVAL, "bias must be 4-byte aligned");
+  if (lda >= (1 << 24) || ldb >= (1 << 24)) return fail(AM_EUNSUPPORTED, "rows of 2^24 codes or more");
   if ((M + 63) / 64 * ((N + 63) / 64) >= (1ll << 24)) return fail(AM_EUNSUPPORTED, "product too large");
   if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need))
     return fail(AM_EWORKSPACE, "needs %lld workspace bytes, 256-byte aligned", (long long)need);

@@ -247,15 +247,6 @@ __device__ __forceinline__ void put4(float* p, int left, f32x4_t v) {
   }
 }
 
-// A thread's number, which the compiler takes for another one in each turn of a loop:
-// what is made from it is made again there, a few instructions, where it would be kept
-// through the loop in more registers than there are.
-__device__ __forceinline__ int this_thread() {
-  int tid = threadIdx.x;
-  asm volatile("" : "+v"(tid));
-  return tid;
-}
-
 // The column of v that a thread's lane has.
 __device__ __forceinline__ int column_of(int tid) { return (tid >> 6) * 16 + (tid & 15); }
 
@@ -658,22 +649,30 @@ template <int DKP, int W> __device__ __forceinline__ float* segment(float* m, co
   return m + ((int64_t)seg * a.B * a.H + bh) * (DKP * 16 * W);
 }
 
-// S += M X: a wave's 16 columns of both; M's rows are DKP apart, and four elements of one
-// lie together.
-template <int DKP>
-__device__ __forceinline__ void join(f32x4_t (&S)[DKP / 16], const float* m, const f32x4_t (&X)[DKP / 16], int lane) {
-  Piece<3> x[DKP / 16];
+// A segment's N and M on their way from memory: a wave's 16 columns of N; of M, whose
+// rows are DKP apart, four elements of a row side by side.
+template <int DKP> struct Segment {
+  static constexpr int KT = DKP / 16;
+  f32x4_t n[KT], m[KT][KT];
+  __device__ __forceinline__ void from(const float* ends, const float* map, int col, int lane) {
 #pragma unroll
-  for (int t = 0; t < DKP / 16; ++t) x[t] = split<3>(X[t]);
+    for (int t = 0; t < KT; ++t) {
+      n[t] = *reinterpret_cast<const f32x4_t*>(ends + col * DKP + 16 * t + 4 * (lane >> 4));
 #pragma unroll
-  for (int t = 0; t < DKP / 16; ++t) {
-    const float* const row = m + (16 * t + (lane & 15)) * DKP + 4 * (lane >> 4);
-#pragma unroll
-    for (int k = 0; k < DKP / 16; k += 2)
-      mma<3, 3>(S[t], split<3>(*reinterpret_cast<const f32x4_t*>(row + 16 * k)),
-                split<3>(*reinterpret_cast<const f32x4_t*>(row + 16 * k + 16)), x[k], x[k + 1]);
+      for (int k = 0; k < KT; ++k) m[t][k] = *reinterpret_cast<const f32x4_t*>(map + (16 * t + (lane & 15)) * DKP + 16 * k + 4 * (lane >> 4));
+    }
   }
-}
+  // N + M X
+  __device__ __forceinline__ void apply(f32x4_t (&X)[KT]) const {
+    Piece<3> x[KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) x[t] = split<3>(X[t]), X[t] = n[t];
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int k = 0; k < KT; k += 2) mma<3, 3>(X[t], split<3>(m[t][k]), split<3>(m[t][k + 1]), x[k], x[k + 1]);
+  }
+};
 
 // Where chunk n of a head keeps what: the state that it starts from (n >= 1) ...
 template <int DKP, int W> __device__ __forceinline__ float* kept_before(const GatedDelta& a, int n, int64_t bh) {

@@ -144,19 +144,25 @@ __global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2)
   }
 }
 
-// The states that segments start from, one after another.
-template <int DKP, int W> __global__ __launch_bounds__(threads_of<W>) void gd_join_kernel(GatedDelta a) {
-  const int lane = threadIdx.x & 63, col = column_of(threadIdx.x), len = a.lens ? a.lens[blockIdx.x / a.H] : a.T;
+// The states that segments start from, one after another: the products of a head's
+// columns wait for the ones before them, so nothing else may (the next segment's maps
+// arrive meanwhile).
+template <int DKP, int W> __global__ __launch_bounds__(64) void gd_join_kernel(GatedDelta a) {
+  const int lane = threadIdx.x, col = 16 * blockIdx.y + (lane & 15), len = a.lens ? a.lens[blockIdx.x / a.H] : a.T;
   f32x4_t S[DKP / 16];
   load_state<DKP>(a.s0 ? a.s0 + (int64_t)blockIdx.x * a.dk * a.dv : nullptr, a, col, lane, S);
-  for (int seg = 0; seg + 1 < a.segs && (seg + 1) * a.per * C < len; ++seg) {
-    f32x4_t N[DKP / 16];
-    float* const at = segment<DKP, W>(a.seg_n, a, seg, blockIdx.x);
-    load_kept<DKP>(at, col, lane, N);
-    join<DKP>(N, segment<DKP, DKP / 16>(a.seg_m, a, seg, blockIdx.x), S, lane);
-    store_kept<DKP>(at, col, lane, N);
-#pragma unroll
-    for (int t = 0; t < DKP / 16; ++t) S[t] = N[t];
+  auto go = [&](int seg) { return seg + 1 < a.segs && (seg + 1) * a.per * C < len; };
+  auto ends = [&](int seg) { return segment<DKP, W>(a.seg_n, a, seg, blockIdx.x); };
+  auto map = [&](int seg) { return segment<DKP, DKP / 16>(a.seg_m, a, seg, blockIdx.x); };
+  Segment<DKP> now, next;
+  constexpr bool AHEAD = DKP == 64;  // (of 128 x 128, one map fills the registers)
+  if (AHEAD && go(0)) now.from(ends(0), map(0), col, lane);
+  for (int seg = 0; go(seg); ++seg) {
+    if (!AHEAD) now.from(ends(seg), map(seg), col, lane);
+    else if (go(seg + 1)) next.from(ends(seg + 1), map(seg + 1), col, lane);
+    now.apply(S);
+    store_kept<DKP>(ends(seg), col, lane, S);
+    if (AHEAD) now = next;
   }
 }
 
@@ -270,7 +276,7 @@ template <typename T, int DKP, int W> hipError_t chunks(const GatedDelta& a, hip
     hipError_t e = pass<T, DKP, DKP / 16, MAPS>(a, a.train ? a.segs : a.segs - 1, s);
     if (e == hipSuccess) e = pass<T, DKP, W, ENDS>(a, a.segs - 1, s);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((gd_join_kernel<DKP, W>), dim3((unsigned)(a.B * a.H)), dim3(threads_of<W>), 0, s, a);
+    hipLaunchKernelGGL((gd_join_kernel<DKP, W>), dim3((unsigned)(a.B * a.H), W), dim3(64), 0, s, a);
   }
   return pass<T, DKP, W, OUTPUTS>(a, a.segs, s);
 }

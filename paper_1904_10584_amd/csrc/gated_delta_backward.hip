@@ -251,19 +251,22 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
 }
 
 // The gradients of the states that segments end in, from the last one on.
-template <int DKP, int W> __global__ __launch_bounds__(threads_of<W>) void gd_join_back_kernel(GatedDelta a) {
-  const int lane = threadIdx.x & 63, col = column_of(threadIdx.x), len = a.lens ? a.lens[blockIdx.x / a.H] : a.T;
+template <int DKP, int W> __global__ __launch_bounds__(64) void gd_join_back_kernel(GatedDelta a) {
+  const int lane = threadIdx.x, col = 16 * blockIdx.y + (lane & 15), len = a.lens ? a.lens[blockIdx.x / a.H] : a.T;
   f32x4_t dS[DKP / 16];
   load_state<DKP>(a.dsT ? a.dsT + (int64_t)blockIdx.x * a.dk * a.dv : nullptr, a, col, lane, dS);
+  auto ends = [&](int seg) { return segment<DKP, W>(a.seg_d, a, seg - 1, blockIdx.x); };
+  auto map = [&](int seg) { return segment<DKP, DKP / 16>(a.seg_mt, a, seg, blockIdx.x); };
   const int frames = a.per * C, last = len > 0 ? (len - 1) / frames : 0;
+  Segment<DKP> now, next;
+  constexpr bool AHEAD = DKP == 64;
+  if (AHEAD && last > 0) now.from(ends(last), map(last), col, lane);
   for (int seg = last; seg > 0; --seg) {
-    f32x4_t D[DKP / 16];
-    float* const at = segment<DKP, W>(a.seg_d, a, seg - 1, blockIdx.x);
-    load_kept<DKP>(at, col, lane, D);
-    join<DKP>(D, segment<DKP, DKP / 16>(a.seg_mt, a, seg, blockIdx.x), dS, lane);
-    store_kept<DKP>(at, col, lane, D);
-#pragma unroll
-    for (int t = 0; t < DKP / 16; ++t) dS[t] = D[t];
+    if (!AHEAD) now.from(ends(seg), map(seg), col, lane);
+    else if (seg > 1) next.from(ends(seg - 1), map(seg - 1), col, lane);
+    now.apply(dS);
+    store_kept<DKP>(ends(seg), col, lane, dS);
+    if (AHEAD) now = next;
   }
 }
 
@@ -543,7 +546,7 @@ template <typename T, int DKP, int W> hipError_t backward(const GatedDelta& a, h
   if (e == hipSuccess && a.segs > 1) {
     e = pass<T, DKP, W, true>(a, a.segs - 1, s);
     if (e == hipSuccess)
-      hipLaunchKernelGGL((gd_join_back_kernel<DKP, W>), dim3((unsigned)(a.B * a.H)), dim3(threads_of<W>), 0, s, a);
+      hipLaunchKernelGGL((gd_join_back_kernel<DKP, W>), dim3((unsigned)(a.B * a.H), W), dim3(64), 0, s, a);
   }
   if (e == hipSuccess) e = pass<T, DKP, W, false>(a, a.segs, s);
   if (e != hipSuccess) return e;

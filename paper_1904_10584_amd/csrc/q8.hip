@@ -153,11 +153,17 @@ __device__ uint4 g_none[1];  // zeros: what lies outside an operand
 constexpr int BK = 128;     // elements of the sum a stage
 constexpr int XCDS = 8;
 
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
-// Four bytes a lane from global memory to LDS at lds_base + 4 * lane.
+// Four bytes a lane from global memory to LDS at lds_base + 4 * lane; and 16 from a
+// base that is the wave's, and an offset below 4 GiB that is the lane's.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma16_at(const void* base, uint32_t offset, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               ::"v"(offset), "s"(base), "s"(lds_base) : "memory", "m0");
+}
 __device__ __forceinline__ void dma4(const void* src, uint32_t lds_base) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds_base) : "memory", "m0");
 }
@@ -179,6 +185,7 @@ template <int BM_, int BN_, int WM_, int WN_, int NS_> struct Shape {
   static constexpr int LDS = NS * STAGE + SETS * SCALE_ROWS * 4;
   static_assert(BM % 64 == 0 && BN % 64 == 0 && (BM + BN) % (8 * WAVES) == 0, "whole loads");
   static_assert(SCALE_WAVES <= WAVES, "one load of scales a wave");
+  static_assert(4 % NS == 0, "a stage's place is known where it is used");
   static_assert(FN == 2 || FN == 4, "columns of a lane in 16-byte pieces");
 };
 
@@ -187,42 +194,33 @@ template <int BM_, int BN_, int WM_, int WN_, int NS_> struct Shape {
 __device__ __forceinline__ int key_a(int row) { return row & 7; }
 template <int FN> __device__ __forceinline__ int key_b(int row) { return (row & 3) | ((row / (4 * FN)) & 1) << 2; }
 
-// One row's 4 FN columns: + bias, + what out holds, rounded once.
+// The bias of a lane's 4 FN columns.
+template <int FN> __device__ __forceinline__ void bias_of(const Q8Matmul& a, int64_t col, f32x4_t (&v)[FN]) {
+#pragma unroll
+  for (int j = 0; j < FN; ++j) v[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  if (a.bias)
+#pragma unroll
+    for (int j = 0; j < 4 * FN; ++j) v[j / 4][j % 4] = a.bias[min(col + j, a.N - 1)];
+}
+// One row's columns: + bias, + what out holds, rounded once.
 template <int FN>
-__device__ __forceinline__ void q8_store(const Q8Matmul& a, int64_t row, int64_t col, const f32x4_t (&v)[FN]) {
+__device__ __forceinline__ void q8_store(const Q8Matmul& a, int64_t row, int64_t col, const f32x4_t (&bias)[FN],
+                                         const f32x4_t (&v)[FN]) {
+  typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+  typedef float f8 __attribute__((ext_vector_type(8)));
   if (row >= a.M || col >= a.N) return;
   bf16_t* p = a.out + row * a.ldo + col;
-  float x[4 * FN];
 #pragma unroll
-  for (int j = 0; j < 4 * FN; ++j) x[j] = v[j / 4][j % 4];
-  if (a.bias) {
+  for (int h = 0; h < FN / 2; ++h) {
+    f8 w = __builtin_shufflevector(v[2 * h] + bias[2 * h], v[2 * h + 1] + bias[2 * h + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+    if (a.wide && col + 8 * h + 8 <= a.N) {
+      if (a.accumulate) w += __builtin_convertvector(reinterpret_cast<const b8*>(p)[h], f8);
+      reinterpret_cast<b8*>(p)[h] = __builtin_convertvector(w, b8);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4 * FN; ++j)
-      if (col + j < a.N) x[j] += a.bias[col + j];
-  }
-  if (a.wide && col + 4 * FN <= a.N) {
-#pragma unroll
-    for (int h = 0; h < FN / 2; ++h) {
-      typedef __bf16 b8 __attribute__((ext_vector_type(8)));
-      typedef float f8 __attribute__((ext_vector_type(8)));
-      f8 w;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = x[8 * h + j];
-      if (a.accumulate) {
-        const uint4 u = reinterpret_cast<const uint4*>(p)[h];
-        const uint32_t o[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          w[2 * j] += __uint_as_float(o[j] << 16);
-          w[2 * j + 1] += __uint_as_float(o[j] & 0xffff0000u);
-        }
-      }
-      reinterpret_cast<uint4*>(p)[h] = __builtin_bit_cast(uint4, __builtin_convertvector(w, b8));
+      for (int j = 0; j < 8; ++j)
+        if (col + 8 * h + j < a.N) p[8 * h + j] = f32_to_bf16(a.accumulate ? w[j] + bf16_to_f32(p[8 * h + j]) : w[j]);
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4 * FN; ++j)
-      if (col + j < a.N) p[j] = f32_to_bf16(a.accumulate ? x[j] + bf16_to_f32(p[j]) : x[j]);
   }
 }
 
@@ -244,19 +242,19 @@ __global__ __launch_bounds__(S::THREADS) void q8_matmul_kernel(Q8Matmul a) {
   const uint32_t base = lds_address(lds), scales = base + S::NS * S::STAGE;
   const uint8_t* scale_lds = lds + S::NS * S::STAGE;
 
-  // where this lane's loads come from; pieces outside an operand come from zeros
-  const uint8_t* src[S::LOADS];
-  bool in[S::LOADS];
-  int piece[S::LOADS];
+  // where this lane's loads come from: offsets from the tile's first rows.  (Rows past an
+  // operand's last are that one again: nothing that they make is stored.)
+  const uint8_t* const base_a = a.a + m0 * a.lda;
+  const uint8_t* const base_b = a.b + n0 * a.ldb;
+  uint32_t offset[S::LOADS];
 #pragma unroll
   for (int i = 0; i < S::LOADS; ++i) {
     const int row = (wave * S::LOADS + i) * 8 + (lane >> 3);  // of both operands' tiles
     const bool is_a = (wave * S::LOADS + i) * 8 < S::BM;
     const int r = is_a ? row : row - S::BM;
-    piece[i] = 16 * ((lane & 7) ^ (is_a ? key_a(r) : key_b<FN>(r)));
-    const int64_t g = (is_a ? m0 : n0) + r;
-    in[i] = g < (is_a ? a.M : a.N);
-    src[i] = (is_a ? a.a + g * a.lda : a.b + g * a.ldb) + piece[i];
+    const int64_t last = (is_a ? a.M - m0 : a.N - n0) - 1;
+    offset[i] = (uint32_t)min((int64_t)r, last) * (uint32_t)(is_a ? a.lda : a.ldb) +
+                16 * ((lane & 7) ^ (is_a ? key_a(r) : key_b<FN>(r)));
   }
   // and one row's scales
   const uint8_t* scale_src = nullptr;
@@ -269,22 +267,31 @@ __global__ __launch_bounds__(S::THREADS) void q8_matmul_kernel(Q8Matmul a) {
       scale_src = a.b_scale + (a.b_tiles ? g / QT : g) * a.ldbs;
     }
   }
-  auto load = [&](int t) {  // stage t of this workgroup's (a constant number of loads but for scales)
+  auto load = [&](int t, int slot) {  // stage t of this workgroup's, t % NS = slot
     const int64_t at = (int64_t)(k0 + t) * BK;
-    const uint32_t to = base + (t % S::NS) * S::STAGE + wave * S::LOADS * 1024;
+    const uint32_t to = base + slot * S::STAGE + wave * S::LOADS * 1024;
     if (t % 4 == 0 && wave < S::SCALE_WAVES)
       dma4(scale_src + at / BK, scales + (t / 4 % S::SETS) * S::SCALE_ROWS * 4 + wave * 256);
+    if (at + BK <= a.K) {
 #pragma unroll
-    for (int i = 0; i < S::LOADS; ++i) {
-      const void* p = in[i] && at + piece[i] < a.K ? (const void*)(src[i] + at) : (const void*)g_none;
-      dma16(p, to + i * 1024);
+      for (int i = 0; i < S::LOADS; ++i)
+        dma16_at(((wave * S::LOADS + i) * 8 < S::BM ? base_a : base_b) + at, offset[i], to + i * 1024);
+    } else {  // pieces past the rows' ends come from zeros
+      const int ln = this_thread() & 63;
+#pragma unroll
+      for (int i = 0; i < S::LOADS; ++i) {
+        const bool is_a = (wave * S::LOADS + i) * 8 < S::BM;
+        const int row = (wave * S::LOADS + i) * 8 - (is_a ? 0 : S::BM) + (ln >> 3);
+        const int piece = 16 * ((ln & 7) ^ (is_a ? key_a(row) : key_b<FN>(row)));
+        dma16(at + piece < a.K ? (const void*)((is_a ? base_a : base_b) + at + offset[i]) : (const void*)g_none, to + i * 1024);
+      }
     }
   };
 #pragma unroll
   for (int t = 0; t < S::NS - 1; ++t)
-    if (t < nk) load(t);
+    if (t < nk) load(t, t);
 
-  const int wm = wave / S::WN, wn = wave % S::WN, i16 = lane & 15, g4 = lane >> 4;
+  const int wm = wave / S::WN, wn = wave % S::WN;
   f32x4_t acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -298,8 +305,9 @@ __global__ __launch_bounds__(S::THREADS) void q8_matmul_kernel(Q8Matmul a) {
     const int later = min(nk - 1 - t, S::NS - 2);
     wait_vm_n<S::LOADS * (S::NS - 2)>(later * S::LOADS);
     lds_barrier();
-    if (t + S::NS - 1 < nk) load(t + S::NS - 1);  // (into the stage that was read before the barrier)
-    const uint8_t* st = lds + (t % S::NS) * S::STAGE;
+    if (t + S::NS - 1 < nk) load(t + S::NS - 1, (OP + S::NS - 1) % S::NS);  // (into the stage read before the barrier)
+    const uint8_t* st = lds + OP % S::NS * S::STAGE;
+    const int ln = this_thread() & 63, i16 = ln & 15, g4 = ln >> 4;
     if constexpr (OP == 0) {
       const uint8_t* sc = scale_lds + (t / 4 % S::SETS) * S::SCALE_ROWS * 4;
 #pragma unroll
@@ -309,12 +317,9 @@ __global__ __launch_bounds__(S::THREADS) void q8_matmul_kernel(Q8Matmul a) {
         sb[j] = *reinterpret_cast<const int*>(sc + 4 * (S::BM + wn * S::TN + (i16 >> 2) * 4 * FN + 4 * j + (i16 & 3)));
     }
     auto fragment = [&](const uint8_t* row, int key) {
-      i32x8_t f;
-      const uint4 lo = *reinterpret_cast<const uint4*>(row + 16 * ((2 * g4) ^ key));
-      const uint4 hi = *reinterpret_cast<const uint4*>(row + 16 * ((2 * g4 + 1) ^ key));
-      f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w;
-      f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
-      return f;
+      return (i32x8_t)__builtin_shufflevector(*reinterpret_cast<const i32x4_t*>(row + 16 * ((2 * g4) ^ key)),
+                                              *reinterpret_cast<const i32x4_t*>(row + 16 * ((2 * g4 + 1) ^ key)), 0, 1,
+                                              2, 3, 4, 5, 6, 7);
     };
     i32x8_t fb[FN];
 #pragma unroll
@@ -347,9 +352,12 @@ __global__ __launch_bounds__(S::THREADS) void q8_matmul_kernel(Q8Matmul a) {
         p[(int64_t)(i * FN + j) * S::THREADS] = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
     return;
   }
+  const int i16 = lane & 15, g4 = lane >> 4;
+  f32x4_t bias[FN];
+  bias_of<FN>(a, n0 + wn * S::TN + g4 * 4 * FN, bias);
 #pragma unroll
   for (int i = 0; i < FM; ++i)
-    q8_store<FN>(a, m0 + wm * S::TM + 16 * i + i16, n0 + wn * S::TN + g4 * 4 * FN, acc[i]);
+    q8_store<FN>(a, m0 + wm * S::TM + 16 * i + i16, n0 + wn * S::TN + g4 * 4 * FN, bias, acc[i]);
 }
 
 // The sums of a split product, added in the order of the splits.
@@ -370,7 +378,10 @@ __global__ __launch_bounds__(S::THREADS) void q8_join_kernel(Q8Matmul a) {
       v[j] += f32x4_t{u.x, u.y, u.z, u.w};
     }
   const int64_t m0 = (int64_t)(tile / a.tiles_n) * S::BM, n0 = (int64_t)(tile % a.tiles_n) * S::BN;
-  q8_store<FN>(a, m0 + wave / S::WN * S::TM + 16 * i + (lane & 15), n0 + wave % S::WN * S::TN + (lane >> 4) * 4 * FN, v);
+  const int64_t col = n0 + wave % S::WN * S::TN + (lane >> 4) * 4 * FN;
+  f32x4_t bias[FN];
+  bias_of<FN>(a, col, bias);
+  q8_store<FN>(a, m0 + wave / S::WN * S::TM + 16 * i + (lane & 15), col, bias, v);
 }
 
 typedef Shape<256, 256, 2, 4, 2> Large;
