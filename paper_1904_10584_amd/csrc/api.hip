@@ -1815,7 +1815,7 @@ am_status q8_quantise(int64_t rows, int64_t cols, int32_t dtype, const void* x, 
   a.ld = ld;
   a.x = x;
   a.tiles = tiles != 0;
-  a.wide = aligned(x, 16) && ld * esz_of(dtype) % 16 == 0;
+  a.wide = aligned(x, 16) && ld * esz_of(dtype) % 16 == 0 && cols % 8 == 0;
   a.codes = static_cast<uint8_t*>(codes);
   a.scales = static_cast<uint8_t*>(scales);
   a.ldc = ldc;

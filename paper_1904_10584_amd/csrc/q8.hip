@@ -28,47 +28,60 @@ __device__ __forceinline__ uint32_t magnitude(float v) {
 }
 __device__ __forceinline__ uint32_t umax32(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// Eight elements from column c of a row of `cols`, zeros past its end.
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, bool wide, float (&v)[8]) {
-  if (wide && c + 8 <= cols) {
-    if constexpr (sizeof(T) == 2) {
-      const uint4 u = *reinterpret_cast<const uint4*>(row + c);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// Eight elements of a row as they lie in memory: the first `left` of those at p, which
+// may be none, then zeros.  Lanes that have fewer read what lies before the row's end in
+// their place, and need no branch.
+template <typename T> struct Eight;
+template <> struct Eight<bf16_t> {
+  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+  u32x4_t w;
+  __device__ __forceinline__ float at(int k) const { return __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16); }
+  __device__ __forceinline__ void load(const bf16_t* p, int left, bool wide) {
+    if (wide) {  // (uniform: whole pieces on 16 bytes)
+      w = *reinterpret_cast<const u32x4_t*>(p + min(left - 8, 0));
+      w = left > 0 ? w : u32x4_t{0, 0, 0, 0};
+    } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        v[2 * k] = __uint_as_float(w[k] << 16);
-        v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+        const uint32_t lo = p[min(2 * k, left - 1)], hi = p[min(2 * k + 1, left - 1)];
+        w[k] = (2 * k < left ? lo : 0u) | (2 * k + 1 < left ? hi << 16 : 0u);
       }
-    } else {
-      const float4 a = *reinterpret_cast<const float4*>(row + c), b = *reinterpret_cast<const float4*>(row + c + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? to_f32(row[c + k]) : 0.f;
   }
-}
+};
+template <> struct Eight<float> {
+  f32x4_t w[2];
+  __device__ __forceinline__ float at(int k) const { return w[k >> 2][k & 3]; }
+  __device__ __forceinline__ void load(const float* p, int left, bool wide) {
+    if (wide) {
+      p += min(left - 8, 0);
+      w[0] = *reinterpret_cast<const f32x4_t*>(p);
+      w[1] = *reinterpret_cast<const f32x4_t*>(p + 4);
+      if (left <= 0) w[0] = w[1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float x = p[min(k, left - 1)];
+        w[k >> 2][k & 3] = k < left ? x : 0.f;
+      }
+    }
+  }
+};
 
 template <typename T>
-__global__ __launch_bounds__(256) void q8_quantise_kernel(Q8Quantise a) {
+__global__ __launch_bounds__(256, 3) void q8_quantise_kernel(Q8Quantise a) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[QT * QPITCH];
   __shared__ uint32_t tops[16][QT + 4];
   const int t = threadIdx.x, cx = t & 15, ry = t >> 4;
   const int64_t ty = blockIdx.x / a.across, tx = blockIdx.x % a.across, r0 = ty * QT, c0 = tx * QT;
   const int64_t rows = a.rows, cols = a.cols, c = c0 + 8 * cx;
-  float v[8][8];
+  Eight<T> v[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 8; ++i) {  // (of a row past the last nothing is kept: it is the last one again, without elements)
     const int64_t r = r0 + 8 * ry + i;
-    if (r < rows) {
-      load8(static_cast<const T*>(a.x) + r * a.ld, c, cols, a.wide, v[i]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
-    }
+    v[i].load(static_cast<const T*>(a.x) + min(r, rows - 1) * a.ld + c, (int)(cols - c), a.wide);
   }
+  const int here = (int)min((int64_t)8, rows - r0 - 8 * ry);  // of this thread's rows
   uint32_t row_top[8], col_top[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) row_top[i] = col_top[i] = 0;
@@ -76,7 +89,7 @@ __global__ __launch_bounds__(256) void q8_quantise_kernel(Q8Quantise a) {
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const uint32_t m = magnitude(v[i][k]);
+      const uint32_t m = i < here ? magnitude(v[i].at(k)) : 0u;
       row_top[i] = umax32(row_top[i], m);
       col_top[k] = umax32(col_top[k], m);
     }
@@ -97,10 +110,15 @@ __global__ __launch_bounds__(256) void q8_quantise_kernel(Q8Quantise a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) tops[ry][8 * cx + k] = col_top[k];
     __syncthreads();
+    if (t < QT) {  // a column a thread
+      uint32_t top = tops[0][t];
 #pragma unroll
-    for (int q = 0; q < 16; ++q)
+      for (int q = 1; q < 16; ++q) top = umax32(top, tops[q][t]);
+      tops[0][t] = top;
+    }
+    __syncthreads();
 #pragma unroll
-      for (int k = 0; k < 8; ++k) col_top[k] = umax32(col_top[k], tops[q][8 * cx + k]);
+    for (int k = 0; k < 8; ++k) col_top[k] = tops[0][8 * cx + k];
   }
   if (a.codes) {
     const int64_t pad = (cols + 15) & ~(int64_t)15;
@@ -112,19 +130,25 @@ __global__ __launch_bounds__(256) void q8_quantise_kernel(Q8Quantise a) {
       if (r < rows) {
         if (c < pad)
           *reinterpret_cast<uint2*>(a.codes + r * a.ldc + c) =
-              make_uint2(q8_codes4(v[i][0], v[i][1], v[i][2], v[i][3], inv), q8_codes4(v[i][4], v[i][5], v[i][6], v[i][7], inv));
+              make_uint2(q8_codes4(v[i].at(0), v[i].at(1), v[i].at(2), v[i].at(3), inv),
+                         q8_codes4(v[i].at(4), v[i].at(5), v[i].at(6), v[i].at(7), inv));
         if (!a.tiles && cx == 0) a.scales[r * a.lds + tx] = (uint8_t)e;
       }
     }
     if (a.tiles && t == 0) a.scales[ty * a.lds + tx] = (uint8_t)q8_exponent(row_top[0]);
   }
   if (!a.codes_t) return;
+  const uint32_t k_lo = here >= 4 ? ~0u : here > 0 ? (1u << 8 * here) - 1 : 0u;
+  const uint32_t k_hi = here >= 8 ? ~0u : here > 4 ? (1u << 8 * (here - 4)) - 1 : 0u;
+  const uint64_t keep = (uint64_t)k_hi << 32 | k_lo;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const uint32_t e = q8_exponent(col_top[k]);
     const float inv = q8_inverse(e);
-    *reinterpret_cast<uint2*>(turned + (8 * cx + k) * QPITCH + 8 * ry) =
-        make_uint2(q8_codes4(v[0][k], v[1][k], v[2][k], v[3][k], inv), q8_codes4(v[4][k], v[5][k], v[6][k], v[7][k], inv));
+    // (rows past the last have zeros: the codes of as many as there are are kept)
+    const uint64_t w = (uint64_t)q8_codes4(v[4].at(k), v[5].at(k), v[6].at(k), v[7].at(k), inv) << 32 |
+                       q8_codes4(v[0].at(k), v[1].at(k), v[2].at(k), v[3].at(k), inv);
+    *reinterpret_cast<uint64_t*>(turned + (8 * cx + k) * QPITCH + 8 * ry) = w & keep;
     if (!a.tiles && ry == 0 && c + k < cols) a.scales_t[(c + k) * a.ldst + ty] = (uint8_t)e;
   }
   if (a.tiles && t == 0) a.scales_t[tx * a.ldst + ty] = (uint8_t)q8_exponent(col_top[0]);
@@ -152,6 +176,7 @@ __device__ uint4 g_none[1];  // zeros: what lies outside an operand
 
 constexpr int BK = 128;     // elements of the sum a stage
 constexpr int XCDS = 8;
+constexpr int ACROSS = 4;  // tiles side by side that a run goes through together
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
@@ -226,6 +251,12 @@ __device__ __forceinline__ void q8_store(const Q8Matmul& a, int64_t row, int64_t
 
 // The tile that a workgroup of a launch takes: each XCD has a run of them, so that
 // tiles with the same rows of a share its L2.
+struct Tile { int m, n; };
+__device__ __forceinline__ Tile tile_at(int T, int tiles_m, int tiles_n) {
+  const int whole = ACROSS * tiles_m, group = T / whole, in = T - group * whole;
+  const int wide = min(ACROSS, tiles_n - group * ACROSS);
+  return {in / wide, group * ACROSS + in % wide};
+}
 __device__ __forceinline__ int tile_of(int b, int tiles) {
   const int x = b % XCDS, q = tiles / XCDS, rem = tiles % XCDS;
   return x * q + min(x, rem) + b / XCDS;
@@ -237,7 +268,8 @@ __global__ __launch_bounds__(S::THREADS) void q8_matmul_kernel(Q8Matmul a) {
   constexpr int FM = S::FM, FN = S::FN;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = tile_of(blockIdx.x, a.tiles_m * a.tiles_n);
-  const int64_t m0 = (int64_t)(tile / a.tiles_n) * S::BM, n0 = (int64_t)(tile % a.tiles_n) * S::BN;
+  const Tile place = tile_at(tile, a.tiles_m, a.tiles_n);
+  const int64_t m0 = (int64_t)place.m * S::BM, n0 = (int64_t)place.n * S::BN;
   const int split = blockIdx.y, k0 = split * a.steps, nk = min(a.blocks - k0, a.steps);  // (blocks of BK)
   const uint32_t base = lds_address(lds), scales = base + S::NS * S::STAGE;
   const uint8_t* scale_lds = lds + S::NS * S::STAGE;
@@ -327,12 +359,17 @@ __global__ __launch_bounds__(S::THREADS) void q8_matmul_kernel(Q8Matmul a) {
       const int r = wn * S::TN + (i16 >> 2) * 4 * FN + 4 * j + (i16 & 3);
       fb[j] = fragment(st + S::A_BYTES + r * BK, key_b<FN>(r));
     }
+    const uint8_t* const rows = st + (wm * S::TM + i16) * BK;
+    i32x8_t fa[2];
+    fa[0] = fragment(rows, key_a(i16));
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      const int r = wm * S::TM + 16 * i + i16;
-      const i32x8_t fa = fragment(st + r * BK, key_a(r));
+      if (i + 1 < FM) fa[(i + 1) & 1] = fragment(rows + 16 * (i + 1) * BK, key_a(i16));
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) mma8<OP>(acc[i][j], fb[j], fa, sb[j], sa[i]);
+      for (int j = 0; j < FN; ++j) mma8<OP>(acc[i][j], fb[j], fa[i & 1], sb[j], sa[i]);
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   for (int t = 0; t < nk; t += 4) {
@@ -377,7 +414,8 @@ __global__ __launch_bounds__(S::THREADS) void q8_join_kernel(Q8Matmul a) {
       const float4 u = p[j * S::THREADS];
       v[j] += f32x4_t{u.x, u.y, u.z, u.w};
     }
-  const int64_t m0 = (int64_t)(tile / a.tiles_n) * S::BM, n0 = (int64_t)(tile % a.tiles_n) * S::BN;
+  const Tile place = tile_at(tile, a.tiles_m, a.tiles_n);
+  const int64_t m0 = (int64_t)place.m * S::BM, n0 = (int64_t)place.n * S::BN;
   const int64_t col = n0 + wave % S::WN * S::TN + (lane >> 4) * 4 * FN;
   f32x4_t bias[FN];
   bias_of<FN>(a, col, bias);
