@@ -1846,8 +1846,10 @@ am_status q8_matmul(int64_t M, int64_t N, int64_t K, const void* a, int64_t lda,
   if ((b_tiles != 0 && b_tiles != 1) || (accumulate != 0 && accumulate != 1))
     return fail(AM_EINVAL, "b_tiles and accumulate must be 0 or 1");
   if (M == 0 || N == 0) return AM_OK;
-  AM_TRY(check_q8(M, K, a, lda, a_scales, ldas, "a"));
-  AM_TRY(check_q8(N, K, b, ldb, b_scales, ldbs, "b"));
+  if (K > 0) {  // (without elements of the sum there is nothing to read)
+    AM_TRY(check_q8(M, K, a, lda, a_scales, ldas, "a"));
+    AM_TRY(check_q8(N, K, b, ldb, b_scales, ldbs, "b"));
+  }
   AM_TRY(check_rows(M, (int32_t)N, AM_BF16, out, ldo, "out"));
   if (!aligned(bias, 4)) return fail(AM_EINVAL, "bias must be 4-byte aligned");
   if (lda >= (1 << 24) || ldb >= (1 << 24)) return fail(AM_EUNSUPPORTED, "rows of 2^24 codes or more");
