@@ -453,6 +453,14 @@ def _row(t, name, N, H, dtype):
     return t.data_ptr(), s0
 
 
+def _here(t, name, stream):
+    """Refuses a tensor of another device than the one whose stream the call takes."""
+    if t.is_cuda:
+        now = stream.device_index if stream is not None else _raw_device() if _raw_device else torch.cuda.current_device()
+        if t.get_device() != now:
+            raise AmError(f"{name} is on GPU {t.get_device()}, the call on GPU {now}")
+
+
 def _rows3(x, r, i, names, N, H, dtype):
     """Device pointers and the one row stride of three matrices."""
     (xp, ld), (rp, lr), (ip, li) = (_row(x, names[0], N, H, dtype), _row(r, names[1], N, H, dtype),
@@ -534,30 +542,33 @@ def gated_delta_workspace_bytes(T, B, heads, dk, dv, key_heads=None, dtype=torch
     return int(n)
 
 
-def _delta(q, k, v, r, b, lam, T, B, heads, key_heads, lengths, s0):
-    """What both passes share: sizes, states' shape and the arguments up to b."""
+def _delta(q, k, v, r, b, T, B, heads, key_heads, lengths, stream):
+    """What both passes share: columns of q and v, frames, type, states' shape, what must
+    live until the call, and its arguments up to b."""
     key_heads = heads if key_heads is None else key_heads
     arr, lp, N = _packed_rows(T, B, lengths)
     if heads < 1 or key_heads < 1 or heads % key_heads:
         raise AmError(f"key_heads = {key_heads} must divide heads = {heads}")
-    dt = _dtype(q, "q")
+    dt, kind = _dtype(q, "q"), q.dtype
     for t, name, n in ((q, "q", key_heads), (v, "v", heads)):
         if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[1] % n:
             raise AmError(f"{name} must be [{N}] rows of {n} heads")
-    dk, dv, kind = q.shape[1] // key_heads, v.shape[1] // heads, q.dtype
-    rows = [x for t, name, n in ((q, "q", key_heads * dk), (k, "k", key_heads * dk), (v, "v", heads * dv),
-                                 (r, "r", heads), (b, "b", heads)) for x in _row(t, name, N, n, kind)]
-    return dk, dv, N, kind, (B, heads, dk, dv), arr, [T, B, heads, key_heads, dk, dv, dt, lp] + rows
+    nq, nv = q.shape[1], v.shape[1]
+    dk, dv = nq // key_heads, nv // heads
+    args = (T, B, heads, key_heads, dk, dv, dt, lp, *_row(q, "q", N, nq, kind), *_row(k, "k", N, nq, kind),
+            *_row(v, "v", N, nv, kind), *_row(r, "r", N, heads, kind), *_row(b, "b", N, heads, kind))
+    _here(q, "q", stream)
+    return nq, nv, N, kind, (B, heads, dk, dv), arr, args
 
 
 def gated_delta_forward(q, k, v, r, b, lam, T, B, o, ws=None, heads=1, key_heads=None, lengths=None, s0=None,
                         sT=None, c=8.0, eps=1e-6, train=False, stream=None):
     """q, k: [N][key_heads dk], v and o: [N][heads dv], r, b: [N][heads] rows (columns of
     one projection, say); lam: [heads]; s0, sT: [B][heads][dk][dv] fp32 (sT may be s0)."""
-    dk, dv, N, kind, state, arr, args = _delta(q, k, v, r, b, lam, T, B, heads, key_heads, lengths, s0)
+    nq, nv, N, kind, state, arr, args = _delta(q, k, v, r, b, T, B, heads, key_heads, lengths, stream)
     wp, wn = _workspace(ws)
     st = (_lib or lib()).gated_delta_forward(
-        *args, _shaped(lam, "lam", (heads,)), c, eps, _shaped(s0, "s0", state), *_row(o, "o", N, heads * dv, kind),
+        *args, _shaped(lam, "lam", (heads,)), c, eps, _shaped(s0, "s0", state), *_row(o, "o", N, nv, kind),
         _shaped(sT, "sT", state), 1 if train else 0, wp, wn, _stream(stream))
     if st:
         _check(st)
@@ -567,14 +578,12 @@ def gated_delta_backward(q, k, v, r, b, lam, T, B, do, ws, dq, dk, dv, dr, db, d
                          lengths=None, s0=None, dsT=None, ds0=None, c=8.0, eps=1e-6, stream=None):
     """The gradient of the forward call (train=True) that filled `ws`, with the s0 that
     it had; dq, dk, dv, dr, db: rows as of q, k, v, r, b."""
-    nk, nv, N, kind, state, arr, args = _delta(q, k, v, r, b, lam, T, B, heads, key_heads, lengths, s0)
-    keys = heads if key_heads is None else key_heads
+    nq, nv, N, kind, state, arr, args = _delta(q, k, v, r, b, T, B, heads, key_heads, lengths, stream)
     wp, wn = _workspace(ws)
     st = (_lib or lib()).gated_delta_backward(
         *args, _shaped(lam, "lam", (heads,)), c, eps, _shaped(s0, "s0", state),
-        *_row(do, "do", N, heads * nv, kind), _shaped(dsT, "dsT", state),
-        *_row(dq, "dq", N, keys * nk, kind), *_row(dk, "dk", N, keys * nk, kind),
-        *_row(dv, "dv", N, heads * nv, kind), *_row(dr, "dr", N, heads, kind), *_row(db, "db", N, heads, kind),
+        *_row(do, "do", N, nv, kind), _shaped(dsT, "dsT", state),
+        *_row(dq, "dq", N, nq, kind), *_row(dk, "dk", N, nq, kind), *_row(dv, "dv", N, nv, kind), *_row(dr, "dr", N, heads, kind), *_row(db, "db", N, heads, kind),
         _shaped(dlam, "dlam", (heads,)), _shaped(ds0, "ds0", state), wp, wn, _stream(stream))
     if st:
         _check(st)
@@ -644,6 +653,12 @@ def _q8(codes, scales, name, rows, cols, tiles=False):
     """Pointers and row strides of a matrix in 8 bits; Nones for None."""
     if codes is None and scales is None:
         return None, 0, None, 0
+    if cols % 16 == 0 and codes is not None and scales is not None:  # (most calls)
+        (ldc, one), (lds, unit), (n, room) = codes.stride(), scales.stride(), scales.shape
+        if (one == 1 and unit == 1 and rows > 1 and n > 1 and n == (-(-rows // Q8_BLOCK) if tiles else rows)
+                and 128 * room >= cols and room % 4 == 0 and codes.shape == (rows, cols) and codes.is_cuda
+                and scales.is_cuda and codes.dtype in _CODES and scales.dtype in _SCALES):
+            return codes.data_ptr(), ldc, scales.data_ptr(), lds
     for t, what, kinds, n, least in (
             (codes, "codes", _CODES, rows, cols),
             (scales, "scales", _SCALES, -(-rows // Q8_BLOCK) if tiles else rows, -(-cols // (4 * Q8_BLOCK)) * 4)):
@@ -669,6 +684,7 @@ def q8_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, tiles=F
     it lies and, with codes_t and scales_t, transposed; see q8_empty."""
     dt, (rows, cols) = _dtype(x, "x"), x.shape
     xp, ld = _row(x, "x", rows, cols, x.dtype)
+    _here(x, "x", stream)
     st = (_lib or lib()).q8_quantise(
         rows, cols, dt, xp, ld, 1 if tiles else 0, *_q8(codes, scales, "x", rows, cols, tiles),
         *_q8(codes_t, scales_t, "x transposed", cols, rows, tiles), _stream(stream))
@@ -690,6 +706,7 @@ def q8_matmul(a, a_scales, b, b_scales, out, tiles=False, bias=None, accumulate=
         raise AmError(f"a and b must be [M][K] and [N][K], got {tuple(a.shape)} and {tuple(b.shape)}")
     (M, K), N = a.shape, b.shape[0]
     op, ldo = _row(out, "out", M, N, torch.bfloat16)
+    _here(out, "out", stream)
     wp, wn = _workspace(ws)
     st = (_lib or lib()).q8_matmul(
         M, N, K, *_q8(a, a_scales, "a", M, K), *_q8(b, b_scales, "b", N, K, tiles), 1 if tiles else 0,
@@ -702,6 +719,7 @@ def gated_norm_forward_q8(res, codes, scales, o=None, gate=None, w_post=None, sc
                           res_out=None, y=None, rstd=None, eps=1e-6, stream=None):
     """gated_norm_forward whose norm leaves in 8 bits, and in y if that is given."""
     (N, H), act = res.shape, o if o is not None else y if y is not None else res
+    _here(res, "res", stream)
     (op, ldo), (gp, ldg) = _row(o, "o", N, H, act.dtype), _row(gate, "gate", N, H, act.dtype)
     st = (_lib or lib()).gated_norm_forward_q8(
         N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
