@@ -9,7 +9,13 @@ against sparse teacher targets with AdamW:
 The recurrence, what stands between two blocks, the loss and the optimizer are
 the library's kernels; the projections are plain matrix products.
 
+With --mixer delta a block's memory is a matrix for each 64 channels, the gated delta
+rule over q, k, v, r, b = y Wp^T in the recurrence's place.  With --projections 8 the
+blocks' products and their gradients are in 8 bits: the norm leaves in 8 bits, Wp and Wg
+are quantised again after each step.
+
     python -m examples.gated_student [--steps 100] [--bits 8] [--dtype f32]
+                                     [--mixer delta] [--projections 8]
 """
 
 import argparse
@@ -27,7 +33,14 @@ class GatedStudent:
     for one batch shape (T frames, B sequences, `lengths` sorted or None)."""
 
     def __init__(self, layers, input_dim, hidden, classes, T, B, K, lengths=None, dtype=BF16, bits=32,
-                 lr=2e-3, weight_decay=0.01, seed=0):
+                 lr=2e-3, weight_decay=0.01, seed=0, mixer="gated", projections=16):
+        assert hidden % 64 == 0 or mixer == "gated", "the delta rule's heads have 64 channels"
+        assert projections == 16 or dtype == BF16, "products in 8 bits are written in bf16"
+        self.delta, self.q8, self.heads = mixer == "delta", projections == 8, hidden // 64
+        # columns of a block's projection: x, r, i, or q, k, v and two gates a head
+        self.at = [0, hidden, 2 * hidden, 3 * hidden]
+        if self.delta:
+            self.at += [3 * hidden + self.heads, 3 * hidden + 2 * self.heads]
         self.layers, self.H, self.T, self.B, self.lengths, self.dtype = layers, hidden, T, B, lengths, dtype
         self.N = T * B if lengths is None else int(sum(lengths))
         self.lr, self.steps, N, H = lr, 0, self.N, hidden
@@ -37,10 +50,10 @@ class GatedStudent:
         self._add("Win", matrix(H, input_dim), dtype)
         self._add("w0", torch.ones(H))
         for l in range(layers):
-            self._add(f"Wp{l}", matrix(3 * H, H), dtype)
+            self._add(f"Wp{l}", matrix(self.at[-1], H), dtype)
             self._add(f"Wg{l}", matrix(H, H), dtype)
             # decays of an open gate between 0.9 and 0.999 (c = 8)
-            rate = -torch.log(torch.rand(H, generator=gen) * 0.099 + 0.9) / 8.0
+            rate = -torch.log(torch.rand(self.heads if self.delta else H, generator=gen) * 0.099 + 0.9) / 8.0
             self._add(f"lam{l}", torch.log(torch.expm1(rate)))
             self._add(f"post{l}", torch.ones(H))
             self._add(f"scale{l}", torch.full((H,), layers ** -0.5))
@@ -53,12 +66,77 @@ class GatedStudent:
         self.y = [new((N, H)) for _ in range(layers + 1)]
         self.rstd = [new((N, 2), F32) for _ in range(layers + 1)]
         self.h = [new((N, H)) for _ in range(layers)]
-        need = am.gated_recurrence_workspace_bytes(T, B, H, lengths, train=True)
+        need = (am.gated_delta_workspace_bytes(T, B, self.heads, 64, 64, dtype=dtype, lengths=lengths, train=True)
+                if self.delta else am.gated_recurrence_workspace_bytes(T, B, H, lengths, train=True))
         self.rec_ws = [new(max(need, 1), torch.uint8) for _ in range(layers)]
         self.norm_ws = new(am.gated_norm_workspace_bytes(N, H), torch.uint8)
         self.ce_ws = new(am.ce_workspace_bytes(N), torch.uint8)
         self.loss, self.dlogits, self.guard = new(1, F32), new((N, classes)), new(1, F32)
         self.optimizer = self._optimizer(bits, weight_decay)
+        self.codes = {}
+        if self.q8:
+            P, sizes = self.at[-1], am.q8_matmul_workspace_bytes
+            self.y8 = am.q8_empty(N, H)
+            self.q8_ws = new(max(1, sizes(P, H, N), sizes(H, H, N), sizes(N, P, H), sizes(N, H, P), sizes(N, H, H)), torch.uint8)
+            self._quantise_weights()
+
+    def _quantise_weights(self):
+        """The blocks' weights in 8 bits, as they lie and transposed."""
+        for k, w in self.master.items():
+            if k[:2] in ("Wp", "Wg"):
+                if k not in self.codes:
+                    self.codes[k] = am.q8_empty(*w.shape, True) + am.q8_empty(*w.shape[::-1], True)
+                am.q8_quantise(w, *self.codes[k], tiles=True)
+
+    def _in_8_bits(self, x, transposed):
+        """x in 8 bits as it lies, or transposed."""
+        if transposed:
+            out = am.q8_empty(*x.shape[::-1])
+            am.q8_quantise(x, codes_t=out[0], scales_t=out[1])
+        else:
+            out = am.q8_empty(*x.shape)
+            am.q8_quantise(x, *out)
+        return out
+
+    def _norm(self, l, res, **parts):
+        """The norm before block l; in 8 bits too where the block's products are."""
+        if self.q8 and l < self.layers:
+            am.gated_norm_forward_q8(res, *self.y8, y=self.y[l], rstd=self.rstd[l], **parts)
+        else:
+            am.gated_norm_forward(res, y=self.y[l], rstd=self.rstd[l], **parts)
+
+    def _project(self, y, y8, name):
+        """y W^T; y8: y in 8 bits."""
+        if not self.q8:
+            return y @ self.weights[name].t()
+        out = torch.empty((y.shape[0], self.master[name].shape[0]), dtype=BF16, device="cuda")
+        am.q8_matmul(*y8, *self.codes[name][:2], out, tiles=True, ws=self.q8_ws)
+        return out
+
+    def _project_back(self, y, grads):
+        """The gradient of y and of the weights from [(name, dL/d(y W^T))]."""
+        g, w = self.grads, self.weights
+        if not self.q8:
+            dy = None
+            for name, d in grads:
+                torch.mm(d.t(), y, out=g[name])
+                dy = d @ w[name] if dy is None else torch.addmm(dy, d, w[name])
+            return dy
+        dy, yt = torch.empty_like(y), self._in_8_bits(y, True)
+        for n, (name, d) in enumerate(grads):
+            am.q8_matmul(*self._in_8_bits(d, True), *yt, g[name], ws=self.q8_ws)
+            am.q8_matmul(*self._in_8_bits(d, False), *self.codes[name][2:], dy, tiles=True, accumulate=n > 0,
+                         ws=self.q8_ws)
+        return dy
+
+    def _mix(self, p, l, o, ws, T, B, lengths, train, s0=None, sT=None):
+        """A block's memory over its projection."""
+        lam = self.weights[f"lam{l}"]
+        if self.delta:
+            am.gated_delta_forward(*self._parts(p), lam, T, B, o, ws, heads=self.heads, lengths=lengths, s0=s0, sT=sT,
+                                   train=train)
+        else:
+            am.gated_recurrence_forward(*self._parts(p), lam, T, B, o, ws, lengths=lengths, h0=s0, hT=sT, train=train)
 
     def _add(self, name, value, kind=F32):
         self.master[name] = value.to("cuda", F32)
@@ -80,8 +158,7 @@ class GatedStudent:
         return [am.AdamWTensors(v) for v in lists.values()]
 
     def _parts(self, t):
-        H = self.H
-        return t[:, :H], t[:, H:2 * H], t[:, 2 * H:]
+        return [t[:, a:b] for a, b in zip(self.at, self.at[1:])]
 
     def forward(self, x):
         """Logits [N][C] fp32 of packed frames x; keeps what backward reads."""
@@ -89,15 +166,13 @@ class GatedStudent:
         self.x = x.to(self.dtype)
         self.p, self.g = [], []
         self.res[0].copy_(self.x @ w["Win"].t())
-        am.gated_norm_forward(self.res[0], w_next=w["w0"], y=self.y[0], rstd=self.rstd[0])
+        self._norm(0, self.res[0], w_next=w["w0"])
         for l in range(self.layers):
-            self.p.append(self.y[l] @ w[f"Wp{l}"].t())
-            self.g.append(self.y[l] @ w[f"Wg{l}"].t())
-            am.gated_recurrence_forward(*self._parts(self.p[l]), w[f"lam{l}"], self.T, self.B, self.h[l],
-                                        self.rec_ws[l], lengths=self.lengths, train=True)
-            am.gated_norm_forward(self.res[l], o=self.h[l], gate=self.g[l], w_post=w[f"post{l}"],
-                                  scale=w[f"scale{l}"], w_next=w[f"next{l}"], res_out=self.res[l + 1],
-                                  y=self.y[l + 1], rstd=self.rstd[l + 1])
+            self.p.append(self._project(self.y[l], self.q8 and self.y8, f"Wp{l}"))
+            self.g.append(self._project(self.y[l], self.q8 and self.y8, f"Wg{l}"))
+            self._mix(self.p[l], l, self.h[l], self.rec_ws[l], self.T, self.B, self.lengths, True)
+            self._norm(l + 1, self.res[l], o=self.h[l], gate=self.g[l], w_post=w[f"post{l}"],
+                       scale=w[f"scale{l}"], w_next=w[f"next{l}"], res_out=self.res[l + 1])
         return torch.addmm(w["bo"], self.y[-1], w["Wo"].t()).float()
 
     def backward(self, dz):
@@ -113,11 +188,10 @@ class GatedStudent:
                                    w_next=w[f"next{l}"], dy=dy, dres_out=dres, do=dh, dgate=dg,
                                    dw_post=g[f"post{l}"], dscale=g[f"scale{l}"], dw_next=g[f"next{l}"])
             dp, dres = torch.empty_like(self.p[l]), below
-            am.gated_recurrence_backward(*self._parts(self.p[l]), w[f"lam{l}"], self.T, self.B, dh,
-                                         self.rec_ws[l], *self._parts(dp), g[f"lam{l}"], lengths=self.lengths)
-            torch.mm(dp.t(), self.y[l], out=g[f"Wp{l}"])
-            torch.mm(dg.t(), self.y[l], out=g[f"Wg{l}"])
-            dy = torch.addmm(dg @ w[f"Wg{l}"], dp, w[f"Wp{l}"])
+            back = am.gated_delta_backward if self.delta else am.gated_recurrence_backward
+            back(*self._parts(self.p[l]), w[f"lam{l}"], self.T, self.B, dh, self.rec_ws[l], *self._parts(dp),
+                 g[f"lam{l}"], lengths=self.lengths, **(dict(heads=self.heads) if self.delta else {}))
+            dy = self._project_back(self.y[l], [(f"Wg{l}", dg), (f"Wp{l}", dp)])
         below = torch.empty_like(self.res[0])
         am.gated_norm_backward(self.res[0], self.rstd[0], below, self.norm_ws, w_next=w["w0"], dy=dy,
                                dres_out=dres, dw_next=g["w0"])
@@ -135,26 +209,36 @@ class GatedStudent:
         for tensors in self.optimizer:
             am.adamw_apply(tensors, lr=self.lr, step=self.steps, beta2=0.99, seed=self.steps,
                            grad_scale=self.guard)
+        if self.q8:
+            self._quantise_weights()
         return self.loss
 
     def check(self):
         """Synchronise; raise if a wait of the last step's recurrences timed out."""
+        if self.delta:  # (which has none)
+            return torch.cuda.synchronize()
         for ws in self.rec_ws:
             am.workspace_check(ws)
 
     def stream(self, states, x):
-        """Logits of the next frame of each stream (x [B][D]); states [layers][B][H]
-        fp32 are carried on in place."""
+        """Logits of the next frame of each stream (x [B][D]); states [layers][B][H] (of the
+        delta rule [layers][B][heads][64][64]) fp32 are carried on in place."""
         w, B = self.weights, x.shape[0]
         res = (x.to(self.dtype) @ w["Win"].t()).float()
         y = torch.empty((B, self.H), dtype=self.dtype, device="cuda")
-        h = torch.empty_like(y)
-        am.gated_norm_forward(res, w_next=w["w0"], y=y)
+        h, y8 = torch.empty_like(y), am.q8_empty(B, self.H) if self.q8 else None
+
+        def norm(l, **parts):
+            if self.q8 and l < self.layers:
+                am.gated_norm_forward_q8(res, *y8, **parts)
+            else:
+                am.gated_norm_forward(res, y=y, **parts)
+
+        norm(0, w_next=w["w0"])
         for l in range(self.layers):
-            p, gate = y @ w[f"Wp{l}"].t(), y @ w[f"Wg{l}"].t()
-            am.gated_recurrence_forward(*self._parts(p), w[f"lam{l}"], 1, B, h, h0=states[l], hT=states[l])
-            am.gated_norm_forward(res, o=h, gate=gate, w_post=w[f"post{l}"], scale=w[f"scale{l}"],
-                                  w_next=w[f"next{l}"], res_out=res, y=y)
+            p, gate = self._project(y, y8, f"Wp{l}"), self._project(y, y8, f"Wg{l}")
+            self._mix(p, l, h, None, 1, B, None, False, states[l], states[l])
+            norm(l + 1, o=h, gate=gate, w_post=w[f"post{l}"], scale=w[f"scale{l}"], w_next=w[f"next{l}"], res_out=res)
         return torch.addmm(w["bo"], y, w["Wo"].t()).float()
 
 
@@ -163,11 +247,14 @@ def main():
     ap.add_argument("--steps", type=int, default=100)
     ap.add_argument("--bits", type=int, default=32, choices=(32, 8))
     ap.add_argument("--dtype", default="bf16", choices=("bf16", "f32"))
+    ap.add_argument("--mixer", default="gated", choices=("gated", "delta"))
+    ap.add_argument("--projections", type=int, default=16, choices=(16, 8))
     a = ap.parse_args()
     s = synth.WORKLOADS["tiny-2x64"]
     T, B, K = s["T"], s["B"], s["K"]
     student = GatedStudent(s["layers"], s["input_dim"], s["hidden"], s["classes"], T, B, K,
-                           dtype=BF16 if a.dtype == "bf16" else F32, bits=a.bits)
+                           dtype=BF16 if a.dtype == "bf16" else F32, bits=a.bits, mixer=a.mixer,
+                           projections=a.projections)
     x = torch.from_numpy(synth.features(T * B, s["input_dim"])).cuda()
     idx, prob = (torch.from_numpy(v).cuda() for v in synth.teacher_targets(T * B, s["classes"], K, s["mass"]))
     for k in range(a.steps):
