@@ -62,15 +62,18 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
   if (begin < chunks) {
     if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, (chunks - 1) * C + threadIdx.x);
     __syncthreads();
-    fetch(s.row[0], max(chunks - 2, 0) * C, threadIdx.x);
+    if (ENDS) fetch(s.row[0], max(chunks - 2, 0) * C, threadIdx.x);
   }
   float dlam = 0.f;  // (of a frame a lane of every chunk, in the last wave)
   int turn = 0;
   for (int n = chunks - 1; n >= begin; --n, turn ^= 1) {
     const int left = hd.len - n * C, tid = this_thread(), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = 16 * wave + l16;
+    // (A chunk's inputs arrive during the one before where only the gradient of the
+    // state goes on.  With everything else in registers that would not fit: the compiler
+    // then kept them in scratch memory, whose waits cost 10 % of the whole.)
+    if (!ENDS) fetch(s.row[turn], max(n - 1, 0) * C, tid);
     const T r_now = fg.r;
-    if constexpr (!ENDS) store_kept<DKP>(kept_after<DKP, W>(a, n, bh), col, lane, dS);
     fk.lengths(s.rk, a.eps, left, tid);
     fq.lengths(s.rq, a.eps, left, tid);
     fk.store(c.k, tid);
@@ -79,12 +82,13 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
     fo.store(&c.v[1], s.row[turn], tid);
     fg.store(s, rate, left, turn, tid);
     __syncthreads();
-    if (n > begin) fetch(s.row[turn ^ 1], max(n - 2, 0) * C, tid);  // the chunk before, which arrives during this one
+    if (ENDS && n > begin) fetch(s.row[turn ^ 1], max(n - 2, 0) * C, tid);
     f32x4_t S[KT];
     if constexpr (!ENDS) {
       if (n > 0) load_kept<DKP>(kept_before<DKP, W>(a, n, bh), col, lane, S);
       else load_state<DKP>(a.s0 ? a.s0 + bh * state : nullptr, a, col, lane, S);
     }
+    if constexpr (!ENDS) store_kept<DKP>(kept_after<DKP, W>(a, n, bh), col, lane, dS);
     triangles<true>(c, tid);
 
     f32x4_t u[NB], o[NB], kd[NB];
@@ -362,11 +366,12 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
         ss[i] = zero;
         if (S) {
           ss[i] = *reinterpret_cast<const f32x4_t*>(S + (c0 + row) * DKP + 4 * u);
-        } else if (S0) {
+        } else if (S0) {  // (as it lies in memory: columns side by side)
+          const int col = c0 + at % 32, key = 4 * (at / 32);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float x = S0[min(4 * u + r, a.dk - 1) * a.dv + min(c0 + row, a.dv - 1)];
-            ss[i][r] = 4 * u + r < a.dk && c0 + row < a.dv ? x : 0.f;
+            const float x = S0[min(key + r, a.dk - 1) * a.dv + min(col, a.dv - 1)];
+            ss[i][r] = key + r < a.dk && col < a.dv ? x : 0.f;
           }
         }
       }
@@ -394,10 +399,11 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         const int at = i * TH + tid, row = at / (DKP / 4), u = at % (DKP / 4);
+        const int mine = S ? row * KEYS + 8 * u : at % 32 * KEYS + 8 * (at / 32);
         const Piece<TO> x = split<TO>(ss[i]), y = split<TO>(sd[i]);
 #pragma unroll
         for (int e = 0; e < TO; ++e) {
-          *reinterpret_cast<u32x2_t*>(all.slice.S[e] + row * KEYS + 8 * u) = x.t[e];
+          *reinterpret_cast<u32x2_t*>(all.slice.S[e] + mine) = x.t[e];
           *reinterpret_cast<u32x2_t*>(all.slice.dS[e] + row * KEYS + 8 * u) = y.t[e];
         }
       }
