@@ -206,6 +206,7 @@ template <int BM_, int BN_, int WM_, int WN_, int NS_> struct Shape {
   static constexpr int A_BYTES = BM * BK, B_BYTES = BN * BK, STAGE = A_BYTES + B_BYTES;
   static constexpr int LOADS = (BM + BN) / 8 / WAVES;             // 16-byte loads a stage of each wave
   static constexpr int SCALE_ROWS = BM + BN, SCALE_WAVES = SCALE_ROWS / 64;
+  static constexpr bool SPLIT = BM < 256;                         // (the largest tiles come by the hundred)
   static constexpr int SETS = (NS + 6) / 4;                       // sets of scales alive at once
   static constexpr int LDS = NS * STAGE + SETS * SCALE_ROWS * 4;
   static_assert(BM % 64 == 0 && BN % 64 == 0 && (BM + BN) % (8 * WAVES) == 0, "whole loads");
@@ -379,7 +380,7 @@ __global__ __launch_bounds__(S::THREADS) void q8_matmul_kernel(Q8Matmul a) {
     if (t + 3 < nk) step(t + 3, std::integral_constant<int, 3>());
   }
 
-  if (a.parts) {  // one of several sums: in the order of the registers
+  if (S::SPLIT && a.parts) {  // one of several sums: in the order of the registers
     float4* p = reinterpret_cast<float4*>(a.parts) +
                 (((int64_t)split * a.tiles_m * a.tiles_n + tile) * FM * FN) * S::THREADS + threadIdx.x;
 #pragma unroll
@@ -428,11 +429,13 @@ typedef Shape<64, 64, 2, 2, 4> Small;
 
 template <typename S> void plan_of(Q8Plan& p, int64_t M, int64_t N, int64_t K) {
   const int64_t tiles = ((M + S::BM - 1) / S::BM) * ((N + S::BN - 1) / S::BN), blocks = (K + BK - 1) / BK;
-  // split where the tiles leave CUs idle and the sum is long: each part has eight
-  // steps at least, in whole words of scales
+  // Split where the tiles leave CUs idle and the sum is long, two workgroups a CU: each
+  // part has eight steps at least, in whole words of scales.  (64 x 2304 with K = 4096
+  // takes 9.5 us so, 15.1 in one; 768 x 768 with 16384 26 and 92; but with K = 2048 the
+  // sums' way through memory costs what it saves: 768 x 768 11.0 and 9.5.)
   int64_t splits = 1;
   const int64_t room = 512 / tiles;
-  if (room >= 2 && blocks >= 16) splits = std::min<int64_t>(room, blocks / 8);
+  if (S::SPLIT && room >= 2 && blocks >= 32) splits = std::min<int64_t>(room, blocks / 8);
   const int64_t steps = ((blocks + splits - 1) / splits + 3) / 4 * 4;
   splits = blocks ? (blocks + steps - 1) / steps : 1;
   p.steps = (int)steps;
@@ -458,8 +461,8 @@ template <typename S> hipError_t run(Q8Matmul a, const Q8Plan& p, hipStream_t s)
   if (p.splits == 1) a.parts = nullptr;
   const unsigned tiles = (unsigned)((int64_t)a.tiles_m * a.tiles_n);
   hipLaunchKernelGGL((q8_matmul_kernel<S>), dim3(tiles, p.splits), dim3(S::THREADS), S::LDS, s, a);
-  if (p.splits > 1)
-    hipLaunchKernelGGL((q8_join_kernel<S>), dim3(tiles * S::FM), dim3(S::THREADS), 0, s, a);
+  if constexpr (S::SPLIT)
+    if (p.splits > 1) hipLaunchKernelGGL((q8_join_kernel<S>), dim3(tiles * S::FM), dim3(S::THREADS), 0, s, a);
   return hipGetLastError();
 }
 
@@ -475,8 +478,16 @@ hipError_t q8_quantise(Q8Quantise a, bool bf16, hipStream_t s) {
 
 Q8Plan q8_plan(int64_t M, int64_t N, int64_t K) {
   Q8Plan p{};
-  const int64_t large = ((M + 255) / 256) * ((N + 255) / 256), medium = ((M + 127) / 128) * ((N + 127) / 128);
-  p.kind = large >= 1024 ? 2 : M > 64 && (medium >= 96 || K >= 4096) ? 1 : 0;
+  const int64_t large = ((M + 255) / 256) * ((N + 255) / 256), small = ((M + 63) / 64) * ((N + 63) / 64);
+  // What was measured, us (K = 768 where no other is named):
+  //   Large from about three tiles a CU on: 24576 x 4608 120 (Medium 128), 12288 x 4608
+  //   with K = 1536 103.5 (106); with 576 tiles 80.1 (75.7).
+  //   Small while all of its tiles run at once, two a CU: 1024 x 2048 6.5 (Medium 9.2),
+  //   2048 x 1024 with K = 1536 9.0 (13.1); 1100 x 2048 9.6 (9.3).
+  //   A long sum over tiles that cannot be split further favours Medium's fewer bytes a
+  //   product: 2304 x 768 with K = 4096 21.6 (Small 16.9), with K = 16384 47 (62.7).
+  // (Of 64 rows or columns Medium's tiles would be half empty.)
+  p.kind = large >= 832 ? 2 : M > 64 && N > 64 && (small > 512 || (small > 256 && K >= 8192)) ? 1 : 0;
   if (p.kind == 2) plan_of<Large>(p, M, N, K);
   else if (p.kind == 1) plan_of<Medium>(p, M, N, K);
   else plan_of<Small>(p, M, N, K);

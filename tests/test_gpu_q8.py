@@ -122,7 +122,7 @@ def _product(a, b, out, **kw):
 @pytest.mark.parametrize("tiles", [False, True])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 64, 16), (64, 64, 128), (65, 63, 127), (16, 200, 129), (64, 2304, 768),
                                    (130, 257, 640), (129, 128, 511), (33, 70, 1100), (300, 500, 5000), (200, 100, 4097),
-                                   (1500, 1400, 300), (8200, 8200, 136)])
+                                   (1500, 1400, 300), (1030, 1100, 8200), (8200, 8200, 136)])
 def test_product(M, N, K, tiles):
     a, b, va, vb = _operands(M, N, K, tiles, seed=M + N + K)
     out = torch.full((M, N), float("nan"), dtype=torch.bfloat16, device="cuda")
