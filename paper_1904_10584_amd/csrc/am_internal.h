@@ -381,9 +381,9 @@ struct GatedDelta {
   float c, eps;
   bool train;                        // forward: keep the states
 };
-// How a batch of up to T frames of `heads` heads of all sequences is cut.
+// How a batch of up to T frames of `heads` heads of all sequences, dv columns each, is cut.
 struct DeltaSegments { int count, per; };
-DeltaSegments delta_segments(int64_t T, int64_t heads);
+DeltaSegments delta_segments(int64_t T, int64_t heads, int dv, bool train);
 constexpr int gd_padded(int dim) { return dim <= 64 ? 64 : 128; }
 constexpr int gd_kept_terms(bool bf16) { return bf16 ? 2 : 3; }
 hipError_t gated_delta_forward(GatedDelta a, bool bf16, hipStream_t s);

@@ -725,9 +725,9 @@ DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int32_t dk, int32_t dv
     l.dsaved = take(chunks * columns * am::gd_padded(dk) * 4);
     l.u = take(chunks * columns * am::GD_CHUNK * am::gd_kept_terms(bf16) * 2);
     l.dr = take(chunks * columns * am::GD_CHUNK * am::gd_kept_terms(bf16) * 2);
-    l.parts = take(B * H * am::delta_segments(T, B * H).count * 4);
+    l.parts = take(B * H * am::delta_segments(T, B * H, dv, train).count * 4);
   }
-  const int64_t segs = T > 0 ? am::delta_segments(T, B * H).count : 1;
+  const int64_t segs = T > 0 ? am::delta_segments(T, B * H, dv, train).count : 1;
   if (segs > 1) {
     const int64_t key = am::gd_padded(dk), state = segs * B * H * key * 4;
     l.seg_n = take(state * am::gd_padded(dv));
@@ -797,7 +797,7 @@ am_status check_delta(int32_t T, int32_t B, int32_t heads, int32_t key_heads, in
     a.lens = at<int32_t>(ws, l.lens);
   }
   // (from T, as the workspace is laid out)
-  const am::DeltaSegments cut = am::delta_segments(T, (int64_t)B * heads);
+  const am::DeltaSegments cut = am::delta_segments(T, (int64_t)B * heads, dv, train);
   a.segs = T > 0 ? cut.count : 1;
   a.per = T > 0 ? cut.per : 1;
   a.seg_n = at<float>(ws, l.seg_n);

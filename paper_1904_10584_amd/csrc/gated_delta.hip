@@ -4,6 +4,7 @@
 #include "gated_delta.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace am {
 namespace {
@@ -301,11 +302,26 @@ template <typename T> hipError_t forward(const GatedDelta& a, hipStream_t s) {
 
 }  // namespace
 
-DeltaSegments delta_segments(int64_t T, int64_t heads) {
-  const int64_t chunks = (T + GD_CHUNK - 1) / GD_CHUNK, most = std::min<int64_t>(512 / heads, chunks / 8);
-  if (most < 3) return {1, (int)chunks};
-  const int64_t per = (chunks + most - 1) / most;
-  return {(int)((chunks + per - 1) / per), (int)per};
+// A forward pass goes through its chunks three times where it is cut (MAPS, ENDS,
+// OUTPUTS, each over all segments at once), a backward pass twice, and the joins take
+// the segments one after another: about 2 us each, a third of a chunk.  n chunks of few
+// heads are so best in segments of about sqrt(n / 8), and heads that fill the chip
+// between them are not cut: two workgroups of 64 columns a CU, one of 128.  Measured, us:
+//   one segment a chunk or longer ones (12 heads of 64 x 64, a training pass): 500
+//   frames 115, in segments of 2 chunks 130, uncut 188; 2000 frames in segments of 1, 2
+//   and 3 chunks 223, 194 and 230, of 8 chunks 351;
+//   workgroups of all segments (40001 frames of 12 heads, forward): up to 384, 512, 768,
+//   1024 508, 440, 440, 507; of 128 x 128 (1500 frames of 24 heads): 192 412, 288 518;
+//   least segments: three in training (2000 frames of 160 heads 734, uncut 839; 190 of
+//   12 88, uncut 93), four in a forward pass alone (2000 of 128 197, uncut 226; in three,
+//   of 160, 252 and 229).
+DeltaSegments delta_segments(int64_t T, int64_t heads, int dv, bool train) {
+  const int64_t chunks = (T + GD_CHUNK - 1) / GD_CHUNK, room = (dv <= 64 ? 512 : 256) / heads, least = train ? 3 : 4;
+  if (room < least) return {1, (int)chunks};
+  const int64_t per = std::max({(chunks + room - 1) / room, (int64_t)std::sqrt(chunks / 8.0), (int64_t)1});
+  const int64_t segs = (chunks + per - 1) / per;
+  if (segs < least) return {1, (int)chunks};
+  return {(int)segs, (int)per};
 }
 
 hipError_t gated_delta_forward(GatedDelta a, bool bf16, hipStream_t s) {

@@ -132,7 +132,19 @@ def test_columns_at_any_offset(pad, dtype):
     Case(66, 2, 1, 23, 41, dtype, pad=pad, seed=pad).check()
 
 
-# segments: at least 24 chunks of few heads; lengths that end in each of them
+# heads that fill the chip between them go through all chunks in one piece
+@BOTH
+@pytest.mark.parametrize("heads,dk,dv", [(180, 16, 24), (90, 70, 66)])
+def test_many_heads(heads, dk, dv, dtype):
+    c = Case(260, 4, heads // 2, dk, dv, dtype, keys=heads // 2, lengths=[260, 200, 129, 3], seed=heads)
+    c.check()
+    o, sT = c.forward()
+    again = c.forward(train=False)
+    assert torch.equal(o, again[0]) and torch.equal(sT, again[1])
+
+
+# segments of several chunks (of few heads: of one, from three chunks on); lengths that
+# end in each of them
 @BOTH
 @pytest.mark.parametrize("T,B,dk,dv,lengths", [(1537, 1, 64, 64, None), (1600, 1, 40, 72, None),
                                                (1700, 4, 16, 16, [1700, 900, 513, 0]), (2000, 1, 128, 128, None),
