@@ -10,8 +10,9 @@
  * Two pieces of the multi-worker trainers run per GPU as well: the aggregate
  * of several workers' compressed updates (§VI-A) and the BMUF-NBM global
  * model step (§VI-B).  Beside the LSTM there are the operators of a student
- * made of gated linear recurrences: the recurrence, what stands between two of
- * its blocks, and an AdamW step.
+ * made of gated linear recurrences: the recurrence, one whose memory is a
+ * matrix (the gated delta rule), what stands between two of its blocks, products
+ * in 8 bits for its projections, and an AdamW step.
  *
  * Conventions for every entry point:
  *  - Pointers are device pointers unless the comment says [host].

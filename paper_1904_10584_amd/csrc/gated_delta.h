@@ -25,6 +25,13 @@
 // below the last place are left out.  (Two terms left states, 4e-6, and the gradient of
 // lam, up to 3e-5, further off than 32 bits do.)  Two terms, off by 2^-18, serve where a
 // sum is only rounded to bf16: O, and the gradients of q and k.
+//
+// What bounds it: neither HBM nor the matrix cores, but a chunk's chain of dependent
+// steps (staging, the triangles, the solve, the state), with two or three workgroups of
+// a CU to fill the waits.  A chunk of 64 x 64 keeps the vector units busy for 28 to 41 %
+// of its time, half of that splitting into terms, and the matrix cores for 10 to 12 %.
+// Blocks of 16 rows in the order of `spot` and rows in that of `place` brought LDS bank
+// conflicts from 12.2 M to 3.5 M cycles (256 sequences of one chunk, 12 heads).
 #pragma once
 
 #include "am_device.h"
