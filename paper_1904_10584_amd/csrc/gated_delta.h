@@ -418,7 +418,9 @@ template <typename T, int W> struct GateRows {
     if (!mine(tid)) return;
     const int t = tid & 63;
     const bool live = t < left;
-    const double c = sums_before(live ? (double)(-rate * sigm(to_f32(r))) * 1.4426950408889634 : 0.0);
+    // (2^-256 is a decay to nothing; a greater one would only cost the sums their places)
+    const double step = (double)(-rate * sigm(to_f32(r))) * 1.4426950408889634;
+    const double c = sums_before(live ? step < -256.0 ? -256.0 : step : 0.0);
     const double last = __shfl(c, C - 1, 64);
     const float hi = (float)c;
     s.ch[t] = hi;

@@ -43,8 +43,8 @@ __global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2)
       for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[t][r] = 16 * t + 4 * (lane >> 4) + r == col ? 1.f : 0.f;
-    } else if (OUT && seg > 0) {
-      load_kept<DKP>(segment<DKP, W>(a.seg_n, a, seg - 1, blockIdx.x), col, lane, S);
+    } else if (OUT && a.segs > 1) {  // (s0 itself may be sT, which the last segment writes)
+      load_kept<DKP>(segment<DKP, W>(a.seg_n, a, seg > 0 ? seg - 1 : a.segs - 1, blockIdx.x), col, lane, S);
     } else {
       load_state<DKP>(OUT && a.s0 ? a.s0 + mine : nullptr, a, col, lane, S);
     }
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2)
 
 // The states that segments start from, one after another: the products of a head's
 // columns wait for the ones before them, so nothing else may (the next segment's maps
-// arrive meanwhile).
+// arrive meanwhile).  The first one's is kept in the last one's place.
 template <int DKP, int W> __global__ __launch_bounds__(64) void gd_join_kernel(GatedDelta a) {
   const int lane = threadIdx.x, col = 16 * blockIdx.y + (lane & 15), len = a.lens ? a.lens[blockIdx.x / a.H] : a.T;
   f32x4_t S[DKP / 16];
@@ -160,6 +160,7 @@ template <int DKP, int W> __global__ __launch_bounds__(64) void gd_join_kernel(G
   auto go = [&](int seg) { return seg + 1 < a.segs && (seg + 1) * a.per * C < len; };
   auto ends = [&](int seg) { return segment<DKP, W>(a.seg_n, a, seg, blockIdx.x); };
   auto map = [&](int seg) { return segment<DKP, DKP / 16>(a.seg_m, a, seg, blockIdx.x); };
+  store_kept<DKP>(ends(a.segs - 1), col, lane, S);
   Segment<DKP> now, next;
   constexpr bool AHEAD = DKP == 64;  // (of 128 x 128, one map fills the registers)
   if (AHEAD && go(0)) now.from(ends(0), map(0), col, lane);

@@ -50,8 +50,8 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
   }
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   f32x4_t dS[KT];
-  if (!ENDS && chunks < all_chunks)
-    load_kept<DKP>(segment<DKP, W>(a.seg_d, a, seg, bh), column_of(threadIdx.x), threadIdx.x & 63, dS);
+  if (!ENDS && a.segs > 1)  // (dsT itself may be ds0, which the first segment writes)
+    load_kept<DKP>(segment<DKP, W>(a.seg_d, a, chunks < all_chunks ? seg : a.segs - 1, bh), column_of(threadIdx.x), threadIdx.x & 63, dS);
   else
     load_state<DKP>(!ENDS && a.dsT ? a.dsT + bh * state : nullptr, a, column_of(threadIdx.x), threadIdx.x & 63, dS);
   Rows<T, DKP, W> fk, fq;
@@ -238,9 +238,13 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
       }
       d += ends;
       if (lane < left) {
+        // Its gradient is a difference of sums that is as small as the decay itself; of one
+        // below e^-69 only their rounding would be left, times any rate.
         const float sr = sigm(to_f32(r_now));
+        const bool lost = rate * sr > 69.f;
         const int64_t row = s.row[turn][lane];
-        static_cast<T*>(a.dr)[row * a.lddr + hd.h] = from_f32<T>(-rate * d * sr * (1.f - sr));
+        if (lost) d = 0.f;
+        static_cast<T*>(a.dr)[row * a.lddr + hd.h] = from_f32<T>(lost ? 0.f : -rate * d * sr * (1.f - sr));
         static_cast<T*>(a.db)[row * a.lddb + hd.h] = from_f32<T>(e * (1.f - s.beta[lane]));
         dlam -= d * sr;
       }
@@ -259,13 +263,15 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
   }
 }
 
-// The gradients of the states that segments end in, from the last one on.
+// The gradients of the states that segments end in, from the last one on; the last
+// one's own is kept behind the others.
 template <int DKP, int W> __global__ __launch_bounds__(64) void gd_join_back_kernel(GatedDelta a) {
   const int lane = threadIdx.x, col = 16 * blockIdx.y + (lane & 15), len = a.lens ? a.lens[blockIdx.x / a.H] : a.T;
   f32x4_t dS[DKP / 16];
   load_state<DKP>(a.dsT ? a.dsT + (int64_t)blockIdx.x * a.dk * a.dv : nullptr, a, col, lane, dS);
   auto ends = [&](int seg) { return segment<DKP, W>(a.seg_d, a, seg - 1, blockIdx.x); };
   auto map = [&](int seg) { return segment<DKP, DKP / 16>(a.seg_mt, a, seg, blockIdx.x); };
+  store_kept<DKP>(segment<DKP, W>(a.seg_d, a, a.segs - 1, blockIdx.x), col, lane, dS);
   const int frames = a.per * C, last = len > 0 ? (len - 1) / frames : 0;
   Segment<DKP> now, next;
   constexpr bool AHEAD = DKP == 64;

@@ -276,6 +276,32 @@ def test_inputs_at_the_edges(what, dtype):
         assert np.abs(_f64(g) - w).max() <= tol * size, (name, np.abs(_f64(g) - w).max(), size)
 
 
+@BOTH
+@pytest.mark.parametrize("lam", [1e3, 1e30, 3e38])
+def test_decays_to_nothing(lam, dtype):
+    """Rates that leave nothing of a state, up to ones past 32 bits: frames alone, and no
+    gradient of the gate that shuts (what rounding leaves of it would be multiplied by
+    the rate)."""
+    c = Case(130, 2, 2, 32, 32, dtype, seed=9, lam=(lam, lam))
+    c.cols(c.proj)[3].fill_(3.0)
+    got, ref = c.forward() + c.backward(), c.oracle()
+    for name, g, w in zip(("o", "sT", "dq", "dk", "dv", "dr", "db", "dlam", "ds0"), got, ref):
+        assert np.isfinite(_f64(g)).all(), name
+        if name in ("dr", "dlam", "ds0"):
+            assert not _f64(g).any() and np.abs(w).max() < 1e-30, name
+        else:
+            assert_close(name, _f64(g), w, BF16_TOL if g.dtype == torch.bfloat16 else F32_TOL)
+
+
+def test_another_gpu_is_refused(monkeypatch):
+    """(As if the call's stream were the second GPU's.)"""
+    c = Case(5, 2, 2, 16, 16, torch.bfloat16, seed=1)
+    monkeypatch.setattr(am, "_raw_device", lambda: 1)
+    for call in (c.forward, c.backward):
+        with pytest.raises(am.AmError, match="GPU"):
+            call()
+
+
 def test_a_nan_stays_in_its_head():
     c = Case(100, 2, 3, 16, 16, torch.float32, seed=1)
     c.cols(c.proj)[2][70, 20] = NAN  # v of head 1, sequence 0, frame 35
