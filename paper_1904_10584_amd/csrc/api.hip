@@ -774,7 +774,8 @@ am_status check_delta(int32_t T, int32_t B, int32_t heads, int32_t key_heads, in
     a.T = lengths[0];
   }
   if (a.N >= (1ll << 31) - 256 || T > (1 << 30)) return fail(AM_EUNSUPPORTED, "too many frames");
-  if (((int64_t)T / am::GD_CHUNK + 1) * B * heads >= (1ll << 31) || (int64_t)heads * am::GD_MAX_DIM >= (1ll << 31))
+  // (2^32 threads a launch, 512 a workgroup)
+  if ((int64_t)B * heads >= (1 << 23) || (train && ((int64_t)T / am::GD_CHUNK + 1) * B * heads >= (1 << 23)))
     return fail(AM_EUNSUPPORTED, "too many heads");
   AM_TRY(check_rows(a.N, key_heads * dk, dtype, q, ldq, "q"));
   AM_TRY(check_rows(a.N, key_heads * dk, dtype, k, ldk, "k"));

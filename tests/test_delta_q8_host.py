@@ -39,6 +39,8 @@ _SHARED = [
     (dict(T=1 << 20, B=1 << 12), am.EUNSUPPORTED, "frames"),
     (dict(T=64, B=1 << 20, heads=1 << 12, key_heads=1 << 11, ldq=1 << 20, ldk=1 << 20, ldv=1 << 20, ldr=1 << 20,
           ldb=1 << 20), am.EUNSUPPORTED, "heads"),
+    (dict(T=1, B=1 << 11, heads=1 << 12, key_heads=1 << 11, ldq=1 << 20, ldk=1 << 20, ldv=1 << 20, ldr=1 << 20,
+          ldb=1 << 20), am.EUNSUPPORTED, "heads"),
 ]
 
 
