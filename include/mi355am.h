@@ -430,9 +430,9 @@ am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dty
  * What is not finite in a frame spreads to what its head does from there on, and may
  * spread to the outputs of the 15 frames before it.
  * 1 <= dk, dv <= 128; key_heads divides heads; N less than 2^31 - 256; B heads, with
- * train = 1 times T / 64 + 1, less than 2^23.  A batch of one frame a sequence with train = 0 and without lengths is one launch that reads and
- * writes the states once.  No atomics and no waits between workgroups: the same inputs
- * give the same bits. */
+ * train = 1 times T / 64 + 1, less than 2^23.  A batch of one frame a sequence with
+ * train = 0 and without lengths is one launch that reads and writes the states once.
+ * No atomics and no waits between workgroups: the same inputs give the same bits. */
 int64_t am_gated_delta_workspace_bytes(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk,
                                        int32_t dv, int32_t dtype, int32_t varlen, int32_t train);
 am_status gated_delta_forward(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv,
