@@ -13,8 +13,8 @@ using namespace gd;
 
 constexpr int THREADS = 256, WAVES = 4;  // of a frame's kernel
 
-// What a launch makes: the outputs, or of each segment but those that nothing follows
-// what it makes of a zero state (ENDS), or of the identity without v (MAPS).
+// What a workgroup makes: the outputs, or of a segment what it makes of a zero state
+// (ENDS), or of the identity without v (MAPS).
 enum Pass { OUTPUTS, ENDS, MAPS };
 
 // All columns of a head are one workgroup's: with 128 of them on two of 64, which share
@@ -22,9 +22,7 @@ enum Pass { OUTPUTS, ENDS, MAPS };
 // 128 x 128 took 357 us and not 335.  The next chunk's rows arrive in registers while one
 // is in hand.  256 x 64 frames, 12 heads of 64 x 64: 92 us (202 MB with both states, 2.2
 // TB/s); 40001 frames of 12 heads in segments 404 us, 4.4 ms without.
-template <typename T, int DKP, int W, Pass PASS>
-__global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2) void gd_forward_kernel(GatedDelta a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+template <typename T, int DKP, int W, Pass PASS> __device__ __forceinline__ void forward_pass(const GatedDelta& a, uint8_t* lds) {
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT, KT = DKP / 16;
   constexpr bool OUT = PASS == OUTPUTS;
   Chunk<T, DKP, W, TO, 1>& c = *reinterpret_cast<Chunk<T, DKP, W, TO, 1>*>(lds);
@@ -150,6 +148,27 @@ __global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2)
   }
 }
 
+template <typename T, int DKP, int W>
+__global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2) void gd_forward_kernel(GatedDelta a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  forward_pass<T, DKP, W, OUTPUTS>(a, lds);
+}
+
+// Both parts of what segments do to a state, in one launch: neither fills the chip.  A
+// training pass needs the last segments' maps too, for the gradient.  (The waves that a
+// part has no columns for end; barriers are the others'.)
+template <int DKP, int W> constexpr int segment_threads = threads_of<(W > DKP / 16 ? W : DKP / 16)>;
+template <typename T, int DKP, int W>
+__global__ __launch_bounds__((segment_threads<DKP, W>), sizeof(T) == 2 && DKP == 64 ? 3 : 2) void gd_segments_kernel(GatedDelta a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  const bool last = (int)blockIdx.y == a.segs - 1;
+  if (blockIdx.z == 0) {
+    if (threadIdx.x < threads_of<DKP / 16> && (!last || a.train)) forward_pass<T, DKP, DKP / 16, MAPS>(a, lds);
+  } else {
+    if (threadIdx.x < threads_of<W> && !last) forward_pass<T, DKP, W, ENDS>(a, lds);
+  }
+}
+
 // The states that segments start from, one after another: the products of a head's
 // columns wait for the ones before them, so nothing else may (the next segment's maps
 // arrive meanwhile).  The first one's is kept in the last one's place.
@@ -270,24 +289,22 @@ __global__ __launch_bounds__(THREADS) void gd_token_kernel(GatedDelta a) {
     }
 }
 
-template <typename T, int DKP, int W, Pass PASS> hipError_t pass(const GatedDelta& a, int segs, hipStream_t s) {
-  constexpr int LDS = sizeof(Chunk<T, DKP, W, Terms<T>::OUT, 1>);
-  static_assert(LDS <= 160 * 1024, "a workgroup's LDS");
-  static PerDevice ready;
-  const hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_forward_kernel<T, DKP, W, PASS>), ready);
-  if (e != hipSuccess || segs == 0) return e;
-  hipLaunchKernelGGL((gd_forward_kernel<T, DKP, W, PASS>), dim3((unsigned)(a.B * a.H), segs), dim3(threads_of<W>), LDS, s, a);
-  return hipGetLastError();
-}
 template <typename T, int DKP, int W> hipError_t chunks(const GatedDelta& a, hipStream_t s) {
+  constexpr int LDS = sizeof(Chunk<T, DKP, W, Terms<T>::OUT, 1>), MAPS_LDS = sizeof(Chunk<T, DKP, DKP / 16, Terms<T>::OUT, 1>);
+  constexpr int BOTH = LDS > MAPS_LDS ? LDS : MAPS_LDS;
+  static_assert(BOTH <= 160 * 1024, "a workgroup's LDS");
+  static PerDevice ready, segments_ready;
+  hipError_t e = allow_lds<LDS>(reinterpret_cast<const void*>(&gd_forward_kernel<T, DKP, W>), ready);
+  if (e == hipSuccess && a.segs > 1)
+    e = allow_lds<BOTH>(reinterpret_cast<const void*>(&gd_segments_kernel<T, DKP, W>), segments_ready);
+  if (e != hipSuccess) return e;
+  const unsigned heads = (unsigned)(a.B * a.H);
   if (a.segs > 1) {
-    // (a training pass needs the last segments' maps too, for the gradient)
-    hipError_t e = pass<T, DKP, DKP / 16, MAPS>(a, a.train ? a.segs : a.segs - 1, s);
-    if (e == hipSuccess) e = pass<T, DKP, W, ENDS>(a, a.segs - 1, s);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((gd_join_kernel<DKP, W>), dim3((unsigned)(a.B * a.H), W), dim3(64), 0, s, a);
+    hipLaunchKernelGGL((gd_segments_kernel<T, DKP, W>), dim3(heads, a.segs, 2), dim3(segment_threads<DKP, W>), BOTH, s, a);
+    hipLaunchKernelGGL((gd_join_kernel<DKP, W>), dim3(heads, W), dim3(64), 0, s, a);
   }
-  return pass<T, DKP, W, OUTPUTS>(a, a.segs, s);
+  hipLaunchKernelGGL((gd_forward_kernel<T, DKP, W>), dim3(heads, a.segs), dim3(threads_of<W>), LDS, s, a);
+  return hipGetLastError();
 }
 
 template <typename T, int CG> hipError_t token(const GatedDelta& a, hipStream_t s) {
