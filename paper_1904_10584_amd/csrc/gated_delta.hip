@@ -21,7 +21,7 @@ enum Pass { OUTPUTS, ENDS, MAPS };
 // nothing but repeat the triangles, 64 utterances of 200 to 1500 frames and 6 heads of
 // 128 x 128 took 357 us and not 335.  The next chunk's rows arrive in registers while one
 // is in hand.  256 x 64 frames, 12 heads of 64 x 64: 92 us (202 MB with both states, 2.2
-// TB/s); 40001 frames of 12 heads in segments 404 us, 4.4 ms without.
+// TB/s); 40001 frames of 12 heads in segments 384 us, 4.4 ms without.
 template <typename T, int DKP, int W, Pass PASS> __device__ __forceinline__ void forward_pass(const GatedDelta& a, uint8_t* lds) {
   constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT, KT = DKP / 16;
   constexpr bool OUT = PASS == OUTPUTS;
@@ -154,7 +154,8 @@ __global__ __launch_bounds__(threads_of<W>, sizeof(T) == 2 && DKP == 64 ? 3 : 2)
   forward_pass<T, DKP, W, OUTPUTS>(a, lds);
 }
 
-// Both parts of what segments do to a state, in one launch: neither fills the chip.  A
+// Both parts of what segments do to a state, in one launch: neither fills the chip.
+// (2000 frames of 12 heads, forward, 70 us and not 79; 8 such of 16 heads 165, 203.)  A
 // training pass needs the last segments' maps too, for the gradient.  (The waves that a
 // part has no columns for end; barriers are the others'.)
 template <int DKP, int W> constexpr int segment_threads = threads_of<(W > DKP / 16 ? W : DKP / 16)>;
@@ -327,11 +328,12 @@ template <typename T> hipError_t forward(const GatedDelta& a, hipStream_t s) {
 
 }  // namespace
 
-// A forward pass goes through its chunks three times where it is cut (MAPS, ENDS,
-// OUTPUTS, each over all segments at once), a backward pass twice, and the joins take
-// the segments one after another: about 2 us each, a third of a chunk.  n chunks of few
+// A forward pass goes through its chunks three times where it is cut (MAPS and ENDS at
+// once, then OUTPUTS, over all segments at once), a backward pass twice, and the joins
+// take the segments one after another: about 2 us each, a third of a chunk.  n chunks of few
 // heads are so best in segments of about sqrt(n / 8), and heads that fill the chip
-// between them are not cut: two workgroups of 64 columns a CU, one of 128.  Measured, us:
+// between them are not cut: two workgroups of 64 columns a CU, one of 128.  Measured, us
+// (with MAPS and ENDS one after another):
 //   one segment a chunk or longer ones (12 heads of 64 x 64, a training pass): 500
 //   frames 115, in segments of 2 chunks 130, uncut 188; 2000 frames in segments of 1, 2
 //   and 3 chunks 223, 194 and 230, of 8 chunks 351;
