@@ -420,7 +420,8 @@ am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dty
  *   dtype    AM_F32 or AM_BF16: type of q, k, v, r, b, o and their gradients
  *   q, k     [N] rows of key_heads dk;  v, o [N] rows of heads dv;  r, b [N] rows of
  *            heads; each with its row stride (columns of one projection, say)
- *   lam      [heads] fp32, finite;  c > 0;  eps > 0
+ *   lam      [heads] fp32, finite;  c > 0;  eps > 0; c softplus(lam) past the largest 32-bit float
+ *            counts as that
  *   lengths  [host] [B] or NULL; variable-length batches allow B <= 1024
  *   s0       [B][heads][dk][dv] fp32 or NULL (zero);  sT the same or NULL: states after
  *            each sequence's last frame (s0 where it has none; may be s0 itself)

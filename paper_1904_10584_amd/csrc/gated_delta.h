@@ -257,6 +257,13 @@ __device__ __forceinline__ void put4(float* p, int left, f32x4_t v) {
 // The column of v that a thread's lane has.
 __device__ __forceinline__ int column_of(int tid) { return (tid >> 6) * 16 + (tid & 15); }
 
+// A head's rate of decay.  What would pass 32 bits is their largest: with a gate that is
+// shut, whose sigmoid is 0, it makes 0 and not a NaN.
+__device__ __forceinline__ float rate_of(const GatedDelta& a, int h) {
+  const float rate = a.c * softplus(a.lam[h]);
+  return rate > 3.402823466e38f ? 3.402823466e38f : rate;
+}
+
 // The sequence and head of a workgroup.
 struct Head {
   int b, h, kh, len;  // sequence, head, key head, frames

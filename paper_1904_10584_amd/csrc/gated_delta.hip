@@ -30,7 +30,7 @@ template <typename T, int DKP, int W, Pass PASS> __device__ __forceinline__ void
   const Head hd(a, blockIdx.x);
   const int seg = blockIdx.y, begin = seg * a.per * C, end = min(hd.len, begin + a.per * C);
   if (seg > 0 && begin >= hd.len) return;
-  const float rate = a.c * softplus(a.lam[hd.h]);
+  const float rate = rate_of(a, hd.h);
   const int64_t mine = (int64_t)blockIdx.x * a.dk * a.dv;
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   f32x4_t S[KT];
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(THREADS) void gd_token_kernel(GatedDelta a) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) kq[wave][lane + 64 * i] = x[i] * r;
   }
-  const float decay = expf(-a.c * softplus(a.lam[hd.h]) * sigm(to_f32(static_cast<const T*>(a.r)[row0 * a.ldr + hd.h])));
+  const float decay = expf(-rate_of(a, hd.h) * sigm(to_f32(static_cast<const T*>(a.r)[row0 * a.ldr + hd.h])));
   const float beta = sigm(to_f32(static_cast<const T*>(a.b)[row0 * a.ldb + hd.h]));
   f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

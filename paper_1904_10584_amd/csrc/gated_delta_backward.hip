@@ -42,7 +42,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
   const int seg = blockIdx.y + (ENDS ? 1 : 0);
   const int64_t bh = blockIdx.x, state = (int64_t)a.dk * a.dv;
   const Head hd(a, blockIdx.x);
-  const float rate = a.c * softplus(a.lam[hd.h]);
+  const float rate = rate_of(a, hd.h);
   const int all_chunks = (hd.len + C - 1) / C, begin = seg * a.per, chunks = min(all_chunks, begin + a.per);
   if (seg > 0 && begin >= all_chunks) {
     if (!ENDS && threadIdx.x == 0) a.parts[seg * (int64_t)gridDim.x + bh] = 0.f;
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
         const bool lost = rate * sr > 69.f;
         const int64_t row = s.row[turn][lane];
         if (lost) d = 0.f;
-        static_cast<T*>(a.dr)[row * a.lddr + hd.h] = from_f32<T>(lost ? 0.f : -rate * d * sr * (1.f - sr));
+        static_cast<T*>(a.dr)[row * a.lddr + hd.h] = from_f32<T>(lost ? 0.f : -rate * sr * ((1.f - sr) * d));
         static_cast<T*>(a.db)[row * a.lddb + hd.h] = from_f32<T>(e * (1.f - s.beta[lane]));
         dlam -= d * sr;
       }
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
     fq.lengths(s.rq, a.eps, left, tid);
     fk.store(all.pairs.k, tid);
     fq.store(all.pairs.q, tid);
-    fg.store(s, a.c * softplus(a.lam[hd.h]), left, 0, tid);
+    fg.store(s, rate_of(a, hd.h), left, 0, tid);
     __syncthreads();
     if (wave == W - 1) combine(s, lane);
 #pragma unroll
