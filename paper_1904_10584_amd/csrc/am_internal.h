@@ -369,8 +369,9 @@ struct GatedDelta {
   float* saved;                      // [chunks - 1][B][H][dv][dk]: states that the second chunk
                                      // and on start from (written by a training forward)
   float* dsaved;                     // [chunks][B][H][dv][dk]: gradients of the chunks' last states
-  uint16_t *u, *dr_rows;             // [chunks][B][H][terms][dv][GD_CHUNK], terms as of gd_kept_terms
-  float* parts;                      // backward: [segments][B][H]
+  uint16_t *u, *dr_rows;             // [chunks][B][H][GD_TERMS][dv][GD_CHUNK]
+  float* parts;                      // backward: [chunks][B][H]: <S, dS'> of a chunk's first state and
+                                     // last gradient, then its share of dlam
   // segments of long sequences (1: none), each of `per` chunks, and padded states of them
   int segs, per;
   float *seg_n, *seg_m, *seg_mt;     // [segs][B][H]: ends, maps, maps transposed
@@ -385,7 +386,7 @@ struct GatedDelta {
 struct DeltaSegments { int count, per; };
 DeltaSegments delta_segments(int64_t T, int64_t heads, int dv, bool train);
 constexpr int gd_padded(int dim) { return dim <= 64 ? 64 : 128; }
-constexpr int gd_kept_terms(bool bf16) { return bf16 ? 2 : 3; }
+constexpr int GD_TERMS = 3;
 hipError_t gated_delta_forward(GatedDelta a, bool bf16, hipStream_t s);
 hipError_t gated_delta_backward(GatedDelta a, bool bf16, hipStream_t s);
 

@@ -723,9 +723,9 @@ DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int32_t dk, int32_t dv
     const int64_t columns = B * H * am::gd_padded(dv);
     l.saved = take(chunks ? (chunks - 1) * columns * am::gd_padded(dk) * 4 : 0);
     l.dsaved = take(chunks * columns * am::gd_padded(dk) * 4);
-    l.u = take(chunks * columns * am::GD_CHUNK * am::gd_kept_terms(bf16) * 2);
-    l.dr = take(chunks * columns * am::GD_CHUNK * am::gd_kept_terms(bf16) * 2);
-    l.parts = take(B * H * am::delta_segments(T, B * H, dv, train).count * 4);
+    l.u = take(chunks * columns * am::GD_CHUNK * am::GD_TERMS * 2);
+    l.dr = take(chunks * columns * am::GD_CHUNK * am::GD_TERMS * 2);
+    l.parts = take(chunks * B * H * 4);
   }
   const int64_t segs = T > 0 ? am::delta_segments(T, B * H, dv, train).count : 1;
   if (segs > 1) {

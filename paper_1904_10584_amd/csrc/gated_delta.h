@@ -24,7 +24,8 @@
 // three terms of 8 bits each, which leave nothing of its 24 bits; products of terms
 // below the last place are left out.  (Two terms left states, 4e-6, and the gradient of
 // lam, up to 3e-5, further off than 32 bits do.)  Two terms, off by 2^-18, serve where a
-// sum is only rounded to bf16: O, and the gradients of q and k.
+// sum is only rounded to bf16: in O, and in what pairs of frames give the gradients of q
+// and k.
 //
 // What bounds it: neither HBM nor the matrix cores, but a chunk's chain of dependent
 // steps (staging, the triangles, the solve, the state), with two or three workgroups of
@@ -364,10 +365,9 @@ template <int W> struct Values<bf16_t, W> {
     v.store(*to, tid);
     m = to;
   }
-  // columns 16 t + lane % 16 over frames of block I; row 16 I + lane % 16, columns 16 t + 4 (lane / 16) and on
+  // columns 16 t + lane % 16 over frames of block I
   __device__ __forceinline__ Piece<1> column(int t, int I, int lane) const;
   __device__ __forceinline__ f32x4_t column_values(int t, int I, int lane) const;
-  __device__ __forceinline__ f32x4_t row_values(int I, int t, int lane) const;
 };
 template <int W> struct Values<float, W> {
   const float* p;
@@ -391,21 +391,6 @@ template <int W> struct Values<float, W> {
     return v;
   }
   __device__ __forceinline__ Piece<3> column(int t, int I, int lane) const { return split<3>(column_values(t, I, lane)); }
-  __device__ __forceinline__ f32x4_t row_values(int I, int t, int lane) const {
-    const int col = 16 * t + 4 * (lane >> 4);
-    const float* const at = p + rows[16 * I + (lane & 15)] * ld + col;
-    f32x4_t v;
-    if (dv % 4 == 0) {
-      v = *reinterpret_cast<const f32x4_a*>(at + min(dv - 4 - col, 0));
-      return col < dv ? v : f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float x = at[min(j, dv - 1 - col)];
-      v[j] = col + j < dv ? x : 0.f;
-    }
-    return v;
-  }
 };
 // The gates of a chunk and the rows of another one; the last wave's.
 template <typename T, int W> struct GateRows {
@@ -477,9 +462,6 @@ template <int W> __device__ __forceinline__ Piece<1> Values<bf16_t, W>::column(i
 }
 template <int W> __device__ __forceinline__ f32x4_t Values<bf16_t, W>::column_values(int t, int I, int lane) const {
   return values(columns_of(*m, t, I, lane));
-}
-template <int W> __device__ __forceinline__ f32x4_t Values<bf16_t, W>::row_values(int I, int t, int lane) const {
-  return values(row4_of(*m, I, t, lane));
 }
 // A block of 16 x 16 has columns 4 g to 4 g + 3 of all rows in 128 bytes, in an order in
 // which neither the 16 lanes that read a column group nor those that read four rows of

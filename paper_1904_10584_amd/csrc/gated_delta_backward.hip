@@ -4,15 +4,20 @@
 //   dU = P^T dO + diag(M_end) K dS',   (I + L)^T dR = dU,   dV = diag(beta) dR,
 //   dS = g_end dS' + Q^T diag(g) dO - K^T diag(g beta) dR.
 // Those go column by column as the forward pass does, backwards in time
-// (gd_backward_kernel), and so do the gates: with  . the product of two rows,
-//   dbeta_i beta_i = dR_i . U_i,   dc_i = dO_i . O_i - dV_i . V_i,  and <dS', S'> at
-// the chunk's end: every sum over pairs of frames has been put together from sums over
-// columns, since P's and L's entries scale with e^c.  What sums over columns, the
-// gradients of q and k, is left to a second kernel, which has no order in time
-// (gd_keys_kernel):
+// (gd_backward_kernel), and with  . the product of two rows so does
+//   dbeta_i beta_i = dR_i . U_i.
+// What sums over columns is left to a second kernel, which has no order in time
+// (gd_keys_kernel): the gradients of q and k,
 //   dQ = diag(g) dO S^T + (M o dO U^T) K,
 //   dK = -diag(g beta) dR S^T + diag(M_end) U dS'^T + (M o dO U^T)^T Q + (B + B^T) K,
-//   B_ij = -beta_i M_ij (dR_i . U_j), j < i.
+//   B_ij = -beta_i M_ij (dR_i . U_j), j < i,
+// and that of each frame's log a, the sum of what crosses it from before to after,
+//   sum_{j < i <= l} X_lj + sum_{l >= i} y_l + sum_{j < i} z_j + g_end <S, dS'>,
+//   X_lj = P_lj (dO_l . U_j) - L_lj (dR_l . U_j),
+//   y_l = g_l q_l . (S dO_l) - beta_l g_l k_l . (S dR_l),   z_j = M_end,j k_j . (dS' U_j):
+// every term has a_i as a factor, however small that is.  (As a difference of sums over
+// columns, dO_l . O_l - dV_l . V_l from i on, its rounding is that of the terms that do
+// not cross: 2 % of dlam where a_i was e^-5, all of it at e^-12.)
 #include "gated_delta.h"
 
 namespace am {
@@ -22,13 +27,13 @@ using namespace gd;
 
 template <typename T, int DKP, int W> struct Backward {
   Chunk<T, DKP, W, Terms<T>::X, 2> c;
-  float rows[2][W][C];  // dO . O - dV . V and dR . U, of a wave's columns
-  float end[W];         // <dS', S'>
+  float rows[W][C];  // dR . U, of a wave's columns
+  float end[W];      // <S, dS'>
 };
 
 // In order of time within a head, as the forward pass, and bound as it is: 256 x 64
-// frames, 12 heads of 64 x 64: 222 us (435 MB, 2 TB/s; two workgroups a CU for their
-// registers); utterances of 200 to 1500 frames, 64 of 6 heads of 128 x 128: 700 us, in
+// frames, 12 heads of 64 x 64: 217 us (485 MB, 2.2 TB/s; two workgroups a CU for their
+// registers); utterances of 200 to 1500 frames, 64 of 6 heads of 128 x 128: 645 us, in
 // which the longest ones have 24 chunks.
 //
 // ENDS: only what each segment makes of a gradient of zero behind it, at its first state.
@@ -44,10 +49,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
   const Head hd(a, blockIdx.x);
   const float rate = rate_of(a, hd.h);
   const int all_chunks = (hd.len + C - 1) / C, begin = seg * a.per, chunks = min(all_chunks, begin + a.per);
-  if (seg > 0 && begin >= all_chunks) {
-    if (!ENDS && threadIdx.x == 0) a.parts[seg * (int64_t)gridDim.x + bh] = 0.f;
-    return;
-  }
+  if (seg > 0 && begin >= all_chunks) return;
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   f32x4_t dS[KT];
   if (!ENDS && a.segs > 1)  // (dsT itself may be ds0, which the first segment writes)
@@ -69,16 +71,14 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
     __syncthreads();
     if (ENDS) fetch(s.row[0], max(chunks - 2, 0) * C, threadIdx.x);
   }
-  float dlam = 0.f;  // (of a frame a lane of every chunk, in the last wave)
   int turn = 0;
   for (int n = chunks - 1; n >= begin; --n, turn ^= 1) {
     const int left = hd.len - n * C, tid = this_thread(), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = 16 * wave + l16;
     // (A chunk's inputs arrive during the one before where only the gradient of the
-    // state goes on.  With everything else in registers that would not fit: the compiler
-    // then kept them in scratch memory, whose waits cost 10 % of the whole.)
+    // state goes on.  With everything else in registers that gave nothing, 217 and 645 us
+    // either way, and spilled where dk is 128 and dv at most 64.)
     if (!ENDS) fetch(s.row[turn], max(n - 1, 0) * C, tid);
-    const T r_now = fg.r;
     fk.lengths(s.rk, a.eps, left, tid);
     fq.lengths(s.rq, a.eps, left, tid);
     fk.store(c.k, tid);
@@ -96,9 +96,9 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
     if constexpr (!ENDS) store_kept<DKP>(kept_after<DKP, W>(a, n, bh), col, lane, dS);
     triangles<true>(c, tid);
 
-    f32x4_t u[NB], o[NB], kd[NB];
+    f32x4_t u[NB], kd[NB];
 #pragma unroll
-    for (int I = 0; I < NB; ++I) u[I] = o[I] = kd[I] = zero;
+    for (int I = 0; I < NB; ++I) u[I] = kd[I] = zero;
     float end = 0.f;
 #pragma unroll
     for (int t = 0; t < DKP / 32; ++t) {
@@ -115,21 +115,13 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
         Piece<TI> a0, a1;
         rows_of(c.k, I, t, lane, a0, a1);
         mma<TI, TX>(kd[I], a0, a1, d0, d1);
-        if constexpr (!ENDS) {
-          mma<TI, TX>(u[I], a0, a1, s0, s1);
-          rows_of(c.q, I, t, lane, a0, a1);
-          mma<TX, TI>(o[I], s0, s1, a0, a1);
-        }
+        if constexpr (!ENDS) mma<TI, TX>(u[I], a0, a1, s0, s1);
       }
     }
     const float g_end = s.g[C - 1];
-    end *= g_end;
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
-      if constexpr (!ENDS) {
-        u[I] = fv.column_values(wave, I, lane) * rows4(s.beta, I, lane) - u[I] * rows4(s.bgk, I, lane);
-        o[I] *= s.gq[16 * I + l16];
-      }
+      if constexpr (!ENDS) u[I] = fv.column_values(wave, I, lane) * rows4(s.beta, I, lane) - u[I] * rows4(s.bgk, I, lane);
       kd[I] *= rows4(s.gk, I, lane);
     }
     // U; transposed, a frame a lane, it is wanted for dR . U
@@ -141,27 +133,15 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
       for (int I = 0; I < NB; ++I) {
         ut[I] = zero;
         mma<TX, TX>(ut[I], r[I], block_of(c.d[I], lane));
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) end = fmaf(u[I][r4], kd[I][r4], end);
-#pragma unroll
-        for (int J = 0; J + 1 <= I; J += 2)
-          mma<TX, TX>(o[I], up[J], up[J + 1], block_of(c.p[lower(I, J)], lane), block_of(c.p[lower(I, J + 1)], lane));
-        if (I % 2 == 0) mma<TX, TX>(o[I], up[I], block_of(c.p[lower(I, I)], lane));
       }
-      uint16_t* const keep = kept_columns<TO, W>(a.u, a, n, bh);
+      uint16_t* const keep = kept_columns<TX, W>(a.u, a, n, bh);
 #pragma unroll
-      for (int e = 0; e < TO; ++e)
+      for (int e = 0; e < TX; ++e)
 #pragma unroll
         for (int I = 0; I < NB; ++I)
           *reinterpret_cast<u32x2_t*>(keep + (e * 16 * W + col) * C + 16 * I + 4 * g4) = up[I].t[e];
     }
-    float y1[NB], y2[NB];
-#pragma unroll
-    for (int I = 0; I < NB; ++I) {
-      if constexpr (ENDS) break;
-      const f32x4_t x = fo.row_values(I, wave, lane) * o[I];
-      y1[I] = (x[0] + x[1]) + (x[2] + x[3]);
-    }
+    float drive[NB];
     // dU in kd, then dR, block after block from the last
 #pragma unroll
     for (int J = 0; J < NB; ++J)
@@ -180,17 +160,16 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
 #pragma unroll
         for (int J = I - 1; J >= 0; --J) mma<TX, TX>(kd[J], block_turned(c.l[below(I, J)], lane), dp[I]);
         if constexpr (ENDS) continue;
-        const f32x4_t dv = dr * s.beta[16 * I + l16], x = dv * fv.row_values(I, wave, lane), y = dr * ut[I];
-        y1[I] -= (x[0] + x[1]) + (x[2] + x[3]);
-        y2[I] = (y[0] + y[1]) + (y[2] + y[3]);
+        const f32x4_t dv = dr * s.beta[16 * I + l16], y = dr * ut[I];
+        drive[I] = (y[0] + y[1]) + (y[2] + y[3]);
         if (16 * I + l16 < left)
           put4(static_cast<T*>(a.dv_) + s.row[turn][16 * I + l16] * a.lddv + (int64_t)hd.h * a.dv + 16 * wave + 4 * g4,
                a.dv - 16 * wave - 4 * g4, dv);
       }
-      uint16_t* const keep = kept_columns<TO, W>(a.dr_rows, a, n, bh);
+      uint16_t* const keep = kept_columns<TX, W>(a.dr_rows, a, n, bh);
       if constexpr (!ENDS)
 #pragma unroll
-      for (int e = 0; e < TO; ++e)
+      for (int e = 0; e < TX; ++e)
 #pragma unroll
         for (int I = 0; I < NB; ++I)
           *reinterpret_cast<u32x2_t*>(keep + (e * 16 * W + col) * C + 16 * I + 4 * g4) = dp[I].t[e];
@@ -215,39 +194,20 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
     if constexpr (!ENDS) {
 #pragma unroll
     for (int I = 0; I < NB; ++I) {
-      y1[I] += __shfl_xor(y1[I], 16, 64);
-      y2[I] += __shfl_xor(y2[I], 16, 64);
-      y1[I] += __shfl_xor(y1[I], 32, 64);
-      y2[I] += __shfl_xor(y2[I], 32, 64);
-      if (g4 == 0) {
-        all.rows[0][wave][16 * I + l16] = y1[I];
-        all.rows[1][wave][16 * I + l16] = y2[I];
-      }
+      drive[I] += __shfl_xor(drive[I], 16, 64);
+      drive[I] += __shfl_xor(drive[I], 32, 64);
+      if (g4 == 0) all.rows[wave][16 * I + l16] = drive[I];
     }
     end = wave_sum_uniform(end);
     if (lane == 0) all.end[wave] = end;
     __syncthreads();
-    if (wave == W - 1) {  // a frame a lane: the gates' gradients
-      float d = 0.f, e = 0.f, ends = 0.f;
+    if (wave == W - 1) {  // a frame a lane
+      float e = 0.f, ends = 0.f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) d += all.rows[0][w][lane], e += all.rows[1][w][lane], ends += all.end[w];
-#pragma unroll
-      for (int k = 1; k < C; k <<= 1) {  // from this frame to the chunk's last
-        const float above = __shfl_down(d, k, 64);
-        if (lane + k < C) d += above;
-      }
-      d += ends;
-      if (lane < left) {
-        // Its gradient is a difference of sums that is as small as the decay itself; of one
-        // below e^-69 only their rounding would be left, times any rate.
-        const float sr = sigm(to_f32(r_now));
-        const bool lost = rate * sr > 69.f;
-        const int64_t row = s.row[turn][lane];
-        if (lost) d = 0.f;
-        static_cast<T*>(a.dr)[row * a.lddr + hd.h] = from_f32<T>(lost ? 0.f : -rate * sr * ((1.f - sr) * d));
-        static_cast<T*>(a.db)[row * a.lddb + hd.h] = from_f32<T>(e * (1.f - s.beta[lane]));
-        dlam -= d * sr;
-      }
+      for (int w = 0; w < W; ++w) e += all.rows[w][lane], ends += all.end[w];
+      if (lane < left)
+        static_cast<T*>(a.db)[s.row[turn][lane] * a.lddb + hd.h] = from_f32<T>(e * (1.f - s.beta[lane]));
+      if (lane == 0) a.parts[n * (int64_t)gridDim.x + bh] = ends;  // (for gd_keys_kernel)
     }
     }
     __syncthreads();
@@ -257,10 +217,6 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
     return;
   }
   if (a.ds0 && seg == 0) store_state<DKP>(a.ds0 + bh * state, a, column_of(threadIdx.x), threadIdx.x & 63, dS);
-  if (threadIdx.x >= threads_of<W> - 64) {
-    dlam = wave_sum_uniform(dlam);
-    if (threadIdx.x == threads_of<W> - 64) a.parts[seg * (int64_t)gridDim.x + bh] = a.c * dlam;
-  }
 }
 
 // The gradients of the states that segments end in, from the last one on; the last
@@ -285,21 +241,93 @@ template <int DKP, int W> __global__ __launch_bounds__(64) void gd_join_back_ker
   }
 }
 
+// Sums over the lanes up to each of them: within rows of 16, and over the wave.
+template <int CTRL, int ROWS> __device__ __forceinline__ float lanes_up(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float row_sums(float v) {
+  v += lanes_up<0x111, 0xf>(v);
+  v += lanes_up<0x112, 0xf>(v);
+  v += lanes_up<0x114, 0xf>(v);
+  return v + lanes_up<0x118, 0xf>(v);
+}
+__device__ __forceinline__ float wave_sums(float v) {
+  v = row_sums(v);
+  v += lanes_up<0x142, 0xa>(v);
+  return v + lanes_up<0x143, 0xc>(v);
+}
+
+// What a tile (I, J) of X gives to the sums over pairs (l, j) with j < i <= l: a lane has
+// row l = lane % 16 and columns j = 4 (lane / 16) to + 3.  On the diagonal sums[0][i] is
+// what crosses frame i within the tile; below it, sums[0][l] are sums of rows and
+// sums[1][j] of columns.
+__device__ __forceinline__ void crossing(f32x4_t x, bool diagonal, float (&sums)[2][16], int lane) {
+  const int l16 = lane & 15, g4 = lane >> 4;
+  float all = (x[0] + x[1]) + (x[2] + x[3]);
+  f32x4_t out;
+  if (diagonal) {
+    float up = __shfl_up(all, 16, 64);
+    all += g4 >= 1 ? up : 0.f;
+    up = __shfl_up(all, 32, 64);
+    all += g4 >= 2 ? up : 0.f;
+    up = __shfl_up(all, 16, 64);
+    float before = g4 >= 1 ? up : 0.f;  // the row's sum before each column
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      out[r] = lanes_sum<16>(l16 >= 4 * g4 + r ? before : 0.f);
+      before += x[r];
+    }
+    if (l16 == 0) *reinterpret_cast<f32x4_t*>(&sums[0][4 * g4]) = out;
+  } else {
+    all += __shfl_xor(all, 16, 64);
+    all += __shfl_xor(all, 32, 64);
+    if (g4 == 0) sums[0][l16] = all;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) out[r] = lanes_sum<16>(x[r]);
+    if (l16 == 0) *reinterpret_cast<f32x4_t*>(&sums[1][4 * g4]) = out;
+  }
+}
+// The sum of X over the pairs that cross frame `lane`, y from it on, and z before it, from
+// the tiles' sums and the waves' parts of y and z.  A suffix is a prefix of the lanes in
+// reverse.
+template <int W>
+__device__ __forceinline__ float crossed(const float (&sums)[10][2][16], const float (&yz)[2][W][C], int lane) {
+  const int b = lane >> 4, i = lane & 15, back = C - 1 - lane, bb = back >> 4, bi = back & 15;
+  float y = 0.f, z = 0.f, rows = 0.f, cols = 0.f, both = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    y += yz[0][w][back];
+    z += lane > 0 ? yz[1][w][max(lane - 1, 0)] : 0.f;
+  }
+#pragma unroll
+  for (int J = 0; J + 1 < NB; ++J) rows += J < bb ? sums[lower(bb, min(J, bb))][0][bi] : 0.f;
+#pragma unroll
+  for (int I = 1; I < NB; ++I) cols += I > b && i > 0 ? sums[lower(max(I, b), b)][1][max(i - 1, 0)] : 0.f;
+#pragma unroll
+  for (int I = 2; I < NB; ++I)
+#pragma unroll
+    for (int J = 0; J + 1 < I; ++J) both += J < b && b < I ? sums[lower(I, J)][0][i] : 0.f;
+  const float from = __shfl(wave_sums(y) + row_sums(rows), back, 64);
+  return (from + wave_sums(z)) + (row_sums(cols) + lanes_sum<16>(both)) + sums[lower(b, b)][0][i];
+}
+
 // The gradients of q and k of a chunk of a key head, summed over its heads: a wave has
 // 16 columns of them, a lane a frame of each block, so that what scales with a frame is
-// a factor of a lane.  It goes through v's columns 32 at a time, then takes the sums
-// over pairs of frames to K and Q, which have the same LDS by then.  Chunks are all
-// independent here; 162 us for 256 x 64 frames, 12 heads of 64 x 64 (325 MB, 2 TB/s),
-// 427 for the utterances: the LDS pipeline, vector and matrix instructions take about a
-// third of it each, one after another between barriers.
+// a factor of a lane; and those of its heads' decays.  It goes through v's columns 32 at
+// a time, then takes the sums over pairs of frames to K and Q, which have the same LDS by
+// then.  S, dS', U and dR enter in three terms, since dlam is a sum of what they make in
+// 32 bits: with two, dlam of 256 x 64 frames in bf16 was off by 4.1e-6 and not 2.9e-7, for
+// 484 and not 517 us of a training pass.  Chunks are all independent here; 202 us for
+// those frames, 12 heads of 64 x 64 (375 MB, 1.9 TB/s), 594 for the utterances: the LDS
+// pipeline, vector and matrix instructions, one after another between barriers.
 template <typename T, int DKP> struct Keys {
-  static constexpr int TI = Terms<T>::IN, TO = Terms<T>::OUT;
+  static constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT;
   static constexpr int FRAMES = C * 2 + 16, KEYS = DKP * 2 + 16;  // bytes of a row of columns, of states
   union {
     struct {
       Matrix<TI, 32> dO;
-      uint8_t u[TO][32 * FRAMES], dR[TO][32 * FRAMES];  // 32 columns over frames
-      uint8_t S[TO][32 * KEYS], dS[TO][32 * KEYS];      // and over keys
+      uint8_t u[TX][32 * FRAMES], dR[TX][32 * FRAMES];  // 32 columns over frames
+      uint8_t S[TX][32 * KEYS], dS[TX][32 * KEYS];      // and over keys
     } slice;
     struct {
       Matrix<TI, DKP> k, q;
@@ -307,6 +335,7 @@ template <typename T, int DKP> struct Keys {
     } pairs;
   };
   float dots[2][DKP / 16][C];
+  float yz[2][DKP / 16][C], cross[10][2][16];  // of a head's decays
   Gates s;
 };
 
@@ -315,7 +344,7 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   Keys<T, DKP>& all = *reinterpret_cast<Keys<T, DKP>*>(lds);
   Gates& s = all.s;
-  constexpr int TI = Terms<T>::IN, TO = Terms<T>::OUT, W = DKP / 16, TH = threads_of<W>, VW = VP / 16;
+  constexpr int TI = Terms<T>::IN, TX = Terms<T>::X, TO = Terms<T>::OUT, W = DKP / 16, TH = threads_of<W>, VW = VP / 16;
   constexpr int FRAMES = Keys<T, DKP>::FRAMES, KEYS = Keys<T, DKP>::KEYS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
   const int group = a.H / a.G, n = blockIdx.x / (a.B * a.G), bg = blockIdx.x % (a.B * a.G), t0 = n * C;
@@ -330,7 +359,10 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
     const int64_t bh = (int64_t)b * a.H + kh * group + member;
     const Head hd(a, (int)bh);
     const int left = hd.len - t0;
-    if (left <= 0) return;  // (all heads of a sequence alike)
+    if (left <= 0) {  // (all heads of a sequence alike)
+      for (int m = threadIdx.x; m < group; m += TH) a.parts[(int64_t)n * a.B * a.H + bh + m] = 0.f;
+      return;
+    }
     if (member == 0) {
       if (threadIdx.x < C) s.row[0][threadIdx.x] = hd.row(a, t0 + threadIdx.x);
       __syncthreads();
@@ -342,7 +374,7 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
     const float* const S = n > 0 ? kept_before<DKP, VW>(a, n, bh) : nullptr;
     const float* const S0 = a.s0 ? a.s0 + bh * ((int64_t)a.dk * a.dv) : nullptr;
     const float* const dS = kept_after<DKP, VW>(a, n, bh);
-    const uint16_t *const U = kept_columns<TO, VW>(a.u, a, n, bh), *const dR = kept_columns<TO, VW>(a.dr_rows, a, n, bh);
+    const uint16_t *const U = kept_columns<TX, VW>(a.u, a, n, bh), *const dR = kept_columns<TX, VW>(a.dr_rows, a, n, bh);
     const T* const d_o = static_cast<const T*>(a.d_o) + (int64_t)hd.h * a.dv;
     f32x4_t pair_q[(10 + W - 1) / W], pair_k[(10 + W - 1) / W], sq[NB], sk[NB], su[NB];
 #pragma unroll
@@ -351,7 +383,7 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
     for (int I = 0; I < NB; ++I) sq[I] = sk[I] = su[I] = zero;
     // a slice on its way: pieces of eight columns of dO, of eight frames of U and dR, of
     // four keys of S and dS
-    constexpr int NC = (TO * 256 + TH - 1) / TH, NS = 8 * DKP / TH;
+    constexpr int NC = (TX * 256 + TH - 1) / TH, NS = 8 * DKP / TH;
     Eight<T> so;
     u32x4_t su4[NC], sr4[NC];
     f32x4_t ss[NS], sd[NS];
@@ -368,7 +400,7 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
       }
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        const int at = min(i * TH + tid, TO * 256 - 1), e = at >> 8, row = (at >> 3) & 31, u = at & 7;
+        const int at = min(i * TH + tid, TX * 256 - 1), e = at >> 8, row = (at >> 3) & 31, u = at & 7;
         const int from = (e * VP + c0 + row) * C + 8 * u;
         su4[i] = *reinterpret_cast<const u32x4_t*>(U + from);
         sr4[i] = *reinterpret_cast<const u32x4_t*>(dR + from);
@@ -405,7 +437,7 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
         const int at = i * TH + tid, e = at >> 8, row = (at >> 3) & 31, u = at & 7;
-        if (at < TO * 256) {
+        if (at < TX * 256) {
           *reinterpret_cast<u32x4_t*>(all.slice.u[e] + row * FRAMES + 16 * u) = su4[i];
           *reinterpret_cast<u32x4_t*>(all.slice.dR[e] + row * FRAMES + 16 * u) = sr4[i];
         }
@@ -414,9 +446,9 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
       for (int i = 0; i < NS; ++i) {
         const int at = i * TH + tid, row = at / (DKP / 4), u = at % (DKP / 4);
         const int mine = S ? row * KEYS + 8 * u : at % 32 * KEYS + 8 * (at / 32);
-        const Piece<TO> x = split<TO>(ss[i]), y = split<TO>(sd[i]);
+        const Piece<TX> x = split<TX>(ss[i]), y = split<TX>(sd[i]);
 #pragma unroll
-        for (int e = 0; e < TO; ++e) {
+        for (int e = 0; e < TX; ++e) {
           *reinterpret_cast<u32x2_t*>(all.slice.S[e] + mine) = x.t[e];
           *reinterpret_cast<u32x2_t*>(all.slice.dS[e] + row * KEYS + 8 * u) = y.t[e];
         }
@@ -424,27 +456,27 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
       __syncthreads();
       if (c0 + 32 < a.dv) arrive(c0 + 32);
       // column 16 j + lane % 16 of those over rows 4 (lane / 16) and on, of both halves of the 32
-      auto over = [&](const auto& m, int pitch, int j, Piece<TO>& x0, Piece<TO>& x1) {
+      auto over = [&](const auto& m, int pitch, int j, Piece<TX>& x0, Piece<TX>& x1) {
         const int at = (4 * g4 + (l16 >> 2)) * pitch + (16 * j + 4 * (lane & 3)) * 2;
 #pragma unroll
-        for (int e = 0; e < TO; ++e) {
+        for (int e = 0; e < TX; ++e) {
           x0.t[e] = turned(m[e] + at);
           x1.t[e] = turned(m[e] + at + 16 * pitch);
         }
       };
-      Piece<TO> s0, s1, d0, d1;
+      Piece<TX> s0, s1, d0, d1;
       over(all.slice.S, KEYS, wave, s0, s1);
       over(all.slice.dS, KEYS, wave, d0, d1);
 #pragma unroll
       for (int I = 0; I < NB; ++I) {
         Piece<TI> o0, o1;
-        Piece<TO> x0, x1;
+        Piece<TX> x0, x1;
         rows_of(all.slice.dO, I, 0, lane, o0, o1);
-        mma<TO, TI>(sq[I], s0, s1, o0, o1);
+        mma<TX, TI>(sq[I], s0, s1, o0, o1);
         over(all.slice.dR, FRAMES, I, x0, x1);
-        mma<TO, TO>(sk[I], s0, s1, x0, x1);
+        mma<TX, TX>(sk[I], s0, s1, x0, x1);
         over(all.slice.u, FRAMES, I, x0, x1);
-        mma<TO, TO>(su[I], d0, d1, x0, x1);
+        mma<TX, TX>(su[I], d0, d1, x0, x1);
       }
 #pragma unroll
       for (int k = 0; k < (10 + W - 1) / W; ++k) {  // ten tiles of U dO^T and of U dR^T
@@ -452,60 +484,99 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
         if (at >= 10) break;
         const int I = block_row(at), J = at - lower(I, 0);
         Piece<TI> o0, o1;
-        Piece<TO> u0, u1, x0, x1;
+        Piece<TX> u0, u1, x0, x1;
         over(all.slice.u, FRAMES, J, u0, u1);
         rows_of(all.slice.dO, I, 0, lane, o0, o1);
-        mma<TO, TI>(pair_q[k], u0, u1, o0, o1);
+        mma<TX, TI>(pair_q[k], u0, u1, o0, o1);
         over(all.slice.dR, FRAMES, I, x0, x1);
-        mma<TO, TO>(pair_k[k], u0, u1, x0, x1);
+        mma<TX, TX>(pair_k[k], u0, u1, x0, x1);
       }
       __syncthreads();
     }
-    fk.lengths(s.rk, a.eps, left, tid);
-    fq.lengths(s.rq, a.eps, left, tid);
-    fk.store(all.pairs.k, tid);
-    fq.store(all.pairs.q, tid);
-    fg.store(s, rate_of(a, hd.h), left, 0, tid);
-    __syncthreads();
-    if (wave == W - 1) combine(s, lane);
+    {  // (places in LDS are made again here: kept through the slices, they were spilled)
+      const int tid = this_thread(), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+      fk.lengths(s.rk, a.eps, left, tid);
+      fq.lengths(s.rq, a.eps, left, tid);
+      fk.store(all.pairs.k, tid);
+      fq.store(all.pairs.q, tid);
+      fg.store(s, rate_of(a, hd.h), left, 0, tid);
+      __syncthreads();
+      if (wave == W - 1) combine(s, lane);
 #pragma unroll
-    for (int k = 0; k < (10 + W - 1) / W; ++k) {
-      const int at = wave + W * k;
-      if (at >= 10) break;
-      const int I = block_row(at), J = at - lower(I, 0), i = 16 * I + l16;
-      const f32x4_t ch = rows4(s.ch, J, lane), cl = rows4(s.cl, J, lane), rk = rows4(s.rk, J, lane);
-      const float hi = s.ch[i], lo = s.cl[i], f = s.rq[i], h = -s.beta[i] * s.rk[i];
-      f32x4_t x, y;
+      for (int I = 0; I < NB; ++I) {
+        const int i = 16 * I + l16;
+        const f32x4_t q = values(row4_of(all.pairs.q, I, wave, lane)), k = values(row4_of(all.pairs.k, I, wave, lane));
+        float qs = 0.f, ks = 0.f, ku = 0.f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int j = 16 * J + 4 * g4 + r;
-        const float m = rk[r] * __builtin_amdgcn_exp2f((hi - ch[r]) + (lo - cl[r]));
-        x[r] = j <= i ? f * m * pair_q[k][r] : 0.f;
-        y[r] = j < i ? h * m * pair_k[k][r] : 0.f;
+        for (int r = 0; r < 4; ++r) qs = fmaf(q[r], sq[I][r], qs), ks = fmaf(k[r], sk[I][r], ks), ku = fmaf(k[r], su[I][r], ku);
+        float y = s.g[i] * (s.rq[i] * qs - s.beta[i] * s.rk[i] * ks), z = s.end[i] * s.rk[i] * ku;
+        y += __shfl_xor(y, 16, 64);
+        z += __shfl_xor(z, 16, 64);
+        y += __shfl_xor(y, 32, 64);
+        z += __shfl_xor(z, 32, 64);
+        if (g4 == 0) {
+          all.yz[0][wave][i] = y;
+          all.yz[1][wave][i] = z;
+        }
       }
-      const Piece<TO> p = split<TO>(x), q = split<TO>(y);
 #pragma unroll
-      for (int e = 0; e < TO; ++e) {
-        *reinterpret_cast<u32x2_t*>(all.pairs.qk[at][e] + spot(l16, g4)) = p.t[e];
-        *reinterpret_cast<u32x2_t*>(all.pairs.kk[at][e] + spot(l16, g4)) = q.t[e];
+      for (int k = 0; k < (10 + W - 1) / W; ++k) {
+        const int at = wave + W * k;
+        if (at >= 10) break;
+        const int I = block_row(at), J = at - lower(I, 0), i = 16 * I + l16;
+        f32x4_t qk = zero, kk = zero;
+#pragma unroll
+        for (int t = 0; t < DKP / 32; ++t) {
+          Piece<TI> a0, a1, b0, b1;
+          rows_of(all.pairs.k, J, t, lane, a0, a1);
+          rows_of(all.pairs.k, I, t, lane, b0, b1);
+          mma<TI, TI>(kk, a0, a1, b0, b1);
+          rows_of(all.pairs.q, I, t, lane, b0, b1);
+          mma<TI, TI>(qk, a0, a1, b0, b1);
+        }
+        const f32x4_t ch = rows4(s.ch, J, lane), cl = rows4(s.cl, J, lane), rk = rows4(s.rk, J, lane);
+        const float hi = s.ch[i], lo = s.cl[i], f = s.rq[i], h = -s.beta[i] * s.rk[i];
+        f32x4_t x, y;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int j = 16 * J + 4 * g4 + r;
+          const float m = rk[r] * __builtin_amdgcn_exp2f((hi - ch[r]) + (lo - cl[r]));
+          x[r] = j <= i ? f * m * pair_q[k][r] : 0.f;
+          y[r] = j < i ? h * m * pair_k[k][r] : 0.f;
+        }
+        const Piece<TO> p = split<TO>(x), q = split<TO>(y);
+#pragma unroll
+        for (int e = 0; e < TO; ++e) {
+          *reinterpret_cast<u32x2_t*>(all.pairs.qk[at][e] + spot(l16, g4)) = p.t[e];
+          *reinterpret_cast<u32x2_t*>(all.pairs.kk[at][e] + spot(l16, g4)) = q.t[e];
+        }
+        crossing(x * qk + y * kk, I == J, all.cross[at], lane);
       }
-    }
-    __syncthreads();
+      __syncthreads();
+      if (wave == W - 1) {  // a frame a lane: the gradient of log a
+        float* const part = a.parts + (int64_t)n * a.B * a.H + bh;
+        const float e = crossed<W>(all.cross, all.yz, lane) + s.g[C - 1] * *part;
+        const float rate = rate_of(a, hd.h), sr = sigm(to_f32(fg.r));
+        if (lane < left) static_cast<T*>(a.dr)[s.row[0][lane] * a.lddr + hd.h] = from_f32<T>(-rate * sr * ((1.f - sr) * e));
+        const float sum = wave_sum_uniform(lane < left ? -e * sr : 0.f);
+        if (lane == 0) *part = a.c * sum;
+      }
 #pragma unroll
-    for (int I = 0; I < NB; ++I) {
-      const int i = 16 * I + l16;
-      dq[I] += sq[I] * s.gq[i];
-      dk[I] += su[I] * s.gk[i] - sk[I] * s.bgk[i];
-    }
+      for (int I = 0; I < NB; ++I) {
+        const int i = 16 * I + l16;
+        dq[I] += sq[I] * s.gq[i];
+        dk[I] += su[I] * s.gk[i] - sk[I] * s.bgk[i];
+      }
 #pragma unroll
-    for (int I = 0; I < NB; ++I) {
-      const Piece<TI> kI = columns_of(all.pairs.k, wave, I, lane), qI = columns_of(all.pairs.q, wave, I, lane);
+      for (int I = 0; I < NB; ++I) {
+        const Piece<TI> kI = columns_of(all.pairs.k, wave, I, lane), qI = columns_of(all.pairs.q, wave, I, lane);
 #pragma unroll
-      for (int J = 0; J < NB; ++J) {
-        if (J >= I) mma<TI, TO>(dq[J], kI, block_of(all.pairs.qk[lower(J, I)], lane));
-        if (J <= I) mma<TI, TO>(dk[J], qI, block_turned(all.pairs.qk[lower(I, J)], lane));
-        if (J >= I) mma<TI, TO>(dk[J], kI, block_of(all.pairs.kk[lower(J, I)], lane));
-        if (J <= I) mma<TI, TO>(dk[J], kI, block_turned(all.pairs.kk[lower(I, J)], lane));
+        for (int J = 0; J < NB; ++J) {
+          if (J >= I) mma<TI, TO>(dq[J], kI, block_of(all.pairs.qk[lower(J, I)], lane));
+          if (J <= I) mma<TI, TO>(dk[J], qI, block_turned(all.pairs.qk[lower(I, J)], lane));
+          if (J >= I) mma<TI, TO>(dk[J], kI, block_of(all.pairs.kk[lower(J, I)], lane));
+          if (J <= I) mma<TI, TO>(dk[J], kI, block_turned(all.pairs.kk[lower(I, J)], lane));
+        }
       }
     }
     if (member + 1 < group) __syncthreads();
@@ -541,10 +612,10 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
   }
 }
 
-// dlam = sigm(lam) times the sum over segments and sequences of parts.
+// dlam = sigm(lam) times the sum over chunks and sequences of parts.
 __global__ __launch_bounds__(1024) void gd_dlam_kernel(GatedDelta a) {
   __shared__ float sum[32][33];
-  const float s = column_sum(a.parts, (int64_t)a.segs * a.B, a.H, sum);
+  const float s = column_sum(a.parts, (int64_t)((a.T + C - 1) / C) * a.B, a.H, sum);
   const int h = blockIdx.x * 32 + threadIdx.x;
   if (threadIdx.x < 32 && h < a.H) a.dlam[h] = s / (1.f + expf(-a.lam[h]));
 }
