@@ -77,5 +77,5 @@ def gated_delta_backward(q, k, v, r, b, lam, T, B, heads, key_heads, d_o, cache,
     # what the gradients are before their parts along q and k are taken away
     cache["along"] = [float(np.abs(inv * d).max(initial=0.0)) for inv, d in ((qi, dqu), (ki, dku))]
     dq, dk = (inv * (d - u * (u * d).sum(-1, keepdims=True)) for u, inv, d in ((qu, qi, dqu), (ku, ki, dku)))
-    return (*(x.reshape(N, x.shape[1] * x.shape[2]) for x in (dq, dk, dv)), dlog * -rate * sr * (1 - sr),
-            dbeta * beta * (1 - beta), (dlog * -c * sr).sum(0) * _sigm(lam), dS)
+    return (*(x.reshape(N, x.shape[1] * x.shape[2]) for x in (dq, dk, dv)), dlog * -rate * sr * _sigm(-r),
+            dbeta * beta * _sigm(-np.asarray(b, np.float64)), (dlog * -c * sr).sum(0) * _sigm(lam), dS)

@@ -79,6 +79,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
     // state goes on.  With everything else in registers that gave nothing, 217 and 645 us
     // either way, and spilled where dk is 128 and dv at most 64.)
     if (!ENDS) fetch(s.row[turn], max(n - 1, 0) * C, tid);
+    const T b_now = fg.b;
     fk.lengths(s.rk, a.eps, left, tid);
     fq.lengths(s.rq, a.eps, left, tid);
     fk.store(c.k, tid);
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(threads_of<W>, 2) void gd_backward_kernel(GatedDelt
 #pragma unroll
       for (int w = 0; w < W; ++w) e += all.rows[w][lane], ends += all.end[w];
       if (lane < left)
-        static_cast<T*>(a.db)[s.row[turn][lane] * a.lddb + hd.h] = from_f32<T>(e * (1.f - s.beta[lane]));
+        static_cast<T*>(a.db)[s.row[turn][lane] * a.lddb + hd.h] = from_f32<T>(e * sigm(-to_f32(b_now)));  // (1 - beta, which may be far below 1)
       if (lane == 0) a.parts[n * (int64_t)gridDim.x + bh] = ends;  // (for gd_keys_kernel)
     }
     }
@@ -556,8 +557,8 @@ __global__ __launch_bounds__(DKP * 4, 2) void gd_keys_kernel(GatedDelta a) {
       if (wave == W - 1) {  // a frame a lane: the gradient of log a
         float* const part = a.parts + (int64_t)n * a.B * a.H + bh;
         const float e = crossed<W>(all.cross, all.yz, lane) + s.g[C - 1] * *part;
-        const float rate = rate_of(a, hd.h), sr = sigm(to_f32(fg.r));
-        if (lane < left) static_cast<T*>(a.dr)[s.row[0][lane] * a.lddr + hd.h] = from_f32<T>(-rate * sr * ((1.f - sr) * e));
+        const float rate = rate_of(a, hd.h), r = to_f32(fg.r), sr = sigm(r);
+        if (lane < left) static_cast<T*>(a.dr)[s.row[0][lane] * a.lddr + hd.h] = from_f32<T>(-rate * sr * (sigm(-r) * e));
         const float sum = wave_sum_uniform(lane < left ? -e * sr : 0.f);
         if (lane == 0) *part = a.c * sum;
       }

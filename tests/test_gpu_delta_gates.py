@@ -114,3 +114,20 @@ def test_shut_gates_of_a_rate_past_32_bits(T, lengths, dtype):
     o, sT = c.forward(train=False)
     assert_close("o, serving", _f64(o), ref[0], tol)
     assert_close("sT, serving", _f64(sT), ref[1], F32_TOL)
+
+
+@BOTH
+@pytest.mark.parametrize("gate", [5.0, 8.0, 12.0, 16.0, 30.0, 60.0])
+def test_gates_nearly_open(gate, dtype):
+    """r and b of 5 to 60: the gradients carry sigm(-r) and sigm(-b), as small as e^-60,
+    and are held to their bounds beside them."""
+    c = Case(130, 2, 2, 32, 32, dtype, seed=int(gate))
+    r, b = c.cols(c.proj)[3:]
+    for t in (r, b):
+        t.mul_(0.3).add_(gate)
+    got, ref = c.forward() + c.backward(), c.oracle()
+    tol = F32_TOL if dtype == torch.float32 else BF16_TOL
+    for name, t, n in (("dr", r, 5), ("db", b, 6)):
+        x = np.exp(_f64(t))  # 1 / sigm(-t), but for 1
+        want = ref[n] * x
+        assert np.abs(_f64(got[n]) * x - want).max() <= tol * np.abs(want).max(), name
