@@ -204,10 +204,11 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(GatedNorm a) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
           const int e = at.e0 + k * at.STEP;
-          const f32x4_t v = t[k] * rstd_n * next[k];
+          f32x4_t v = t[k] * rstd_n * next[k];
           uint32_t top = 0;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
+            if (!inside(k) && e + j >= H) v[j] = 0.f;  // (rstd_n may not be finite)
             const uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
             top = m < 0x7f800000u && m > top ? m : top;
           }
