@@ -105,12 +105,16 @@ class GatedStudent:
         else:
             am.gated_norm_forward(res, y=self.y[l], rstd=self.rstd[l], **parts)
 
-    def _project(self, y, y8, name):
-        """y W^T; y8: y in 8 bits."""
+    def _project(self, y, y8, name, ws=None):
+        """y W^T; y8: y in 8 bits.  A stream's few rows may need more workspace than
+        training's many, and may run beside them: without `ws` they have their own."""
         if not self.q8:
             return y @ self.weights[name].t()
-        out = torch.empty((y.shape[0], self.master[name].shape[0]), dtype=BF16, device="cuda")
-        am.q8_matmul(*y8, *self.codes[name][:2], out, tiles=True, ws=self.q8_ws)
+        (N, K), n = y.shape, self.master[name].shape[0]
+        out = torch.empty((N, n), dtype=BF16, device="cuda")
+        if ws is None:
+            ws = torch.empty(am.q8_matmul_workspace_bytes(N, n, K), dtype=torch.uint8, device="cuda")
+        am.q8_matmul(*y8, *self.codes[name][:2], out, tiles=True, ws=ws)
         return out
 
     def _project_back(self, y, grads):
@@ -168,8 +172,8 @@ class GatedStudent:
         self.res[0].copy_(self.x @ w["Win"].t())
         self._norm(0, self.res[0], w_next=w["w0"])
         for l in range(self.layers):
-            self.p.append(self._project(self.y[l], self.q8 and self.y8, f"Wp{l}"))
-            self.g.append(self._project(self.y[l], self.q8 and self.y8, f"Wg{l}"))
+            for parts, name in ((self.p, "Wp"), (self.g, "Wg")):
+                parts.append(self._project(self.y[l], self.q8 and self.y8, f"{name}{l}", self.q8 and self.q8_ws))
             self._mix(self.p[l], l, self.h[l], self.rec_ws[l], self.T, self.B, self.lengths, True)
             self._norm(l + 1, self.res[l], o=self.h[l], gate=self.g[l], w_post=w[f"post{l}"],
                        scale=w[f"scale{l}"], w_next=w[f"next{l}"], res_out=self.res[l + 1])
