@@ -453,11 +453,13 @@ def _row(t, name, N, H, dtype):
     return t.data_ptr(), s0
 
 
-def _here(t, name, stream):
-    """Refuses a tensor of another device than the one whose stream the call takes."""
-    if t.is_cuda:
-        now = stream.device_index if stream is not None else _raw_device() if _raw_device else torch.cuda.current_device()
-        if t.get_device() != now:
+def _here(stream, names, *tensors):
+    """Refuses tensors (of these names, or Nones) of another GPU than the one whose stream
+    the call takes."""
+    now = stream.device_index if stream is not None else _raw_device() if _raw_device else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != now:
+            name = next(n for n, x in zip(names.split(), tensors) if x is t)
             raise AmError(f"{name} is on GPU {t.get_device()}, the call on GPU {now}")
 
 
@@ -542,7 +544,7 @@ def gated_delta_workspace_bytes(T, B, heads, dk, dv, key_heads=None, dtype=torch
     return int(n)
 
 
-def _delta(q, k, v, r, b, T, B, heads, key_heads, lengths, stream):
+def _delta(q, k, v, r, b, T, B, heads, key_heads, lengths):
     """What both passes share: columns of q and v, frames, type, states' shape, what must
     live until the call, and its arguments up to b."""
     key_heads = heads if key_heads is None else key_heads
@@ -557,7 +559,6 @@ def _delta(q, k, v, r, b, T, B, heads, key_heads, lengths, stream):
     dk, dv = nq // key_heads, nv // heads
     args = (T, B, heads, key_heads, dk, dv, dt, lp, *_row(q, "q", N, nq, kind), *_row(k, "k", N, nq, kind),
             *_row(v, "v", N, nv, kind), *_row(r, "r", N, heads, kind), *_row(b, "b", N, heads, kind))
-    _here(q, "q", stream)
     return nq, nv, N, kind, (B, heads, dk, dv), arr, args
 
 
@@ -565,11 +566,12 @@ def gated_delta_forward(q, k, v, r, b, lam, T, B, o, ws=None, heads=1, key_heads
                         sT=None, c=8.0, eps=1e-6, train=False, stream=None):
     """q, k: [N][key_heads dk], v and o: [N][heads dv], r, b: [N][heads] rows (columns of
     one projection, say); lam: [heads]; s0, sT: [B][heads][dk][dv] fp32 (sT may be s0)."""
-    nq, nv, N, kind, state, arr, args = _delta(q, k, v, r, b, T, B, heads, key_heads, lengths, stream)
+    nq, nv, N, kind, state, arr, args = _delta(q, k, v, r, b, T, B, heads, key_heads, lengths)
     wp, wn = _workspace(ws)
-    st = (_lib or lib()).gated_delta_forward(
-        *args, _shaped(lam, "lam", (heads,)), c, eps, _shaped(s0, "s0", state), *_row(o, "o", N, nv, kind),
-        _shaped(sT, "sT", state), 1 if train else 0, wp, wn, _stream(stream))
+    call = (*args, _shaped(lam, "lam", (heads,)), c, eps, _shaped(s0, "s0", state), *_row(o, "o", N, nv, kind),
+            _shaped(sT, "sT", state), 1 if train else 0, wp, wn)
+    _here(stream, "q k v r b lam s0 o sT ws", q, k, v, r, b, lam, s0, o, sT, ws)
+    st = (_lib or lib()).gated_delta_forward(*call, _stream(stream))
     if st:
         _check(st)
 
@@ -578,13 +580,15 @@ def gated_delta_backward(q, k, v, r, b, lam, T, B, do, ws, dq, dk, dv, dr, db, d
                          lengths=None, s0=None, dsT=None, ds0=None, c=8.0, eps=1e-6, stream=None):
     """The gradient of the forward call (train=True) that filled `ws`, with the s0 that
     it had; dq, dk, dv, dr, db: rows as of q, k, v, r, b."""
-    nq, nv, N, kind, state, arr, args = _delta(q, k, v, r, b, T, B, heads, key_heads, lengths, stream)
+    nq, nv, N, kind, state, arr, args = _delta(q, k, v, r, b, T, B, heads, key_heads, lengths)
     wp, wn = _workspace(ws)
-    st = (_lib or lib()).gated_delta_backward(
-        *args, _shaped(lam, "lam", (heads,)), c, eps, _shaped(s0, "s0", state),
-        *_row(do, "do", N, nv, kind), _shaped(dsT, "dsT", state),
-        *_row(dq, "dq", N, nq, kind), *_row(dk, "dk", N, nq, kind), *_row(dv, "dv", N, nv, kind), *_row(dr, "dr", N, heads, kind), *_row(db, "db", N, heads, kind),
-        _shaped(dlam, "dlam", (heads,)), _shaped(ds0, "ds0", state), wp, wn, _stream(stream))
+    call = (*args, _shaped(lam, "lam", (heads,)), c, eps, _shaped(s0, "s0", state),
+            *_row(do, "do", N, nv, kind), _shaped(dsT, "dsT", state), *_row(dq, "dq", N, nq, kind),
+            *_row(dk, "dk", N, nq, kind), *_row(dv, "dv", N, nv, kind), *_row(dr, "dr", N, heads, kind),
+            *_row(db, "db", N, heads, kind), _shaped(dlam, "dlam", (heads,)), _shaped(ds0, "ds0", state), wp, wn)
+    _here(stream, "q k v r b lam s0 do dsT dq dk dv dr db dlam ds0 ws", q, k, v, r, b, lam, s0, do, dsT, dq, dk, dv, dr,
+          db, dlam, ds0, ws)
+    st = (_lib or lib()).gated_delta_backward(*call, _stream(stream))
     if st:
         _check(st)
 
@@ -684,10 +688,10 @@ def q8_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, tiles=F
     it lies and, with codes_t and scales_t, transposed; see q8_empty."""
     dt, (rows, cols) = _dtype(x, "x"), x.shape
     xp, ld = _row(x, "x", rows, cols, x.dtype)
-    _here(x, "x", stream)
-    st = (_lib or lib()).q8_quantise(
-        rows, cols, dt, xp, ld, 1 if tiles else 0, *_q8(codes, scales, "x", rows, cols, tiles),
-        *_q8(codes_t, scales_t, "x transposed", cols, rows, tiles), _stream(stream))
+    call = (rows, cols, dt, xp, ld, 1 if tiles else 0, *_q8(codes, scales, "x", rows, cols, tiles),
+            *_q8(codes_t, scales_t, "x transposed", cols, rows, tiles))
+    _here(stream, "x codes scales codes_t scales_t", x, codes, scales, codes_t, scales_t)
+    st = (_lib or lib()).q8_quantise(*call, _stream(stream))
     if st:
         _check(st)
 
@@ -706,11 +710,11 @@ def q8_matmul(a, a_scales, b, b_scales, out, tiles=False, bias=None, accumulate=
         raise AmError(f"a and b must be [M][K] and [N][K], got {tuple(a.shape)} and {tuple(b.shape)}")
     (M, K), N = a.shape, b.shape[0]
     op, ldo = _row(out, "out", M, N, torch.bfloat16)
-    _here(out, "out", stream)
     wp, wn = _workspace(ws)
-    st = (_lib or lib()).q8_matmul(
-        M, N, K, *_q8(a, a_scales, "a", M, K), *_q8(b, b_scales, "b", N, K, tiles), 1 if tiles else 0,
-        _shaped(bias, "bias", (N,)), op, ldo, 1 if accumulate else 0, wp, wn, _stream(stream))
+    call = (M, N, K, *_q8(a, a_scales, "a", M, K), *_q8(b, b_scales, "b", N, K, tiles), 1 if tiles else 0,
+            _shaped(bias, "bias", (N,)), op, ldo, 1 if accumulate else 0, wp, wn)
+    _here(stream, "a a_scales b b_scales bias out ws", a, a_scales, b, b_scales, bias, out, ws)
+    st = (_lib or lib()).q8_matmul(*call, _stream(stream))
     if st:
         _check(st)
 
@@ -719,14 +723,15 @@ def gated_norm_forward_q8(res, codes, scales, o=None, gate=None, w_post=None, sc
                           res_out=None, y=None, rstd=None, eps=1e-6, stream=None):
     """gated_norm_forward whose norm leaves in 8 bits, and in y if that is given."""
     (N, H), act = res.shape, o if o is not None else y if y is not None else res
-    _here(res, "res", stream)
     (op, ldo), (gp, ldg) = _row(o, "o", N, H, act.dtype), _row(gate, "gate", N, H, act.dtype)
-    st = (_lib or lib()).gated_norm_forward_q8(
-        N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
-        _shaped(scale, "scale", (H,)), _shaped(res, "res", (N, H), res.dtype),
-        _shaped(w_next, "w_next", (H,)), float(eps), _shaped(res_out, "res_out", (N, H), res.dtype),
-        _shaped(y, "y", (N, H), act.dtype), _shaped(rstd, "rstd", (N, 2)),
-        *_q8(codes, scales, "y", N, H), _stream(stream))
+    call = (N, H, _dtype(act, "o"), _dtype(res, "res"), op, ldo, gp, ldg, _shaped(w_post, "w_post", (H,)),
+            _shaped(scale, "scale", (H,)), _shaped(res, "res", (N, H), res.dtype),
+            _shaped(w_next, "w_next", (H,)), float(eps), _shaped(res_out, "res_out", (N, H), res.dtype),
+            _shaped(y, "y", (N, H), act.dtype), _shaped(rstd, "rstd", (N, 2)),
+            *_q8(codes, scales, "y", N, H))
+    _here(stream, "res o gate w_post scale w_next res_out y rstd codes scales", res, o, gate, w_post, scale, w_next,
+          res_out, y, rstd, codes, scales)
+    st = (_lib or lib()).gated_norm_forward_q8(*call, _stream(stream))
     if st:
         _check(st)
 
