@@ -704,8 +704,7 @@ am_status check_gated(int32_t T, int32_t B, int32_t H, int32_t dtype, const int3
 }
 
 struct DeltaLayout { int64_t offs, lens, tails, saved, dsaved, u, dr, parts, seg_n, seg_m, seg_mt, seg_d, total; };
-DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int32_t dk, int32_t dv, bool bf16, bool varlen,
-                         bool train) {
+DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int32_t dk, int32_t dv, bool varlen, bool train) {
   DeltaLayout l{};
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -737,6 +736,13 @@ DeltaLayout delta_layout(int64_t T, int64_t B, int64_t H, int32_t dk, int32_t dv
   }
   l.total = at;
   return l;
+}
+
+// Heads that a launch has workgroups for (2^32 threads, 512 a workgroup), of a training
+// pass those of every chunk.
+bool delta_heads(int64_t T, int64_t B, int64_t heads, bool train) {
+  const int64_t most = 1 << 23;
+  return B < most && heads < most && B * heads * (train ? T / am::GD_CHUNK + 1 : 1) < most;
 }
 
 bool delta_sizes(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv) {
@@ -774,15 +780,13 @@ am_status check_delta(int32_t T, int32_t B, int32_t heads, int32_t key_heads, in
     a.T = lengths[0];
   }
   if (a.N >= (1ll << 31) - 256 || T > (1 << 30)) return fail(AM_EUNSUPPORTED, "too many frames");
-  // (2^32 threads a launch, 512 a workgroup)
-  if ((int64_t)B * heads >= (1 << 23) || (train && ((int64_t)T / am::GD_CHUNK + 1) * B * heads >= (1 << 23)))
-    return fail(AM_EUNSUPPORTED, "too many heads");
+  if (!delta_heads(T, B, heads, train)) return fail(AM_EUNSUPPORTED, "too many heads");
   AM_TRY(check_rows(a.N, key_heads * dk, dtype, q, ldq, "q"));
   AM_TRY(check_rows(a.N, key_heads * dk, dtype, k, ldk, "k"));
   AM_TRY(check_rows(a.N, heads * dv, dtype, v, ldv, "v"));
   AM_TRY(check_rows(a.N, heads, dtype, r, ldr, "r"));
   AM_TRY(check_rows(a.N, heads, dtype, b, ldb, "b"));
-  l = delta_layout(T, B, heads, dk, dv, dtype == AM_BF16, lengths != nullptr, train);
+  l = delta_layout(T, B, heads, dk, dv, lengths != nullptr, train);
   if (l.total > 0 && (!ws || !aligned(ws, 256) || ws_bytes < l.total))
     return fail(AM_EWORKSPACE, "needs %lld workspace bytes, 256-byte aligned", (long long)l.total);
   a.q = q; a.k = k; a.v = v; a.r = r; a.b = b;
@@ -1627,8 +1631,9 @@ am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dty
 int64_t am_gated_delta_workspace_bytes(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk,
                                        int32_t dv, int32_t dtype, int32_t varlen, int32_t train) {
   if (!delta_sizes(T, B, heads, key_heads, dk, dv) || dk > am::GD_MAX_DIM || dv > am::GD_MAX_DIM) return -1;
-  if ((dtype != AM_F32 && dtype != AM_BF16) || (int64_t)T * B >= (1ll << 32) || (int64_t)B * heads >= (1ll << 31)) return -1;
-  return delta_layout(T, B, heads, dk, dv, dtype == AM_BF16, varlen != 0, train != 0).total;
+  if ((dtype != AM_F32 && dtype != AM_BF16) || T > (1 << 30) || (int64_t)T * B >= (1ll << 32) || (varlen && B > 1024)) return -1;
+  if (!delta_heads(T, B, heads, train != 0) || (!varlen && (int64_t)T * B >= (1ll << 31) - 256)) return -1;
+  return delta_layout(T, B, heads, dk, dv, varlen != 0, train != 0).total;
 }
 
 am_status gated_delta_forward(int32_t T, int32_t B, int32_t heads, int32_t key_heads, int32_t dk, int32_t dv,
