@@ -424,7 +424,7 @@ struct Q8Quantise {
   int64_t ldc, lds;
   uint8_t *codes_t, *scales_t;  // or null
   int64_t ldct, ldst;
-  uint32_t across;              // (set by the launcher: tiles side by side)
+  uint32_t across, first;       // (set by the launcher: tiles side by side, a launch's first one)
 };
 hipError_t q8_quantise(Q8Quantise a, bool bf16, hipStream_t s);
 // out = a b^T (see q8_matmul in the C ABI).

@@ -75,7 +75,8 @@ __global__ __launch_bounds__(256, 3) void q8_quantise_kernel(Q8Quantise a) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[QT * QPITCH];
   __shared__ uint32_t tops[16][QT + 4];
   const int t = threadIdx.x, cx = t & 15, ry = t >> 4;
-  const int64_t ty = blockIdx.x / a.across, tx = blockIdx.x % a.across, r0 = ty * QT, c0 = tx * QT;
+  const uint32_t tile = a.first + blockIdx.x;
+  const int64_t ty = tile / a.across, tx = tile % a.across, r0 = ty * QT, c0 = tx * QT;
   const int64_t rows = a.rows, cols = a.cols, c = c0 + 8 * cx;
   Eight<T> v[8];
 #pragma unroll
@@ -482,10 +483,16 @@ template <typename S> hipError_t run(Q8Matmul a, const Q8Plan& p, hipStream_t s)
 
 hipError_t q8_quantise(Q8Quantise a, bool bf16, hipStream_t s) {
   a.across = (unsigned)((a.cols + QT - 1) / QT);
-  const dim3 grid((unsigned)(a.across * ((a.rows + QT - 1) / QT)));
-  if (bf16) hipLaunchKernelGGL((q8_quantise_kernel<bf16_t>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((q8_quantise_kernel<float>), grid, dim3(256), 0, s, a);
-  return hipGetLastError();
+  const int64_t tiles = a.across * ((a.rows + QT - 1) / QT), most = (1 << 24) - 1;  // (a launch has less than 2^32 threads)
+  hipError_t e = hipSuccess;
+  for (int64_t first = 0; first < tiles && e == hipSuccess; first += most) {
+    const dim3 grid((unsigned)std::min(most, tiles - first));
+    a.first = (uint32_t)first;
+    if (bf16) hipLaunchKernelGGL((q8_quantise_kernel<bf16_t>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((q8_quantise_kernel<float>), grid, dim3(256), 0, s, a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 Q8Plan q8_plan(int64_t M, int64_t N, int64_t K) {

@@ -33,3 +33,22 @@ def test_norm_of_rows_that_are_not_finite(bad, H, dtype):
         assert torch.equal(scales[row].view(torch.uint8), want[1][row].view(torch.uint8))
     for row in (1, 3):
         assert np.any((raw[row, :H] & 0x7F) == 0x7F)
+
+
+def test_quantise_more_tiles_than_a_launch_has():
+    """2^24 tiles of 256 threads: the ends and a part of the middle are those of the same
+    rows by themselves."""
+    rows = (1 << 31) - 1
+    x = torch.empty((rows, 1), dtype=torch.bfloat16, device="cuda")
+    for at in range(0, rows, 1 << 28):
+        x[at:at + (1 << 28)].normal_()
+    codes, scales = am.q8_empty(1, rows)
+    am.q8_quantise(x, codes_t=codes, scales_t=scales)
+    for first in (0, 128 << 20, 128 * ((1 << 24) - 5)):
+        part = x[first:first + 128 * 8]
+        one, e = am.q8_empty(1, part.shape[0])
+        am.q8_quantise(part, codes_t=one, scales_t=e)
+        at = slice(first, first + part.shape[0])
+        assert torch.equal(codes.view(torch.uint8)[:, at], one.view(torch.uint8)), first
+        blocks = -(-part.shape[0] // 128)
+        assert torch.equal(scales.view(torch.uint8)[:, first // 128:first // 128 + blocks], e.view(torch.uint8)[:, :blocks])
