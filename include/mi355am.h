@@ -417,8 +417,12 @@ am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dty
  * the state forgets by a_t, and what it holds under the key k_t moves to v_t by
  * beta_t.  `heads` heads share `key_heads` pairs of q and k, heads / key_heads of them
  * (neighbours) one pair.  Sums and states are in 32 bits, each output is rounded once.
+ * Of bf16 frames, o is formed from states and updates, and what pairs of frames give to
+ * dq and dk from their sums, rounded to 16 bits (2^-18 of them, where the output's own
+ * rounding is 2^-8); states, dv, dr, db, dlam and ds0 from all 32.
  *   dtype    AM_F32 or AM_BF16: type of q, k, v, r, b, o and their gradients
- *   q, k     [N] rows of key_heads dk;  v, o [N] rows of heads dv;  r, b [N] rows of
+ *   q, k     [N] rows of key_heads dk, elements below 2^59 in magnitude (their squares
+ *            are added in 32 bits);  v, o [N] rows of heads dv;  r, b [N] rows of
  *            heads; each with its row stride (columns of one projection, say)
  *   lam      [heads] fp32, finite;  c > 0;  eps > 0; c softplus(lam) past the largest 32-bit float
  *            counts as that
@@ -427,7 +431,8 @@ am_status gated_recurrence_backward(int32_t T, int32_t B, int32_t H, int32_t dty
  *            each sequence's last frame (s0 where it has none; may be s0 itself)
  *   ws       workspace of am_gated_delta_workspace_bytes (256-byte aligned; may be NULL
  *            where that is 0).  train = 1 keeps in it what gated_delta_backward reads;
- *            it must not be modified between.
+ *            it must not be modified between.  It has room for T frames of every
+ *            sequence, however short some are.
  * What is not finite in a frame spreads to what its head does from there on, and may
  * spread to the outputs of the 15 frames before it.
  * 1 <= dk, dv <= 128; key_heads divides heads; N less than 2^31 - 256; B heads, with
@@ -521,8 +526,11 @@ am_status q8_quantise(int64_t rows, int64_t cols, int32_t dtype, const void* x, 
  *   b   [N] rows of K, a scale for each 128 of a row, or each tile (b_tiles = 1)
  *   bias [N] fp32 or NULL;  out [M] rows of N, ldo elements apart;  accumulate = 1
  *   adds to what out holds
- * The matrix cores form products of 8-bit floats exactly and their sums to about 16
- * bits of their size, in fixed order.  ws: workspace of am_q8_matmul_workspace_bytes
+ * The matrix cores form products of 8-bit floats exactly and add 128 of them at a time,
+ * small ones beside large ones not to their last bits: where products are of like size
+ * the rounding to bf16 is all that is off; where they span the codes' whole range, a sum
+ * of 128 may be off by 2^-12 of the sum of their magnitudes.  Sums of 128 are added in
+ * 32 bits, in fixed order.  ws: workspace of am_q8_matmul_workspace_bytes
  * (256-byte aligned; may be NULL where that is 0).  M and N below 2^31, rows of codes
  * less than 2^24 apart. */
 int64_t am_q8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
