@@ -332,16 +332,17 @@ template <typename T> hipError_t forward(const GatedDelta& a, hipStream_t s) {
 // once, then OUTPUTS, over all segments at once), a backward pass twice, and the joins
 // take the segments one after another: about 2 us each, a third of a chunk.  n chunks of few
 // heads are so best in segments of about sqrt(n / 8), and heads that fill the chip
-// between them are not cut: two workgroups of 64 columns a CU, one of 128.  Measured, us
-// (with MAPS and ENDS one after another):
-//   one segment a chunk or longer ones (12 heads of 64 x 64, a training pass): 500
-//   frames 115, in segments of 2 chunks 130, uncut 188; 2000 frames in segments of 1, 2
-//   and 3 chunks 223, 194 and 230, of 8 chunks 351;
-//   workgroups of all segments (40001 frames of 12 heads, forward): up to 384, 512, 768,
-//   1024 508, 440, 440, 507; of 128 x 128 (1500 frames of 24 heads): 192 412, 288 518;
-//   least segments: three in training (2000 frames of 160 heads 734, uncut 839; 190 of
-//   12 88, uncut 93), four in a forward pass alone (2000 of 128 197, uncut 226; in three,
-//   of 160, 252 and 229).
+// between them are not cut: two workgroups of 64 columns a CU, one of 128.  Measured, us:
+//   short segments or longer ones (12 heads of 64 x 64, a training pass): 500 frames in
+//   segments of 1, 2 and 8 chunks (uncut) 108, 119 and 178; 2000 frames of 1, 2, 3, 4 and
+//   8 212, 181, 187, 205 and 302, uncut 622; 8000 of 3, 4 and 6 388, 371 and 377;
+//   workgroups of all segments: 40001 frames of 12 heads, forward, 276, 384, 504, 756 and
+//   948 491, 381, 380, 376 and 425; 1500 frames of 24 heads of 128 x 128 96, 144, 192 and
+//   288 443, 443, 399 and 504 in training (forward 134 and 121 with 96 and 144, 142 with
+//   192, which the rule takes);
+//   least segments: three in training (2000 frames of 160 heads 761, uncut 845; 190 of
+//   12 86, uncut 93), four in a forward pass alone (2000 of 128 161, uncut 221; in three,
+//   190 of 12 30 and 28, 1500 of 84 of 128 x 128 231 and 219, but 2000 of 160 199 and 224).
 DeltaSegments delta_segments(int64_t T, int64_t heads, int dv, bool train) {
   const int64_t chunks = (T + GD_CHUNK - 1) / GD_CHUNK, room = (dv <= 64 ? 512 : 256) / heads, least = train ? 3 : 4;
   if (room < least) return {1, (int)chunks};
