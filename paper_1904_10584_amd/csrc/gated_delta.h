@@ -29,8 +29,8 @@
 //
 // What bounds it: neither HBM nor the matrix cores, but a chunk's chain of dependent
 // steps (staging, the triangles, the solve, the state), with two or three workgroups of
-// a CU to fill the waits.  A chunk of 64 x 64 keeps the vector units busy for 28 to 41 %
-// of its time, half of that splitting into terms, and the matrix cores for 10 to 12 %.
+// a CU to fill the waits.  A chunk of 64 x 64 keeps the vector units busy for 25 to 37 %
+// of its time, half of that splitting into terms, and the matrix cores for 8 to 10 %.
 // Blocks of 16 rows in the order of `spot` and rows in that of `place` brought LDS bank
 // conflicts from 12.2 M to 3.5 M cycles (256 sequences of one chunk, 12 heads).
 #pragma once
@@ -101,7 +101,7 @@ __device__ __forceinline__ bf16x8_t join(u32x2_t a, u32x2_t b) {
 // acc += A B over 16, or over two blocks of 16, of the inner axis; small terms first.
 // Over 16, an instruction of 32 takes two products of terms.  (Instructions of 16 are
 // not used: one that added to what an instruction of 32 had just written gave wrong
-// sums, since the compiler left too little room between the two.)
+// sums.  Why is not known.)
 template <int TA, int TB>
 __device__ __forceinline__ void mma(f32x4_t& acc, const Piece<TA>& a, const Piece<TB>& b) {
   constexpr int N = TA > TB ? TA : TB;

@@ -16,9 +16,12 @@ namespace {
 //
 // One workgroup takes a tile of 128 x 128: a thread has 8 x 8 elements of it, so its
 // rows leave as words and its columns, through LDS, as 16-byte pieces.  The matrix is
-// read once for both layouts; HBM bounds it: 16384 x 2304 in bf16, both layouts, takes
-// 38 us for 151 MB (4.0 TB/s; a copy of its size reaches 5.1 to 7).  Loads and stores
-// without branches, so that all are in flight, brought it there from 57.
+// read once for both layouts: 16384 x 2304 in bf16, both layouts, takes 38 us for 151 MB
+// (4.0 TB/s; a copy of its size reaches 5.1 to 7).  Nothing is busy throughout: the vector
+// units for 19 us of it, LDS for 9 (8 of them conflicts of the transposed tile's rows),
+// HBM for 21 to 29; a workgroup loads, computes and stores one after another, three of
+// them a CU.  Loads and stores without branches, so that all are in flight, brought it
+// there from 57.
 
 constexpr int QT = 128;           // rows and columns of a tile, elements of a scale
 constexpr int QPITCH = QT + 16;   // bytes between the transposed tile's rows in LDS

@@ -131,3 +131,10 @@ def test_gates_nearly_open(gate, dtype):
         x = np.exp(_f64(t))  # 1 / sigm(-t), but for 1
         want = ref[n] * x
         assert np.abs(_f64(got[n]) * x - want).max() <= tol * np.abs(want).max(), name
+
+
+@BOTH
+def test_more_heads_of_a_key_than_a_workgroup_has_threads(dtype):
+    """Chunks that a sequence does not reach have no part in dlam, of any head."""
+    c = Case(66, 2, 600, 4, 4, dtype, keys=1, lengths=[65, 3], seed=4)
+    c.check()
